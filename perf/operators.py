@@ -202,7 +202,7 @@ def _own(s):
     elif s["op"] == "append":
         cache.append(s["qkv"], s["cu"], s["pos"], s["slots"], k_norm=s["gain"], rope=s["rope"], eps=EPS)
     else:
-        cache.attention(s["qkv"], s["start"], s["cu"], s["out"], q_norm=s["gain"], rope=s["rope"], eps=EPS)
+        cache.attention(s["qkv"], s["start"], s["cu"], s["out"], q_norm=s["gain"], rope=s["rope"], eps=EPS, max_new=s["most_rows"])
 
 
 # ------------------------------------------------------------------------------------------------ plain forms
