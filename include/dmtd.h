@@ -301,13 +301,88 @@ int dmtd_masked_forward(dmtd_ctx* ctx, const int32_t* tokens, int32_t batch, int
  * of the pass) without writing logits, 0 if it holds logits of some rows at a time.  Needs no GPU.  Errors: DMTD_EINVAL. */
 int dmtd_score_plan(const dmtd_config* cfg, int32_t batch, int32_t n, int32_t plan[2]);
 
+/* ---- A paged key/value cache ----
+ * For batches whose requests come and go: their keys and values lie in pages of a shared pool, found through a block table per request,
+ * so a request takes room for the tokens it has and gives it back when it ends.  The calls below are operators on DEVICE arrays of the
+ * caller's: no context, no allocation, no synchronisation, capturable into a HIP graph; they are enqueued on `stream` (hipStream_t, NULL = the
+ * default stream), which must belong to the current device.  Arguments are checked on the host before anything is enqueued
+ * (DMTD_EINVAL, DMTD_ECAPACITY; DMTD_EHIP if a launch failed; the message is dmtd_last_error(NULL) on the calling thread); lengths, page numbers
+ * and places, which only the device holds, are checked there, as stated at each call.
+ *
+ * One step of a batch of n_req requests: request i has start[i] tokens in the cache and brings rows[i] new ones (none, one, or a
+ * chunk of its prompt).  The new tokens of all requests, in the requests' order, are the rows of the step; cu_rows[i] is request i's first
+ * row, cu_rows[n_req] their number.  dmtd_page_tables once a step; per layer dmtd_paged_append, then dmtd_paged_attention.
+ * Buffers with a row per new token have room for max_rows; what lies behind the last row is neither read nor written. */
+
+typedef struct dmtd_page_pool {
+  int32_t  n_pages;        /* pages of the pool */
+  int32_t  page_size;      /* tokens of a page: 16, 32, 64, 128 or 256 */
+  int32_t  n_req;          /* requests, at most 8192 */
+  int32_t  max_pages;      /* entries of a request's block table; max_pages * page_size <= 2^30 */
+  int32_t* block_table;    /* DEVICE [n_req, max_pages]: page of a request's tokens j * page_size .. ; -1 where it holds none */
+  int32_t* held;           /* DEVICE [n_req]: pages a request holds */
+  int32_t* free_pages;     /* DEVICE [n_pages]: the free pages, a stack: entries 0 .. n_free - 1, those behind are -1 */
+  int32_t* n_free;         /* DEVICE [1] */
+} dmtd_page_pool;
+
+/* Pages for a step, and its rows' places.  Afterwards request i holds ceil((start[i] + rows[i]) / page_size) pages: first the surplus of requests that
+ * hold more goes back to the pool, then what the others lack comes off it, in the order of the requests and their pages (start = rows = 0 releases a
+ * request).  Pages that a step took and the next gives back return to the stack in the order they lay in.
+ * start, rows: DEVICE int32 [n_req].  Out, all DEVICE: cu_rows int32 [n_req + 1]; row_pos int32 [max_rows], a row's position start[i] + j;
+ * slots int64 [max_rows], its place page * page_size + position % page_size; status int32 [2].
+ * status[0] = 0: done.  Otherwise the step has no rows (cu_rows all 0) and block_table, held, free_pages, n_free, row_pos and slots are as
+ * they were: DMTD_ECAPACITY, the pool lacks status[1] pages; DMTD_EINVAL, status[1] = i: request i's lengths are negative or beyond its block table (the first
+ * such request), -1: more than max_rows rows, or held and n_free do not fit the pool.  Page numbers are moved, not checked.
+ * start and rows must not overlap what is written.  Errors: DMTD_EINVAL, DMTD_EHIP. */
+int dmtd_page_tables(const dmtd_page_pool* pool, const int32_t* start, const int32_t* rows, int32_t max_rows, int32_t* cu_rows, int32_t* row_pos,
+                     int64_t* slots, int32_t* status, void* stream);
+
+typedef struct dmtd_paged_cache {
+  void*    k;              /* DEVICE [n_pages][n_kv_heads][page_size][head_dim] of dtype, 16-byte aligned */
+  void*    v;              /* DEVICE, as k */
+  int64_t  page_stride;    /* elements from one page to the next, of k and of v, a multiple of 8; 0: pages follow each other */
+  const int32_t* block_table;
+  int32_t  n_pages, page_size, n_req, max_pages;
+  int32_t  n_q_heads;      /* a multiple of n_kv_heads, at most 16 times as many */
+  int32_t  n_kv_heads, head_dim /* 64 or 128 */, dtype /* DMTD_DTYPE_* of k, v, gains and output */;
+  int32_t  max_rows;       /* rows there is room for, at most 2^24 */
+} dmtd_paged_cache;
+
+/* The new tokens' keys and values into their places: a head's key is normalised (RMS norm with gain k_norm, DEVICE [head_dim] of dtype; NULL: not),
+ * rotated by the angles of its position, and rounded to dtype; values are rounded as they are.
+ * qkv: DEVICE float32 [max_rows, ld], the fused projection's rows: n_q_heads query heads, then n_kv_heads keys, then n_kv_heads values, of head_dim
+ * each; 16-byte aligned, ld a multiple of 4.  cu_rows, row_pos, slots: of dmtd_page_tables (of cu_rows only the last entry is read).
+ * rope: DEVICE float32 [rope_len][head_dim / 2][2], (cos, sin) of the pair (i, i + head_dim / 2) at each position; NULL: no rotation.
+ * Rows with a place outside the pool, or a position outside the block table or the rotary table, are not stored.  Two rows with the same place leave either's values there.
+ * Errors: DMTD_EINVAL, DMTD_EHIP. */
+int dmtd_paged_append(const dmtd_paged_cache* cache, const float* qkv, int64_t ld, const int32_t* cu_rows, const int32_t* row_pos, const int64_t* slots,
+                      const void* k_norm, float eps, const float* rope, int32_t rope_len, void* stream);
+
+/* Bytes of DEVICE workspace dmtd_paged_attention needs; 0 if the cache is invalid (its pointers are checked too). */
+size_t dmtd_paged_workspace_bytes(const dmtd_paged_cache* cache);
+
+/* Attention of a step's rows over their requests' pages: out[t, h] = sum_j p_j v_j with p = softmax(q_t,h . k_j / sqrt(head_dim)) over the keys
+ * j = 0 .. position of row t of its request, whose own key is in the cache already; queries are normalised (q_norm, eps) and rotated (rope) as the keys
+ * were by dmtd_paged_append.  Softmax and sums in float32; products of bf16 caches on the matrix cores, queries and probabilities as two bf16 parts each.
+ * qkv: as above; only its query heads are read (ld >= n_q_heads * head_dim).  start: DEVICE int32 [n_req].  cu_rows: DEVICE int32 [n_req + 1], ascending from 0 on.
+ * max_new: HOST, the most rows that one request brings (0: max_rows): a launch of many rows per request is left out where none has them.
+ * out: DEVICE [max_rows, ldo] of dtype, n_q_heads heads of head_dim; 16-byte aligned, ldo a multiple of 8.
+ * workspace: DEVICE, 256-byte aligned, zeroed once before its first use; calls leave it fit for the next.  Calls that may overlap need one each.
+ * Requests whose lengths do not fit (negative, more than max_new rows, beyond max_rows, the block table or the rotary table) are left out, their rows of out
+ * as they were.  Keys in pages outside the pool are left out; a row without any key comes out as 0.  Values that are not finite reach the rows that see them,
+ * as NaN, and no others.  Results do not depend on which workgroup ends first.
+ * Errors: DMTD_EINVAL, DMTD_ECAPACITY (workspace too small), DMTD_EHIP. */
+int dmtd_paged_attention(const dmtd_paged_cache* cache, const float* qkv, int64_t ld, const int32_t* start, const int32_t* cu_rows, int32_t max_new,
+                         const void* q_norm, float eps, const float* rope, int32_t rope_len, void* out, int64_t ldo, void* workspace,
+                         size_t workspace_bytes, void* stream);
+
 /* Back to the state right after dmtd_create (caches are treated as empty). */
 int dmtd_reset(dmtd_ctx* ctx);
 
 void dmtd_destroy(dmtd_ctx* ctx);
 
 /* Message for the last failed call on ctx (or, with ctx == NULL, the last failed
- * dmtd_create on this thread).  Never NULL. */
+ * dmtd_create or call without a context on this thread).  Never NULL. */
 const char* dmtd_last_error(const dmtd_ctx* ctx);
 
 #ifdef __cplusplus

@@ -27,6 +27,16 @@ class _Config(C.Structure):
         ("full_pos_add_embed", C.c_int32), ("use_graphs", C.c_int32), ("dry_run", C.c_int32), ("stream", C.c_void_p)]
 
 
+class _PagePool(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_pages", "page_size", "n_req", "max_pages")] + [
+        (n, C.c_void_p) for n in ("block_table", "held", "free_pages", "n_free")]
+
+
+class _PagedCache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("page_stride", C.c_int64), ("block_table", C.c_void_p)] + [
+        (n, C.c_int32) for n in ("n_pages", "page_size", "n_req", "max_pages", "n_q_heads", "n_kv_heads", "head_dim", "dtype", "max_rows")]
+
+
 class DmtdError(RuntimeError):
     def __init__(self, code: int, msg: str):
         super().__init__(f"{_CODES.get(code, code)}: {msg}")
@@ -96,6 +106,16 @@ def load_library():
     lib.dmtd_masked_forward.restype = C.c_int
     lib.dmtd_masked_forward.argtypes = [C.c_void_p, P(C.c_int32), C.c_int32, C.c_int32, P(C.c_uint8), C.c_int32, P(C.c_float),
                                         P(C.c_int32), P(C.c_float), C.c_size_t, P(C.c_float)]
+    lib.dmtd_page_tables.restype = C.c_int
+    lib.dmtd_page_tables.argtypes = [P(_PagePool), C.c_void_p, C.c_void_p, C.c_int32] + [C.c_void_p] * 5
+    lib.dmtd_paged_append.restype = C.c_int
+    lib.dmtd_paged_append.argtypes = [P(_PagedCache), C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_float,
+                                      C.c_void_p, C.c_int32, C.c_void_p]
+    lib.dmtd_paged_workspace_bytes.restype = C.c_size_t
+    lib.dmtd_paged_workspace_bytes.argtypes = [P(_PagedCache)]
+    lib.dmtd_paged_attention.restype = C.c_int
+    lib.dmtd_paged_attention.argtypes = [P(_PagedCache), C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_float,
+                                         C.c_void_p, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_size_t, C.c_void_p]
     lib.dmtd_reset.restype = C.c_int
     lib.dmtd_reset.argtypes = [C.c_void_p]
     lib.dmtd_destroy.restype = None
@@ -372,3 +392,139 @@ class Engine:
 
     def reset(self):
         self._check(self.lib.dmtd_reset(self._h))
+
+
+# ------------------------------------------------------------------------------- paged key/value cache
+
+def _raise(lib, rc):
+    if rc != DMTD_OK:
+        raise DmtdError(rc, lib.dmtd_last_error(None).decode())
+
+
+def _want(t, name, dtype, device, shape=None, contiguous=True):
+    """A GPU tensor of that type on that device, and of that shape where one is given (None: any extent)."""
+    if t.dtype is not dtype or t.device != device:
+        raise ValueError(f"{name} must be a {dtype} tensor on {device}")
+    if contiguous and not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    if shape is not None and (t.dim() != len(shape) or any(n is not None and n != m for n, m in zip(shape, t.shape))):
+        raise ValueError(f"{name} must have the shape {tuple('any' if n is None else n for n in shape)}, not {tuple(t.shape)}")
+    return t.data_ptr()
+
+
+class _OnDevice:
+    """What the handles of the paged cache share: the library, a device, and calls on torch's current stream of that device."""
+
+    def _open(self, device):
+        import torch
+        if device.type != "cuda":
+            raise ValueError("the paged cache lives on the GPU")
+        self._torch, self._lib, self.device = torch, load_library(), device
+        self._i32, self._i64, self._f32 = torch.int32, torch.int64, torch.float32
+
+    def _call(self, fn, *args):
+        cuda = self._torch.cuda
+        stream = cuda.current_stream(self.device)
+        if cuda.current_device() == self.device.index:
+            rc = fn(*args, stream.cuda_stream)
+        else:
+            with cuda.device(self.device):
+                rc = fn(*args, stream.cuda_stream)
+        if rc != DMTD_OK:
+            _raise(self._lib, rc)
+        return stream
+
+
+class PageTables(_OnDevice):
+    """Block tables of ``n_req`` requests over a pool of pages (``dmtd_page_tables``), on torch's current stream.
+
+    ``block_table`` int32 ``[n_req, max_pages]``, ``held`` int32 ``[n_req]``, ``free_pages`` int32 ``[n_pages]`` and ``n_free`` int32 ``[1]`` are the
+    caller's GPU tensors, changed in place; :meth:`empty` makes those of an empty pool."""
+
+    def __init__(self, block_table, held, free_pages, n_free, page_size: int):
+        self._open(block_table.device)
+        dev, i32 = self.device, self._i32
+        n_req, max_pages = block_table.shape
+        self.block_table, self.held, self.free_pages, self.n_free, self.page_size = block_table, held, free_pages, n_free, int(page_size)
+        self._c = _PagePool(free_pages.numel(), self.page_size, n_req, max_pages, _want(block_table, "block_table", i32, dev, (None, None)),
+                            _want(held, "held", i32, dev, (n_req,)), _want(free_pages, "free_pages", i32, dev, (None,)), _want(n_free, "n_free", i32, dev, (1,)))
+        self._p = C.byref(self._c)
+
+    @classmethod
+    def empty(cls, n_pages: int, page_size: int, n_req: int, max_pages: int, device="cuda"):
+        """A pool whose pages are all free, handed out from page 0 on."""
+        import torch
+        free = torch.arange(n_pages - 1, -1, -1, dtype=torch.int32, device=device)
+        return cls(torch.full((n_req, max_pages), -1, dtype=torch.int32, device=device), torch.zeros(n_req, dtype=torch.int32, device=device), free,
+                   torch.full((1,), n_pages, dtype=torch.int32, device=device), page_size)
+
+    def build(self, start, rows, cu_rows, row_pos, slots, status):
+        """Pages and places for a step: request i has ``start[i]`` tokens and brings ``rows[i]``.  Writes ``cu_rows`` int32 ``[n_req + 1]``, ``row_pos`` int32
+        ``[max_rows]``, ``slots`` int64 ``[max_rows]`` and ``status`` int32 ``[2]`` (0, or why the step has no rows: see the header)."""
+        i32, dev, n = self._i32, self.device, self._c.n_req
+        room = row_pos.numel()
+        self._call(self._lib.dmtd_page_tables, self._p, _want(start, "start", i32, dev, (n,)), _want(rows, "rows", i32, dev, (n,)), room,
+                   _want(cu_rows, "cu_rows", i32, dev, (n + 1,)), _want(row_pos, "row_pos", i32, dev, (room,)), _want(slots, "slots", self._i64, dev, (room,)),
+                   _want(status, "status", i32, dev, (2,)))
+
+
+class PagedCache(_OnDevice):
+    """One layer's keys and values in pages, ``k`` and ``v`` ``[n_pages, n_kv_heads, page_size, head_dim]`` (bfloat16 or float32; pages may lie apart,
+    a page itself is contiguous), read and filled through ``block_table`` int32 ``[n_req, max_pages]`` (``dmtd_paged_append``, ``dmtd_paged_attention``) on
+    torch's current stream.  Steps have up to ``max_rows`` rows.  The handle holds the attention's workspace: calls of one handle must not overlap."""
+
+    def __init__(self, k, v, block_table, n_q_heads: int, max_rows: int):
+        self._open(k.device)
+        torch, dev = self._torch, self.device
+        if k.dtype not in (torch.bfloat16, torch.float32):
+            raise ValueError("k and v must be bfloat16 or float32")
+        n_pages, n_kv, page_size, hd = k.shape
+        for name, t in (("k", k), ("v", v)):
+            _want(t, name, k.dtype, dev, tuple(k.shape), contiguous=False)
+            if t.stride() != (k.stride(0), page_size * hd, hd, 1):
+                raise ValueError("pages must be contiguous, and k and v laid out alike")
+        self.k, self.v, self.block_table, self.dtype, self.max_rows = k, v, block_table, k.dtype, int(max_rows)
+        self._c = _PagedCache(k.data_ptr(), v.data_ptr(), k.stride(0) if n_pages > 1 else 0, _want(block_table, "block_table", self._i32, dev, (None, None)), n_pages,
+                              page_size, block_table.shape[0], block_table.shape[1], n_q_heads, n_kv, hd, 1 if k.dtype is torch.bfloat16 else 0, max_rows)
+        self._p = C.byref(self._c)
+        self._n, self._hd, self._q_cols, self._cols = block_table.shape[0], hd, n_q_heads * hd, (n_q_heads + 2 * n_kv) * hd
+        self._ws_bytes = self._lib.dmtd_paged_workspace_bytes(self._p)
+        if self._ws_bytes == 0:
+            _raise(self._lib, DMTD_EINVAL)
+        self._ws = torch.zeros(self._ws_bytes, dtype=torch.uint8, device=dev)
+        stream = torch.cuda.current_stream(dev)
+        stream.synchronize()              # zeroed, whichever stream the first call is on
+        self._streams = {stream.cuda_stream}
+
+    def _rows(self, qkv, cols, norm, rope):
+        dev = self.device
+        if qkv.dim() != 2 or qkv.dtype is not self._f32 or qkv.device != dev or qkv.stride(1) != 1 or qkv.shape[0] < self.max_rows or qkv.shape[1] < cols:
+            raise ValueError(f"qkv must be float32 [at least {self.max_rows}, at least {cols}] on {dev} with contiguous rows")
+        gain = None if norm is None else _want(norm, "the norm's gain", self.dtype, dev, (self._hd,))
+        if rope is None:
+            return qkv.data_ptr(), qkv.stride(0), gain, None, 0
+        return qkv.data_ptr(), qkv.stride(0), gain, _want(rope, "rope", self._f32, dev, (None, self._hd // 2, 2)), rope.shape[0]
+
+    def append(self, qkv, cu_rows, row_pos, slots, k_norm=None, rope=None, eps: float = 1e-6):
+        """Keys (normalised with ``k_norm``, rotated by ``rope`` [positions, head_dim / 2, (cos, sin)]) and values of the fused projection's rows
+        ``qkv`` into the places that :meth:`PageTables.build` gave them."""
+        x, ld, gain, tab, n_tab = self._rows(qkv, self._cols, k_norm, rope)
+        dev = self.device
+        self._call(self._lib.dmtd_paged_append, self._p, x, ld, _want(cu_rows, "cu_rows", self._i32, dev, (self._n + 1,)), _want(row_pos, "row_pos", self._i32, dev, (self.max_rows,)),
+                   _want(slots, "slots", self._i64, dev, (self.max_rows,)), gain, eps, tab, n_tab)
+
+    def attention(self, qkv, start, cu_rows, out=None, q_norm=None, rope=None, eps: float = 1e-6, max_new: int = 0):
+        """The rows' queries over their requests' pages, into ``out`` ``[max_rows, n_q_heads, head_dim]`` of the cache's type (made if not given; rows behind
+        the last one are not written).  ``max_new``: the most rows one request brings, if known."""
+        x, ld, gain, tab, n_tab = self._rows(qkv, self._q_cols, q_norm, rope)
+        dev = self.device
+        if out is None:
+            out = self._torch.empty(self.max_rows, self._q_cols // self._hd, self._hd, dtype=self.dtype, device=dev)
+        if out.dim() != 3 or out.shape[1:] != (self._q_cols // self._hd, self._hd) or out.shape[0] < self.max_rows or out.stride()[1:] != (self._hd, 1):
+            raise ValueError(f"out must be [at least {self.max_rows}, {self._q_cols // self._hd}, {self._hd}] with contiguous rows")
+        stream = self._call(self._lib.dmtd_paged_attention, self._p, x, ld, _want(start, "start", self._i32, dev, (self._n,)), _want(cu_rows, "cu_rows", self._i32, dev, (self._n + 1,)),
+                            max_new, gain, eps, tab, n_tab, _want(out, "out", self.dtype, dev, contiguous=False), out.stride(0), self._ws.data_ptr(), self._ws_bytes)
+        if stream.cuda_stream not in self._streams:
+            self._streams.add(stream.cuda_stream)
+            self._ws.record_stream(stream)      # the workspace is not reused before this stream's work has ended
+        return out

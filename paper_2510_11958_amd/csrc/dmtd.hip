@@ -1673,6 +1673,8 @@ void destroy_graphs(dmtd_ctx* c) {
 
 // ============================================================================ C ABI
 
+#include "paged_calls.hpp"
+
 extern "C" {
 
 size_t dmtd_workspace_bytes(const dmtd_config* cfg) {

@@ -1,0 +1,229 @@
+// A paged key/value cache: requests keep their keys and values in pages of a shared pool, found through a block table per request.
+// Here are the pages' bookkeeping (page_tables_kernel, page_rows_kernel), the append (paged_append_kernel) and what the attention kernels
+// share; the attention itself is in attention_paged.hpp.
+//
+// Pool: K and V each [n_pages][n_kv_heads][page_size][head_dim], so that the keys of one head in one page are one contiguous run of
+// page_size * head_dim elements (4 KiB at 16 keys of 128 bf16 values).  Page sizes are powers of two from 16 to 256: a group of 16 keys,
+// which is what a wave of the attention kernels loads together, never leaves its page.
+#pragma once
+#include <limits.h>
+
+#include "attention.hpp"
+#include "gemv_mfma.hpp"
+
+namespace dmtd {
+
+constexpr int kPagedMaxRequests = 8192;      // requests of a call: their prefix sums lie in LDS
+
+// What the append and the attention know of the cache
+struct PagedView {
+  void *k, *v;
+  long page_stride;                 // elements from page to page
+  const int* table;                 // [n_req][max_pages]
+  int n_pages, page_shift, n_req, max_pages, nh, nkv, max_rows;
+  int limit;                        // positions a request may have: the block table's, or the rotary table's where that is shorter
+};
+
+// Sum of v over the threads before this one, and over all of them, in a block of NT threads
+template <int NT, typename T>
+__device__ __forceinline__ T block_scan(T v, T* wave_sums /* LDS, NT / 64 */, T& total) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  T incl = v;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const T u = __shfl_up(incl, o, 64);
+    if (lane >= o) incl += u;
+  }
+  if (NT == 64) {
+    total = __shfl(incl, 63, 64);
+    return incl - v;
+  }
+  __syncthreads();                  // the sums of an earlier call have been read
+  if (lane == 63) wave_sums[wave] = incl;
+  __syncthreads();
+  T before = 0, all = 0;
+#pragma unroll
+  for (int w = 0; w < NT / 64; ++w) {
+    const T s = wave_sums[w];
+    if (w < wave) before += s;
+    all += s;
+  }
+  total = all;
+  return before + incl - v;
+}
+
+// Last i in [0, n) with first[i] <= x (first ascending, first[0] <= x): among equal entries the last, so that of requests without rows in
+// front of one that has some the latter is found
+__device__ __forceinline__ int last_at_most(const int* first, int n, int x) {
+  int lo = 0, hi = n;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (first[mid] <= x) lo = mid; else hi = mid;
+  }
+  return lo;
+}
+
+// Position and place of row t of the new tokens, which is token t - cu[i] of request i
+__device__ __forceinline__ void page_row(const int* table, const int* start, int max_pages, int page_shift, int i, int t_in_req, int t,
+                                         int* row_pos, long long* slots) {
+  const int pos = start[i] + t_in_req;
+  row_pos[t] = pos;
+  slots[t] = ((long long)table[(size_t)i * max_pages + (pos >> page_shift)] << page_shift) + (pos & ((1 << page_shift) - 1));
+}
+
+// Pages for a step.  Request i holds held[i] pages and needs ceil((start[i] + rows[i]) / page size) of them.  Its surplus goes onto the
+// pool's stack, what it lacks comes off the stack, in the order of the requests and of their pages.  The k-th page given back lies k below
+// the new top, so the next step takes it as its k-th: giving back what a step took restores the stack.
+// One block of NT threads, each with the requests ipt t .. ipt t + ipt - 1: three prefix sums, and a search in one of them for each
+// page that moves.  Everything is checked before anything is written; a step that does not fit has no rows (cu all 0) and changes nothing.
+// Bound by latency: a chain of five round trips to memory (lengths; pages given back; pages taken off; their table entries read for the places; the last
+// stores), and a few barriers.
+template <int NT>
+__global__ void __launch_bounds__(NT) page_tables_kernel(int* __restrict__ table, int* __restrict__ held, int* __restrict__ stack, int* __restrict__ n_free,
+                                                         const int* __restrict__ start, const int* __restrict__ rows, int n_req, int max_pages, int n_pages,
+                                                         int page_shift, int max_rows, int* __restrict__ cu, int* __restrict__ row_pos,
+                                                         long long* __restrict__ slots /* null: page_rows_kernel follows */, int* __restrict__ status) {
+  __shared__ int first_s[kPagedMaxRequests + 1];
+  __shared__ long long sums_s[NT / 64 < 1 ? 1 : NT / 64];
+  __shared__ int bad_s;
+  const int tid = threadIdx.x, ipt = (n_req + NT - 1) / NT, i0 = min(tid * ipt, n_req), i1 = min(i0 + ipt, n_req);
+  const long long limit = (long long)max_pages << page_shift;
+  const int top0 = n_free[0];
+  if (tid == 0) bad_s = top0 < 0 || top0 > n_pages ? -1 : INT_MAX;
+  __syncthreads();
+  long long sg = 0, st = 0, sr = 0;
+  for (int i = i0; i < i1; ++i) {
+    const int s = start[i], r = rows[i], h = held[i];
+    if (s < 0 || r < 0 || h < 0 || h > max_pages || (long long)s + r > limit) { atomicMin(&bad_s, i); continue; }
+    const int need = (int)(((long long)s + r + (1 << page_shift) - 1) >> page_shift);
+    sg += max(h - need, 0);
+    st += max(need - h, 0);
+    sr += r;
+  }
+  long long give, take, total;
+  const long long g0 = block_scan<NT>(sg, sums_s, give), t0 = block_scan<NT>(st, sums_s, take), r0 = block_scan<NT>(sr, sums_s, total);
+  __syncthreads();
+  const int bad = bad_s;
+  int code = 0, detail = 0;
+  if (bad != INT_MAX) { code = -1; detail = bad; }
+  else if (total > max_rows || top0 + give > n_pages) { code = -1; detail = -1; }
+  else if (top0 + give < take) { code = -3; detail = (int)min(take - give - top0, (long long)INT_MAX); }
+  if (tid == 0) { status[0] = code; status[1] = detail; }
+  if (code) {
+    for (int i = tid; i <= n_req; i += NT) cu[i] = 0;
+    return;
+  }
+  const int top = top0 + (int)give, left = top - (int)take;
+  auto need_of = [&](int i) { return (start[i] + rows[i] + (1 << page_shift) - 1) >> page_shift; };
+  if (give) {
+    int at = (int)g0;
+    for (int i = i0; i < i1; ++i) { first_s[i] = at; at += max(held[i] - need_of(i), 0); }
+    __syncthreads();
+    for (int k = tid; k < (int)give; k += NT) {
+      const int i = last_at_most(first_s, n_req, k);
+      int* entry = table + (size_t)i * max_pages + need_of(i) + k - first_s[i];
+      stack[top - 1 - k] = *entry;
+      *entry = -1;
+    }
+    __syncthreads();                // the stack is whole before pages come off it, the search's array free again
+  }
+  if (take) {
+    int at = (int)t0;
+    for (int i = i0; i < i1; ++i) { first_s[i] = at; at += max(need_of(i) - held[i], 0); }
+    __syncthreads();
+    for (int k = tid; k < (int)take; k += NT) {
+      const int i = last_at_most(first_s, n_req, k);
+      table[(size_t)i * max_pages + held[i] + k - first_s[i]] = stack[top - 1 - k];
+      stack[top - 1 - k] = -1;
+    }
+    __syncthreads();                // held is read above
+  }
+  {
+    int at = (int)r0;
+    for (int i = i0; i < i1; ++i) {
+      first_s[i] = at;
+      cu[i] = at;
+      at += rows[i];
+      held[i] = need_of(i);
+    }
+    if (tid == 0) { cu[n_req] = (int)total; n_free[0] = left; }
+  }
+  if (!slots) return;
+  __syncthreads();
+  for (int t = tid; t < (int)total; t += NT) {
+    const int i = last_at_most(first_s, n_req, t);
+    page_row(table, start, max_pages, page_shift, i, t - first_s[i], t, row_pos, slots);
+  }
+}
+
+// Positions and places of the rows where they are many: a block per 1024 rows, the requests' first rows in LDS
+__global__ void __launch_bounds__(256) page_rows_kernel(const int* __restrict__ table, const int* __restrict__ start, int n_req, int max_pages, int page_shift,
+                                                        const int* __restrict__ cu, int* __restrict__ row_pos, long long* __restrict__ slots) {
+  __shared__ int first_s[kPagedMaxRequests];
+  const int total = cu[n_req], base = blockIdx.x * 1024;
+  if (base >= total) return;
+  for (int i = threadIdx.x; i < n_req; i += 256) first_s[i] = cu[i];
+  __syncthreads();
+  for (int t = base + threadIdx.x; t < min(base + 1024, total); t += 256) {
+    const int i = last_at_most(first_s, n_req, t);
+    page_row(table, start, max_pages, page_shift, i, t - first_s[i], t, row_pos, slots);
+  }
+}
+
+// Elements of one type to the pool, four or two at a time, each rounded to nearest even once
+template <int N> __device__ __forceinline__ void store_elems(float* p, const float (&x)[N]) {
+#pragma unroll
+  for (int e = 0; e < N; ++e) p[e] = x[e];
+}
+template <int N> __device__ __forceinline__ void store_elems(bf16_t* p, const float (&x)[N]) {
+#pragma unroll
+  for (int e = 0; e < N; e += 2) *(uint32_t*)(p + e) = pack_bf16x2(x[e], x[e + 1]);
+}
+
+// The new tokens' keys - RMS norm with gain (k_gain null: none), then the rotation of the pairs (i, i + HD/2) by the angles of the token's
+// position (rope_tab null: none) - and values, rounded to the pool's type and stored in their places.  16 lanes take one (row, KV head):
+// its key and its value, HD/32 pairs a lane, so that a wave's loads are runs of 256 bytes and the norm's sum stays inside a DPP row.  Rows at
+// and behind cu[n_req], and rows whose place or position is out of range, are not stored.
+template <typename CT, int HD>
+__global__ void __launch_bounds__(256) paged_append_kernel(const float* __restrict__ qkv, long ld, const int* __restrict__ cu, const int* __restrict__ row_pos,
+                                                           const long long* __restrict__ slots, const CT* __restrict__ k_gain, const float2* __restrict__ rope_tab,
+                                                           float eps, PagedView pv) {
+  constexpr int half = HD / 2, HL = AttRow<HD>::HL;
+  const int l = threadIdx.x & 15;
+  const long v = (long)blockIdx.x * 16 + (threadIdx.x >> 4);
+  const int t = (int)(v / pv.nkv), g = (int)(v - (long)t * pv.nkv);
+  if (t >= min(pv.max_rows, cu[pv.n_req])) return;          // whole rows of 16 lanes
+  const int pos = row_pos[t];
+  const long long slot = slots[t];
+  AttRow<HD> k, w;
+  k.load(qkv + (size_t)t * ld + (size_t)(pv.nh + g) * HD, l);
+  w.load(qkv + (size_t)t * ld + (size_t)(pv.nh + pv.nkv + g) * HD, l);
+  if (pos < 0 || pos >= pv.limit || slot < 0 || slot >= ((long long)pv.n_pages << pv.page_shift)) return;
+  float x0[HL], x1[HL], ss = 0.f;
+#pragma unroll
+  for (int e = 0; e < HL; ++e) { x0[e] = k.a[e]; x1[e] = k.b[e]; ss += x0[e] * x0[e] + x1[e] * x1[e]; }
+  if (k_gain) {
+    const float rs = rsqrtf(row16_sum(ss) / (float)HD + eps);
+#pragma unroll
+    for (int e = 0; e < HL; ++e) { x0[e] *= rs * Elem<CT>::to_f32(k_gain[HL * l + e]); x1[e] *= rs * Elem<CT>::to_f32(k_gain[half + HL * l + e]); }
+  }
+  if (rope_tab) {
+    const float2* rp = rope_tab + (size_t)pos * half + HL * l;
+#pragma unroll
+    for (int e = 0; e < HL; ++e) {
+      const float2 cs = rp[e];
+      const float a = x0[e], b = x1[e];
+      x0[e] = a * cs.x - b * cs.y;
+      x1[e] = b * cs.x + a * cs.y;
+    }
+  }
+  const size_t at = (size_t)(slot >> pv.page_shift) * pv.page_stride + (((size_t)g << pv.page_shift) + (size_t)(slot & ((1 << pv.page_shift) - 1))) * HD + HL * l;
+  store_elems<HL>((CT*)pv.k + at, x0);
+  store_elems<HL>((CT*)pv.k + at + half, x1);
+#pragma unroll
+  for (int e = 0; e < HL; ++e) { x0[e] = w.a[e]; x1[e] = w.b[e]; }
+  store_elems<HL>((CT*)pv.v + at, x0);
+  store_elems<HL>((CT*)pv.v + at + half, x1);
+}
+
+}  // namespace dmtd

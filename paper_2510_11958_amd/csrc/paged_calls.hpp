@@ -1,0 +1,175 @@
+// The calls of the paged key/value cache (see include/dmtd.h): checks of their arguments, and the launches.
+// Part of dmtd.hip: a failure's message goes where dmtd_last_error(NULL) finds it.
+#pragma once
+#include "attention_paged.hpp"
+
+namespace {
+
+int paged_fail(int code, const char* why) {
+  g_create_error = why;
+  return code;
+}
+
+bool aligned(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
+bool page_size_ok(int p) { return p == 16 || p == 32 || p == 64 || p == 128 || p == 256; }
+int log2_of(int p) { int s = 0; while ((1 << s) < p) ++s; return s; }
+
+// A launch goes to the device that is current; on a stream of another one it would fail or, worse, read that one's addresses here
+int check_stream_device(hipStream_t s) {
+  if (!s) return DMTD_OK;
+  int cur = 0;
+  hipDevice_t dev = 0;
+  hipError_t e = hipGetDevice(&cur);
+  if (e == hipSuccess) e = hipStreamGetDevice(s, &dev);
+  if (e != hipSuccess) return paged_fail(DMTD_EHIP, hipGetErrorString(e));
+  if ((int)dev != cur) return paged_fail(DMTD_EINVAL, "the stream belongs to another device than the current one");
+  return DMTD_OK;
+}
+
+int paged_done() {
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? DMTD_OK : paged_fail(DMTD_EHIP, hipGetErrorString(e));
+}
+
+int check_table(int n_req, int max_pages, int n_pages, int page_size) {
+  if (!page_size_ok(page_size)) return paged_fail(DMTD_EINVAL, "page_size must be 16, 32, 64, 128 or 256");
+  if (n_req < 1 || n_req > kPagedMaxRequests) return paged_fail(DMTD_EINVAL, "n_req must be in [1, 8192]");
+  if (max_pages < 1 || (long)max_pages * page_size > (1L << 30)) return paged_fail(DMTD_EINVAL, "max_pages must be >= 1 and max_pages * page_size <= 2^30");
+  if (n_pages < 1) return paged_fail(DMTD_EINVAL, "n_pages must be >= 1");
+  return DMTD_OK;
+}
+
+int check_cache(const dmtd_paged_cache* c) {
+  if (!c) return paged_fail(DMTD_EINVAL, "null cache");
+  const int rc = check_table(c->n_req, c->max_pages, c->n_pages, c->page_size);
+  if (rc != DMTD_OK) return rc;
+  if (c->dtype != DMTD_DTYPE_F32 && c->dtype != DMTD_DTYPE_BF16) return paged_fail(DMTD_EINVAL, "unknown dtype");
+  if (c->head_dim != 64 && c->head_dim != 128) return paged_fail(DMTD_EINVAL, "head_dim must be 64 or 128");
+  if (c->n_kv_heads < 1 || c->n_kv_heads > 1024 || c->n_q_heads < 1 || c->n_q_heads % c->n_kv_heads || c->n_q_heads / c->n_kv_heads > QV_MAX)
+    return paged_fail(DMTD_EINVAL, "n_q_heads must be a multiple of n_kv_heads (at most 1024), at most 16 times as many");
+  if (c->max_rows < 1 || c->max_rows > (1 << 24)) return paged_fail(DMTD_EINVAL, "max_rows must be in [1, 2^24]");
+  if (!c->k || !c->v || !c->block_table) return paged_fail(DMTD_EINVAL, "null cache pointer");
+  if (!aligned(c->k, 16) || !aligned(c->v, 16) || !aligned(c->block_table, 4)) return paged_fail(DMTD_EINVAL, "k and v must be 16-byte aligned");
+  const long one = (long)c->n_kv_heads * c->page_size * c->head_dim;
+  if (c->page_stride != 0 && (c->page_stride < one || c->page_stride % 8)) return paged_fail(DMTD_EINVAL, "page_stride must be 0 or a multiple of 8 that holds a page");
+  return DMTD_OK;
+}
+
+// qkv rows of at least `cols` values, the norm's gain and the rotary table
+int check_rows(const float* qkv, int64_t ld, int64_t cols, const void* gain, float eps, const float* rope, int32_t rope_len) {
+  if (!qkv || !aligned(qkv, 16)) return paged_fail(DMTD_EINVAL, "qkv must be a 16-byte aligned pointer");
+  if (ld < cols || ld % 4 || ld > (1 << 24)) return paged_fail(DMTD_EINVAL, "ld must be a multiple of 4 that holds a row");
+  if (gain && !aligned(gain, 16)) return paged_fail(DMTD_EINVAL, "a norm's gain must be 16-byte aligned");
+  if (gain && !(eps >= 0.f && eps < 1e30f)) return paged_fail(DMTD_EINVAL, "eps must be finite and not negative");
+  if (rope && (!aligned(rope, 16) || rope_len < 1)) return paged_fail(DMTD_EINVAL, "the rotary table must be 16-byte aligned and hold a position");
+  return DMTD_OK;
+}
+
+PagedView paged_view(const dmtd_paged_cache* c, const float* rope, int32_t rope_len) {
+  PagedView v{};
+  v.k = c->k; v.v = c->v; v.table = c->block_table;
+  v.page_stride = c->page_stride ? c->page_stride : (long)c->n_kv_heads * c->page_size * c->head_dim;
+  v.n_pages = c->n_pages; v.page_shift = log2_of(c->page_size); v.n_req = c->n_req; v.max_pages = c->max_pages;
+  v.nh = c->n_q_heads; v.nkv = c->n_kv_heads; v.max_rows = c->max_rows;
+  v.limit = c->max_pages * c->page_size;
+  if (rope && rope_len < v.limit) v.limit = rope_len;
+  return v;
+}
+
+// Rows that the block of the bookkeeping places by itself; more go through page_rows_kernel's blocks
+constexpr int kTableRows = 2048;
+
+template <typename CT>
+void launch_paged_append(const PagedView& v, int head_dim, const float* qkv, long ld, const int* cu, const int* row_pos, const int64_t* slots, const void* gain,
+                         float eps, const float* rope, hipStream_t s) {
+  const dim3 grid((unsigned)(((long)v.max_rows * v.nkv + 15) / 16));
+  if (head_dim == 128)
+    hipLaunchKernelGGL((paged_append_kernel<CT, 128>), grid, dim3(256), 0, s, qkv, ld, cu, row_pos, (const long long*)slots, (const CT*)gain, (const float2*)rope, eps, v);
+  else
+    hipLaunchKernelGGL((paged_append_kernel<CT, 64>), grid, dim3(256), 0, s, qkv, ld, cu, row_pos, (const long long*)slots, (const CT*)gain, (const float2*)rope, eps, v);
+}
+
+template <typename CT>
+void launch_paged_attention(const PagedView& v, int head_dim, const float* qkv, long ld, const int* start, const int* cu, int max_new, const void* gain, float eps,
+                            const float* rope, void* out, long ldo, hipStream_t s) {
+  const dim3 grid(v.max_rows, v.nh);
+  if (head_dim == 128)
+    hipLaunchKernelGGL((paged_attention_rows_kernel<CT, 128>), grid, dim3(256), 0, s, qkv, ld, start, cu, (const CT*)gain, (const float2*)rope, eps, max_new, (CT*)out, ldo, v);
+  else
+    hipLaunchKernelGGL((paged_attention_rows_kernel<CT, 64>), grid, dim3(256), 0, s, qkv, ld, start, cu, (const CT*)gain, (const float2*)rope, eps, max_new, (CT*)out, ldo, v);
+}
+
+}  // namespace
+
+extern "C" {
+
+int dmtd_page_tables(const dmtd_page_pool* p, const int32_t* start, const int32_t* rows, int32_t max_rows, int32_t* cu_rows, int32_t* row_pos,
+                     int64_t* slots, int32_t* status, void* stream) {
+  if (!p) return paged_fail(DMTD_EINVAL, "null pool");
+  int rc = check_table(p->n_req, p->max_pages, p->n_pages, p->page_size);
+  if (rc != DMTD_OK) return rc;
+  if (!p->block_table || !p->held || !p->free_pages || !p->n_free || !start || !rows || !cu_rows || !row_pos || !slots || !status)
+    return paged_fail(DMTD_EINVAL, "null pointer");
+  for (const void* q : {(const void*)p->block_table, (const void*)p->held, (const void*)p->free_pages, (const void*)p->n_free, (const void*)start, (const void*)rows,
+                        (const void*)cu_rows, (const void*)row_pos, (const void*)status})
+    if (!aligned(q, 4)) return paged_fail(DMTD_EINVAL, "int32 arrays must be 4-byte aligned");
+  if (!aligned(slots, 8)) return paged_fail(DMTD_EINVAL, "slots must be 8-byte aligned");
+  if (max_rows < 1 || max_rows > (1 << 24)) return paged_fail(DMTD_EINVAL, "max_rows must be in [1, 2^24]");
+  const hipStream_t s = (hipStream_t)stream;
+  if ((rc = check_stream_device(s)) != DMTD_OK) return rc;
+  const bool many = max_rows > kTableRows;
+  const int shift = log2_of(p->page_size);
+  auto launch = [&](auto nt_c) {
+    constexpr int NT = decltype(nt_c)::value;
+    hipLaunchKernelGGL(page_tables_kernel<NT>, dim3(1), dim3(NT), 0, s, p->block_table, p->held, p->free_pages, p->n_free, start, rows, p->n_req, p->max_pages,
+                       p->n_pages, shift, max_rows, cu_rows, row_pos, many ? (long long*)nullptr : (long long*)slots, status);
+  };
+  if (p->n_req <= 64 && max_rows <= 64) launch(std::integral_constant<int, 64>());
+  else launch(std::integral_constant<int, 1024>());
+  if (many)
+    hipLaunchKernelGGL(page_rows_kernel, dim3((max_rows + 1023) / 1024), dim3(256), 0, s, (const int*)p->block_table, start, p->n_req, p->max_pages, shift,
+                       (const int*)cu_rows, row_pos, (long long*)slots);
+  return paged_done();
+}
+
+int dmtd_paged_append(const dmtd_paged_cache* c, const float* qkv, int64_t ld, const int32_t* cu_rows, const int32_t* row_pos, const int64_t* slots,
+                      const void* k_norm, float eps, const float* rope, int32_t rope_len, void* stream) {
+  int rc = check_cache(c);
+  if (rc == DMTD_OK) rc = check_rows(qkv, ld, (int64_t)(c->n_q_heads + 2 * c->n_kv_heads) * c->head_dim, k_norm, eps, rope, rope_len);
+  if (rc != DMTD_OK) return rc;
+  if (!cu_rows || !row_pos || !slots || !aligned(cu_rows, 4) || !aligned(row_pos, 4) || !aligned(slots, 8)) return paged_fail(DMTD_EINVAL, "bad row map pointer");
+  const hipStream_t s = (hipStream_t)stream;
+  if ((rc = check_stream_device(s)) != DMTD_OK) return rc;
+  const PagedView v = paged_view(c, rope, rope_len);
+  if (c->dtype == DMTD_DTYPE_BF16) launch_paged_append<bf16_t>(v, c->head_dim, qkv, ld, cu_rows, row_pos, slots, k_norm, eps, rope, s);
+  else launch_paged_append<float>(v, c->head_dim, qkv, ld, cu_rows, row_pos, slots, k_norm, eps, rope, s);
+  return paged_done();
+}
+
+size_t dmtd_paged_workspace_bytes(const dmtd_paged_cache* c) {
+  if (check_cache(c) != DMTD_OK) return 0;
+  return 256;
+}
+
+int dmtd_paged_attention(const dmtd_paged_cache* c, const float* qkv, int64_t ld, const int32_t* start, const int32_t* cu_rows, int32_t max_new,
+                         const void* q_norm, float eps, const float* rope, int32_t rope_len, void* out, int64_t ldo, void* workspace,
+                         size_t workspace_bytes, void* stream) {
+  int rc = check_cache(c);
+  if (rc == DMTD_OK) rc = check_rows(qkv, ld, (int64_t)c->n_q_heads * c->head_dim, q_norm, eps, rope, rope_len);
+  if (rc != DMTD_OK) return rc;
+  if (!start || !cu_rows || !aligned(start, 4) || !aligned(cu_rows, 4)) return paged_fail(DMTD_EINVAL, "bad length pointer");
+  if (max_new < 0 || max_new > c->max_rows) return paged_fail(DMTD_EINVAL, "max_new must be in [0, max_rows]");
+  if (!out || !aligned(out, 16)) return paged_fail(DMTD_EINVAL, "out must be a 16-byte aligned pointer");
+  if (ldo < (int64_t)c->n_q_heads * c->head_dim || ldo % 8 || ldo > (1 << 24)) return paged_fail(DMTD_EINVAL, "ldo must be a multiple of 8 that holds a row");
+  if (!workspace || !aligned(workspace, 256)) return paged_fail(DMTD_EINVAL, "workspace must be a 256-byte aligned pointer");
+  if (workspace_bytes < dmtd_paged_workspace_bytes(c)) return paged_fail(DMTD_ECAPACITY, "workspace too small");
+  const hipStream_t s = (hipStream_t)stream;
+  if ((rc = check_stream_device(s)) != DMTD_OK) return rc;
+  const PagedView v = paged_view(c, rope, rope_len);
+  if (max_new == 0) max_new = c->max_rows;
+  if (c->dtype == DMTD_DTYPE_BF16) launch_paged_attention<bf16_t>(v, c->head_dim, qkv, ld, start, cu_rows, max_new, q_norm, eps, rope, out, ldo, s);
+  else launch_paged_attention<float>(v, c->head_dim, qkv, ld, start, cu_rows, max_new, q_norm, eps, rope, out, ldo, s);
+  return paged_done();
+}
+
+}  // extern "C"
