@@ -1,9 +1,22 @@
 // Attention of a step's new tokens over the paged cache of their requests (paged.hpp).  The new tokens' own keys and values are in the cache
 // already (paged_append_kernel); row t of request i, at position start[i] + t, sees the request's keys 0 .. start[i] + t.
+//
+// Two kernels for bf16 caches.  paged_attention_few_mfma_kernel takes the requests with few query vectors per KV head (rows x query heads that share
+// it, up to PAGED_FEW): blocks of 16 vectors, which read keys and values straight from the cache at the rate of the memory.
+// paged_attention_tall_mfma_kernel takes the others: blocks of 128 vectors, whose keys and values pass through LDS, bound by the matrix cores.
+// A block serves one KV head, one group of a request's rows and one range of its keys.  The ranges are found by every block itself from the
+// requests' lengths (paged_find): all of one length, such that the blocks fill the chip about once, whatever the lengths are.  Where a group has several
+// ranges, their partial results go through the workspace and the block that ends last joins them, in the order of the ranges: no second
+// launch, and the same bits whichever block that is.
 #pragma once
 #include "paged.hpp"
+#include "gemm_wide.hpp"
 
 namespace dmtd {
+
+constexpr int PAGED_SLOTS_FEW = 1024, PAGED_SLOTS_TALL = 512;     // blocks the chip holds: 4 and 2 on each of 256 CUs
+constexpr int PAGED_FEW = 64;                                      // query vectors per KV head of a request that the few-rows kernel takes
+constexpr int PAGED_KEYS_FEW = 64, PAGED_KEYS_TALL = 256;          // shortest key ranges
 
 // Rows of a request as the kernels read them: none where the lengths do not fit the buffers or the tables
 struct PagedReq { int first, n, start; };
@@ -11,6 +24,715 @@ __device__ __forceinline__ PagedReq paged_req(const PagedView& pv, const int* cu
   PagedReq q{cu[i], cu[i + 1] - cu[i], start[i]};
   if (q.first < 0 || q.n < 0 || q.n > max_new || q.first > pv.max_rows - q.n || q.start < 0 || q.start > pv.limit - q.n) q.n = 0;
   return q;
+}
+
+// Where a launch's results go: rows of the cache's type, or (PLANES) the two bf16 planes that the projections read, in their layout
+struct PagedOut { void* out; bf16_t* lo; long ld; int blocked; };
+
+struct PagedWork {
+  int shift;            // log2 of the blocks per KV head that the key ranges are chosen for
+  int* count;           // [groups with several ranges][nkv]: ranges that have ended; 0 between launches
+  float* part;          // [ranges of such groups][nkv]: QVT x HD sums, then QVT x (maximum, sum of weights)
+};
+
+// A block's share: rows row0 .. row0 + r - 1 of the request (its first row in the step is `first`), the first of them at position pos0; keys kb .. ke - 1;
+// the range's number of n of its group; where partial results and the count lie (in slots of all KV heads)
+struct PagedItem { int req, first, row0, r, pos0, kb, ke, split, n, slot, group; };
+
+// Item y of the launch that takes requests with lo < rows x GQ <= hi in groups of rpb rows.  All ranges have kps keys: with T = sum of groups x
+// keys over the requests, kps >= T / 2^shift, so there are at most 2^shift + groups items; those of groups with several ranges (keys > kps, hence ceil(keys / kps) < 2
+// keys / kps) are fewer than 2^(shift + 1), and such groups fewer than 2^shift: what the workspace holds.  Called by whole blocks.
+struct PagedShare { int groups, splits; };
+__device__ __forceinline__ int paged_groups(const PagedReq& q, int GQ, int lo, int hi, int rpb) {
+  return q.n > 0 && q.n * GQ > lo && q.n * GQ <= hi ? (q.n + rpb - 1) / rpb : 0;
+}
+template <int NT, int STEP>
+__device__ __forceinline__ bool paged_find(const PagedView& pv, const int* cu, const int* start, int max_new, int GQ, int lo, int hi, int rpb, int shift, int min_keys,
+                                           int y, PagedItem& it) {
+  auto keys_of = [&](unsigned long long total) {
+    const unsigned long long per = (total + (1ull << shift) - 1) >> shift;
+    return (int)max((unsigned long long)min_keys, (per + STEP - 1) / STEP * STEP);
+  };
+  int i, kps, splits, before, slots, multi;
+  PagedReq q;
+  if (pv.n_req <= 64) {       // a request per lane, every wave for itself
+    const int lane = threadIdx.x & 63;
+    q = PagedReq{0, 0, 0};
+    if (lane < pv.n_req) q = paged_req(pv, cu, start, max_new, lane);
+    const int gr = paged_groups(q, GQ, lo, hi, rpb);
+    kps = keys_of(wave_reduce((unsigned long long)gr * (unsigned)(q.start + q.n), [](unsigned long long a, unsigned long long b) { return a + b; }));
+    const int sp = (int)((unsigned)(q.start + q.n + kps - 1) / (unsigned)kps), items = gr * sp;
+    int incl = items;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int u = __shfl_up(incl, o, 64);
+      if (lane >= o) incl += u;
+    }
+    const unsigned long long behind = __ballot(incl > y);
+    if (!behind) return false;
+    i = __builtin_ctzll(behind);
+    const bool m = lane < i && sp > 1;
+    slots = (int)wave_reduce((uint32_t)(m ? items : 0), [](uint32_t a, uint32_t b) { return a + b; });
+    multi = (int)wave_reduce((uint32_t)(m ? gr : 0), [](uint32_t a, uint32_t b) { return a + b; });
+    before = __builtin_amdgcn_readlane(incl - items, i);
+    splits = __builtin_amdgcn_readlane(sp, i);
+    q.first = __builtin_amdgcn_readlane(q.first, i);
+    q.n = __builtin_amdgcn_readlane(q.n, i);
+    q.start = __builtin_amdgcn_readlane(q.start, i);
+  } else {
+    __shared__ long long sums_s[NT / 64];
+    __shared__ int found_s[8];
+    const int tid = threadIdx.x, ipt = (pv.n_req + NT - 1) / NT, i0 = min(tid * ipt, pv.n_req), i1 = min(i0 + ipt, pv.n_req);
+    long long mine = 0, total;
+    for (int j = i0; j < i1; ++j) {
+      const PagedReq r = paged_req(pv, cu, start, max_new, j);
+      mine += (long long)paged_groups(r, GQ, lo, hi, rpb) * (r.start + r.n);
+    }
+    (void)block_scan<NT>(mine, sums_s, total);
+    kps = keys_of((unsigned long long)total);
+    // items in the low half, those of groups with several ranges in the upper one, and such groups
+    long long n_items = 0, n_multi = 0;
+    auto share = [&](int j) {
+      const PagedReq r = paged_req(pv, cu, start, max_new, j);
+      return PagedShare{paged_groups(r, GQ, lo, hi, rpb), (int)((unsigned)(r.start + r.n + kps - 1) / (unsigned)kps)};
+    };
+    for (int j = i0; j < i1; ++j) {
+      const PagedShare s = share(j);
+      n_items += (long long)s.groups * s.splits;
+      if (s.splits > 1) n_multi += ((long long)s.groups << 32) | (unsigned)(s.groups * s.splits);
+    }
+    long long all, all_multi;
+    long long at = block_scan<NT>(n_items, sums_s, all), at_multi = block_scan<NT>(n_multi, sums_s, all_multi);
+    if (y >= all) return false;
+    if (at <= y && y < at + n_items) {
+      for (int j = i0; j < i1; ++j) {
+        const PagedShare s = share(j);
+        const int n = s.groups * s.splits;
+        if (y < at + n) {
+          found_s[0] = j; found_s[1] = s.splits; found_s[2] = (int)at; found_s[3] = (int)(at_multi & 0xFFFFFFFF); found_s[4] = (int)(at_multi >> 32);
+          break;
+        }
+        at += n;
+        if (s.splits > 1) at_multi += ((long long)s.groups << 32) | (unsigned)n;
+      }
+    }
+    __syncthreads();
+    i = __builtin_amdgcn_readfirstlane(found_s[0]);
+    splits = found_s[1]; before = found_s[2]; slots = found_s[3]; multi = found_s[4];
+    q = paged_req(pv, cu, start, max_new, i);
+  }
+  // the same in every lane: in scalar registers from here on
+  kps = __builtin_amdgcn_readfirstlane(kps);
+  splits = __builtin_amdgcn_readfirstlane(splits);
+  before = __builtin_amdgcn_readfirstlane(before);
+  slots = __builtin_amdgcn_readfirstlane(slots);
+  multi = __builtin_amdgcn_readfirstlane(multi);
+  q = PagedReq{__builtin_amdgcn_readfirstlane(q.first), __builtin_amdgcn_readfirstlane(q.n), __builtin_amdgcn_readfirstlane(q.start)};
+  const int rel = y - before, group = (int)((unsigned)rel / (unsigned)splits);
+  it.req = i;
+  it.first = q.first;
+  it.row0 = group * rpb;
+  it.r = min(rpb, q.n - it.row0);
+  it.pos0 = q.start + it.row0;
+  it.split = rel - group * splits;
+  it.kb = it.split * kps;
+  const int end = it.pos0 + it.r;                   // the group's last row sees the keys in front of this
+  it.ke = min(end, it.kb + kps);
+  it.n = (int)((unsigned)(end + kps - 1) / (unsigned)kps);      // of the request's ranges, those the group sees
+  it.slot = slots + group * splits;
+  it.group = multi + group;
+  return it.kb < it.ke;
+}
+
+// The end of a block whose group has several ranges: `write` has stored the block's partial results in its slot; the last of the group's blocks joins
+// all of them.  o: QVT x HD sums relative to the maximum m (powers of two), l: sum of weights; out = sum 2^(m - M) o / sum 2^(m - M) l.
+// The counter's block sees what the others wrote before they counted (a release by each, an acquire by the last).
+template <int HD, int QVT, int NT, typename STORE>
+__device__ __forceinline__ void paged_join(const PagedWork& w, const PagedItem& it, int nkv, int g, int QV, STORE store) {
+  __shared__ int last_s;
+  __threadfence();
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    int* c = w.count + (size_t)it.group * nkv + g;
+    last_s = atomicAdd(c, 1) == it.n - 1;
+    if (last_s) *c = 0;
+  }
+  __syncthreads();
+  if (!last_s) return;
+  __threadfence();
+  constexpr size_t SLOT = (size_t)QVT * (HD + 2);
+  const float* part = w.part + ((size_t)it.slot * nkv + g) * SLOT;
+  const size_t step = (size_t)nkv * SLOT;
+  // a thread takes 4 dims of a vector; the ranges' weights are worked out once a vector, by the HD / 4 threads that share it
+  constexpr int T4 = HD / 4, PER = NT / T4;
+  const int tid = threadIdx.x, d = (tid % T4) * 4, lane4 = tid % T4;
+  for (int q0 = 0; q0 < QV; q0 += PER) {
+    const int qv = q0 + tid / T4;
+    const bool on = qv < QV;
+    const float* ml = part + (size_t)QVT * HD + 2 * (on ? qv : 0);
+    const float* po = part + (size_t)(on ? qv : 0) * HD + d;
+    float m = -INFINITY;
+    for (int s = lane4; s < it.n; s += T4) m = fmaxf(m, ml[s * step]);
+#pragma unroll
+    for (int o = 1; o < T4; o <<= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+    const float mu = m == -INFINITY ? 0.f : m;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    float l = 0.f;
+    for (int s0 = 0; s0 < it.n; s0 += T4) {
+      const int s = s0 + lane4;
+      const float2 mine = s < it.n ? *(const float2*)(ml + s * step) : make_float2(-INFINITY, 0.f);
+      const float f = __builtin_amdgcn_exp2f(mine.x - mu);
+      l += f * mine.y;
+      const int n = min(T4, it.n - s0);
+#pragma unroll 8
+      for (int j = 0; j < n; ++j) {
+        const float fj = __shfl(f, (tid & 63 & ~(T4 - 1)) + j, 64);
+        acc += fj * *(const f32x4*)(po + (size_t)(s0 + j) * step);
+      }
+    }
+#pragma unroll
+    for (int o = 1; o < T4; o <<= 1) l += __shfl_xor(l, o, 64);
+    if (on) {
+      const float inv = l == 0.f ? 0.f : 1.0f / l;
+      store(qv, d, f32x4{acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv});
+    }
+  }
+}
+
+// Four values of one head from dim d on, rounded once
+template <bool PLANES>
+__device__ __forceinline__ void paged_store4(const PagedOut& o, int row, int col, const f32x4& v) {
+  if (PLANES) {
+    const size_t at = packed_at(o.blocked, row, col, (int)o.ld);
+    const uint2 h = make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
+    *(uint2*)((bf16_t*)o.out + at) = h;
+    *(uint2*)(o.lo + at) = make_uint2(pack_bf16x2(v.x - __uint_as_float(h.x << 16), v.y - __uint_as_float(h.x & 0xFFFF0000u)),
+                                      pack_bf16x2(v.z - __uint_as_float(h.y << 16), v.w - __uint_as_float(h.y & 0xFFFF0000u)));
+  } else {
+    *(uint2*)((bf16_t*)o.out + (size_t)row * o.ld + col) = make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
+  }
+}
+
+// Requests with few query vectors.  16 vectors of one KV head are the 16 columns of the matrix tiles, so a block reads each key and value once; its 4
+// waves take groups of 16 keys in turn, which never leave a page, the next group's loads in flight.  Per group, in one wave (lane: sl = lane % 16, kq = lane / 16):
+//   scores   S^T[key, q] = sum_d K[key, d] Q[q, d], 16x16x32: K rows as they lie in the cache, the queries as two bf16 parts (16 bits);
+//   output   O[q, d] += sum_key P[q, key] V[key, d], 16x16x16: a lane's operand is 4 consecutive keys of one row or column, so nothing moves between
+//            lanes; a probability goes in as two bf16 parts.
+// Bound by the memory: 8 KiB per wave and group against 2 x HD / 16 + 2 x HD / 32 products.
+template <int HD, bool PLANES>
+__global__ void __launch_bounds__(256, 4) paged_attention_few_mfma_kernel(const int* __restrict__ cu, const int* __restrict__ start, const float* __restrict__ qkv, long ld,
+                                                                  const bf16_t* __restrict__ q_gain, const float2* __restrict__ rope_tab, float eps, int max_new, int hi,
+                                                                  PagedOut po, PagedView pv, PagedWork wk) {
+  constexpr int QVT = 16, NW = 4, NT = 64 * NW, KS = HD / 32, DPL = HD / 16, half = HD / 2, HL = HD / 32;
+  typedef unsigned int vraw_t __attribute__((ext_vector_type(DPL / 2)));
+  typedef float fvec_t __attribute__((ext_vector_type(HL)));
+  typedef unsigned short hvec_t __attribute__((ext_vector_type(HL)));
+  const int g = blockIdx.x, GQ = pv.nh / pv.nkv, rpb = QVT / GQ;
+  PagedItem it;
+  if (!paged_find<NT, 16 * NW>(pv, cu, start, max_new, GQ, 0, hi, rpb, wk.shift, PAGED_KEYS_FEW, blockIdx.y, it)) return;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), sl = lane & 15, kq = lane >> 4;
+  const int QV = it.r * GQ, ke = it.ke;
+  __shared__ float wm[NW][QVT], wl[NW][QVT];
+  __shared__ int poison_s;
+  extern __shared__ float4 paged_dyn_smem[];
+  float* wacc = (float*)paged_dyn_smem;                       // [NW][QV][HD], in the place of the queries' two parts when these are done with
+  bf16_t (*qhi_s)[HD + ATT_QPAD] = (bf16_t (*)[HD + ATT_QPAD])paged_dyn_smem, (*qlo_s)[HD + ATT_QPAD] = qhi_s + QVT;
+  // pages of this wave's next 64 groups, one a lane
+  const int* trow = pv.table + (size_t)it.req * pv.max_pages;
+  auto load_pages = [&](int base) { return base + 64 * lane < ke ? trow[(base + 64 * lane) >> pv.page_shift] : 0; };
+  const int first = it.kb + 16 * wave;
+  int pages = load_pages(first);
+  // query vector tid / 16, 2 HL values a lane
+  fvec_t xa, xb;
+  const int qv = tid >> 4, l16 = tid & 15, qrow = it.row0 + (qv < QV ? qv / GQ : 0), qhead = g * GQ + (qv < QV ? qv % GQ : 0);
+  {
+    const float* src = qkv + (size_t)(it.first + qrow) * ld + (size_t)qhead * HD + HL * l16;
+    xa = *(const fvec_t*)src; xb = *(const fvec_t*)(src + half);
+  }
+  if (tid == 0) poison_s = INT_MAX;
+  u32x4 kr[KS];
+  vraw_t vr[4];
+  bool ok;
+  auto load_kv = [&](int base, int page) {
+    ok = page >= 0 && page < pv.n_pages;
+    const size_t at = (size_t)(ok ? page : 0) * pv.page_stride + (((size_t)g << pv.page_shift) + (base & ((1 << pv.page_shift) - 1))) * HD;
+    const bf16_t* kp = (const bf16_t*)pv.k + at;
+    const bf16_t* vp = (const bf16_t*)pv.v + at;
+#pragma unroll
+    for (int t = 0; t < KS; ++t) kr[t] = __builtin_nontemporal_load((const u32x4*)(kp + sl * HD + 32 * t + 8 * kq));
+#pragma unroll
+    for (int m = 0; m < 4; ++m) vr[m] = __builtin_nontemporal_load((const vraw_t*)(vp + (4 * kq + m) * HD + DPL * sl));
+  };
+  if (first < ke) load_kv(first, __builtin_amdgcn_readlane(pages, 0));
+  {
+    const int pos = it.pos0 + (qrow - it.row0);
+    float x0[HL], x1[HL], ss = 0.f;
+#pragma unroll
+    for (int e = 0; e < HL; ++e) { x0[e] = xa[e]; x1[e] = xb[e]; ss += x0[e] * x0[e] + x1[e] * x1[e]; }
+    if (q_gain) {
+      const hvec_t g0 = *(const hvec_t*)(q_gain + HL * l16), g1 = *(const hvec_t*)(q_gain + half + HL * l16);
+      const float rs = rsqrtf(row16_sum(ss) / (float)HD + eps);
+#pragma unroll
+      for (int e = 0; e < HL; ++e) { x0[e] *= rs * bf16_to_f32(g0[e]); x1[e] *= rs * bf16_to_f32(g1[e]); }
+    }
+    if (rope_tab) {
+      const float2* rp = rope_tab + (size_t)pos * half + HL * l16;
+#pragma unroll
+      for (int e = 0; e < HL; ++e) {
+        const float2 cs = rp[e];
+        const float a = x0[e], b = x1[e];
+        x0[e] = a * cs.x - b * cs.y;
+        x1[e] = b * cs.x + a * cs.y;
+      }
+    }
+    const float scale = rsqrtf((float)HD) * 1.4426950408889634f;
+    hvec_t h0, h1, l0, l1;
+#pragma unroll
+    for (int e = 0; e < HL; ++e) {
+      bf16_t h, l;
+      split_bf16(qv < QV ? x0[e] * scale : 0.f, h, l); h0[e] = h; l0[e] = l;
+      split_bf16(qv < QV ? x1[e] * scale : 0.f, h, l); h1[e] = h; l1[e] = l;
+    }
+    *(hvec_t*)&qhi_s[qv][HL * l16] = h0; *(hvec_t*)&qhi_s[qv][half + HL * l16] = h1;
+    *(hvec_t*)&qlo_s[qv][HL * l16] = l0; *(hvec_t*)&qlo_s[qv][half + HL * l16] = l1;
+  }
+  __syncthreads();
+  const int my_pos = it.pos0 + sl / GQ;
+  float m_run = -INFINITY, l_run = 0.f;
+  f32x4 acc[DPL];
+#pragma unroll
+  for (int e = 0; e < DPL; ++e) acc[e] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int base = first, j = 0; base < ke; base += 16 * NW, ++j) {
+    u32x4 ka[KS];
+    vraw_t va[4];
+    const bool here = ok;
+#pragma unroll
+    for (int t = 0; t < KS; ++t) ka[t] = kr[t];
+#pragma unroll
+    for (int m = 0; m < 4; ++m) va[m] = vr[m];
+    const int next = base + 16 * NW;
+    if (next < ke) {
+      if ((j & 63) == 63) pages = load_pages(next);
+      load_kv(next, __builtin_amdgcn_readlane(pages, (j + 1) & 63));
+    }
+    if (!here) continue;                                      // a page outside the pool
+    f32x4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int t = 0; t < KS; ++t) {
+      const bf16x8_t ql = __builtin_bit_cast(bf16x8_t, *(const u32x4*)&qlo_s[sl][32 * t + 8 * kq]), qh = __builtin_bit_cast(bf16x8_t, *(const u32x4*)&qhi_s[sl][32 * t + 8 * kq]);
+      s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, ka[t]), ql, s, 0, 0, 0);
+      s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, ka[t]), qh, s, 0, 0, 0);
+    }
+    float sc[4] = {s.x, s.y, s.z, s.w};
+    if (base + 16 > it.pos0 + 1) {
+      // Keys that some row does not see: their scores are out; values behind the last key are whatever lies there, and values of the group's own
+      // positions may be infinite or NaN, which a probability of 0 would not silence: both go in as 0, and the rows that see such a one become NaN
+#pragma unroll
+      for (int m = 0; m < 4; ++m) {
+        const int key = base + 4 * kq + m;
+        if (key > my_pos || key >= ke) sc[m] = -INFINITY;
+        if (key > it.pos0) {
+          bool bad = false;
+#pragma unroll
+          for (int u = 0; u < DPL / 2; ++u) bad |= (va[m][u] & 0x7F80u) == 0x7F80u || (va[m][u] & 0x7F800000u) == 0x7F800000u;
+          if (bad && key < ke) atomicMin(&poison_s, key);
+          if (bad || key >= ke) {
+#pragma unroll
+            for (int u = 0; u < DPL / 2; ++u) va[m][u] = 0u;
+          }
+        }
+      }
+    }
+    float mx = fmaxf(fmaxf(sc[0], sc[1]), fmaxf(sc[2], sc[3]));
+    mx = column_max(mx);
+    const float m_new = fmaxf(m_run, mx), m_use = m_new == -INFINITY ? 0.f : m_new;
+    const float f = __builtin_amdgcn_exp2f(m_run - m_use);
+    float p[4];
+    float psum = 0.f;
+#pragma unroll
+    for (int m = 0; m < 4; ++m) { p[m] = __builtin_amdgcn_exp2f(sc[m] - m_use); psum += p[m]; }
+    l_run = l_run * f + psum;
+    if (__any(m_new > m_run)) {                               // the sums this lane holds are those of queries 4 kq + j
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const float fq = __shfl(f, 4 * kq + q, 64);
+#pragma unroll
+        for (int e = 0; e < DPL; ++e) acc[e][q] *= fq;
+      }
+    }
+    m_run = m_new;
+    uint2 ph, pl;
+    ph.x = pack_bf16x2(p[0], p[1]);
+    ph.y = pack_bf16x2(p[2], p[3]);
+    pl.x = pack_bf16x2(p[0] - __uint_as_float(ph.x << 16), p[1] - __uint_as_float(ph.x & 0xFFFF0000u));
+    pl.y = pack_bf16x2(p[2] - __uint_as_float(ph.y << 16), p[3] - __uint_as_float(ph.y & 0xFFFF0000u));
+#pragma unroll
+    for (int e = 0; e < DPL; ++e) {
+      const unsigned int sel = (e & 1) ? 0x07060302u : 0x05040100u;
+      const uint2 v4 = make_uint2(__builtin_amdgcn_perm(va[1][e >> 1], va[0][e >> 1], sel), __builtin_amdgcn_perm(va[3][e >> 1], va[2][e >> 1], sel));
+      acc[e] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(bf16x4s_t, pl), __builtin_bit_cast(bf16x4s_t, v4), acc[e], 0, 0, 0);
+      acc[e] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(bf16x4s_t, ph), __builtin_bit_cast(bf16x4s_t, v4), acc[e], 0, 0, 0);
+    }
+  }
+  // the waves' results of a vector, 4 consecutive dims a thread
+  l_run = column_sum(l_run);
+  __syncthreads();
+  if (kq == 0 && sl < QV) { wm[wave][sl] = m_run; wl[wave][sl] = l_run; }
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    if (4 * kq + q < QV) {
+      float* dst = wacc + ((size_t)wave * QV + 4 * kq + q) * HD + DPL * sl;
+#pragma unroll
+      for (int e = 0; e < DPL; ++e) dst[e] = acc[e][q];
+    }
+  }
+  __syncthreads();
+  constexpr size_t SLOT = (size_t)QVT * (HD + 2);
+  float* part = wk.part + ((size_t)(it.slot + it.split) * pv.nkv + g) * SLOT;
+  auto store = [&](int v, int d, const f32x4& x) { paged_store4<PLANES>(po, it.first + it.row0 + v / GQ, (g * GQ + v % GQ) * HD + d, x); };
+  for (int e = tid; e < QV * (HD / 4); e += NT) {
+    const int v = e / (HD / 4), d = (e % (HD / 4)) * 4;
+    float mm = wm[0][v];
+#pragma unroll
+    for (int w = 1; w < NW; ++w) mm = fmaxf(mm, wm[w][v]);
+    const float mu = mm == -INFINITY ? 0.f : mm;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    float l = 0.f;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      const float fw = __builtin_amdgcn_exp2f(wm[w][v] - mu);
+      o += fw * *(const f32x4*)(wacc + ((size_t)w * QV + v) * HD + d);
+      l += fw * wl[w][v];
+    }
+    if (it.pos0 + v / GQ >= poison_s) l = __uint_as_float(0x7FC00000u);
+    if (it.n == 1) {
+      const float inv = l == 0.f ? 0.f : 1.0f / l;
+      store(v, d, f32x4{o.x * inv, o.y * inv, o.z * inv, o.w * inv});
+    } else {
+      *(f32x4*)(part + (size_t)v * HD + d) = o;
+      if (d == 0) *(float2*)(part + (size_t)QVT * HD + 2 * v) = make_float2(mm, l);
+    }
+  }
+  if (it.n > 1) paged_join<HD, QVT, NT>(wk, it, pv.nkv, g, QV, store);
+}
+
+// Requests with many query vectors (chunks of a prompt).  A block takes 128 vectors of one KV head - 128 / GQ rows x the GQ query heads that share it, 32 per
+// wave - and walks its range of keys in tiles of 64 through LDS.  Per tile and wave, with 32x32x16 products:
+//   scores   S^T[key, q]: K rows from LDS, the queries in registers as two bf16 parts; a lane ends up with 16 keys of one vector per 32 keys;
+//   output   O^T[d, q] += sum_key V^T[d, key] P^T[key, q]: a lane's own probabilities are the operand as they stand, V^T comes from LDS; a
+//            probability goes in as two bf16 parts (16 bits, as the planes that the O projection reads keep).
+// K goes from the pages straight into LDS, a wave 16 keys of a tile (one page), rows' 16-byte chunks permuted by the key number; V through registers, transposed
+// on the way (4 keys x HD / 16 dims per thread; 8-byte pieces permuted by the dim).  Two buffers of each: the next tile's loads fly during
+// a tile, and a tile's page numbers are fetched a tile earlier still, one per 4 keys and lane.
+// The products run over whole tiles: keys behind the block's last row are that row's key again (its value is finite or poisoned), with probability 0.  Values of the
+// block's own positions may be infinite or NaN, which 0 does not silence: the block looks at them first; if one is not finite, it and its like behind
+// it go into LDS as 0 and the rows that see it become NaN.
+template <int HD, bool PLANES>
+__global__ void __launch_bounds__(256, 2) paged_attention_tall_mfma_kernel(const int* __restrict__ cu, const int* __restrict__ start, const float* __restrict__ qkv, long ld,
+                                                                           const bf16_t* __restrict__ q_gain, const float2* __restrict__ rope_tab, float eps, int max_new, int lo,
+                                                                           PagedOut po, PagedView pv, PagedWork wk) {
+  constexpr int QVT = 128, NT = 256, KT = 64;
+  constexpr int T = HD / 16;           // steps over d for the scores
+  constexpr int DT = HD / 32;          // 32-dim tiles of the output
+  constexpr int DV = HD / 16;          // dims of V a thread carries
+  constexpr int CH = HD / 8;           // 16-byte chunks of a K row
+  constexpr int KI = KT * CH / 256;    // K pieces (16 bytes per lane) per wave and tile
+  constexpr int TILE = KT * HD;
+  typedef unsigned int vraw_t __attribute__((ext_vector_type(DV / 2)));
+  extern __shared__ float4 paged_dyn_smem[];
+  __shared__ int poison_s;
+  const int g = blockIdx.x, GQ = pv.nh / pv.nkv, rpb = QVT / GQ;
+  PagedItem it;
+  if (!paged_find<NT, KT>(pv, cu, start, max_new, GQ, lo, INT_MAX, rpb, wk.shift, PAGED_KEYS_TALL, blockIdx.y, it)) return;
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), hi = lane >> 5;
+  bf16_t* ring = (bf16_t*)paged_dyn_smem;                      // K, K, V^T, V^T
+  const int QV = it.r * GQ, qv = 32 * w + (lane & 31), kb = it.kb, ke = it.ke;
+  const bool valid = qv < QV;
+  const int row = it.row0 + (valid ? qv / GQ : 0), head = g * GQ + (valid ? qv % GQ : 0), my_pos = it.pos0 + (row - it.row0);
+  const int* trow = pv.table + (size_t)it.req * pv.max_pages;
+  const int in_page = (1 << pv.page_shift) - 1;
+
+  // the page of this lane's 4 keys of a tile (the last key's where they lie behind it)
+  auto load_pages = [&](int base) { return trow[min(base + 4 * (lane & 15), ke - 1) >> pv.page_shift]; };
+  auto outside = [&](int page) { return page < 0 || page >= pv.n_pages; };
+  // K: piece i of the wave's 16 keys holds 64 / CH of them, a chunk of one per lane, permuted by the key number
+  auto load_k = [&](int ln, int base, int page, int buf, int i) {
+    static_assert(64 / CH <= CH && KI * (64 / CH) == 16, "a wave's pieces are 16 keys, and a piece's permutation is that of piece 0, exclusive-or its first key");
+    const int pg = __builtin_amdgcn_readlane(page, 4 * w), k0 = ln / CH, c0 = (ln % CH) ^ k0, ki = (w * KI + i) * (64 / CH);
+    const bf16_t* src = (const bf16_t*)pv.k + (size_t)(outside(pg) ? 0 : pg) * pv.page_stride + (((size_t)g << pv.page_shift) + ((base + 16 * w) & in_page)) * HD;
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(src + (uint32_t)((i * (64 / CH) + k0) * HD + (c0 ^ (ki & (CH - 1))) * 8)),
+                                     (__attribute__((address_space(3))) void*)(ring + buf * TILE + (w * KI + i) * 512), 16, 0, 0);
+  };
+  const int kgp = lane & 15, dg = w * 4 + (lane >> 4), vslot = 2 * (kgp >> 2) + (kgp & 1), vhalf = ((kgp >> 1) & 1) * 4;
+  vraw_t vr[4];
+  auto load_v = [&](int ln, int base, int page, int m) {
+    const int key = min(base + 4 * (ln & 15), ke - 1);
+    const bf16_t* src = (const bf16_t*)pv.v + (size_t)(outside(page) ? 0 : page) * pv.page_stride + (uint32_t)(((g << pv.page_shift) + (key & in_page)) * HD + (w * 4 + (ln >> 4)) * DV);
+    vr[m] = *(const vraw_t*)(src + min(m, ke - 1 - key) * HD);
+  };
+  // values of pages outside the pool become 0; so do those from poison_s on that are not finite
+  auto clean_v = [&](int base, int page, bool drop) {
+#pragma unroll
+    for (int m = 0; m < 4; ++m) {
+      if (outside(page)) {
+#pragma unroll
+        for (int u = 0; u < DV / 2; ++u) vr[m][u] = 0u;
+      } else if (drop && min(base + 4 * kgp + m, ke - 1) >= poison_s) {
+#pragma unroll
+        for (int u = 0; u < DV / 2; ++u)
+          vr[m][u] = ((vr[m][u] & 0x7F80u) == 0x7F80u ? 0u : vr[m][u] & 0xFFFFu) | ((vr[m][u] & 0x7F800000u) == 0x7F800000u ? 0u : vr[m][u] & 0xFFFF0000u);
+      }
+    }
+  };
+  auto store_v = [&](int buf) {
+#pragma unroll
+    for (int u = 0; u < DV / 2; ++u)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int d = dg * DV + 2 * u + h;
+        const unsigned int s = h ? 0x07060302u : 0x05040100u;
+        *(uint2*)(ring + (2 + buf) * TILE + d * KT + ((vslot ^ ((d >> 1) & 7)) * 8 + vhalf)) =
+            make_uint2(__builtin_amdgcn_perm(vr[1][u], vr[0][u], s), __builtin_amdgcn_perm(vr[3][u], vr[2][u], s));
+      }
+  };
+  const int n_tiles = (ke - kb + KT - 1) / KT;
+  int pages = load_pages(kb), pages_next = load_pages(kb + KT);
+  if (tid == 0) poison_s = INT_MAX;
+
+  // the lane's query vector: dims 16 t + 8 hi + 0..7; its rotary partner dims (i, i + HD/2) are the lane's own
+  bf16x8_t qh[T], ql[T];
+  {
+    float x[T][8];
+    const float* src = qkv + (size_t)(it.first + row) * ld + (size_t)head * HD + 8 * hi;
+    float ss = 0.f;
+#pragma unroll
+    for (int t = 0; t < T; ++t) {
+      const f32x4 a = *(const f32x4*)(src + 16 * t), c = *(const f32x4*)(src + 16 * t + 4);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) { x[t][e] = a[e]; x[t][4 + e] = c[e]; }
+    }
+#pragma unroll
+    for (int i = 0; i < KI; ++i) load_k(lane, kb, pages, 0, i);
+#pragma unroll
+    for (int m = 0; m < 4; ++m) load_v(lane, kb, pages, m);
+#pragma unroll
+    for (int t = 0; t < T; ++t)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) ss += x[t][e] * x[t][e];
+    ss = pair_sum<32>(ss);
+    const float scale = rsqrtf((float)HD) * 1.4426950408889634f;
+    if (q_gain) {
+      const float rs = rsqrtf(ss / (float)HD + eps);
+#pragma unroll
+      for (int t = 0; t < T; ++t) {
+        float gn[8];
+        Elem<bf16_t>::unpack(*(const u32x4*)(q_gain + 16 * t + 8 * hi), gn);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[t][e] *= rs * gn[e];
+      }
+    }
+    if (rope_tab) {
+      const float2* rp = rope_tab + (size_t)my_pos * (HD / 2) + 8 * hi;
+#pragma unroll
+      for (int t = 0; t < T / 2; ++t)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float2 cs = rp[16 * t + e];
+          const float a = x[t][e], b = x[t + T / 2][e];
+          x[t][e] = a * cs.x - b * cs.y;
+          x[t + T / 2][e] = b * cs.x + a * cs.y;
+        }
+    }
+#pragma unroll
+    for (int t = 0; t < T; ++t) {
+      uint32_t h4[4], l4[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float a = x[t][2 * e] * scale, b = x[t][2 * e + 1] * scale;
+        h4[e] = pack_bf16x2(a, b);
+        l4[e] = pack_bf16x2(a - __uint_as_float(h4[e] << 16), b - __uint_as_float(h4[e] & 0xFFFF0000u));
+      }
+      qh[t] = __builtin_bit_cast(bf16x8_t, u32x4{h4[0], h4[1], h4[2], h4[3]});
+      ql[t] = __builtin_bit_cast(bf16x8_t, u32x4{l4[0], l4[1], l4[2], l4[3]});
+    }
+  }
+  float m_run = -INFINITY, l_run = 0.f;
+  f32x16 acc[DT];
+#pragma unroll
+  for (int t = 0; t < DT; ++t)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) acc[t][e] = 0.f;
+  __syncthreads();
+  // values at positions that some row of the block does not see, 16 bytes each: is one of them not finite?
+  for (int c = tid; c < (ke - max(it.pos0 + 1, kb)) * CH; c += NT) {
+    const int key = max(it.pos0 + 1, kb) + c / CH, page = trow[key >> pv.page_shift];
+    if (outside(page)) continue;
+    const u32x4 v = *(const u32x4*)((const bf16_t*)pv.v + (size_t)page * pv.page_stride + (((size_t)g << pv.page_shift) + (key & in_page)) * HD + c % CH * 8);
+    bool bad = false;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) bad |= (v[u] & 0x7F80u) == 0x7F80u || (v[u] & 0x7F800000u) == 0x7F800000u;
+    if (bad) atomicMin(&poison_s, key);
+  }
+  __syncthreads();
+  const int poison = __builtin_amdgcn_readfirstlane(poison_s);
+  const bool drop = poison != INT_MAX;
+  if (drop || __any(outside(pages))) clean_v(kb, pages, drop);
+  store_v(0);
+  __syncthreads();
+
+  for (int tl = 0; tl < n_tiles; ++tl) {
+    const int buf = tl & 1, base = kb + tl * KT, ahead = base + KT;
+    const bool more = tl + 1 < n_tiles;
+    const unsigned long long missing = __ballot(outside(pages));
+    const int pages_after = more ? load_pages(ahead + KT) : 0;
+    // Fragment offsets: chunk 2 t + hi of a K row and slot 2 q + hi of a V^T row, permuted, differ from chunk and slot hi by an exclusive or
+    int ko = (lane & 31) * HD + ((hi ^ (lane & (CH - 1))) << 3), vo = (lane & 31) * KT + ((hi ^ ((lane >> 1) & 7)) << 3), ln = lane;
+    asm volatile("" : "+v"(ko), "+v"(vo), "+v"(ln));
+    const bf16_t* kbuf = ring + buf * TILE;
+    const bf16_t* vbuf = ring + (2 + buf) * TILE;
+    auto read_k = [&](int k, int t) { return __builtin_bit_cast(bf16x8_t, *(const u32x4*)(kbuf + (ko ^ (t << 4)) + k * 32 * HD)); };
+    auto read_v = [&](int q, int t) { return __builtin_bit_cast(bf16x8_t, *(const u32x4*)(vbuf + (vo ^ (q << 4)) + t * 32 * KT)); };
+    // scores (in units of log2) of keys base + 32 k + 8 (e / 4) + 4 hi + e % 4 for the lane's query
+    f32x16 s[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[k][e] = 0.f;
+    bf16x8_t kf[2][2];
+    kf[0][0] = read_k(0, 0);
+    kf[0][1] = read_k(1, 0);
+    auto scores = [&](auto more_c) {
+      constexpr int LD = decltype(more_c)::value ? KI + 4 : 0;          // loads of the next tile, shared out over the steps
+#pragma unroll
+      for (int t = 0; t < T; ++t) {
+        if (t + 1 < T) {
+          kf[(t + 1) & 1][0] = read_k(0, t + 1);
+          kf[(t + 1) & 1][1] = read_k(1, t + 1);
+        }
+        s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[t & 1][0], ql[t], s[0], 0, 0, 0);
+        s[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[t & 1][1], ql[t], s[1], 0, 0, 0);
+#pragma unroll
+        for (int z = t * LD / T; z < (t + 1) * LD / T; ++z) {
+          if (z < KI) load_k(ln, ahead, pages_next, buf ^ 1, z);
+          else load_v(ln, ahead, pages_next, z - KI);
+        }
+        s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[t & 1][0], qh[t], s[0], 0, 0, 0);
+        s[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[t & 1][1], qh[t], s[1], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    };
+    if (more) scores(std::integral_constant<bool, true>());
+    else scores(std::integral_constant<bool, false>());
+    bf16x8_t vf[2];
+    vf[0] = read_v(0, 0);
+    if (base + KT > it.pos0 + 1) {      // keys beyond some row's position in this tile
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (base + 32 * k + 8 * (e >> 2) + 4 * hi + (e & 3) > my_pos) s[k][e] = -INFINITY;
+    }
+    if (missing) {                      // pages outside the pool: bit 8 k + 2 (e / 4) + hi is the group of 4 keys
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if ((missing >> (8 * k + 2 * (e >> 2) + hi)) & 1) s[k][e] = -INFINITY;
+    }
+    float mx = s[0][0];
+#pragma unroll
+    for (int e = 1; e < 16; ++e) mx = fmaxf(mx, s[0][e]);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[1][e]);
+    mx = pair_max<32>(mx);
+    const float m_new = fmaxf(m_run, mx), m_use = m_new == -INFINITY ? 0.f : m_new;
+    if (__any(m_new > m_run)) {
+      const float f = __builtin_amdgcn_exp2f(m_run - m_use);
+      l_run *= f;
+#pragma unroll
+      for (int t = 0; t < DT; ++t)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[t][e] *= f;
+      m_run = m_new;
+    }
+    // the 8 probabilities of a contraction step q as two bf16 parts, pair j of them in two pieces
+    uint32_t pp[2][2][4];
+    auto piece = [&](int q, int j, int z) {
+      const int e = 8 * (q & 1) + 2 * j;
+      const float a = s[q >> 1][e], d = s[q >> 1][e + 1];
+      if (z == 0) {
+        s[q >> 1][e] = __builtin_amdgcn_exp2f(a - m_use);
+        s[q >> 1][e + 1] = __builtin_amdgcn_exp2f(d - m_use);
+      } else {
+        l_run += a;
+        l_run += d;
+        const uint32_t h = pack_bf16x2(a, d);
+        pp[q & 1][0][j] = h;
+        pp[q & 1][1][j] = pack_bf16x2(a - __uint_as_float(h << 16), d - __uint_as_float(h & 0xFFFF0000u));
+      }
+    };
+    constexpr int PG = 4 / DT;          // pairs of the next step beside a V fragment's two products
+#pragma unroll
+    for (int z = 0; z < 2; ++z)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) piece(0, j, z);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+#pragma unroll
+      for (int t = 0; t < DT; ++t) {
+        const int n = q * DT + t;
+        if (n + 1 < 4 * DT) vf[(n + 1) & 1] = read_v((n + 1) / DT, (n + 1) % DT);
+#pragma unroll
+        for (int z = 0; z < 2; ++z) {
+          const uint32_t* f = pp[q & 1][1 - z];
+          acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[n & 1], __builtin_bit_cast(bf16x8_t, u32x4{f[0], f[1], f[2], f[3]}), acc[t], 0, 0, 0);
+          if (q < 3) {
+#pragma unroll
+            for (int j = 0; j < PG; ++j) piece(q + 1, t * PG + j, z);
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+    }
+    if (more) {
+      if (drop || __any(outside(pages_next))) clean_v(ahead, pages_next, drop);
+      store_v(buf ^ 1);
+    }
+    pages = pages_next;
+    pages_next = pages_after;
+    __builtin_amdgcn_s_waitcnt(7 << 4);      // vmcnt(0) lgkmcnt(0): this wave's share of the next tile has landed
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  }
+  l_run = pair_sum<32>(l_run);
+  // where the vector goes, worked out anew: kept through the loop it would be spilled
+  int ln = lane;
+  asm volatile("" : "+v"(ln));
+  const int qo = 32 * w + (ln & 31), ro = it.row0 + qo / GQ, co = (g * GQ + qo % GQ) * HD + 4 * (ln >> 5);
+  if (it.pos0 + qo / GQ >= poison) l_run = __uint_as_float(0x7FC00000u);
+  constexpr size_t SLOT = (size_t)QVT * (HD + 2);
+  if (it.n == 1) {
+    if (qo < QV) {
+      const float inv = l_run == 0.f ? 0.f : 1.0f / l_run;
+#pragma unroll
+      for (int t = 0; t < DT; ++t)
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          paged_store4<PLANES>(po, it.first + ro, co + 32 * t + 8 * q, f32x4{acc[t][4 * q] * inv, acc[t][4 * q + 1] * inv, acc[t][4 * q + 2] * inv, acc[t][4 * q + 3] * inv});
+    }
+    return;
+  }
+  float* part = wk.part + ((size_t)(it.slot + it.split) * pv.nkv + g) * SLOT;
+  if (qo < QV) {
+#pragma unroll
+    for (int t = 0; t < DT; ++t)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) *(f32x4*)(part + (size_t)qo * HD + 32 * t + 8 * q + 4 * (ln >> 5)) = f32x4{acc[t][4 * q], acc[t][4 * q + 1], acc[t][4 * q + 2], acc[t][4 * q + 3]};
+    if (ln < 32) *(float2*)(part + (size_t)QVT * HD + 2 * qo) = make_float2(m_run, l_run);
+  }
+  paged_join<HD, QVT, NT>(wk, it, pv.nkv, g, QV,
+                          [&](int v, int d, const f32x4& x) { paged_store4<PLANES>(po, it.first + it.row0 + v / GQ, (g * GQ + v % GQ) * HD + d, x); });
 }
 
 // One block per (row, query head); its 4 waves take 64 keys each in turn, a lane scores one key and then carries HD / 64 dims of the output.

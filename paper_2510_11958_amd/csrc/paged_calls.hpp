@@ -89,14 +89,78 @@ void launch_paged_append(const PagedView& v, int head_dim, const float* qkv, lon
     hipLaunchKernelGGL((paged_append_kernel<CT, 64>), grid, dim3(256), 0, s, qkv, ld, cu, row_pos, (const long long*)slots, (const CT*)gain, (const float2*)rope, eps, v);
 }
 
-template <typename CT>
-void launch_paged_attention(const PagedView& v, int head_dim, const float* qkv, long ld, const int* start, const int* cu, int max_new, const void* gain, float eps,
-                            const float* rope, void* out, long ldo, hipStream_t s) {
-  const dim3 grid(v.max_rows, v.nh);
-  if (head_dim == 128)
-    hipLaunchKernelGGL((paged_attention_rows_kernel<CT, 128>), grid, dim3(256), 0, s, qkv, ld, start, cu, (const CT*)gain, (const float2*)rope, eps, max_new, (CT*)out, ldo, v);
-  else
-    hipLaunchKernelGGL((paged_attention_rows_kernel<CT, 64>), grid, dim3(256), 0, s, qkv, ld, start, cu, (const CT*)gain, (const float2*)rope, eps, max_new, (CT*)out, ldo, v);
+// How an attention call of a bf16 cache is laid out: blocks per KV head of either kernel (0: no launch), log2 of those that the key ranges are chosen
+// for, and the workspace: the counts of the groups with several ranges, then their partial results (paged_find), the larger of the two kernels'.
+struct PagedPlan { int few, tall, few_shift, tall_shift; size_t count_bytes, part_bytes; };
+int floor_log2(int v) { int s = 0; while ((2 << s) <= v) ++s; return s; }
+PagedPlan paged_plan(const dmtd_paged_cache* c, int max_new) {
+  PagedPlan p{};
+  if (c->dtype != DMTD_DTYPE_BF16) return p;
+  const int GQ = c->n_q_heads / c->n_kv_heads;
+  const long limit = (long)c->max_pages * c->page_size;
+  p.few_shift = floor_log2(std::max(PAGED_SLOTS_FEW / c->n_kv_heads, 1));
+  p.tall_shift = floor_log2(std::max(PAGED_SLOTS_TALL / c->n_kv_heads, 1));
+  auto blocks = [&](long groups, int shift, int min_keys) { return (int)std::min((1L << shift) + groups, groups * ((limit + min_keys - 1) / min_keys)); };
+  // a request with n rows is in ceil(n / rows of a group) groups
+  const long few_rows = std::min<long>(c->max_rows, max_new), all = std::min(c->n_req, c->max_rows);
+  const int rpb_few = 16 / GQ, rpb_tall = 128 / GQ, tall_from = PAGED_FEW / GQ + 1;
+  p.few = blocks(std::min<long>(c->max_rows, all + c->max_rows / rpb_few), p.few_shift, PAGED_KEYS_FEW);
+  size_t slot = (size_t)16 * (c->head_dim + 2) * 4 << p.few_shift;
+  if (few_rows >= tall_from) {
+    p.tall = blocks(std::min<long>(c->n_req, c->max_rows / tall_from) + c->max_rows / rpb_tall, p.tall_shift, PAGED_KEYS_TALL);
+    slot = std::max(slot, (size_t)128 * (c->head_dim + 2) * 4 << p.tall_shift);
+  }
+  p.count_bytes = align_up(((size_t)4 << std::max(p.few_shift, p.tall_shift)) * c->n_kv_heads, 256);
+  p.part_bytes = 2 * slot * c->n_kv_heads;
+  return p;
+}
+
+struct PagedCall {
+  const float* qkv; long ld;
+  const int *start, *cu;
+  int max_new;
+  const void* gain;
+  float eps;
+  const float* rope;
+  char* ws;
+  hipStream_t stream;
+};
+
+template <int HD, bool PLANES>
+hipError_t launch_paged_mfma(const PagedView& v, const PagedPlan& p, const PagedCall& a, const PagedOut& out) {
+  const int GQ = v.nh / v.nkv;
+  PagedWork wk{p.few_shift, (int*)a.ws, (float*)(a.ws + p.count_bytes)};
+  const int qv_max = std::min(16 / GQ, a.max_new) * GQ;
+  hipLaunchKernelGGL((paged_attention_few_mfma_kernel<HD, PLANES>), dim3(v.nkv, p.few), dim3(256), std::max((size_t)4 * qv_max * HD * 4, (size_t)2 * 16 * (HD + ATT_QPAD) * 2), a.stream, a.cu, a.start, a.qkv, a.ld, (const bf16_t*)a.gain,
+                     (const float2*)a.rope, a.eps, a.max_new, PAGED_FEW, out, v, wk);
+  if (p.tall > 0) {
+    wk.shift = p.tall_shift;
+    auto kern = paged_attention_tall_mfma_kernel<HD, PLANES>;
+    constexpr size_t lds = (size_t)4 * 64 * HD * 2;
+    static bool big_lds = false;
+    if (lds > 48 * 1024 && !big_lds) {
+      hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+      if (e != hipSuccess) return e;
+      big_lds = true;
+    }
+    hipLaunchKernelGGL(kern, dim3(v.nkv, p.tall), dim3(256), lds, a.stream, a.cu, a.start, a.qkv, a.ld, (const bf16_t*)a.gain, (const float2*)a.rope, a.eps, a.max_new, PAGED_FEW, out, v, wk);
+  }
+  return hipGetLastError();
+}
+
+template <int HD>
+hipError_t launch_paged_fp32(const PagedView& v, const PagedCall& a, const PagedOut& out) {
+  hipLaunchKernelGGL((paged_attention_rows_kernel<float, HD>), dim3(v.max_rows, v.nh), dim3(256), 0, a.stream, a.qkv, a.ld, a.start, a.cu, (const float*)a.gain, (const float2*)a.rope,
+                     a.eps, a.max_new, (float*)out.out, out.ld, v);
+  return hipGetLastError();
+}
+
+hipError_t launch_paged_attention(const dmtd_paged_cache* c, const PagedView& v, const PagedCall& a, const PagedOut& out) {
+  if (c->dtype == DMTD_DTYPE_BF16) {
+    const PagedPlan p = paged_plan(c, a.max_new);
+    return c->head_dim == 128 ? launch_paged_mfma<128, false>(v, p, a, out) : launch_paged_mfma<64, false>(v, p, a, out);
+  }
+  return c->head_dim == 128 ? launch_paged_fp32<128>(v, a, out) : launch_paged_fp32<64>(v, a, out);
 }
 
 }  // namespace
@@ -148,7 +212,8 @@ int dmtd_paged_append(const dmtd_paged_cache* c, const float* qkv, int64_t ld, c
 
 size_t dmtd_paged_workspace_bytes(const dmtd_paged_cache* c) {
   if (check_cache(c) != DMTD_OK) return 0;
-  return 256;
+  const PagedPlan p = paged_plan(c, c->max_rows);
+  return std::max<size_t>(256, p.count_bytes + p.part_bytes);
 }
 
 int dmtd_paged_attention(const dmtd_paged_cache* c, const float* qkv, int64_t ld, const int32_t* start, const int32_t* cu_rows, int32_t max_new,
@@ -167,9 +232,8 @@ int dmtd_paged_attention(const dmtd_paged_cache* c, const float* qkv, int64_t ld
   if ((rc = check_stream_device(s)) != DMTD_OK) return rc;
   const PagedView v = paged_view(c, rope, rope_len);
   if (max_new == 0) max_new = c->max_rows;
-  if (c->dtype == DMTD_DTYPE_BF16) launch_paged_attention<bf16_t>(v, c->head_dim, qkv, ld, start, cu_rows, max_new, q_norm, eps, rope, out, ldo, s);
-  else launch_paged_attention<float>(v, c->head_dim, qkv, ld, start, cu_rows, max_new, q_norm, eps, rope, out, ldo, s);
-  return paged_done();
+  const hipError_t e = launch_paged_attention(c, v, PagedCall{qkv, (long)ld, start, cu_rows, max_new, q_norm, eps, rope, (char*)workspace, s}, PagedOut{out, nullptr, (long)ldo, 0});
+  return e == hipSuccess ? DMTD_OK : paged_fail(DMTD_EHIP, hipGetErrorString(e));
 }
 
 }  // extern "C"
