@@ -144,15 +144,11 @@ __device__ __forceinline__ bool paged_find(const PagedView& pv, const int* cu, c
   return it.kb < it.ke;
 }
 
-// Partial results pass from block to block, maybe from die to die, whose L2 caches do not see each other's lines.  They are written through and read past
-// those caches, 8 bytes at a time, by relaxed atomics of the device's scope; a fence of that scope would write a whole L2 back for each block
-// (31 single tokens behind up to 2111 keys: 204 us with fences, us below).
+// Partial results pass from block to block, maybe from die to die, whose L2 caches do not see each other's lines.  They are written through
+// those caches, 8 bytes at a time, by relaxed atomics of the device's scope, and only the block that joins them has its die's caches drop what is stale; a
+// fence on the writers' side would write a whole L2 back for each block (31 single tokens behind up to 2111 keys: 204 us with such fences, 26 without).
 __device__ __forceinline__ void put_through(float* p, float a, float b) {
   __hip_atomic_store((unsigned long long*)p, ((unsigned long long)__float_as_uint(b) << 32) | __float_as_uint(a), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
-__device__ __forceinline__ float2 get_past(const float* p) {
-  const unsigned long long v = __hip_atomic_load((const unsigned long long*)p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  return make_float2(__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32)));
 }
 __device__ __forceinline__ void put_through4(float* p, const f32x4& v) { put_through(p, v.x, v.y); put_through(p + 2, v.z, v.w); }
 
@@ -160,53 +156,82 @@ __device__ __forceinline__ void put_through4(float* p, const f32x4& v) { put_thr
 // all of them.  o: QVT x HD sums relative to the maximum m (powers of two), l: sum of weights; out = sum 2^(m - M) o / sum 2^(m - M) l.
 // A wave waits for its writes before the block counts.
 template <int HD, int QVT, int NT, typename STORE>
-__device__ __forceinline__ void paged_join(const PagedWork& w, const PagedItem& it, int nkv, int g, int QV, STORE store) {
+__device__ __forceinline__ void paged_join(const PagedWork& w, const PagedItem& it, int nkv, int g, int QV, f32x4* sums /* LDS, NT of them */, STORE store) {
   __shared__ int last_s;
+  __shared__ float max_s[QVT], inv_s[QVT];
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
-  if (threadIdx.x == 0) {
+  const int tid = threadIdx.x;
+  if (tid == 0) {
     int* c = w.count + (size_t)it.group * nkv + g;
     last_s = __hip_atomic_fetch_add(c, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == it.n - 1;
     if (last_s) __hip_atomic_store(c, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   }
   __syncthreads();
   if (!last_s) return;
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");      // what this die's caches hold of the others' slots is stale
   constexpr size_t SLOT = (size_t)QVT * (HD + 2);
   const float* part = w.part + ((size_t)it.slot * nkv + g) * SLOT;
   const size_t step = (size_t)nkv * SLOT;
-  // a thread takes 4 dims of a vector; the ranges' weights are worked out once a vector, by the HD / 4 threads that share it
-  constexpr int T4 = HD / 4, PER = NT / T4;
-  const int tid = threadIdx.x, d = (tid % T4) * 4, lane4 = tid % T4;
-  for (int q0 = 0; q0 < QV; q0 += PER) {
-    const int qv = q0 + tid / T4;
-    const bool on = qv < QV;
-    const float* ml = part + (size_t)QVT * HD + 2 * (on ? qv : 0);
-    const float* po = part + (size_t)(on ? qv : 0) * HD + d;
-    float m = -INFINITY;
-    for (int s = lane4; s < it.n; s += T4) m = fmaxf(m, get_past(ml + s * step).x);
-#pragma unroll
-    for (int o = 1; o < T4; o <<= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
-    const float mu = m == -INFINITY ? 0.f : m;
-    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-    float l = 0.f;
-    for (int s0 = 0; s0 < it.n; s0 += T4) {
-      const int s = s0 + lane4;
-      const float2 mine = s < it.n ? get_past(ml + s * step) : make_float2(-INFINITY, 0.f);
-      const float f = __builtin_amdgcn_exp2f(mine.x - mu);
-      l += f * mine.y;
-      const int n = min(T4, it.n - s0);
-#pragma unroll 8
-      for (int j = 0; j < n; ++j) {
-        const float fj = __shfl(f, (tid & 63 & ~(T4 - 1)) + j, 64);
-        const float2 a = get_past(po + (size_t)(s0 + j) * step), b = get_past(po + (size_t)(s0 + j) * step + 2);
-        acc += fj * f32x4{a.x, a.y, b.x, b.y};
+  const float* ml = part + (size_t)QVT * HD;
+  // a vector's maximum and sum over the ranges, by LPV lanes
+  constexpr int LPV = NT / QVT;
+  {
+    const int v = tid / LPV, ln = tid % LPV;
+    float m = -INFINITY, l = 0.f;
+    if (v < QV) {
+#pragma unroll 4
+      for (int s = ln; s < it.n; s += LPV) {
+        const float2 x = *(const float2*)(ml + 2 * v + s * step);
+        const float mn = fmaxf(m, x.x), mu = mn == -INFINITY ? 0.f : mn;
+        l = l * __builtin_amdgcn_exp2f(m - mu) + x.y * __builtin_amdgcn_exp2f(x.x - mu);
+        m = mn;
       }
     }
 #pragma unroll
-    for (int o = 1; o < T4; o <<= 1) l += __shfl_xor(l, o, 64);
-    if (on) {
-      const float inv = l == 0.f ? 0.f : 1.0f / l;
-      store(qv, d, f32x4{acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv});
+    for (int o = 1; o < LPV; o <<= 1) {
+      const float mo = __shfl_xor(m, o, 64), lo = __shfl_xor(l, o, 64), mn = fmaxf(m, mo), mu = mn == -INFINITY ? 0.f : mn;
+      l = l * __builtin_amdgcn_exp2f(m - mu) + lo * __builtin_amdgcn_exp2f(mo - mu);
+      m = mn;
+    }
+    if (ln == 0 && v < QV) { max_s[v] = m == -INFINITY ? 0.f : m; inv_s[v] = l == 0.f ? 0.f : 1.0f / l; }
+  }
+  __syncthreads();
+  // 4 dims of a vector a thread; where the vectors are few, several threads share the ranges of one and meet in LDS, in their order
+  constexpr int T4 = HD / 4;
+  int share = 1;
+  while (2 * share * QV * T4 <= NT && 2 * share <= it.n) share *= 2;
+  const int cells = QV * T4;
+  for (int e0 = 0; e0 < cells; e0 += NT) {
+    const int e = e0 + tid, part_no = share > 1 ? e / cells : 0, cell = share > 1 ? e - part_no * cells : e;
+    const bool on = part_no < share && cell < cells;
+    const int v = on ? cell / T4 : 0, d = on ? (cell % T4) * 4 : 0;
+    const float mx = max_s[v];
+    const float *pm = ml + 2 * v, *po = part + (size_t)v * HD + d;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    constexpr int U = 8;
+    for (int s0 = on ? part_no : it.n; s0 < it.n; s0 += U * share) {
+      float f[U];
+      f32x4 x[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int s = min(s0 + u * share, it.n - 1);
+        f[u] = pm[s * step];
+        x[u] = *(const f32x4*)(po + s * step);
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (s0 + u * share < it.n) acc += __builtin_amdgcn_exp2f(f[u] - mx) * x[u];
+    }
+    if (share > 1) {
+      sums[tid] = acc;
+      __syncthreads();
+      if (part_no == 0 && on)
+        for (int k = 1; k < share; ++k) acc += sums[k * cells + cell];
+    }
+    if (on && part_no == 0) {
+      const float inv = inv_s[v];
+      store(v, d, f32x4{acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv});
     }
   }
 }
@@ -425,7 +450,7 @@ __global__ void __launch_bounds__(256, 4) paged_attention_few_mfma_kernel(const 
       if (d == 0) put_through(part + (size_t)QVT * HD + 2 * v, mm, l);
     }
   }
-  if (it.n > 1) paged_join<HD, QVT, NT>(wk, it, pv.nkv, g, QV, store);
+  if (it.n > 1) paged_join<HD, QVT, NT>(wk, it, pv.nkv, g, QV, (f32x4*)paged_dyn_smem, store);
 }
 
 // Requests with many query vectors (chunks of a prompt).  A block takes 128 vectors of one KV head - 128 / GQ rows x the GQ query heads that share it, 32 per
@@ -743,7 +768,7 @@ __global__ void __launch_bounds__(256, 2) paged_attention_tall_mfma_kernel(const
       for (int q = 0; q < 4; ++q) put_through4(part + (size_t)qo * HD + 32 * t + 8 * q + 4 * (ln >> 5), f32x4{acc[t][4 * q], acc[t][4 * q + 1], acc[t][4 * q + 2], acc[t][4 * q + 3]});
     if (ln < 32) put_through(part + (size_t)QVT * HD + 2 * qo, m_run, l_run);
   }
-  paged_join<HD, QVT, NT>(wk, it, pv.nkv, g, QV,
+  paged_join<HD, QVT, NT>(wk, it, pv.nkv, g, QV, (f32x4*)paged_dyn_smem,
                           [&](int v, int d, const f32x4& x) { paged_store4<PLANES>(po, it.first + it.row0 + v / GQ, (g * GQ + v % GQ) * HD + d, x); });
 }
 
