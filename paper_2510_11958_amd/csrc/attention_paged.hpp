@@ -41,12 +41,13 @@ struct PagedItem { int req, first, row0, r, pos0, kb, ke, split, n, slot, group;
 
 // Item y of the launch that takes requests with lo < rows x GQ <= hi in groups of rpb rows.  All ranges have kps keys: with T = sum of groups x
 // keys over the requests, kps >= T / 2^shift, so there are at most 2^shift + groups items; those of groups with several ranges (keys > kps, hence ceil(keys / kps) < 2
-// keys / kps) are fewer than 2^(shift + 1), and such groups fewer than 2^shift: what the workspace holds.  Called by whole blocks.
+// keys / kps) are fewer than 2^(shift + 1), and such groups fewer than 2^shift: what the workspace holds.  Called by whole blocks.  GROUP: y counts the
+// groups with several ranges instead (split and range of the result mean nothing).
 struct PagedShare { int groups, splits; };
 __device__ __forceinline__ int paged_groups(const PagedReq& q, int GQ, int lo, int hi, int rpb) {
   return q.n > 0 && q.n * GQ > lo && q.n * GQ <= hi ? (q.n + rpb - 1) / rpb : 0;
 }
-template <int NT, int STEP>
+template <int NT, int STEP, bool GROUP>
 __device__ __forceinline__ bool paged_find(const PagedView& pv, const int* cu, const int* start, int max_new, int GQ, int lo, int hi, int rpb, int shift, int min_keys,
                                            int y, PagedItem& it) {
   auto keys_of = [&](unsigned long long total) {
@@ -61,7 +62,7 @@ __device__ __forceinline__ bool paged_find(const PagedView& pv, const int* cu, c
     if (lane < pv.n_req) q = paged_req(pv, cu, start, max_new, lane);
     const int gr = paged_groups(q, GQ, lo, hi, rpb);
     kps = keys_of(wave_reduce((unsigned long long)gr * (unsigned)(q.start + q.n), [](unsigned long long a, unsigned long long b) { return a + b; }));
-    const int sp = (int)((unsigned)(q.start + q.n + kps - 1) / (unsigned)kps), items = gr * sp;
+    const int sp = (int)((unsigned)(q.start + q.n + kps - 1) / (unsigned)kps), items = GROUP ? (sp > 1 ? gr : 0) : gr * sp;
     int incl = items;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
@@ -72,7 +73,7 @@ __device__ __forceinline__ bool paged_find(const PagedView& pv, const int* cu, c
     if (!behind) return false;
     i = __builtin_ctzll(behind);
     const bool m = lane < i && sp > 1;
-    slots = (int)wave_reduce((uint32_t)(m ? items : 0), [](uint32_t a, uint32_t b) { return a + b; });
+    slots = (int)wave_reduce((uint32_t)(m ? gr * sp : 0), [](uint32_t a, uint32_t b) { return a + b; });
     multi = (int)wave_reduce((uint32_t)(m ? gr : 0), [](uint32_t a, uint32_t b) { return a + b; });
     before = __builtin_amdgcn_readlane(incl - items, i);
     splits = __builtin_amdgcn_readlane(sp, i);
@@ -98,7 +99,7 @@ __device__ __forceinline__ bool paged_find(const PagedView& pv, const int* cu, c
     };
     for (int j = i0; j < i1; ++j) {
       const PagedShare s = share(j);
-      n_items += (long long)s.groups * s.splits;
+      n_items += GROUP ? (s.splits > 1 ? s.groups : 0) : (long long)s.groups * s.splits;
       if (s.splits > 1) n_multi += ((long long)s.groups << 32) | (unsigned)(s.groups * s.splits);
     }
     long long all, all_multi;
@@ -107,13 +108,13 @@ __device__ __forceinline__ bool paged_find(const PagedView& pv, const int* cu, c
     if (at <= y && y < at + n_items) {
       for (int j = i0; j < i1; ++j) {
         const PagedShare s = share(j);
-        const int n = s.groups * s.splits;
+        const int n = GROUP ? (s.splits > 1 ? s.groups : 0) : s.groups * s.splits;
         if (y < at + n) {
           found_s[0] = j; found_s[1] = s.splits; found_s[2] = (int)at; found_s[3] = (int)(at_multi & 0xFFFFFFFF); found_s[4] = (int)(at_multi >> 32);
           break;
         }
         at += n;
-        if (s.splits > 1) at_multi += ((long long)s.groups << 32) | (unsigned)n;
+        if (s.splits > 1) at_multi += ((long long)s.groups << 32) | (unsigned)(s.groups * s.splits);
       }
     }
     __syncthreads();
@@ -128,13 +129,13 @@ __device__ __forceinline__ bool paged_find(const PagedView& pv, const int* cu, c
   slots = __builtin_amdgcn_readfirstlane(slots);
   multi = __builtin_amdgcn_readfirstlane(multi);
   q = PagedReq{__builtin_amdgcn_readfirstlane(q.first), __builtin_amdgcn_readfirstlane(q.n), __builtin_amdgcn_readfirstlane(q.start)};
-  const int rel = y - before, group = (int)((unsigned)rel / (unsigned)splits);
+  const int rel = y - before, group = GROUP ? rel : (int)((unsigned)rel / (unsigned)splits);
   it.req = i;
   it.first = q.first;
   it.row0 = group * rpb;
   it.r = min(rpb, q.n - it.row0);
   it.pos0 = q.start + it.row0;
-  it.split = rel - group * splits;
+  it.split = GROUP ? 0 : rel - group * splits;
   it.kb = it.split * kps;
   const int end = it.pos0 + it.r;                   // the group's last row sees the keys in front of this
   it.ke = min(end, it.kb + kps);
@@ -152,13 +153,45 @@ __device__ __forceinline__ void put_through(float* p, float a, float b) {
 }
 __device__ __forceinline__ void put_through4(float* p, const f32x4& v) { put_through(p, v.x, v.y); put_through(p + 2, v.z, v.w); }
 
+// 4 dims of a vector summed over ranges: o = sum of weights x values and l = sum of weights, both relative to the maximum m (powers of two)
+struct PagedSum {
+  float m = -INFINITY, l = 0.f;
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  __device__ __forceinline__ void add(float m2, float l2, const f32x4& o2) {
+    const float mn = fmaxf(m, m2), mu = mn == -INFINITY ? 0.f : mn, f = __builtin_amdgcn_exp2f(m - mu), f2 = __builtin_amdgcn_exp2f(m2 - mu);
+    l = l * f + l2 * f2;
+    o = f * o + f2 * o2;
+    m = mn;
+  }
+  // ranges s0, s0 + by, ... below n, of partial results `step` floats apart
+  __device__ __forceinline__ void add_ranges(const float* ml, const float* po, size_t step, int s0, int n, int by) {
+    constexpr int U = 8;                  // of them in flight
+    for (; s0 < n; s0 += U * by) {
+      float2 w[U];
+      f32x4 x[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const size_t at = (size_t)min(s0 + u * by, n - 1) * step;
+        w[u] = *(const float2*)(ml + at);
+        x[u] = *(const f32x4*)(po + at);
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (s0 + u * by < n) add(w[u].x, w[u].y, x[u]);
+    }
+  }
+  __device__ __forceinline__ f32x4 result() const {
+    const float inv = l == 0.f ? 0.f : 1.0f / l;
+    return f32x4{o.x * inv, o.y * inv, o.z * inv, o.w * inv};
+  }
+};
+
 // The end of a block whose group has several ranges: `write` has stored the block's partial results in its slot; the last of the group's blocks joins
 // all of them.  o: QVT x HD sums relative to the maximum m (powers of two), l: sum of weights; out = sum 2^(m - M) o / sum 2^(m - M) l.
 // A wave waits for its writes before the block counts.
 template <int HD, int QVT, int NT, typename STORE>
-__device__ __forceinline__ void paged_join(const PagedWork& w, const PagedItem& it, int nkv, int g, int QV, f32x4* sums /* LDS, NT of them */, STORE store) {
+__device__ __forceinline__ void paged_join(const PagedWork& w, const PagedItem& it, int nkv, int g, int QV, f32x4* sums /* LDS, 2 NT of them */, STORE store) {
   __shared__ int last_s;
-  __shared__ float max_s[QVT], inv_s[QVT];
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
   const int tid = threadIdx.x;
@@ -173,66 +206,25 @@ __device__ __forceinline__ void paged_join(const PagedWork& w, const PagedItem& 
   constexpr size_t SLOT = (size_t)QVT * (HD + 2);
   const float* part = w.part + ((size_t)it.slot * nkv + g) * SLOT;
   const size_t step = (size_t)nkv * SLOT;
-  const float* ml = part + (size_t)QVT * HD;
-  // a vector's maximum and sum over the ranges, by LPV lanes
-  constexpr int LPV = NT / QVT;
-  {
-    const int v = tid / LPV, ln = tid % LPV;
-    float m = -INFINITY, l = 0.f;
-    if (v < QV) {
-#pragma unroll 4
-      for (int s = ln; s < it.n; s += LPV) {
-        const float2 x = *(const float2*)(ml + 2 * v + s * step);
-        const float mn = fmaxf(m, x.x), mu = mn == -INFINITY ? 0.f : mn;
-        l = l * __builtin_amdgcn_exp2f(m - mu) + x.y * __builtin_amdgcn_exp2f(x.x - mu);
-        m = mn;
-      }
-    }
-#pragma unroll
-    for (int o = 1; o < LPV; o <<= 1) {
-      const float mo = __shfl_xor(m, o, 64), lo = __shfl_xor(l, o, 64), mn = fmaxf(m, mo), mu = mn == -INFINITY ? 0.f : mn;
-      l = l * __builtin_amdgcn_exp2f(m - mu) + lo * __builtin_amdgcn_exp2f(mo - mu);
-      m = mn;
-    }
-    if (ln == 0 && v < QV) { max_s[v] = m == -INFINITY ? 0.f : m; inv_s[v] = l == 0.f ? 0.f : 1.0f / l; }
-  }
-  __syncthreads();
   // 4 dims of a vector a thread; where the vectors are few, several threads share the ranges of one and meet in LDS, in their order
   constexpr int T4 = HD / 4;
-  int share = 1;
-  while (2 * share * QV * T4 <= NT && 2 * share <= it.n) share *= 2;
   const int cells = QV * T4;
+  int share = 1;
+  while (2 * share * cells <= NT && 2 * share <= it.n) share *= 2;
   for (int e0 = 0; e0 < cells; e0 += NT) {
-    const int e = e0 + tid, part_no = share > 1 ? e / cells : 0, cell = share > 1 ? e - part_no * cells : e;
-    const bool on = part_no < share && cell < cells;
+    const int e = e0 + tid, turn = share > 1 ? e / cells : 0, cell = share > 1 ? e - turn * cells : e;
+    const bool on = turn < share && cell < cells;
     const int v = on ? cell / T4 : 0, d = on ? (cell % T4) * 4 : 0;
-    const float mx = max_s[v];
-    const float *pm = ml + 2 * v, *po = part + (size_t)v * HD + d;
-    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-    constexpr int U = 8;
-    for (int s0 = on ? part_no : it.n; s0 < it.n; s0 += U * share) {
-      float f[U];
-      f32x4 x[U];
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int s = min(s0 + u * share, it.n - 1);
-        f[u] = pm[s * step];
-        x[u] = *(const f32x4*)(po + s * step);
-      }
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (s0 + u * share < it.n) acc += __builtin_amdgcn_exp2f(f[u] - mx) * x[u];
-    }
+    PagedSum sum;
+    sum.add_ranges(part + (size_t)QVT * HD + 2 * v, part + (size_t)v * HD + d, step, on ? turn : it.n, it.n, share);
     if (share > 1) {
-      sums[tid] = acc;
+      sums[tid] = sum.o;
+      sums[NT + tid] = f32x4{sum.m, sum.l, 0.f, 0.f};
       __syncthreads();
-      if (part_no == 0 && on)
-        for (int k = 1; k < share; ++k) acc += sums[k * cells + cell];
+      if (turn == 0 && on)
+        for (int k = 1; k < share; ++k) sum.add(sums[NT + k * cells + cell].x, sums[NT + k * cells + cell].y, sums[k * cells + cell]);
     }
-    if (on && part_no == 0) {
-      const float inv = inv_s[v];
-      store(v, d, f32x4{acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv});
-    }
+    if (on && turn == 0) store(v, d, sum.result());
   }
 }
 
@@ -266,7 +258,7 @@ __global__ void __launch_bounds__(256, 4) paged_attention_few_mfma_kernel(const 
   typedef unsigned short hvec_t __attribute__((ext_vector_type(HL)));
   const int g = blockIdx.x, GQ = pv.nh / pv.nkv, rpb = QVT / GQ;
   PagedItem it;
-  if (!paged_find<NT, 16 * NW>(pv, cu, start, max_new, GQ, 0, hi, rpb, wk.shift, PAGED_KEYS_FEW, blockIdx.y, it)) return;
+  if (!paged_find<NT, 16 * NW, false>(pv, cu, start, max_new, GQ, 0, hi, rpb, wk.shift, PAGED_KEYS_FEW, blockIdx.y, it)) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), sl = lane & 15, kq = lane >> 4;
   const int QV = it.r * GQ, ke = it.ke;
   __shared__ float wm[NW][QVT], wl[NW][QVT];
@@ -480,7 +472,7 @@ __global__ void __launch_bounds__(256, 2) paged_attention_tall_mfma_kernel(const
   __shared__ int poison_s;
   const int g = blockIdx.x, GQ = pv.nh / pv.nkv, rpb = QVT / GQ;
   PagedItem it;
-  if (!paged_find<NT, KT>(pv, cu, start, max_new, GQ, lo, INT_MAX, rpb, wk.shift, PAGED_KEYS_TALL, blockIdx.y, it)) return;
+  if (!paged_find<NT, KT, false>(pv, cu, start, max_new, GQ, lo, INT_MAX, rpb, wk.shift, PAGED_KEYS_TALL, blockIdx.y, it)) return;
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), hi = lane >> 5;
   bf16_t* ring = (bf16_t*)paged_dyn_smem;                      // K, K, V^T, V^T
   const int QV = it.r * GQ, qv = 32 * w + (lane & 31), kb = it.kb, ke = it.ke;
@@ -765,11 +757,27 @@ __global__ void __launch_bounds__(256, 2) paged_attention_tall_mfma_kernel(const
 #pragma unroll
     for (int t = 0; t < DT; ++t)
 #pragma unroll
-      for (int q = 0; q < 4; ++q) put_through4(part + (size_t)qo * HD + 32 * t + 8 * q + 4 * (ln >> 5), f32x4{acc[t][4 * q], acc[t][4 * q + 1], acc[t][4 * q + 2], acc[t][4 * q + 3]});
-    if (ln < 32) put_through(part + (size_t)QVT * HD + 2 * qo, m_run, l_run);
+      for (int q = 0; q < 4; ++q) *(f32x4*)(part + (size_t)qo * HD + 32 * t + 8 * q + 4 * (ln >> 5)) = f32x4{acc[t][4 * q], acc[t][4 * q + 1], acc[t][4 * q + 2], acc[t][4 * q + 3]};
+    if (ln < 32) *(float2*)(part + (size_t)QVT * HD + 2 * qo) = make_float2(m_run, l_run);
   }
-  paged_join<HD, QVT, NT>(wk, it, pv.nkv, g, QV, (f32x4*)paged_dyn_smem,
-                          [&](int v, int d, const f32x4& x) { paged_store4<PLANES>(po, it.first + it.row0 + v / GQ, (g * GQ + v % GQ) * HD + d, x); });
+}
+
+// The ranges of the tall kernel's groups joined: 64 KiB of partial results a group and range are too much for the block that ends last (64 rows behind
+// 4096, 32/8 heads: 87 us by it, here us).  A block takes NT / (HD / 4) vectors of a group.
+template <int HD, bool PLANES>
+__global__ void __launch_bounds__(256) paged_attention_merge_kernel(const int* __restrict__ cu, const int* __restrict__ start, int max_new, int lo, PagedOut po, PagedView pv,
+                                                                    PagedWork wk) {
+  constexpr int QVT = 128, NT = 256, T4 = HD / 4;
+  constexpr size_t SLOT = (size_t)QVT * (HD + 2);
+  const int g = blockIdx.x, GQ = pv.nh / pv.nkv;
+  PagedItem it;
+  if (!paged_find<NT, 64, true>(pv, cu, start, max_new, GQ, lo, INT_MAX, QVT / GQ, wk.shift, PAGED_KEYS_TALL, blockIdx.z, it)) return;
+  const int v = blockIdx.y * (NT / T4) + threadIdx.x / T4, d = (threadIdx.x % T4) * 4;
+  if (it.n < 2 || v >= it.r * GQ) return;      // a group in the request's first range has been written
+  const float* part = wk.part + ((size_t)it.slot * pv.nkv + g) * SLOT;
+  PagedSum sum;
+  sum.add_ranges(part + (size_t)QVT * HD + 2 * v, part + (size_t)v * HD + d, (size_t)pv.nkv * SLOT, 0, it.n, 1);
+  paged_store4<PLANES>(po, it.first + it.row0 + v / GQ, (g * GQ + v % GQ) * HD + d, sum.result());
 }
 
 // One block per (row, query head); its 4 waves take 64 keys each in turn, a lane scores one key and then carries HD / 64 dims of the output.

@@ -131,7 +131,7 @@ hipError_t launch_paged_mfma(const PagedView& v, const PagedPlan& p, const Paged
   const int GQ = v.nh / v.nkv;
   PagedWork wk{p.few_shift, (int*)a.ws, (float*)(a.ws + p.count_bytes)};
   const int qv_max = std::min(16 / GQ, a.max_new) * GQ;
-  hipLaunchKernelGGL((paged_attention_few_mfma_kernel<HD, PLANES>), dim3(v.nkv, p.few), dim3(256), std::max((size_t)4 * qv_max * HD * 4, (size_t)2 * 16 * (HD + ATT_QPAD) * 2), a.stream, a.cu, a.start, a.qkv, a.ld, (const bf16_t*)a.gain,
+  hipLaunchKernelGGL((paged_attention_few_mfma_kernel<HD, PLANES>), dim3(v.nkv, p.few), dim3(256), std::max({(size_t)4 * qv_max * HD * 4, (size_t)2 * 16 * (HD + ATT_QPAD) * 2, (size_t)2 * 256 * 16}), a.stream, a.cu, a.start, a.qkv, a.ld, (const bf16_t*)a.gain,
                      (const float2*)a.rope, a.eps, a.max_new, PAGED_FEW, out, v, wk);
   if (p.tall > 0) {
     wk.shift = p.tall_shift;
@@ -144,6 +144,7 @@ hipError_t launch_paged_mfma(const PagedView& v, const PagedPlan& p, const Paged
       big_lds = true;
     }
     hipLaunchKernelGGL(kern, dim3(v.nkv, p.tall), dim3(256), lds, a.stream, a.cu, a.start, a.qkv, a.ld, (const bf16_t*)a.gain, (const float2*)a.rope, a.eps, a.max_new, PAGED_FEW, out, v, wk);
+    hipLaunchKernelGGL((paged_attention_merge_kernel<HD, PLANES>), dim3(v.nkv, 128 * HD / 4 / 256, 1 << p.tall_shift), dim3(256), 0, a.stream, a.cu, a.start, a.max_new, PAGED_FEW, out, v, wk);
   }
   return hipGetLastError();
 }
