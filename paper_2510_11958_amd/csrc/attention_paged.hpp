@@ -43,11 +43,18 @@ struct PagedItem { int req, first, row0, r, pos0, kb, ke, split, n, slot, group;
 // keys over the requests, kps >= T / 2^shift, so there are at most 2^shift + groups items; those of groups with several ranges (keys > kps, hence ceil(keys / kps) < 2
 // keys / kps) are fewer than 2^(shift + 1), and such groups fewer than 2^shift: what the workspace holds.  Called by whole blocks.  GROUP: y counts the
 // groups with several ranges instead (split and range of the result mean nothing).
+// The tall kernel's order of n items.  A chunk's later groups see more keys.  Up to 2^shift blocks are all resident from the start, two on a CU: the first round of the
+// CUs goes from the longest down, the second from the shortest up, and a CU's two come to about the same.  More blocks than that start as
+// others end, longest first.
+__device__ __forceinline__ int paged_turn(int y, int n, int shift) {
+  const int down = n <= (1 << shift) ? min(n, 1 << (shift - 1)) : n;
+  return y < down ? n - 1 - y : (y < n ? y - down : y);
+}
 struct PagedShare { int groups, splits; };
 __device__ __forceinline__ int paged_groups(const PagedReq& q, int GQ, int lo, int hi, int rpb) {
   return q.n > 0 && q.n * GQ > lo && q.n * GQ <= hi ? (q.n + rpb - 1) / rpb : 0;
 }
-template <int NT, int STEP, bool GROUP>
+template <int NT, int STEP, bool GROUP, bool TALL = false>
 __device__ __forceinline__ bool paged_find(const PagedView& pv, const int* cu, const int* start, int max_new, int GQ, int lo, int hi, int rpb, int shift, int min_keys,
                                            int y, PagedItem& it) {
   auto keys_of = [&](unsigned long long total) {
@@ -69,6 +76,7 @@ __device__ __forceinline__ bool paged_find(const PagedView& pv, const int* cu, c
       const int u = __shfl_up(incl, o, 64);
       if (lane >= o) incl += u;
     }
+    if (TALL) y = paged_turn(y, __builtin_amdgcn_readlane(incl, 63), shift);
     const unsigned long long behind = __ballot(incl > y);
     if (!behind) return false;
     i = __builtin_ctzll(behind);
@@ -104,6 +112,7 @@ __device__ __forceinline__ bool paged_find(const PagedView& pv, const int* cu, c
     }
     long long all, all_multi;
     long long at = block_scan<NT>(n_items, sums_s, all), at_multi = block_scan<NT>(n_multi, sums_s, all_multi);
+    if (TALL) y = paged_turn(y, (int)all, shift);
     if (y >= all) return false;
     if (at <= y && y < at + n_items) {
       for (int j = i0; j < i1; ++j) {
@@ -229,7 +238,7 @@ __device__ __forceinline__ void paged_join(const PagedWork& w, const PagedItem& 
 }
 
 // Four values of one head from dim d on, rounded once
-template <bool PLANES>
+template <typename CT, bool PLANES>
 __device__ __forceinline__ void paged_store4(const PagedOut& o, int row, int col, const f32x4& v) {
   if (PLANES) {
     const size_t at = packed_at(o.blocked, row, col, (int)o.ld);
@@ -237,6 +246,8 @@ __device__ __forceinline__ void paged_store4(const PagedOut& o, int row, int col
     *(uint2*)((bf16_t*)o.out + at) = h;
     *(uint2*)(o.lo + at) = make_uint2(pack_bf16x2(v.x - __uint_as_float(h.x << 16), v.y - __uint_as_float(h.x & 0xFFFF0000u)),
                                       pack_bf16x2(v.z - __uint_as_float(h.y << 16), v.w - __uint_as_float(h.y & 0xFFFF0000u)));
+  } else if (sizeof(CT) == 4) {
+    *(f32x4*)((float*)o.out + (size_t)row * o.ld + col) = v;
   } else {
     *(uint2*)((bf16_t*)o.out + (size_t)row * o.ld + col) = make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
   }
@@ -247,13 +258,18 @@ __device__ __forceinline__ void paged_store4(const PagedOut& o, int row, int col
 //   scores   S^T[key, q] = sum_d K[key, d] Q[q, d], 16x16x32: K rows as they lie in the cache, the queries as two bf16 parts (16 bits);
 //   output   O[q, d] += sum_key P[q, key] V[key, d], 16x16x16: a lane's operand is 4 consecutive keys of one row or column, so nothing moves between
 //            lanes; a probability goes in as two bf16 parts.
+// fp32 caches: 16x16x4 for both, the queries and probabilities as they are, any number of rows (a chunk's groups of 16 vectors find the keys in the L2).
 // Bound by the memory: 8 KiB per wave and group against 2 x HD / 16 + 2 x HD / 32 products.
-template <int HD, bool PLANES>
-__global__ void __launch_bounds__(256, 4) paged_attention_few_mfma_kernel(const int* __restrict__ cu, const int* __restrict__ start, const float* __restrict__ qkv, long ld,
-                                                                  const bf16_t* __restrict__ q_gain, const float2* __restrict__ rope_tab, float eps, int max_new, int hi,
+template <typename CT, int HD, bool PLANES>
+__global__ void __launch_bounds__(256, sizeof(CT) == 2 ? 4 : 2) paged_attention_few_mfma_kernel(const int* __restrict__ cu, const int* __restrict__ start, const float* __restrict__ qkv, long ld,
+                                                                  const CT* __restrict__ q_gain, const float2* __restrict__ rope_tab, float eps, int max_new, int hi,
                                                                   PagedOut po, PagedView pv, PagedWork wk) {
-  constexpr int QVT = 16, NW = 4, NT = 64 * NW, KS = HD / 32, DPL = HD / 16, half = HD / 2, HL = HD / 32;
-  typedef unsigned int vraw_t __attribute__((ext_vector_type(DPL / 2)));
+  constexpr bool BF = sizeof(CT) == 2;
+  constexpr int QVT = 16, NW = 4, NT = 64 * NW, DPL = HD / 16, half = HD / 2, HL = HD / 32;
+  constexpr int KS = BF ? HD / 32 : HD / 16;                 // 16-byte pieces of a key a lane carries
+  constexpr int QLD = BF ? HD + ATT_QPAD : HD + 4;           // a query row in LDS
+  constexpr int VW = DPL * sizeof(CT) / 4;                   // 32-bit words of a value a lane carries: its DPL dims
+  typedef unsigned int vraw_t __attribute__((ext_vector_type(VW)));
   typedef float fvec_t __attribute__((ext_vector_type(HL)));
   typedef unsigned short hvec_t __attribute__((ext_vector_type(HL)));
   const int g = blockIdx.x, GQ = pv.nh / pv.nkv, rpb = QVT / GQ;
@@ -265,7 +281,7 @@ __global__ void __launch_bounds__(256, 4) paged_attention_few_mfma_kernel(const 
   __shared__ int poison_s;
   extern __shared__ float4 paged_dyn_smem[];
   float* wacc = (float*)paged_dyn_smem;                       // [NW][QV][HD], in the place of the queries' two parts when these are done with
-  bf16_t (*qhi_s)[HD + ATT_QPAD] = (bf16_t (*)[HD + ATT_QPAD])paged_dyn_smem, (*qlo_s)[HD + ATT_QPAD] = qhi_s + QVT;
+  CT (*qhi_s)[QLD] = (CT (*)[QLD])paged_dyn_smem, (*qlo_s)[QLD] = qhi_s + QVT;      // (fp32: one part)
   // pages of this wave's next 64 groups, one a lane
   const int* trow = pv.table + (size_t)it.req * pv.max_pages;
   auto load_pages = [&](int base) { return base + 64 * lane < ke ? trow[(base + 64 * lane) >> pv.page_shift] : 0; };
@@ -285,10 +301,10 @@ __global__ void __launch_bounds__(256, 4) paged_attention_few_mfma_kernel(const 
   auto load_kv = [&](int base, int page) {
     ok = page >= 0 && page < pv.n_pages;
     const size_t at = (size_t)(ok ? page : 0) * pv.page_stride + (((size_t)g << pv.page_shift) + (base & ((1 << pv.page_shift) - 1))) * HD;
-    const bf16_t* kp = (const bf16_t*)pv.k + at;
-    const bf16_t* vp = (const bf16_t*)pv.v + at;
+    const CT* kp = (const CT*)pv.k + at;
+    const CT* vp = (const CT*)pv.v + at;
 #pragma unroll
-    for (int t = 0; t < KS; ++t) kr[t] = __builtin_nontemporal_load((const u32x4*)(kp + sl * HD + 32 * t + 8 * kq));
+    for (int t = 0; t < KS; ++t) kr[t] = __builtin_nontemporal_load((const u32x4*)(kp + sl * HD + (HD / KS) * t + (16 / (int)sizeof(CT)) * kq));
 #pragma unroll
     for (int m = 0; m < 4; ++m) vr[m] = __builtin_nontemporal_load((const vraw_t*)(vp + (4 * kq + m) * HD + DPL * sl));
   };
@@ -299,10 +315,9 @@ __global__ void __launch_bounds__(256, 4) paged_attention_few_mfma_kernel(const 
 #pragma unroll
     for (int e = 0; e < HL; ++e) { x0[e] = xa[e]; x1[e] = xb[e]; ss += x0[e] * x0[e] + x1[e] * x1[e]; }
     if (q_gain) {
-      const hvec_t g0 = *(const hvec_t*)(q_gain + HL * l16), g1 = *(const hvec_t*)(q_gain + half + HL * l16);
       const float rs = rsqrtf(row16_sum(ss) / (float)HD + eps);
 #pragma unroll
-      for (int e = 0; e < HL; ++e) { x0[e] *= rs * bf16_to_f32(g0[e]); x1[e] *= rs * bf16_to_f32(g1[e]); }
+      for (int e = 0; e < HL; ++e) { x0[e] *= rs * Elem<CT>::to_f32(q_gain[HL * l16 + e]); x1[e] *= rs * Elem<CT>::to_f32(q_gain[half + HL * l16 + e]); }
     }
     if (rope_tab) {
       const float2* rp = rope_tab + (size_t)pos * half + HL * l16;
@@ -315,15 +330,20 @@ __global__ void __launch_bounds__(256, 4) paged_attention_few_mfma_kernel(const 
       }
     }
     const float scale = rsqrtf((float)HD) * 1.4426950408889634f;
-    hvec_t h0, h1, l0, l1;
+    if constexpr (BF) {
+      hvec_t h0, h1, l0, l1;
 #pragma unroll
-    for (int e = 0; e < HL; ++e) {
-      bf16_t h, l;
-      split_bf16(qv < QV ? x0[e] * scale : 0.f, h, l); h0[e] = h; l0[e] = l;
-      split_bf16(qv < QV ? x1[e] * scale : 0.f, h, l); h1[e] = h; l1[e] = l;
+      for (int e = 0; e < HL; ++e) {
+        bf16_t h, l;
+        split_bf16(qv < QV ? x0[e] * scale : 0.f, h, l); h0[e] = h; l0[e] = l;
+        split_bf16(qv < QV ? x1[e] * scale : 0.f, h, l); h1[e] = h; l1[e] = l;
+      }
+      *(hvec_t*)&qhi_s[qv][HL * l16] = h0; *(hvec_t*)&qhi_s[qv][half + HL * l16] = h1;
+      *(hvec_t*)&qlo_s[qv][HL * l16] = l0; *(hvec_t*)&qlo_s[qv][half + HL * l16] = l1;
+    } else {
+#pragma unroll
+      for (int e = 0; e < HL; ++e) { qhi_s[qv][HL * l16 + e] = qv < QV ? x0[e] * scale : 0.f; qhi_s[qv][half + HL * l16 + e] = qv < QV ? x1[e] * scale : 0.f; }
     }
-    *(hvec_t*)&qhi_s[qv][HL * l16] = h0; *(hvec_t*)&qhi_s[qv][half + HL * l16] = h1;
-    *(hvec_t*)&qlo_s[qv][HL * l16] = l0; *(hvec_t*)&qlo_s[qv][half + HL * l16] = l1;
   }
   __syncthreads();
   const int my_pos = it.pos0 + sl / GQ;
@@ -348,9 +368,16 @@ __global__ void __launch_bounds__(256, 4) paged_attention_few_mfma_kernel(const 
     f32x4 s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int t = 0; t < KS; ++t) {
+      if constexpr (!BF) {
+        const f32x4 k4 = __builtin_bit_cast(f32x4, ka[t]), q4 = *(const f32x4*)&qhi_s[sl][16 * t + 4 * kq];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_16x16x4f32(k4[e], q4[e], s, 0, 0, 0);
+        continue;
+      } else {
       const bf16x8_t ql = __builtin_bit_cast(bf16x8_t, *(const u32x4*)&qlo_s[sl][32 * t + 8 * kq]), qh = __builtin_bit_cast(bf16x8_t, *(const u32x4*)&qhi_s[sl][32 * t + 8 * kq]);
       s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, ka[t]), ql, s, 0, 0, 0);
       s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, ka[t]), qh, s, 0, 0, 0);
+      }
     }
     float sc[4] = {s.x, s.y, s.z, s.w};
     if (base + 16 > it.pos0 + 1) {
@@ -363,11 +390,11 @@ __global__ void __launch_bounds__(256, 4) paged_attention_few_mfma_kernel(const 
         if (key > it.pos0) {
           bool bad = false;
 #pragma unroll
-          for (int u = 0; u < DPL / 2; ++u) bad |= (va[m][u] & 0x7F80u) == 0x7F80u || (va[m][u] & 0x7F800000u) == 0x7F800000u;
+          for (int u = 0; u < VW; ++u) bad |= (BF && (va[m][u] & 0x7F80u) == 0x7F80u) || (va[m][u] & 0x7F800000u) == 0x7F800000u;
           if (bad && key < ke) atomicMin(&poison_s, key);
           if (bad || key >= ke) {
 #pragma unroll
-            for (int u = 0; u < DPL / 2; ++u) va[m][u] = 0u;
+            for (int u = 0; u < VW; ++u) va[m][u] = 0u;
           }
         }
       }
@@ -390,6 +417,12 @@ __global__ void __launch_bounds__(256, 4) paged_attention_few_mfma_kernel(const 
       }
     }
     m_run = m_new;
+    if constexpr (!BF) {
+#pragma unroll
+      for (int e = 0; e < DPL; ++e)
+#pragma unroll
+        for (int m = 0; m < 4; ++m) acc[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(p[m], __uint_as_float(va[m][e]), acc[e], 0, 0, 0);
+    } else {
     uint2 ph, pl;
     ph.x = pack_bf16x2(p[0], p[1]);
     ph.y = pack_bf16x2(p[2], p[3]);
@@ -401,6 +434,7 @@ __global__ void __launch_bounds__(256, 4) paged_attention_few_mfma_kernel(const 
       const uint2 v4 = make_uint2(__builtin_amdgcn_perm(va[1][e >> 1], va[0][e >> 1], sel), __builtin_amdgcn_perm(va[3][e >> 1], va[2][e >> 1], sel));
       acc[e] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(bf16x4s_t, pl), __builtin_bit_cast(bf16x4s_t, v4), acc[e], 0, 0, 0);
       acc[e] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(bf16x4s_t, ph), __builtin_bit_cast(bf16x4s_t, v4), acc[e], 0, 0, 0);
+    }
     }
   }
   // the waves' results of a vector, 4 consecutive dims a thread
@@ -418,7 +452,7 @@ __global__ void __launch_bounds__(256, 4) paged_attention_few_mfma_kernel(const 
   __syncthreads();
   constexpr size_t SLOT = (size_t)QVT * (HD + 2);
   float* part = wk.part + ((size_t)(it.slot + it.split) * pv.nkv + g) * SLOT;
-  auto store = [&](int v, int d, const f32x4& x) { paged_store4<PLANES>(po, it.first + it.row0 + v / GQ, (g * GQ + v % GQ) * HD + d, x); };
+  auto store = [&](int v, int d, const f32x4& x) { paged_store4<CT, PLANES>(po, it.first + it.row0 + v / GQ, (g * GQ + v % GQ) * HD + d, x); };
   for (int e = tid; e < QV * (HD / 4); e += NT) {
     const int v = e / (HD / 4), d = (e % (HD / 4)) * 4;
     float mm = wm[0][v];
@@ -472,7 +506,7 @@ __global__ void __launch_bounds__(256, 2) paged_attention_tall_mfma_kernel(const
   __shared__ int poison_s;
   const int g = blockIdx.x, GQ = pv.nh / pv.nkv, rpb = QVT / GQ;
   PagedItem it;
-  if (!paged_find<NT, KT, false>(pv, cu, start, max_new, GQ, lo, INT_MAX, rpb, wk.shift, PAGED_KEYS_TALL, blockIdx.y, it)) return;
+  if (!paged_find<NT, KT, false, true>(pv, cu, start, max_new, GQ, lo, INT_MAX, rpb, wk.shift, PAGED_KEYS_TALL, blockIdx.y, it)) return;
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), hi = lane >> 5;
   bf16_t* ring = (bf16_t*)paged_dyn_smem;                      // K, K, V^T, V^T
   const int QV = it.r * GQ, qv = 32 * w + (lane & 31), kb = it.kb, ke = it.ke;
@@ -748,7 +782,7 @@ __global__ void __launch_bounds__(256, 2) paged_attention_tall_mfma_kernel(const
       for (int t = 0; t < DT; ++t)
 #pragma unroll
         for (int q = 0; q < 4; ++q)
-          paged_store4<PLANES>(po, it.first + ro, co + 32 * t + 8 * q, f32x4{acc[t][4 * q] * inv, acc[t][4 * q + 1] * inv, acc[t][4 * q + 2] * inv, acc[t][4 * q + 3] * inv});
+          paged_store4<bf16_t, PLANES>(po, it.first + ro, co + 32 * t + 8 * q, f32x4{acc[t][4 * q] * inv, acc[t][4 * q + 1] * inv, acc[t][4 * q + 2] * inv, acc[t][4 * q + 3] * inv});
     }
     return;
   }
@@ -763,7 +797,7 @@ __global__ void __launch_bounds__(256, 2) paged_attention_tall_mfma_kernel(const
 }
 
 // The ranges of the tall kernel's groups joined: 64 KiB of partial results a group and range are too much for the block that ends last (64 rows behind
-// 4096, 32/8 heads: 87 us by it, here us).  A block takes NT / (HD / 4) vectors of a group.
+// 4096, 32/8 heads: 87 us by it, 41 with this launch).
 template <int HD, bool PLANES>
 __global__ void __launch_bounds__(256) paged_attention_merge_kernel(const int* __restrict__ cu, const int* __restrict__ start, int max_new, int lo, PagedOut po, PagedView pv,
                                                                     PagedWork wk) {
@@ -772,93 +806,13 @@ __global__ void __launch_bounds__(256) paged_attention_merge_kernel(const int* _
   const int g = blockIdx.x, GQ = pv.nh / pv.nkv;
   PagedItem it;
   if (!paged_find<NT, 64, true>(pv, cu, start, max_new, GQ, lo, INT_MAX, QVT / GQ, wk.shift, PAGED_KEYS_TALL, blockIdx.z, it)) return;
-  const int v = blockIdx.y * (NT / T4) + threadIdx.x / T4, d = (threadIdx.x % T4) * 4;
-  if (it.n < 2 || v >= it.r * GQ) return;      // a group in the request's first range has been written
+  if (it.n < 2) return;      // the request's first range is all that the group sees: written
   const float* part = wk.part + ((size_t)it.slot * pv.nkv + g) * SLOT;
-  PagedSum sum;
-  sum.add_ranges(part + (size_t)QVT * HD + 2 * v, part + (size_t)v * HD + d, (size_t)pv.nkv * SLOT, 0, it.n, 1);
-  paged_store4<PLANES>(po, it.first + it.row0 + v / GQ, (g * GQ + v % GQ) * HD + d, sum.result());
-}
-
-// One block per (row, query head); its 4 waves take 64 keys each in turn, a lane scores one key and then carries HD / 64 dims of the output.
-template <typename CT, int HD>
-__global__ void __launch_bounds__(256) paged_attention_rows_kernel(const float* __restrict__ qkv, long ld, const int* __restrict__ start, const int* __restrict__ cu,
-                                                                   const CT* __restrict__ q_gain, const float2* __restrict__ rope_tab, float eps, int max_new,
-                                                                   CT* __restrict__ out, long ldo, PagedView pv) {
-  constexpr int half = HD / 2, DPL = HD / 64;
-  __shared__ __attribute__((aligned(16))) float q_s[HD];
-  __shared__ float o_s[4][HD], m_s[4], l_s[4];
-  const int t = blockIdx.x, head = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  if (t >= cu[pv.n_req] || t < cu[0]) return;
-  const int i = last_at_most(cu, pv.n_req, t);
-  const PagedReq rq = paged_req(pv, cu, start, max_new, i);
-  if (t >= rq.first + rq.n) return;
-  const int pos = rq.start + t - rq.first;
-  const int g = head / (pv.nh / pv.nkv);
-  if (wave == 0) {
-    const float* src = qkv + (size_t)t * ld + (size_t)head * HD;
-    const bool act = lane < half;
-    float a = act ? src[lane] : 0.f, b = act ? src[lane + half] : 0.f;
-    const float rs = q_gain ? rsqrtf(wave_sum(a * a + b * b) / (float)HD + eps) : 1.f;
-    if (act) {
-      if (q_gain) { a *= rs * Elem<CT>::to_f32(q_gain[lane]); b *= rs * Elem<CT>::to_f32(q_gain[lane + half]); }
-      const float2 cs = rope_tab ? rope_tab[(size_t)pos * half + lane] : make_float2(1.f, 0.f);
-      const float scale = rsqrtf((float)HD);
-      q_s[lane] = (a * cs.x - b * cs.y) * scale;
-      q_s[lane + half] = (b * cs.x + a * cs.y) * scale;
-    }
-  }
-  __syncthreads();
-  const int* table = pv.table + (size_t)i * pv.max_pages;
-  auto at = [&](int key, int page) { return (size_t)page * pv.page_stride + (((size_t)g << pv.page_shift) + (key & ((1 << pv.page_shift) - 1))) * HD; };
-  float m = -INFINITY, l = 0.f, acc[DPL];
-#pragma unroll
-  for (int e = 0; e < DPL; ++e) acc[e] = 0.f;
-  for (int base = 64 * wave; base <= pos; base += 256) {
-    const int key = base + lane;
-    const int page = key <= pos ? table[key >> pv.page_shift] : -1;
-    const bool seen = page >= 0 && page < pv.n_pages;
-    float s = -INFINITY;
-    if (seen) {
-      const CT* kp = (const CT*)pv.k + at(key, page);
-      s = 0.f;
-      for (int d = 0; d < HD; d += 8) {
-        float w[8];
-        Elem<CT>::load8(kp + d, w);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) s += w[e] * q_s[d + e];
-      }
-    }
-    const float m_new = fmaxf(m, wave_max(s)), m_use = m_new == -INFINITY ? 0.f : m_new;
-    const float p = seen ? __expf(s - m_use) : 0.f, f = __expf(m - m_use);
-    m = m_new;
-    l = l * f + wave_sum(p);
-#pragma unroll
-    for (int e = 0; e < DPL; ++e) acc[e] *= f;
-    for (int kk = 0; kk < 64 && base + kk <= pos; ++kk) {
-      const int pg = __shfl(page, kk, 64);
-      const float pk = __shfl(p, kk, 64);
-      if (pg < 0 || pg >= pv.n_pages) continue;
-      const CT* vp = (const CT*)pv.v + at(base + kk, pg) + DPL * lane;
-#pragma unroll
-      for (int e = 0; e < DPL; ++e) acc[e] += pk * Elem<CT>::to_f32(vp[e]);
-    }
-  }
-  if (lane == 0) { m_s[wave] = m; l_s[wave] = l; }
-#pragma unroll
-  for (int e = 0; e < DPL; ++e) o_s[wave][DPL * lane + e] = acc[e];
-  __syncthreads();
-  if (threadIdx.x < HD) {
-    const int d = threadIdx.x;
-    const float mm = fmaxf(fmaxf(m_s[0], m_s[1]), fmaxf(m_s[2], m_s[3])), mu = mm == -INFINITY ? 0.f : mm;
-    float o = 0.f, ll = 0.f;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      const float f = __expf(m_s[w] - mu);
-      o += f * o_s[w][d];
-      ll += f * l_s[w];
-    }
-    out[(size_t)t * ldo + (size_t)head * HD + d] = Elem<CT>::from_f32(ll == 0.f ? 0.f : o / ll);
+  const int d = (threadIdx.x % T4) * 4;
+  for (int v = blockIdx.y * (NT / T4) + threadIdx.x / T4; v < it.r * GQ; v += gridDim.y * (NT / T4)) {
+    PagedSum sum;
+    sum.add_ranges(part + (size_t)QVT * HD + 2 * v, part + (size_t)v * HD + d, (size_t)pv.nkv * SLOT, 0, it.n, 1);
+    paged_store4<bf16_t, PLANES>(po, it.first + it.row0 + v / GQ, (g * GQ + v % GQ) * HD + d, sum.result());
   }
 }
 

@@ -89,13 +89,12 @@ void launch_paged_append(const PagedView& v, int head_dim, const float* qkv, lon
     hipLaunchKernelGGL((paged_append_kernel<CT, 64>), grid, dim3(256), 0, s, qkv, ld, cu, row_pos, (const long long*)slots, (const CT*)gain, (const float2*)rope, eps, v);
 }
 
-// How an attention call of a bf16 cache is laid out: blocks per KV head of either kernel (0: no launch), log2 of those that the key ranges are chosen
+// How an attention call is laid out: blocks per KV head of either kernel (0: no launch), log2 of those that the key ranges are chosen
 // for, and the workspace: the counts of the groups with several ranges, then their partial results (paged_find), the larger of the two kernels'.
 struct PagedPlan { int few, tall, few_shift, tall_shift; size_t count_bytes, part_bytes; };
 int floor_log2(int v) { int s = 0; while ((2 << s) <= v) ++s; return s; }
 PagedPlan paged_plan(const dmtd_paged_cache* c, int max_new) {
   PagedPlan p{};
-  if (c->dtype != DMTD_DTYPE_BF16) return p;
   const int GQ = c->n_q_heads / c->n_kv_heads;
   const long limit = (long)c->max_pages * c->page_size;
   p.few_shift = floor_log2(std::max(PAGED_SLOTS_FEW / c->n_kv_heads, 1));
@@ -104,9 +103,12 @@ PagedPlan paged_plan(const dmtd_paged_cache* c, int max_new) {
   // a request with n rows is in ceil(n / rows of a group) groups
   const long few_rows = std::min<long>(c->max_rows, max_new), all = std::min(c->n_req, c->max_rows);
   const int rpb_few = 16 / GQ, rpb_tall = 128 / GQ, tall_from = PAGED_FEW / GQ + 1;
-  p.few = blocks(std::min<long>(c->max_rows, all + c->max_rows / rpb_few), p.few_shift, PAGED_KEYS_FEW);
+  const bool bf16 = c->dtype == DMTD_DTYPE_BF16;
+  long few = std::min<long>(c->max_rows, all + c->max_rows / rpb_few);
+  if (bf16) few = std::min<long>(few, (long)c->n_req * ((tall_from - 1 + rpb_few - 1) / rpb_few));
+  p.few = blocks(few, p.few_shift, PAGED_KEYS_FEW);
   size_t slot = (size_t)16 * (c->head_dim + 2) * 4 << p.few_shift;
-  if (few_rows >= tall_from) {
+  if (bf16 && few_rows >= tall_from) {
     p.tall = blocks(std::min<long>(c->n_req, c->max_rows / tall_from) + c->max_rows / rpb_tall, p.tall_shift, PAGED_KEYS_TALL);
     slot = std::max(slot, (size_t)128 * (c->head_dim + 2) * 4 << p.tall_shift);
   }
@@ -126,42 +128,39 @@ struct PagedCall {
   hipStream_t stream;
 };
 
-template <int HD, bool PLANES>
-hipError_t launch_paged_mfma(const PagedView& v, const PagedPlan& p, const PagedCall& a, const PagedOut& out) {
+template <typename CT, int HD, bool PLANES>
+hipError_t launch_paged_attention_t(const PagedView& v, const PagedPlan& p, const PagedCall& a, const PagedOut& out) {
   const int GQ = v.nh / v.nkv;
+  constexpr bool BF = sizeof(CT) == 2;
   PagedWork wk{p.few_shift, (int*)a.ws, (float*)(a.ws + p.count_bytes)};
+  // the queries' parts, then the waves' results, then what the join exchanges
   const int qv_max = std::min(16 / GQ, a.max_new) * GQ;
-  hipLaunchKernelGGL((paged_attention_few_mfma_kernel<HD, PLANES>), dim3(v.nkv, p.few), dim3(256), std::max({(size_t)4 * qv_max * HD * 4, (size_t)2 * 16 * (HD + ATT_QPAD) * 2, (size_t)2 * 256 * 16}), a.stream, a.cu, a.start, a.qkv, a.ld, (const bf16_t*)a.gain,
-                     (const float2*)a.rope, a.eps, a.max_new, PAGED_FEW, out, v, wk);
-  if (p.tall > 0) {
-    wk.shift = p.tall_shift;
-    auto kern = paged_attention_tall_mfma_kernel<HD, PLANES>;
-    constexpr size_t lds = (size_t)4 * 64 * HD * 2;
-    static bool big_lds = false;
-    if (lds > 48 * 1024 && !big_lds) {
-      hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-      if (e != hipSuccess) return e;
-      big_lds = true;
+  const size_t few_lds = std::max({(size_t)4 * qv_max * HD * 4, (size_t)16 * (BF ? 2 * (HD + ATT_QPAD) * 2 : (HD + 4) * 4), (size_t)2 * 256 * 16});
+  hipLaunchKernelGGL((paged_attention_few_mfma_kernel<CT, HD, PLANES>), dim3(v.nkv, p.few), dim3(256), few_lds, a.stream, a.cu, a.start, a.qkv, a.ld, (const CT*)a.gain,
+                     (const float2*)a.rope, a.eps, a.max_new, BF ? PAGED_FEW : INT_MAX, out, v, wk);
+  if constexpr (BF) {
+    if (p.tall > 0) {
+      wk.shift = p.tall_shift;
+      auto kern = paged_attention_tall_mfma_kernel<HD, PLANES>;
+      constexpr size_t lds = (size_t)4 * 64 * HD * 2;
+      static bool big_lds = false;
+      if (lds > 48 * 1024 && !big_lds) {
+        hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+        if (e != hipSuccess) return e;
+        big_lds = true;
+      }
+      hipLaunchKernelGGL(kern, dim3(v.nkv, p.tall), dim3(256), lds, a.stream, a.cu, a.start, a.qkv, a.ld, (const bf16_t*)a.gain, (const float2*)a.rope, a.eps, a.max_new, PAGED_FEW, out,
+                         v, wk);
+      hipLaunchKernelGGL((paged_attention_merge_kernel<HD, PLANES>), dim3(v.nkv, HD / 32, 1 << p.tall_shift), dim3(256), 0, a.stream, a.cu, a.start, a.max_new, PAGED_FEW, out, v, wk);
     }
-    hipLaunchKernelGGL(kern, dim3(v.nkv, p.tall), dim3(256), lds, a.stream, a.cu, a.start, a.qkv, a.ld, (const bf16_t*)a.gain, (const float2*)a.rope, a.eps, a.max_new, PAGED_FEW, out, v, wk);
-    hipLaunchKernelGGL((paged_attention_merge_kernel<HD, PLANES>), dim3(v.nkv, 128 * HD / 4 / 256, 1 << p.tall_shift), dim3(256), 0, a.stream, a.cu, a.start, a.max_new, PAGED_FEW, out, v, wk);
   }
-  return hipGetLastError();
-}
-
-template <int HD>
-hipError_t launch_paged_fp32(const PagedView& v, const PagedCall& a, const PagedOut& out) {
-  hipLaunchKernelGGL((paged_attention_rows_kernel<float, HD>), dim3(v.max_rows, v.nh), dim3(256), 0, a.stream, a.qkv, a.ld, a.start, a.cu, (const float*)a.gain, (const float2*)a.rope,
-                     a.eps, a.max_new, (float*)out.out, out.ld, v);
   return hipGetLastError();
 }
 
 hipError_t launch_paged_attention(const dmtd_paged_cache* c, const PagedView& v, const PagedCall& a, const PagedOut& out) {
-  if (c->dtype == DMTD_DTYPE_BF16) {
-    const PagedPlan p = paged_plan(c, a.max_new);
-    return c->head_dim == 128 ? launch_paged_mfma<128, false>(v, p, a, out) : launch_paged_mfma<64, false>(v, p, a, out);
-  }
-  return c->head_dim == 128 ? launch_paged_fp32<128>(v, a, out) : launch_paged_fp32<64>(v, a, out);
+  const PagedPlan p = paged_plan(c, a.max_new);
+  if (c->dtype == DMTD_DTYPE_BF16) return c->head_dim == 128 ? launch_paged_attention_t<bf16_t, 128, false>(v, p, a, out) : launch_paged_attention_t<bf16_t, 64, false>(v, p, a, out);
+  return c->head_dim == 128 ? launch_paged_attention_t<float, 128, false>(v, p, a, out) : launch_paged_attention_t<float, 64, false>(v, p, a, out);
 }
 
 }  // namespace
