@@ -14,9 +14,11 @@
 
 namespace dmtd {
 
-constexpr int PAGED_SLOTS_FEW = 1024, PAGED_SLOTS_TALL = 512;     // blocks the chip holds: 4 and 2 on each of 256 CUs
+constexpr int PAGED_SLOTS_FEW = 256, PAGED_SLOTS_TALL = 256;       // blocks that the key ranges are chosen for
+constexpr int PAGED_RESIDENT_TALL = 512;                           // blocks of the tall kernel that the chip holds
+constexpr int PAGED_WAVES = 8;                                     // waves of a block of the few-rows kernel
 constexpr int PAGED_FEW = 64;                                      // query vectors per KV head of a request that the few-rows kernel takes
-constexpr int PAGED_KEYS_FEW = 64, PAGED_KEYS_TALL = 256;          // shortest key ranges
+constexpr int PAGED_KEYS_FEW = 128, PAGED_KEYS_TALL = 256;          // shortest key ranges
 
 // Rows of a request as the kernels read them: none where the lengths do not fit the buffers or the tables
 struct PagedReq { int first, n, start; };
@@ -43,11 +45,11 @@ struct PagedItem { int req, first, row0, r, pos0, kb, ke, split, n, slot, group;
 // keys over the requests, kps >= T / 2^shift, so there are at most 2^shift + groups items; those of groups with several ranges (keys > kps, hence ceil(keys / kps) < 2
 // keys / kps) are fewer than 2^(shift + 1), and such groups fewer than 2^shift: what the workspace holds.  Called by whole blocks.  GROUP: y counts the
 // groups with several ranges instead (split and range of the result mean nothing).
-// The tall kernel's order of n items.  A chunk's later groups see more keys.  Up to 2^shift blocks are all resident from the start, two on a CU: the first round of the
-// CUs goes from the longest down, the second from the shortest up, and a CU's two come to about the same.  More blocks than that start as
-// others end, longest first.
-__device__ __forceinline__ int paged_turn(int y, int n, int shift) {
-  const int down = n <= (1 << shift) ? min(n, 1 << (shift - 1)) : n;
+// The tall kernel's order of n items per KV head.  A chunk's later groups see more keys.  Up to PAGED_RESIDENT_TALL blocks are all resident from the start, two
+// on a CU: the first round of the CUs goes from the longest down, the second from the shortest up, and a CU's two come to about the same.
+// More blocks than that start as others end, longest first.
+__device__ __forceinline__ int paged_turn(int y, int n, int nkv) {
+  const int down = n * nkv <= PAGED_RESIDENT_TALL ? min(n, (PAGED_RESIDENT_TALL / 2 + nkv - 1) / nkv) : n;
   return y < down ? n - 1 - y : (y < n ? y - down : y);
 }
 struct PagedShare { int groups, splits; };
@@ -76,7 +78,7 @@ __device__ __forceinline__ bool paged_find(const PagedView& pv, const int* cu, c
       const int u = __shfl_up(incl, o, 64);
       if (lane >= o) incl += u;
     }
-    if (TALL) y = paged_turn(y, __builtin_amdgcn_readlane(incl, 63), shift);
+    if (TALL) y = paged_turn(y, __builtin_amdgcn_readlane(incl, 63), pv.nkv);
     const unsigned long long behind = __ballot(incl > y);
     if (!behind) return false;
     i = __builtin_ctzll(behind);
@@ -112,7 +114,7 @@ __device__ __forceinline__ bool paged_find(const PagedView& pv, const int* cu, c
     }
     long long all, all_multi;
     long long at = block_scan<NT>(n_items, sums_s, all), at_multi = block_scan<NT>(n_multi, sums_s, all_multi);
-    if (TALL) y = paged_turn(y, (int)all, shift);
+    if (TALL) y = paged_turn(y, (int)all, pv.nkv);
     if (y >= all) return false;
     if (at <= y && y < at + n_items) {
       for (int j = i0; j < i1; ++j) {
@@ -261,11 +263,11 @@ __device__ __forceinline__ void paged_store4(const PagedOut& o, int row, int col
 // fp32 caches: 16x16x4 for both, the queries and probabilities as they are, any number of rows (a chunk's groups of 16 vectors find the keys in the L2).
 // Bound by the memory: 8 KiB per wave and group against 2 x HD / 16 + 2 x HD / 32 products.
 template <typename CT, int HD, bool PLANES>
-__global__ void __launch_bounds__(256, sizeof(CT) == 2 ? 4 : 2) paged_attention_few_mfma_kernel(const int* __restrict__ cu, const int* __restrict__ start, const float* __restrict__ qkv, long ld,
+__global__ void __launch_bounds__(64 * PAGED_WAVES, sizeof(CT) == 2 ? 4 : 2) paged_attention_few_mfma_kernel(const int* __restrict__ cu, const int* __restrict__ start, const float* __restrict__ qkv, long ld,
                                                                   const CT* __restrict__ q_gain, const float2* __restrict__ rope_tab, float eps, int max_new, int hi,
                                                                   PagedOut po, PagedView pv, PagedWork wk) {
   constexpr bool BF = sizeof(CT) == 2;
-  constexpr int QVT = 16, NW = 4, NT = 64 * NW, DPL = HD / 16, half = HD / 2, HL = HD / 32;
+  constexpr int QVT = 16, NW = PAGED_WAVES, NT = 64 * NW, DPL = HD / 16, half = HD / 2, HL = HD / 32;
   constexpr int KS = BF ? HD / 32 : HD / 16;                 // 16-byte pieces of a key a lane carries
   constexpr int QLD = BF ? HD + ATT_QPAD : HD + 4;           // a query row in LDS
   constexpr int VW = DPL * sizeof(CT) / 4;                   // 32-bit words of a value a lane carries: its DPL dims
@@ -290,7 +292,7 @@ __global__ void __launch_bounds__(256, sizeof(CT) == 2 ? 4 : 2) paged_attention_
   // query vector tid / 16, 2 HL values a lane
   fvec_t xa, xb;
   const int qv = tid >> 4, l16 = tid & 15, qrow = it.row0 + (qv < QV ? qv / GQ : 0), qhead = g * GQ + (qv < QV ? qv % GQ : 0);
-  {
+  if (qv < QVT) {
     const float* src = qkv + (size_t)(it.first + qrow) * ld + (size_t)qhead * HD + HL * l16;
     xa = *(const fvec_t*)src; xb = *(const fvec_t*)(src + half);
   }
@@ -304,12 +306,12 @@ __global__ void __launch_bounds__(256, sizeof(CT) == 2 ? 4 : 2) paged_attention_
     const CT* kp = (const CT*)pv.k + at;
     const CT* vp = (const CT*)pv.v + at;
 #pragma unroll
-    for (int t = 0; t < KS; ++t) kr[t] = __builtin_nontemporal_load((const u32x4*)(kp + sl * HD + (HD / KS) * t + (16 / (int)sizeof(CT)) * kq));
+    for (int t = 0; t < KS; ++t) kr[t] = *(const u32x4*)(kp + sl * HD + (HD / KS) * t + (16 / (int)sizeof(CT)) * kq);
 #pragma unroll
-    for (int m = 0; m < 4; ++m) vr[m] = __builtin_nontemporal_load((const vraw_t*)(vp + (4 * kq + m) * HD + DPL * sl));
+    for (int m = 0; m < 4; ++m) vr[m] = *(const vraw_t*)(vp + (4 * kq + m) * HD + DPL * sl);
   };
   if (first < ke) load_kv(first, __builtin_amdgcn_readlane(pages, 0));
-  {
+  if (qv < QVT) {
     const int pos = it.pos0 + (qrow - it.row0);
     float x0[HL], x1[HL], ss = 0.f;
 #pragma unroll
@@ -809,7 +811,7 @@ __global__ void __launch_bounds__(256) paged_attention_merge_kernel(const int* _
   if (it.n < 2) return;      // the request's first range is all that the group sees: written
   const float* part = wk.part + ((size_t)it.slot * pv.nkv + g) * SLOT;
   const int d = (threadIdx.x % T4) * 4;
-  for (int v = blockIdx.y * (NT / T4) + threadIdx.x / T4; v < it.r * GQ; v += gridDim.y * (NT / T4)) {
+  for (int v = blockIdx.y * (NT / T4) + threadIdx.x / T4; v < it.r * GQ; v += gridDim.y * (NT / T4)) {      // one each, unless the groups are many
     PagedSum sum;
     sum.add_ranges(part + (size_t)QVT * HD + 2 * v, part + (size_t)v * HD + d, (size_t)pv.nkv * SLOT, 0, it.n, 1);
     paged_store4<bf16_t, PLANES>(po, it.first + it.row0 + v / GQ, (g * GQ + v % GQ) * HD + d, sum.result());

@@ -89,9 +89,9 @@ void launch_paged_append(const PagedView& v, int head_dim, const float* qkv, lon
     hipLaunchKernelGGL((paged_append_kernel<CT, 64>), grid, dim3(256), 0, s, qkv, ld, cu, row_pos, (const long long*)slots, (const CT*)gain, (const float2*)rope, eps, v);
 }
 
-// How an attention call is laid out: blocks per KV head of either kernel (0: no launch), log2 of those that the key ranges are chosen
+// How an attention call is laid out: blocks per KV head of either kernel (0: no launch), groups that the merge looks at, log2 of those that the key ranges are chosen
 // for, and the workspace: the counts of the groups with several ranges, then their partial results (paged_find), the larger of the two kernels'.
-struct PagedPlan { int few, tall, few_shift, tall_shift; size_t count_bytes, part_bytes; };
+struct PagedPlan { int few, tall, merge, few_shift, tall_shift; size_t count_bytes, part_bytes; };
 int floor_log2(int v) { int s = 0; while ((2 << s) <= v) ++s; return s; }
 PagedPlan paged_plan(const dmtd_paged_cache* c, int max_new) {
   PagedPlan p{};
@@ -109,7 +109,9 @@ PagedPlan paged_plan(const dmtd_paged_cache* c, int max_new) {
   p.few = blocks(few, p.few_shift, PAGED_KEYS_FEW);
   size_t slot = (size_t)16 * (c->head_dim + 2) * 4 << p.few_shift;
   if (bf16 && few_rows >= tall_from) {
-    p.tall = blocks(std::min<long>(c->n_req, c->max_rows / tall_from) + c->max_rows / rpb_tall, p.tall_shift, PAGED_KEYS_TALL);
+    const long groups = std::min<long>(c->n_req, c->max_rows / tall_from) + c->max_rows / rpb_tall;
+    p.tall = blocks(groups, p.tall_shift, PAGED_KEYS_TALL);
+    p.merge = (int)std::min(groups, 1L << p.tall_shift);
     slot = std::max(slot, (size_t)128 * (c->head_dim + 2) * 4 << p.tall_shift);
   }
   p.count_bytes = align_up(((size_t)4 << std::max(p.few_shift, p.tall_shift)) * c->n_kv_heads, 256);
@@ -135,8 +137,8 @@ hipError_t launch_paged_attention_t(const PagedView& v, const PagedPlan& p, cons
   PagedWork wk{p.few_shift, (int*)a.ws, (float*)(a.ws + p.count_bytes)};
   // the queries' parts, then the waves' results, then what the join exchanges
   const int qv_max = std::min(16 / GQ, a.max_new) * GQ;
-  const size_t few_lds = std::max({(size_t)4 * qv_max * HD * 4, (size_t)16 * (BF ? 2 * (HD + ATT_QPAD) * 2 : (HD + 4) * 4), (size_t)2 * 256 * 16});
-  hipLaunchKernelGGL((paged_attention_few_mfma_kernel<CT, HD, PLANES>), dim3(v.nkv, p.few), dim3(256), few_lds, a.stream, a.cu, a.start, a.qkv, a.ld, (const CT*)a.gain,
+  const size_t few_lds = std::max({(size_t)PAGED_WAVES * qv_max * HD * 4, (size_t)16 * (BF ? 2 * (HD + ATT_QPAD) * 2 : (HD + 4) * 4), (size_t)2 * 64 * PAGED_WAVES * 16});
+  hipLaunchKernelGGL((paged_attention_few_mfma_kernel<CT, HD, PLANES>), dim3(v.nkv, p.few), dim3(64 * PAGED_WAVES), few_lds, a.stream, a.cu, a.start, a.qkv, a.ld, (const CT*)a.gain,
                      (const float2*)a.rope, a.eps, a.max_new, BF ? PAGED_FEW : INT_MAX, out, v, wk);
   if constexpr (BF) {
     if (p.tall > 0) {
@@ -151,7 +153,9 @@ hipError_t launch_paged_attention_t(const PagedView& v, const PagedPlan& p, cons
       }
       hipLaunchKernelGGL(kern, dim3(v.nkv, p.tall), dim3(256), lds, a.stream, a.cu, a.start, a.qkv, a.ld, (const bf16_t*)a.gain, (const float2*)a.rope, a.eps, a.max_new, PAGED_FEW, out,
                          v, wk);
-      hipLaunchKernelGGL((paged_attention_merge_kernel<HD, PLANES>), dim3(v.nkv, HD / 32, 1 << p.tall_shift), dim3(256), 0, a.stream, a.cu, a.start, a.max_new, PAGED_FEW, out, v, wk);
+      // a vector per thread as long as that makes at most 1024 blocks, most of which have nothing to do
+      const int merge_blocks = std::min(HD / 8, std::max(HD / 32, 1024 / (v.nkv * p.merge)));
+      hipLaunchKernelGGL((paged_attention_merge_kernel<HD, PLANES>), dim3(v.nkv, merge_blocks, p.merge), dim3(256), 0, a.stream, a.cu, a.start, a.max_new, PAGED_FEW, out, v, wk);
     }
   }
   return hipGetLastError();
