@@ -401,35 +401,32 @@ def _raise(lib, rc):
         raise DmtdError(rc, lib.dmtd_last_error(None).decode())
 
 
-def _want(t, name, dtype, device, shape=None, contiguous=True):
-    """A GPU tensor of that type on that device, and of that shape where one is given (None: any extent)."""
-    if t.dtype is not dtype or t.device != device:
-        raise ValueError(f"{name} must be a {dtype} tensor on {device}")
-    if contiguous and not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous")
-    if shape is not None and (t.dim() != len(shape) or any(n is not None and n != m for n, m in zip(shape, t.shape))):
-        raise ValueError(f"{name} must have the shape {tuple('any' if n is None else n for n in shape)}, not {tuple(t.shape)}")
+def _want(t, name, dtype, index, shape):
+    """The address of a contiguous GPU tensor of that type and shape on that device."""
+    if t.dtype is not dtype or t.get_device() != index or t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on GPU {index}, not {t.dtype} {tuple(t.shape)} on {t.device}")
     return t.data_ptr()
 
 
 class _OnDevice:
     """What the handles of the paged cache share: the library, a device, and calls on torch's current stream of that device."""
 
-    def _open(self, device):
+    def _open(self, t):
         import torch
-        if device.type != "cuda":
+        if not t.is_cuda:
             raise ValueError("the paged cache lives on the GPU")
-        self._torch, self._lib, self.device = torch, load_library(), device
+        self._torch, self._lib, self.device, self._index = torch, load_library(), t.device, t.get_device()
         self._i32, self._i64, self._f32 = torch.int32, torch.int64, torch.float32
+        # the stream's handle without the Stream object around it: a microsecond less a call
+        self._stream_of = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
 
     def _call(self, fn, *args):
-        cuda = self._torch.cuda
-        stream = cuda.current_stream(self.device)
-        if cuda.current_device() == self.device.index:
-            rc = fn(*args, stream.cuda_stream)
+        stream = self._stream_of(self._index)
+        if self._torch.cuda.current_device() == self._index:
+            rc = fn(*args, stream)
         else:
-            with cuda.device(self.device):
-                rc = fn(*args, stream.cuda_stream)
+            with self._torch.cuda.device(self._index):
+                rc = fn(*args, stream)
         if rc != DMTD_OK:
             _raise(self._lib, rc)
         return stream
@@ -442,13 +439,13 @@ class PageTables(_OnDevice):
     caller's GPU tensors, changed in place; :meth:`empty` makes those of an empty pool."""
 
     def __init__(self, block_table, held, free_pages, n_free, page_size: int):
-        self._open(block_table.device)
-        dev, i32 = self.device, self._i32
+        self._open(block_table)
         n_req, max_pages = block_table.shape
+        i32, dev = self._i32, self._index
         self.block_table, self.held, self.free_pages, self.n_free, self.page_size = block_table, held, free_pages, n_free, int(page_size)
-        self._c = _PagePool(free_pages.numel(), self.page_size, n_req, max_pages, _want(block_table, "block_table", i32, dev, (None, None)),
-                            _want(held, "held", i32, dev, (n_req,)), _want(free_pages, "free_pages", i32, dev, (None,)), _want(n_free, "n_free", i32, dev, (1,)))
-        self._p = C.byref(self._c)
+        self._c = _PagePool(free_pages.numel(), self.page_size, n_req, max_pages, _want(block_table, "block_table", i32, dev, (n_req, max_pages)),
+                            _want(held, "held", i32, dev, (n_req,)), _want(free_pages, "free_pages", i32, dev, (free_pages.numel(),)), _want(n_free, "n_free", i32, dev, (1,)))
+        self._p, self._per_req, self._per_end = C.byref(self._c), (n_req,), (n_req + 1,)
 
     @classmethod
     def empty(cls, n_pages: int, page_size: int, n_req: int, max_pages: int, device="cuda"):
@@ -461,10 +458,10 @@ class PageTables(_OnDevice):
     def build(self, start, rows, cu_rows, row_pos, slots, status):
         """Pages and places for a step: request i has ``start[i]`` tokens and brings ``rows[i]``.  Writes ``cu_rows`` int32 ``[n_req + 1]``, ``row_pos`` int32
         ``[max_rows]``, ``slots`` int64 ``[max_rows]`` and ``status`` int32 ``[2]`` (0, or why the step has no rows: see the header)."""
-        i32, dev, n = self._i32, self.device, self._c.n_req
-        room = row_pos.numel()
-        self._call(self._lib.dmtd_page_tables, self._p, _want(start, "start", i32, dev, (n,)), _want(rows, "rows", i32, dev, (n,)), room,
-                   _want(cu_rows, "cu_rows", i32, dev, (n + 1,)), _want(row_pos, "row_pos", i32, dev, (room,)), _want(slots, "slots", self._i64, dev, (room,)),
+        i32, dev = self._i32, self._index
+        room = row_pos.shape
+        self._call(self._lib.dmtd_page_tables, self._p, _want(start, "start", i32, dev, self._per_req), _want(rows, "rows", i32, dev, self._per_req), room[0] if len(room) == 1 else 0,
+                   _want(cu_rows, "cu_rows", i32, dev, self._per_end), _want(row_pos, "row_pos", i32, dev, room), _want(slots, "slots", self._i64, dev, room),
                    _want(status, "status", i32, dev, (2,)))
 
 
@@ -474,57 +471,66 @@ class PagedCache(_OnDevice):
     torch's current stream.  Steps have up to ``max_rows`` rows.  The handle holds the attention's workspace: calls of one handle must not overlap."""
 
     def __init__(self, k, v, block_table, n_q_heads: int, max_rows: int):
-        self._open(k.device)
-        torch, dev = self._torch, self.device
-        if k.dtype not in (torch.bfloat16, torch.float32):
-            raise ValueError("k and v must be bfloat16 or float32")
+        self._open(k)
+        torch, dev = self._torch, self._index
+        if k.dtype not in (torch.bfloat16, torch.float32) or v.dtype is not k.dtype:
+            raise ValueError("k and v must be bfloat16 or float32, both alike")
         n_pages, n_kv, page_size, hd = k.shape
-        for name, t in (("k", k), ("v", v)):
-            _want(t, name, k.dtype, dev, tuple(k.shape), contiguous=False)
-            if t.stride() != (k.stride(0), page_size * hd, hd, 1):
+        if v.shape != k.shape or v.device != k.device:
+            raise ValueError("k and v must have one shape and lie on one GPU")
+        stride = (k.stride(0) if n_pages > 1 else n_kv * page_size * hd, page_size * hd, hd, 1)
+        for t in (k, v):
+            if any(n > 1 and a != b for n, a, b in zip(t.shape, t.stride(), stride)):
                 raise ValueError("pages must be contiguous, and k and v laid out alike")
+        n_req, max_pages = block_table.shape
         self.k, self.v, self.block_table, self.dtype, self.max_rows = k, v, block_table, k.dtype, int(max_rows)
-        self._c = _PagedCache(k.data_ptr(), v.data_ptr(), k.stride(0) if n_pages > 1 else 0, _want(block_table, "block_table", self._i32, dev, (None, None)), n_pages,
-                              page_size, block_table.shape[0], block_table.shape[1], n_q_heads, n_kv, hd, 1 if k.dtype is torch.bfloat16 else 0, max_rows)
+        self._c = _PagedCache(k.data_ptr(), v.data_ptr(), stride[0], _want(block_table, "block_table", self._i32, dev, (n_req, max_pages)), n_pages, page_size, n_req, max_pages,
+                              n_q_heads, n_kv, hd, 1 if k.dtype is torch.bfloat16 else 0, max_rows)
         self._p = C.byref(self._c)
-        self._n, self._hd, self._q_cols, self._cols = block_table.shape[0], hd, n_q_heads * hd, (n_q_heads + 2 * n_kv) * hd
+        self._q_heads, self._q_cols, self._cols = (n_q_heads, hd), n_q_heads * hd, (n_q_heads + 2 * n_kv) * hd
+        self._per_req, self._per_end, self._per_row, self._gain, self._angles = (n_req,), (n_req + 1,), (self.max_rows,), (hd,), (hd // 2, 2)
         self._ws_bytes = self._lib.dmtd_paged_workspace_bytes(self._p)
         if self._ws_bytes == 0:
             _raise(self._lib, DMTD_EINVAL)
-        self._ws = torch.zeros(self._ws_bytes, dtype=torch.uint8, device=dev)
-        stream = torch.cuda.current_stream(dev)
+        self._ws = torch.zeros(self._ws_bytes, dtype=torch.uint8, device=k.device)
+        self._ws_ptr = self._ws.data_ptr()
+        stream = torch.cuda.current_stream(k.device)
         stream.synchronize()              # zeroed, whichever stream the first call is on
         self._streams = {stream.cuda_stream}
 
     def _rows(self, qkv, cols, norm, rope):
-        dev = self.device
-        if qkv.dim() != 2 or qkv.dtype is not self._f32 or qkv.device != dev or qkv.stride(1) != 1 or qkv.shape[0] < self.max_rows or qkv.shape[1] < cols:
-            raise ValueError(f"qkv must be float32 [at least {self.max_rows}, at least {cols}] on {dev} with contiguous rows")
-        gain = None if norm is None else _want(norm, "the norm's gain", self.dtype, dev, (self._hd,))
+        dev, shape = self._index, qkv.shape
+        if len(shape) != 2 or qkv.dtype is not self._f32 or qkv.get_device() != dev or shape[0] < self.max_rows or shape[1] < cols or qkv.stride(1) != 1:
+            raise ValueError(f"qkv must be float32 [at least {self.max_rows}, at least {cols}] on GPU {dev} with contiguous rows")
+        gain = None if norm is None else _want(norm, "the norm's gain", self.dtype, dev, self._gain)
+        ld = qkv.stride(0) if shape[0] > 1 else (shape[1] + 3) // 4 * 4
         if rope is None:
-            return qkv.data_ptr(), qkv.stride(0), gain, None, 0
-        return qkv.data_ptr(), qkv.stride(0), gain, _want(rope, "rope", self._f32, dev, (None, self._hd // 2, 2)), rope.shape[0]
+            return qkv.data_ptr(), ld, gain, None, 0
+        n = rope.shape[0]
+        return qkv.data_ptr(), ld, gain, _want(rope, "rope", self._f32, dev, (n, *self._angles)), n
 
     def append(self, qkv, cu_rows, row_pos, slots, k_norm=None, rope=None, eps: float = 1e-6):
         """Keys (normalised with ``k_norm``, rotated by ``rope`` [positions, head_dim / 2, (cos, sin)]) and values of the fused projection's rows
         ``qkv`` into the places that :meth:`PageTables.build` gave them."""
         x, ld, gain, tab, n_tab = self._rows(qkv, self._cols, k_norm, rope)
-        dev = self.device
-        self._call(self._lib.dmtd_paged_append, self._p, x, ld, _want(cu_rows, "cu_rows", self._i32, dev, (self._n + 1,)), _want(row_pos, "row_pos", self._i32, dev, (self.max_rows,)),
-                   _want(slots, "slots", self._i64, dev, (self.max_rows,)), gain, eps, tab, n_tab)
+        i32, dev = self._i32, self._index
+        self._call(self._lib.dmtd_paged_append, self._p, x, ld, _want(cu_rows, "cu_rows", i32, dev, self._per_end), _want(row_pos, "row_pos", i32, dev, self._per_row),
+                   _want(slots, "slots", self._i64, dev, self._per_row), gain, eps, tab, n_tab)
 
     def attention(self, qkv, start, cu_rows, out=None, q_norm=None, rope=None, eps: float = 1e-6, max_new: int = 0):
         """The rows' queries over their requests' pages, into ``out`` ``[max_rows, n_q_heads, head_dim]`` of the cache's type (made if not given; rows behind
         the last one are not written).  ``max_new``: the most rows one request brings, if known."""
         x, ld, gain, tab, n_tab = self._rows(qkv, self._q_cols, q_norm, rope)
-        dev = self.device
+        i32, dev = self._i32, self._index
         if out is None:
-            out = self._torch.empty(self.max_rows, self._q_cols // self._hd, self._hd, dtype=self.dtype, device=dev)
-        if out.dim() != 3 or out.shape[1:] != (self._q_cols // self._hd, self._hd) or out.shape[0] < self.max_rows or out.stride()[1:] != (self._hd, 1):
-            raise ValueError(f"out must be [at least {self.max_rows}, {self._q_cols // self._hd}, {self._hd}] with contiguous rows")
-        stream = self._call(self._lib.dmtd_paged_attention, self._p, x, ld, _want(start, "start", self._i32, dev, (self._n,)), _want(cu_rows, "cu_rows", self._i32, dev, (self._n + 1,)),
-                            max_new, gain, eps, tab, n_tab, _want(out, "out", self.dtype, dev, contiguous=False), out.stride(0), self._ws.data_ptr(), self._ws_bytes)
-        if stream.cuda_stream not in self._streams:
-            self._streams.add(stream.cuda_stream)
-            self._ws.record_stream(stream)      # the workspace is not reused before this stream's work has ended
+            out = self._torch.empty(self.max_rows, *self._q_heads, dtype=self.dtype, device=self.device)
+        shape = out.shape
+        if (len(shape) != 3 or shape[1:] != self._q_heads or shape[0] < self.max_rows or out.dtype is not self.dtype or out.get_device() != dev or
+                out.stride(2) != 1 or (shape[1] > 1 and out.stride(1) != shape[2])):
+            raise ValueError(f"out must be {self.dtype} [at least {self.max_rows}, {self._q_heads[0]}, {self._q_heads[1]}] on GPU {dev} with contiguous rows")
+        stream = self._call(self._lib.dmtd_paged_attention, self._p, x, ld, _want(start, "start", i32, dev, self._per_req), _want(cu_rows, "cu_rows", i32, dev, self._per_end),
+                            max_new, gain, eps, tab, n_tab, out.data_ptr(), out.stride(0) if shape[0] > 1 else self._q_cols, self._ws_ptr, self._ws_bytes)
+        if stream not in self._streams:
+            self._streams.add(stream)
+            self._ws.record_stream(self._torch.cuda.current_stream(self._index))      # the workspace is not reused before this stream's work has ended
         return out

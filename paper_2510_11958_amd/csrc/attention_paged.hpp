@@ -14,11 +14,18 @@
 
 namespace dmtd {
 
-constexpr int PAGED_SLOTS_FEW = 256, PAGED_SLOTS_TALL = 256;       // blocks that the key ranges are chosen for
+// Blocks that the key ranges are chosen for.  bf16, few rows: one of four waves on each CU reads as fast as more do, and shorter ranges cost more joins (us, 32/8 heads of 128,
+// 256 / 512 / 1024 blocks: 3 rows of 8 requests behind 16384 86 / 95 / 107, one row behind 16384 20 / 23 / 28, 4 rows of 32 behind 1024 26 / 35 / 35).  fp32, whose
+// products weigh more: 512 (16/8 heads, 200 rows behind 1000 55 / 41 / 46).  Tall: half of the blocks that the chip holds (64 rows behind 4096 29, with 512 46).
+constexpr int PAGED_SLOTS_FEW = 256, PAGED_SLOTS_FP32 = 512, PAGED_SLOTS_TALL = 256;
 constexpr int PAGED_RESIDENT_TALL = 512;                           // blocks of the tall kernel that the chip holds
-constexpr int PAGED_WAVES = 8;                                     // waves of a block of the few-rows kernel
-constexpr int PAGED_FEW = 64;                                      // query vectors per KV head of a request that the few-rows kernel takes
-constexpr int PAGED_KEYS_FEW = 128, PAGED_KEYS_TALL = 256;          // shortest key ranges
+constexpr int PAGED_WAVES = 4;                                     // waves of a block of the few-rows kernel
+// Query vectors per KV head of a request that the few-rows kernel takes, which reads its keys once per 16 of them (us, few / tall: 64 vectors behind 4096 18 / 24, of 16
+// requests behind 2000 43 / 51; 128 vectors 22 / 26 and 78 / 57).
+constexpr int PAGED_FEW = 64;
+// Shortest key ranges (few, us at 64 / 128 / 256: one row behind 100 8.2 / 6.6 / 6.6, behind 1024 10.6 / 9.7 / 10.9; tall, at 256 / 512 / 1024: a chunk of 330 rows beside
+// single tokens, 14/2 heads of 64, 33 / 35 / 45)
+constexpr int PAGED_KEYS_FEW = 128, PAGED_KEYS_TALL = 256;
 
 // Rows of a request as the kernels read them: none where the lengths do not fit the buffers or the tables
 struct PagedReq { int first, n, start; };
@@ -72,12 +79,7 @@ __device__ __forceinline__ bool paged_find(const PagedView& pv, const int* cu, c
     const int gr = paged_groups(q, GQ, lo, hi, rpb);
     kps = keys_of(wave_reduce((unsigned long long)gr * (unsigned)(q.start + q.n), [](unsigned long long a, unsigned long long b) { return a + b; }));
     const int sp = (int)((unsigned)(q.start + q.n + kps - 1) / (unsigned)kps), items = GROUP ? (sp > 1 ? gr : 0) : gr * sp;
-    int incl = items;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int u = __shfl_up(incl, o, 64);
-      if (lane >= o) incl += u;
-    }
+    const int incl = wave_scan(items);
     if (TALL) y = paged_turn(y, __builtin_amdgcn_readlane(incl, 63), pv.nkv);
     const unsigned long long behind = __ballot(incl > y);
     if (!behind) return false;
@@ -261,6 +263,9 @@ __device__ __forceinline__ void paged_store4(const PagedOut& o, int row, int col
 //   output   O[q, d] += sum_key P[q, key] V[key, d], 16x16x16: a lane's operand is 4 consecutive keys of one row or column, so nothing moves between
 //            lanes; a probability goes in as two bf16 parts.
 // fp32 caches: 16x16x4 for both, the queries and probabilities as they are, any number of rows (a chunk's groups of 16 vectors find the keys in the L2).
+// Values are loaded past the L2, keys through it: a key's 256 bytes take four loads, which share cache lines (us, both through the caches / values past
+// them / both: 3 rows of 8 requests behind 16384 103 / 86 / 92, 31 ragged rows in pages of 16 tokens 24 / 26 / 30, out of cold memory 30 / 28 / 31, one row of 64
+// behind 1024 out of cold memory 53 / 49 / 48).
 // Bound by the memory: 8 KiB per wave and group against 2 x HD / 16 + 2 x HD / 32 products.
 template <typename CT, int HD, bool PLANES>
 __global__ void __launch_bounds__(64 * PAGED_WAVES, sizeof(CT) == 2 ? 4 : 2) paged_attention_few_mfma_kernel(const int* __restrict__ cu, const int* __restrict__ start, const float* __restrict__ qkv, long ld,
@@ -286,7 +291,7 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, sizeof(CT) == 2 ? 4 : 2) pag
   CT (*qhi_s)[QLD] = (CT (*)[QLD])paged_dyn_smem, (*qlo_s)[QLD] = qhi_s + QVT;      // (fp32: one part)
   // pages of this wave's next 64 groups, one a lane
   const int* trow = pv.table + (size_t)it.req * pv.max_pages;
-  auto load_pages = [&](int base) { return base + 64 * lane < ke ? trow[(base + 64 * lane) >> pv.page_shift] : 0; };
+  auto load_pages = [&](int base) { return base + 16 * NW * lane < ke ? trow[(base + 16 * NW * lane) >> pv.page_shift] : 0; };
   const int first = it.kb + 16 * wave;
   int pages = load_pages(first);
   // query vector tid / 16, 2 HL values a lane
@@ -308,7 +313,7 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, sizeof(CT) == 2 ? 4 : 2) pag
 #pragma unroll
     for (int t = 0; t < KS; ++t) kr[t] = *(const u32x4*)(kp + sl * HD + (HD / KS) * t + (16 / (int)sizeof(CT)) * kq);
 #pragma unroll
-    for (int m = 0; m < 4; ++m) vr[m] = *(const vraw_t*)(vp + (4 * kq + m) * HD + DPL * sl);
+    for (int m = 0; m < 4; ++m) vr[m] = __builtin_nontemporal_load((const vraw_t*)(vp + (4 * kq + m) * HD + DPL * sl));
   };
   if (first < ke) load_kv(first, __builtin_amdgcn_readlane(pages, 0));
   if (qv < QVT) {

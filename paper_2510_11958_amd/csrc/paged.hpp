@@ -24,6 +24,17 @@ struct PagedView {
   int limit;                        // positions a request may have: the block table's, or the rotary table's where that is shorter
 };
 
+// Sums over the lanes up to and with this one, without LDS: within rows of 16, then the rows' last values onto the rows behind them
+__device__ __forceinline__ int wave_scan(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false);      // row_shr:1, 2, 4, 8
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);      // row_bcast:15 into rows 1 and 3
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);      // row_bcast:31 into rows 2 and 3
+  return v;
+}
+
 // Sum of v over the threads before this one, and over all of them, in a block of NT threads
 template <int NT, typename T>
 __device__ __forceinline__ T block_scan(T v, T* wave_sums /* LDS, NT / 64 */, T& total) {

@@ -97,13 +97,13 @@ PagedPlan paged_plan(const dmtd_paged_cache* c, int max_new) {
   PagedPlan p{};
   const int GQ = c->n_q_heads / c->n_kv_heads;
   const long limit = (long)c->max_pages * c->page_size;
-  p.few_shift = floor_log2(std::max(PAGED_SLOTS_FEW / c->n_kv_heads, 1));
+  const bool bf16 = c->dtype == DMTD_DTYPE_BF16;
+  p.few_shift = floor_log2(std::max((bf16 ? PAGED_SLOTS_FEW : PAGED_SLOTS_FP32) / c->n_kv_heads, 1));
   p.tall_shift = floor_log2(std::max(PAGED_SLOTS_TALL / c->n_kv_heads, 1));
   auto blocks = [&](long groups, int shift, int min_keys) { return (int)std::min((1L << shift) + groups, groups * ((limit + min_keys - 1) / min_keys)); };
   // a request with n rows is in ceil(n / rows of a group) groups
   const long few_rows = std::min<long>(c->max_rows, max_new), all = std::min(c->n_req, c->max_rows);
   const int rpb_few = 16 / GQ, rpb_tall = 128 / GQ, tall_from = PAGED_FEW / GQ + 1;
-  const bool bf16 = c->dtype == DMTD_DTYPE_BF16;
   long few = std::min<long>(c->max_rows, all + c->max_rows / rpb_few);
   if (bf16) few = std::min<long>(few, (long)c->n_req * ((tall_from - 1 + rpb_few - 1) / rpb_few));
   p.few = blocks(few, p.few_shift, PAGED_KEYS_FEW);

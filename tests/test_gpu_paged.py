@@ -199,6 +199,8 @@ ATTENTION = [
     (H8, 32, [40, 50, 60, 70], [0, 2, 0, 1]), (H8, 32, [40, 50, 60], [1, 0, 0]),
     # a few rows: refills
     (H8, 64, [100, 1, 700], [3, 2, 4]), (H8, 16, [33], [5]), (H4, 16, [0, 90], [16, 13]), (H16, 32, [64, 5], [2, 3]), (H7, 16, [61, 200], [7, 3]),
+    # several groups of a request's rows, each over several key ranges; ranges of several rounds of a block's waves
+    (H4, 16, [1000, 2000], [20, 30]), (H16, 32, [1500], [4]), (H8, 16, [1100, 700], [16, 9]), (H4, 16, [3000] * 40, [1] * 40), (H8, 64, [2500] * 20, [2] * 20),
     # chunks, from the start and behind keys; beside single tokens
     (H8, 64, [0], [130]), (H4, 16, [0, 7], [65, 1]), (H6, 32, [300], [97]), (H7, 256, [130, 0], [75, 40]), (H8, 128, [513, 90, 0, 1100], [200, 1, 1, 1]), (H1, 16, [31], [200]),
     (H16, 64, [20], [40]),
@@ -211,6 +213,10 @@ ATTENTION = [
 @pytest.mark.parametrize("dtype", [BF, F32])
 def test_attention(heads, page, start, rows, dtype):
     Setup(heads, dtype, page, start, rows, seed=len(start) + sum(rows)).check()
+
+
+def test_ranges_longer_than_a_wave_keeps_page_numbers_for():
+    Setup((128, 128, 64), BF, 16, [8999], [1], seed=21).check()
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
