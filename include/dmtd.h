@@ -376,6 +376,35 @@ int dmtd_paged_attention(const dmtd_paged_cache* cache, const float* qkv, int64_
                          const void* q_norm, float eps, const float* rope, int32_t rope_len, void* out, int64_t ldo, void* workspace,
                          size_t workspace_bytes, void* stream);
 
+/* ---- Paged steps of a context ----
+ * Requests that come and go, over a context's model: the memory of its caches (max_batch x max_seq_len positions a layer) becomes a pool of pages, and each step takes
+ * whatever the requests bring - a chunk of one's prompt beside the next tokens of others, each at its own point of its cycle (Sec. 2.2).  A request
+ * has a slot in [0, max_batch) from its first tokens to its release.
+ *
+ * dmtd_paged_begin: turns an empty context (fresh or reset) over to paged steps; dmtd_reset ends them.  Until then dmtd_prefill*, dmtd_masked_forward and dmtd_read_kv return
+ * DMTD_ESTATE, decode calls as before prefill.  memory_dev: DEVICE, 256-byte aligned, dmtd_paged_step_bytes(cfg, page_size) bytes (0: invalid), the caller's and left alone by others until
+ * then.  Errors: DMTD_EINVAL, DMTD_ESTATE (not empty, n_early > 0, dry run), DMTD_ECAPACITY (memory too small), DMTD_EHIP. */
+size_t dmtd_paged_step_bytes(const dmtd_config* cfg, int32_t page_size);
+int dmtd_paged_begin(dmtd_ctx* ctx, int32_t page_size, void* memory_dev, size_t memory_bytes);
+
+/* One step.  n requests; HOST arrays: slots[n], each at most once; counts[n], the new tokens a request brings (>= 1); tokens, those of all requests, in the order of
+ * the requests; full[n].  All new tokens pass the late layers.  full[j] != 0 (a full step; the chunks of a prompt): request j's tokens that await their
+ * refill and its new ones pass the front layers first, and the late layers read the front output at the new ones (with full_pos_add_embed the literal sum).  full[j] == 0 (a
+ * late-only step): the late layers read the embeddings (Eq. 4), and the tokens await their refill.
+ * next_tokens: HOST int32 [n] or NULL: greedy choice behind each request's last new token, whose logits dmtd_logits returns as float32 [n, vocab].
+ * A request's results are those of the other calls for the same tokens and cycles (up to the rounding of other sums), whatever the other requests do.
+ * Steps run kernel by kernel (use_graphs is ignored); dmtd_get_state and dmtd_get_trace do not follow them.  After DMTD_EHIP only dmtd_reset is left.
+ * Errors: DMTD_EINVAL; DMTD_ESTATE (no dmtd_paged_begin; sampling on; n_late changed while tokens await refill); DMTD_ECAPACITY (max_seq_len; more new tokens, or more rows for
+ * the front layers, than a pass carries: 2048 for a bf16 model, or as many as its workspace holds, at least 16 max_batch; too few free pages); DMTD_EHIP. */
+int dmtd_paged_step(dmtd_ctx* ctx, int32_t n, const int32_t* slots, const int32_t* counts, const int32_t* tokens, const uint8_t* full, int32_t n_late,
+                    int32_t* next_tokens);
+
+/* The request in a slot ends: its pages go back to the pool.  Errors: DMTD_EINVAL, DMTD_ESTATE, DMTD_EHIP. */
+int dmtd_paged_release(dmtd_ctx* ctx, int32_t slot);
+
+/* A slot's tokens in the late (n_tok) and front (n_front) layers' caches, and the pool's free pages.  Any pointer may be NULL.  Errors: DMTD_EINVAL (no dmtd_paged_begin, slot). */
+int dmtd_paged_get_state(const dmtd_ctx* ctx, int32_t slot, int32_t* n_tok, int32_t* n_front, int32_t* free_pages);
+
 /* Back to the state right after dmtd_create (caches are treated as empty). */
 int dmtd_reset(dmtd_ctx* ctx);
 

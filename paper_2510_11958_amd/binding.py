@@ -106,6 +106,16 @@ def load_library():
     lib.dmtd_masked_forward.restype = C.c_int
     lib.dmtd_masked_forward.argtypes = [C.c_void_p, P(C.c_int32), C.c_int32, C.c_int32, P(C.c_uint8), C.c_int32, P(C.c_float),
                                         P(C.c_int32), P(C.c_float), C.c_size_t, P(C.c_float)]
+    lib.dmtd_paged_step_bytes.restype = C.c_size_t
+    lib.dmtd_paged_step_bytes.argtypes = [P(_Config), C.c_int32]
+    lib.dmtd_paged_begin.restype = C.c_int
+    lib.dmtd_paged_begin.argtypes = [C.c_void_p, C.c_int32, C.c_void_p, C.c_size_t]
+    lib.dmtd_paged_step.restype = C.c_int
+    lib.dmtd_paged_step.argtypes = [C.c_void_p, C.c_int32, P(C.c_int32), P(C.c_int32), P(C.c_int32), P(C.c_uint8), C.c_int32, P(C.c_int32)]
+    lib.dmtd_paged_release.restype = C.c_int
+    lib.dmtd_paged_release.argtypes = [C.c_void_p, C.c_int32]
+    lib.dmtd_paged_get_state.restype = C.c_int
+    lib.dmtd_paged_get_state.argtypes = [C.c_void_p, C.c_int32, P(C.c_int32), P(C.c_int32), P(C.c_int32)]
     lib.dmtd_page_tables.restype = C.c_int
     lib.dmtd_page_tables.argtypes = [P(_PagePool), C.c_void_p, C.c_void_p, C.c_int32] + [C.c_void_p] * 5
     lib.dmtd_paged_append.restype = C.c_int
@@ -389,6 +399,38 @@ class Engine:
         if want_logits:
             out["logits"] = logits
         return out
+
+    def paged_begin(self, page_size: int = 64):
+        """Requests that come and go from here on, until ``reset``: the caches become a pool of pages, steps are :meth:`paged_step`."""
+        import torch
+        cc = self.cfg.to_c(0)
+        nbytes = self.lib.dmtd_paged_step_bytes(C.byref(cc), page_size)
+        if nbytes == 0 or self.cfg.dry_run:
+            self._check(self.lib.dmtd_paged_begin(self._h, page_size, None, 0))
+        memory = torch.empty(nbytes, dtype=torch.uint8, device=self._workspace.device)
+        self._check(self.lib.dmtd_paged_begin(self._h, page_size, memory.data_ptr(), nbytes))
+        self._paged_memory = memory
+
+    def paged_step(self, slots, tokens, full, n_late: int) -> np.ndarray:
+        """One step of the requests in ``slots``: ``tokens`` holds one sequence of new tokens per request, ``full`` whether it passes the front layers (a full step, a
+        chunk of a prompt) or only the late ones.  Returns the greedy next token of each; ``logits`` then has a row per request."""
+        parts = [np.atleast_1d(np.asarray(t, dtype=np.int32)) for t in tokens]
+        s, f = np.ascontiguousarray(slots, dtype=np.int32), np.ascontiguousarray(full, dtype=np.uint8)
+        if s.shape != (len(parts),) or f.shape != s.shape:
+            raise ValueError("one slot, one sequence of tokens and one mark per request")
+        counts, flat, out = np.array([p.size for p in parts], np.int32), np.concatenate(parts) if parts else np.empty(0, np.int32), np.empty(len(parts), np.int32)
+        self._check(self.lib.dmtd_paged_step(self._h, len(parts), _i32p(s), _i32p(counts), _i32p(flat), f.ctypes.data_as(C.POINTER(C.c_uint8)), n_late, _i32p(out)))
+        self._batch = len(parts)
+        return out
+
+    def paged_release(self, slot: int):
+        """The request in ``slot`` ends; its pages go back to the pool."""
+        self._check(self.lib.dmtd_paged_release(self._h, slot))
+
+    def paged_state(self, slot: int) -> dict:
+        a, b, f = C.c_int32(), C.c_int32(), C.c_int32()
+        self._check(self.lib.dmtd_paged_get_state(self._h, slot, C.byref(a), C.byref(b), C.byref(f)))
+        return {"n_tok": a.value, "n_front": b.value, "free_pages": f.value}
 
     def reset(self):
         self._check(self.lib.dmtd_reset(self._h))

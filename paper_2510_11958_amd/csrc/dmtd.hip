@@ -178,6 +178,20 @@ struct Rows {
 
 }  // namespace
 
+struct PagedPass;
+
+// Requests that come and go (dmtd_paged_begin): the host's view of the slots.  The device's tables are in the caller's memory (PagedLayout).
+struct PagedState {
+  struct Seq {
+    int n_tok = 0, n_front = 0;      // tokens in the late and in the front layers' caches
+    std::vector<int32_t> pending;    // those that only the late layers have seen
+  };
+  bool on = false, failed = false;
+  int page = 0, free_pages = 0, n_late = 0, last_n = 0;      // last_n: requests of the last step
+  char* mem = nullptr;
+  std::vector<Seq> seqs;
+};
+
 struct dmtd_ctx {
   dmtd_config cfg;
   Sched sched;
@@ -228,6 +242,8 @@ struct dmtd_ctx {
   int part_rows = 0;          // rows per sequence the partials are laid out for (stride between ranges: part_rows * query heads per KV head)
   int test_fail_step = -1;    // tests of the failure path: the next decode call reports a launch failure before this step (once)
   char* static_scratch = nullptr;   // this device's copy of the library's own scratch array (address taken at create)
+  PagedState paged;                 // requests that come and go
+  const PagedPass* paged_pass = nullptr;      // run_layer: the rows are theirs
   std::vector<Step> plan_buf;       // dmtd_decode_cycle_noalloc: the call's steps (capacity reserved at create)
 };
 
@@ -975,6 +991,40 @@ hipError_t launch_attention(dmtd_ctx* c, int l, const float* qkv, OT* attn, OT* 
   return hipGetLastError();
 }
 
+}  // namespace
+
+#include "paged_calls.hpp"
+
+// What the layers of a pass over paged requests (paged_steps.hpp) need beside their rows: the cache (k and v are set per layer), the rows' maps and lengths
+struct PagedPass {
+  dmtd_paged_cache cache;
+  const int *cu, *start, *pos;
+  const int64_t* slots;
+  int max_new;
+  char* ws;
+};
+
+namespace {
+
+// a3 + a4 of such a pass: append, then attention, whose result goes where the O projection reads it (bf16: two planes)
+hipError_t paged_layer_attention(dmtd_ctx* c, int l, const float* qkv, void* out, bf16_t* out_lo) {
+  const dmtd_config& cf = c->cfg;
+  const PagedPass& p = *c->paged_pass;
+  dmtd_paged_cache pc = p.cache;
+  char* kv = c->ws + c->o.kv + (size_t)l * c->o.kv_layer_stride;
+  pc.k = kv;
+  pc.v = kv + c->o.kv_v_off;
+  const float* rope = (const float*)(c->ws + c->o.rope_tab);
+  const PagedView v = paged_view(&pc, rope, cf.max_seq_len);
+  const long nqkv = (long)(cf.n_q_heads + 2 * cf.n_kv_heads) * cf.head_dim;
+  if (pc.dtype == DMTD_DTYPE_BF16) launch_paged_append<bf16_t>(v, cf.head_dim, qkv, nqkv, p.cu, p.pos, p.slots, c->layers[l].k_norm, cf.rms_eps, rope, c->stream);
+  else launch_paged_append<float>(v, cf.head_dim, qkv, nqkv, p.cu, p.pos, p.slots, c->layers[l].k_norm, cf.rms_eps, rope, c->stream);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  return launch_paged_attention(&pc, v, PagedCall{qkv, nqkv, p.start, p.cu, p.max_new, c->layers[l].q_norm, cf.rms_eps, rope, p.ws, c->stream},
+                                PagedOut{out, out_lo, (long)cf.n_q_heads * cf.head_dim, blocked_rows(c, pc.max_rows)});
+}
+
 // ---------------------------------------------------------------- the steps of a pass
 
 // a1: rows <- embeddings of the tokens at the rows' positions (next reader: the norm of layer next_layer)
@@ -1072,16 +1122,20 @@ hipError_t run_layer(dmtd_ctx* c, int l, Rows& R, int r, int sel, int offset) {
     a.W = s.qkv; a.xb = R.xb; a.xb_lo = R.xb_lo; a.ldxb = d; a.N = nqkv; a.K = d; a.ssp = R.ssp; a.n_parts = R.n_parts; a.ssp_ld = c->ssp_ld;
     a.eps = cf.rms_eps; a.y = qkv; a.ldy = nqkv;
     const bool wide = r > kMaxRows;      // more rows per sequence than an attention block keeps in LDS: the append is a launch of its own
-    c->fold_qkv = !wide;
+    c->fold_qkv = !wide && !c->paged_pass;
     e = launch_qkv(c, a, rows);
     c->fold_qkv = false;
     if (e != hipSuccess) { c->qkv_pending = QkvSrc{}; return e; }
     // a3 + a4: QK-RMSNorm + RoPE + KV append + split-K attention, then the merge (output packed for the O projection)
-    if (wide && (e = launch_kv_append<bf16_t>(c, l, qkv, sel, offset, r)) != hipSuccess) return e;
-    c->fold_merge = true;
-    e = launch_attention<bf16_t, bf16_t>(c, l, qkv, ab, ab_lo, sel, offset, r, wide ? 2 : 1);
-    c->fold_merge = false;
-    if (e != hipSuccess) { c->merge_pending = MergeSrc{}; return e; }
+    if (c->paged_pass) {
+      if ((e = paged_layer_attention(c, l, qkv, ab, ab_lo)) != hipSuccess) return e;
+    } else {
+      if (wide && (e = launch_kv_append<bf16_t>(c, l, qkv, sel, offset, r)) != hipSuccess) return e;
+      c->fold_merge = true;
+      e = launch_attention<bf16_t, bf16_t>(c, l, qkv, ab, ab_lo, sel, offset, r, wide ? 2 : 1);
+      c->fold_merge = false;
+      if (e != hipSuccess) { c->merge_pending = MergeSrc{}; return e; }
+    }
     // a5: O projection + residual; emits the MLP norm's input
     a = MfmaArgs{};
     a.W = s.o; a.xb = ab; a.xb_lo = ab_lo; a.ldxb = qd; a.N = d; a.K = qd; a.y = R.h; a.ldy = d; a.yb = R.xb; a.yb_lo = R.xb_lo; a.ldyb = d;
@@ -1109,8 +1163,10 @@ hipError_t run_layer(dmtd_ctx* c, int l, Rows& R, int r, int sel, int offset) {
   a.W = w.q; a.gain = w.attn_norm; a.x = R.h; a.ldx = d; a.y = qkv; a.ldy = nqkv; a.N = nqkv; a.K = d;
   if ((e = gemv_rows<EPI_STORE, true>(c, a, rows)) != hipSuccess) return e;
   // a3 + a4: QK-RMSNorm + RoPE + KV append + split-K attention, then the merge
-  if (r > kMaxRows && (e = launch_kv_append<float>(c, l, qkv, sel, offset, r)) != hipSuccess) return e;
-  if ((e = launch_attention<float, float>(c, l, qkv, attn, (float*)nullptr, sel, offset, r, r > kMaxRows ? 2 : 1)) != hipSuccess) return e;
+  if (c->paged_pass) {
+    if ((e = paged_layer_attention(c, l, qkv, attn, nullptr)) != hipSuccess) return e;
+  } else if (r > kMaxRows && (e = launch_kv_append<float>(c, l, qkv, sel, offset, r)) != hipSuccess) return e;
+  if (!c->paged_pass && (e = launch_attention<float, float>(c, l, qkv, attn, (float*)nullptr, sel, offset, r, r > kMaxRows ? 2 : 1)) != hipSuccess) return e;
   // a5: O projection + residual
   a = GemvArgs{};
   a.W = w.o; a.x = attn; a.ldx = qd; a.y = R.h; a.ldy = d; a.N = d; a.K = qd;
@@ -1673,7 +1729,7 @@ void destroy_graphs(dmtd_ctx* c) {
 
 // ============================================================================ C ABI
 
-#include "paged_calls.hpp"
+#include "paged_steps.hpp"
 
 extern "C" {
 
@@ -1798,7 +1854,7 @@ static int prefill_impl(dmtd_ctx* c, const int32_t* tokens, int32_t batch, int32
   if (prompt_len < 1) { c->err = "prompt_len must be >= 1"; return DMTD_EINVAL; }
   if (cf.full_pos_add_embed && (n_late < 1 || n_late > cf.n_layers)) { c->err = "the literal Eq. 4 reading needs n_late at prefill"; return DMTD_EINVAL; }
   if (cf.full_pos_add_embed && c->sched.n_early + n_late > cf.n_layers) { c->err = "n_early + n_late exceeds the number of layers"; return DMTD_EINVAL; }
-  if (c->sched.n_tok != 0) { c->err = "already prefilled; call dmtd_reset first"; return DMTD_ESTATE; }
+  if (c->sched.n_tok != 0 || c->paged.on) { c->err = "already prefilled; call dmtd_reset first"; return DMTD_ESTATE; }
   if (prompt_len >= cf.max_seq_len) { c->err = "prompt does not leave room for a generated token"; return DMTD_ECAPACITY; }
   bool ragged = false;
   if (lengths) {
@@ -2219,8 +2275,9 @@ int dmtd_get_seq_state(const dmtd_ctx* c, int32_t b, int32_t* n_front, int32_t* 
 int dmtd_logits(dmtd_ctx* c, float* out, size_t out_elems) {
   if (!c) return DMTD_EINVAL;
   if (!out) { c->err = "null output pointer"; return DMTD_EINVAL; }
-  if (c->sched.n_tok == 0 || c->cfg.dry_run) { c->err = "no logits before prefill"; return DMTD_ESTATE; }
-  const size_t need = (size_t)c->batch * c->cfg.vocab;
+  const int rows = c->paged.on ? c->paged.last_n : c->sched.n_tok == 0 ? 0 : c->batch;
+  if (rows == 0 || c->cfg.dry_run) { c->err = "no logits before prefill"; return DMTD_ESTATE; }
+  const size_t need = (size_t)rows * c->cfg.vocab;
   if (out_elems < need) { c->err = "logits buffer too small"; return DMTD_ECAPACITY; }
   HIP_TRY(c, hipMemcpyAsync(out, c->ws + c->o.logits, need * 4, hipMemcpyDeviceToHost, c->stream));
   HIP_TRY(c, hipStreamSynchronize(c->stream));
@@ -2259,6 +2316,7 @@ int dmtd_read_kv(dmtd_ctx* c, int32_t layer, int32_t b, int32_t n_pos, float* ou
     c->err = "bad argument to dmtd_read_kv"; return DMTD_EINVAL;
   }
   if (cf.dry_run) { c->err = "no device state in a dry run"; return DMTD_ESTATE; }
+  if (c->paged.on) { c->err = "the caches hold pages"; return DMTD_ESTATE; }
   const size_t half = (size_t)cf.n_kv_heads * n_pos * cf.head_dim;
   if (out_elems < 2 * half) { c->err = "KV buffer too small"; return DMTD_ECAPACITY; }
   // each (b, g) owns a contiguous run of positions in the cache: copy the raw rows and widen on the host
@@ -2397,7 +2455,7 @@ int dmtd_masked_forward(dmtd_ctx* c, const int32_t* tokens, int32_t batch, int32
   if (n < 1) { c->err = "sequence length must be >= 1"; return DMTD_EINVAL; }
   if (n_late < 1 || n_late > cf.n_layers) { c->err = "n_late must be in [1, n_layers]"; return DMTD_EINVAL; }
   if (c->sched.n_early + n_late > cf.n_layers) { c->err = "n_early + n_late exceeds the number of layers"; return DMTD_EINVAL; }
-  if (c->sched.n_tok != 0) { c->err = "the masked forward needs an empty context; call dmtd_reset first"; return DMTD_ESTATE; }
+  if (c->sched.n_tok != 0 || c->paged.on) { c->err = "the masked forward needs an empty context; call dmtd_reset first"; return DMTD_ESTATE; }
   if (n > cf.max_seq_len) { c->err = "sequence longer than max_seq_len"; return DMTD_ECAPACITY; }
   if (logits && logits_elems < (size_t)batch * n * cf.vocab) { c->err = "logits buffer too small"; return DMTD_ECAPACITY; }
   for (size_t i = 0; i < (size_t)batch * n; ++i)
@@ -2478,6 +2536,7 @@ int dmtd_set_n_early(dmtd_ctx* c, int32_t n_early) {
   if (!c) return DMTD_EINVAL;
   if (n_early < 0 || n_early >= c->cfg.n_layers) { c->err = "n_early must be in [0, n_layers - 1]"; return DMTD_EINVAL; }
   if (c->sched.n_tok != c->sched.n_front || c->diverged) { c->err = "n_early changed while tokens await refill"; return DMTD_ESTATE; }
+  if (c->paged.on && n_early != 0) { c->err = "paged steps are not available in the ExDy variant"; return DMTD_ESTATE; }
   if (c->sched.n_tok != 0 && c->cfg.full_pos_add_embed && n_early != c->sched.n_early) {
     c->err = "under the literal Eq. 4 reading n_early is fixed at prefill"; return DMTD_ESTATE;
   }
@@ -2499,6 +2558,7 @@ int dmtd_reset(dmtd_ctx* c) {
   c->diverged = false;
   c->seq_phase.clear();
   c->seq_front.clear();
+  c->paged = PagedState{};
   return DMTD_OK;
 }
 

@@ -5,6 +5,7 @@
 
 namespace {
 
+
 int paged_fail(int code, const char* why) {
   g_create_error = why;
   return code;
@@ -161,8 +162,10 @@ hipError_t launch_paged_attention_t(const PagedView& v, const PagedPlan& p, cons
   return hipGetLastError();
 }
 
+// out.lo not null (bf16): the two planes that the projections read, instead of rows of the cache's type
 hipError_t launch_paged_attention(const dmtd_paged_cache* c, const PagedView& v, const PagedCall& a, const PagedOut& out) {
   const PagedPlan p = paged_plan(c, a.max_new);
+  if (c->dtype == DMTD_DTYPE_BF16 && out.lo) return c->head_dim == 128 ? launch_paged_attention_t<bf16_t, 128, true>(v, p, a, out) : launch_paged_attention_t<bf16_t, 64, true>(v, p, a, out);
   if (c->dtype == DMTD_DTYPE_BF16) return c->head_dim == 128 ? launch_paged_attention_t<bf16_t, 128, false>(v, p, a, out) : launch_paged_attention_t<bf16_t, 64, false>(v, p, a, out);
   return c->head_dim == 128 ? launch_paged_attention_t<float, 128, false>(v, p, a, out) : launch_paged_attention_t<float, 64, false>(v, p, a, out);
 }
