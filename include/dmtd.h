@@ -315,7 +315,7 @@ int dmtd_score_plan(const dmtd_config* cfg, int32_t batch, int32_t n, int32_t pl
  * Buffers with a row per new token have room for max_rows; what lies behind the last row is neither read nor written. */
 
 typedef struct dmtd_page_pool {
-  int32_t  n_pages;        /* pages of the pool */
+  int32_t  n_pages;        /* pages of the pool, at most 2^30 */
   int32_t  page_size;      /* tokens of a page: 16, 32, 64, 128 or 256 */
   int32_t  n_req;          /* requests, at most 8192 */
   int32_t  max_pages;      /* entries of a request's block table; max_pages * page_size <= 2^30 */

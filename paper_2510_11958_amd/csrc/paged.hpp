@@ -85,83 +85,134 @@ __device__ __forceinline__ void page_row(const int* table, const int* start, int
 // Pages for a step.  Request i holds held[i] pages and needs ceil((start[i] + rows[i]) / page size) of them.  Its surplus goes onto the
 // pool's stack, what it lacks comes off the stack, in the order of the requests and of their pages.  The k-th page given back lies k below
 // the new top, so the next step takes it as its k-th: giving back what a step took restores the stack.
-// One block of NT threads, each with the requests ipt t .. ipt t + ipt - 1: three prefix sums, and a search in one of them for each
-// page that moves.  Everything is checked before anything is written; a step that does not fit has no rows (cu all 0) and changes nothing.
-// Bound by latency: a chain of five round trips to memory (lengths; pages given back; pages taken off; their table entries read for the places; the last
-// stores), and a few barriers.
+// One block, whose threads hold up to RPT requests each: three prefix sums, and a search in one of them for each page that moves and for
+// each row.  Everything is checked before anything is written; a step that does not fit has no rows (cu all 0) and changes nothing.
+// Bound by latency: a chain of four round trips to memory (lengths; pages off the stack; their entries read for the rows' places; the last stores) and five
+// barriers.  us in a stream of calls: one request 2.9; 256, of which 19 grow by a page 6.2 with 1024 threads, three sums one after the other and
+// lengths read again, 22 for 200 prompts of 2000 tokens; as it stands see below.
+constexpr int PAGE_RPT = kPagedMaxRequests / 1024;
 template <int NT>
 __global__ void __launch_bounds__(NT) page_tables_kernel(int* __restrict__ table, int* __restrict__ held, int* __restrict__ stack, int* __restrict__ n_free,
                                                          const int* __restrict__ start, const int* __restrict__ rows, int n_req, int max_pages, int n_pages,
                                                          int page_shift, int max_rows, int* __restrict__ cu, int* __restrict__ row_pos,
                                                          long long* __restrict__ slots /* null: page_rows_kernel follows */, int* __restrict__ status) {
-  __shared__ int first_s[kPagedMaxRequests + 1];
-  __shared__ long long sums_s[NT / 64 < 1 ? 1 : NT / 64];
+  constexpr int NWV = NT / 64, RPT = NT == 1024 ? PAGE_RPT : 1;
+  __shared__ int first_s[NT * RPT];
+  __shared__ int sums_s[3][NWV];
+  __shared__ float sizes_s[3][NWV];
   __shared__ int bad_s;
-  const int tid = threadIdx.x, ipt = (n_req + NT - 1) / NT, i0 = min(tid * ipt, n_req), i1 = min(i0 + ipt, n_req);
-  const long long limit = (long long)max_pages << page_shift;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, ipt = (n_req + NT - 1) / NT, i0 = tid * ipt;
+  const int limit = max_pages << page_shift;             // at most 2^30
+  if (tid == 0) bad_s = INT_MAX;
   const int top0 = n_free[0];
-  if (tid == 0) bad_s = top0 < 0 || top0 > n_pages ? -1 : INT_MAX;
-  __syncthreads();
-  long long sg = 0, st = 0, sr = 0;
-  for (int i = i0; i < i1; ++i) {
-    const int s = start[i], r = rows[i], h = held[i];
-    if (s < 0 || r < 0 || h < 0 || h > max_pages || (long long)s + r > limit) { atomicMin(&bad_s, i); continue; }
-    const int need = (int)(((long long)s + r + (1 << page_shift) - 1) >> page_shift);
-    sg += max(h - need, 0);
-    st += max(need - h, 0);
-    sr += r;
+  int s[RPT], r[RPT], h[RPT], need[RPT];
+#pragma unroll
+  for (int j = 0; j < RPT; ++j) {
+    const bool on = j < ipt && i0 + j < n_req;
+    s[j] = on ? start[i0 + j] : 0;
+    r[j] = on ? rows[i0 + j] : 0;
+    h[j] = on ? held[i0 + j] : 0;
   }
-  long long give, take, total;
-  const long long g0 = block_scan<NT>(sg, sums_s, give), t0 = block_scan<NT>(st, sums_s, take), r0 = block_scan<NT>(sr, sums_s, total);
   __syncthreads();
-  const int bad = bad_s;
+  // pages given back, pages taken, rows: as integers, and as floats, which tell whether the integers have run over
+  int sum[3] = {0, 0, 0};
+  float size[3] = {0.f, 0.f, 0.f};
+#pragma unroll
+  for (int j = 0; j < RPT; ++j) {
+    const bool fits = s[j] >= 0 && r[j] >= 0 && h[j] >= 0 && h[j] <= max_pages && s[j] <= limit && r[j] <= limit - s[j];
+    if (!fits) atomicMin(&bad_s, i0 + j);
+    need[j] = fits ? (s[j] + r[j] + (1 << page_shift) - 1) >> page_shift : 0;
+    const int v[3] = {max(h[j] - need[j], 0), max(need[j] - h[j], 0), r[j]};
+#pragma unroll
+    for (int k = 0; k < 3; ++k) { sum[k] += fits ? v[k] : 0; size[k] += fits ? (float)v[k] : 0.f; }
+  }
+  int before[3], total[3] = {0, 0, 0};
+  float all[3] = {0.f, 0.f, 0.f};
+#pragma unroll
+  for (int k = 0; k < 3; ++k) {
+    const int incl = wave_scan(sum[k]);
+    before[k] = incl - sum[k];
+    size[k] = wave_sum(size[k]);
+    if (lane == 63) { sums_s[k][wave] = incl; sizes_s[k][wave] = size[k]; }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < 3; ++k)
+#pragma unroll
+    for (int w = 0; w < NWV; ++w) {
+      const int u = sums_s[k][w];
+      if (w < wave) before[k] += u;
+      total[k] += u;
+      all[k] += sizes_s[k][w];
+    }
+  const bool over[3] = {all[0] >= 1.1e9f, all[1] >= 1.1e9f, all[2] >= 1.1e9f};      // 2^30 and more
   int code = 0, detail = 0;
-  if (bad != INT_MAX) { code = -1; detail = bad; }
-  else if (total > max_rows || top0 + give > n_pages) { code = -1; detail = -1; }
-  else if (top0 + give < take) { code = -3; detail = (int)min(take - give - top0, (long long)INT_MAX); }
+  if (top0 < 0 || top0 > n_pages) { code = -1; detail = -1; }
+  else if (bad_s != INT_MAX) { code = -1; detail = bad_s; }
+  else if (over[2] || total[2] > max_rows || over[0] || total[0] > n_pages - top0) { code = -1; detail = -1; }
+  else if (over[1] || total[1] > top0 + total[0]) { code = -3; detail = over[1] ? INT_MAX : total[1] - total[0] - top0; }
   if (tid == 0) { status[0] = code; status[1] = detail; }
   if (code) {
     for (int i = tid; i <= n_req; i += NT) cu[i] = 0;
     return;
   }
-  const int top = top0 + (int)give, left = top - (int)take;
-  auto need_of = [&](int i) { return (start[i] + rows[i] + (1 << page_shift) - 1) >> page_shift; };
-  if (give) {
-    int at = (int)g0;
-    for (int i = i0; i < i1; ++i) { first_s[i] = at; at += max(held[i] - need_of(i), 0); }
+  const int give = total[0], take = total[1], n_rows = total[2], top = top0 + give;
+  // a prefix sum into LDS, for searches in it
+  auto lay_out = [&](int k) {
+    int at = before[k];
+#pragma unroll
+    for (int j = 0; j < RPT; ++j)
+      if (j < ipt && i0 + j < n_req) {
+        first_s[i0 + j] = at;
+        at += k == 0 ? max(h[j] - need[j], 0) : k == 1 ? max(need[j] - h[j], 0) : r[j];
+      }
     __syncthreads();
-    for (int k = tid; k < (int)give; k += NT) {
-      const int i = last_at_most(first_s, n_req, k);
-      int* entry = table + (size_t)i * max_pages + need_of(i) + k - first_s[i];
-      stack[top - 1 - k] = *entry;
-      *entry = -1;
+  };
+  constexpr int U = NT == 1024 ? 4 : 1;       // pages in flight per thread
+  if (give) {
+    lay_out(0);
+    for (int k0 = tid; k0 < give; k0 += U * NT) {
+      int* entry[U];
+      int page[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int k = min(k0 + u * NT, give - 1), i = last_at_most(first_s, n_req, k);
+        entry[u] = table + (size_t)i * max_pages + ((start[i] + rows[i] + (1 << page_shift) - 1) >> page_shift) + k - first_s[i];
+        page[u] = *entry[u];
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (k0 + u * NT < give) { stack[top - 1 - k0 - u * NT] = page[u]; *entry[u] = -1; }
     }
     __syncthreads();                // the stack is whole before pages come off it, the search's array free again
   }
   if (take) {
-    int at = (int)t0;
-    for (int i = i0; i < i1; ++i) { first_s[i] = at; at += max(need_of(i) - held[i], 0); }
-    __syncthreads();
-    for (int k = tid; k < (int)take; k += NT) {
-      const int i = last_at_most(first_s, n_req, k);
-      table[(size_t)i * max_pages + held[i] + k - first_s[i]] = stack[top - 1 - k];
-      stack[top - 1 - k] = -1;
+    lay_out(1);
+    for (int k0 = tid; k0 < take; k0 += U * NT) {
+      int page[U];
+      int* entry[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int k = min(k0 + u * NT, take - 1), i = last_at_most(first_s, n_req, k);
+        page[u] = stack[top - 1 - k];
+        entry[u] = table + (size_t)i * max_pages + held[i] + k - first_s[i];
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (k0 + u * NT < take) { *entry[u] = page[u]; stack[top - 1 - k0 - u * NT] = -1; }
     }
-    __syncthreads();                // held is read above
+    __syncthreads();                // held is read above; entries are read below
   }
-  {
-    int at = (int)r0;
-    for (int i = i0; i < i1; ++i) {
-      first_s[i] = at;
-      cu[i] = at;
-      at += rows[i];
-      held[i] = need_of(i);
+  lay_out(2);
+#pragma unroll
+  for (int j = 0; j < RPT; ++j)
+    if (j < ipt && i0 + j < n_req) {
+      cu[i0 + j] = first_s[i0 + j];
+      if (need[j] != h[j]) held[i0 + j] = need[j];
     }
-    if (tid == 0) { cu[n_req] = (int)total; n_free[0] = left; }
-  }
+  if (tid == 0) { cu[n_req] = n_rows; n_free[0] = top - take; }
   if (!slots) return;
-  __syncthreads();
-  for (int t = tid; t < (int)total; t += NT) {
+  for (int t = tid; t < n_rows; t += NT) {
     const int i = last_at_most(first_s, n_req, t);
     page_row(table, start, max_pages, page_shift, i, t - first_s[i], t, row_pos, slots);
   }

@@ -36,7 +36,7 @@ int check_table(int n_req, int max_pages, int n_pages, int page_size) {
   if (!page_size_ok(page_size)) return paged_fail(DMTD_EINVAL, "page_size must be 16, 32, 64, 128 or 256");
   if (n_req < 1 || n_req > kPagedMaxRequests) return paged_fail(DMTD_EINVAL, "n_req must be in [1, 8192]");
   if (max_pages < 1 || (long)max_pages * page_size > (1L << 30)) return paged_fail(DMTD_EINVAL, "max_pages must be >= 1 and max_pages * page_size <= 2^30");
-  if (n_pages < 1) return paged_fail(DMTD_EINVAL, "n_pages must be >= 1");
+  if (n_pages < 1 || n_pages > (1 << 30)) return paged_fail(DMTD_EINVAL, "n_pages must be in [1, 2^30]");
   return DMTD_OK;
 }
 
@@ -195,7 +195,8 @@ int dmtd_page_tables(const dmtd_page_pool* p, const int32_t* start, const int32_
     hipLaunchKernelGGL(page_tables_kernel<NT>, dim3(1), dim3(NT), 0, s, p->block_table, p->held, p->free_pages, p->n_free, start, rows, p->n_req, p->max_pages,
                        p->n_pages, shift, max_rows, cu_rows, row_pos, many ? (long long*)nullptr : (long long*)slots, status);
   };
-  if (p->n_req <= 64 && max_rows <= 64) launch(std::integral_constant<int, 64>());
+  if (p->n_req <= 64 && max_rows <= 256) launch(std::integral_constant<int, 64>());
+  else if (p->n_req <= 256 && max_rows <= 1024) launch(std::integral_constant<int, 256>());
   else launch(std::integral_constant<int, 1024>());
   if (many)
     hipLaunchKernelGGL(page_rows_kernel, dim3((max_rows + 1023) / 1024), dim3(256), 0, s, (const int*)p->block_table, start, p->n_req, p->max_pages, shift,
