@@ -268,9 +268,9 @@ __device__ __forceinline__ void paged_store4(const PagedOut& o, int row, int col
 // behind 1024 out of cold memory 53 / 49 / 48).
 // Bound by the memory: 8 KiB per wave and group against 2 x HD / 16 + 2 x HD / 32 products.
 template <typename CT, int HD, bool PLANES>
-__global__ void __launch_bounds__(64 * PAGED_WAVES, sizeof(CT) == 2 ? 4 : 2) paged_attention_few_mfma_kernel(const int* __restrict__ cu, const int* __restrict__ start, const float* __restrict__ qkv, long ld,
-                                                                  const CT* __restrict__ q_gain, const float2* __restrict__ rope_tab, float eps, int max_new, int hi,
-                                                                  PagedOut po, PagedView pv, PagedWork wk) {
+__device__ __forceinline__ void paged_attention_few(int y, const int* __restrict__ cu, const int* __restrict__ start, const float* __restrict__ qkv, long ld,
+                                                    const CT* __restrict__ q_gain, const float2* __restrict__ rope_tab, float eps, int max_new, int hi, const PagedOut& po,
+                                                    const PagedView& pv, const PagedWork& wk) {
   constexpr bool BF = sizeof(CT) == 2;
   constexpr int QVT = 16, NW = PAGED_WAVES, NT = 64 * NW, DPL = HD / 16, half = HD / 2, HL = HD / 32;
   constexpr int KS = BF ? HD / 32 : HD / 16;                 // 16-byte pieces of a key a lane carries
@@ -281,7 +281,7 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, sizeof(CT) == 2 ? 4 : 2) pag
   typedef unsigned short hvec_t __attribute__((ext_vector_type(HL)));
   const int g = blockIdx.x, GQ = pv.nh / pv.nkv, rpb = QVT / GQ;
   PagedItem it;
-  if (!paged_find<NT, 16 * NW, false>(pv, cu, start, max_new, GQ, 0, hi, rpb, wk.shift, PAGED_KEYS_FEW, blockIdx.y, it)) return;
+  if (!paged_find<NT, 16 * NW, false>(pv, cu, start, max_new, GQ, 0, hi, rpb, wk.shift, PAGED_KEYS_FEW, y, it)) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), sl = lane & 15, kq = lane >> 4;
   const int QV = it.r * GQ, ke = it.ke;
   __shared__ float wm[NW][QVT], wl[NW][QVT];
@@ -498,9 +498,9 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, sizeof(CT) == 2 ? 4 : 2) pag
 // block's own positions may be infinite or NaN, which 0 does not silence: the block looks at them first; if one is not finite, it and its like behind
 // it go into LDS as 0 and the rows that see it become NaN.
 template <int HD, bool PLANES>
-__global__ void __launch_bounds__(256, 2) paged_attention_tall_mfma_kernel(const int* __restrict__ cu, const int* __restrict__ start, const float* __restrict__ qkv, long ld,
-                                                                           const bf16_t* __restrict__ q_gain, const float2* __restrict__ rope_tab, float eps, int max_new, int lo,
-                                                                           PagedOut po, PagedView pv, PagedWork wk) {
+__device__ __forceinline__ void paged_attention_tall(int y, const int* __restrict__ cu, const int* __restrict__ start, const float* __restrict__ qkv, long ld,
+                                                     const bf16_t* __restrict__ q_gain, const float2* __restrict__ rope_tab, float eps, int max_new, int lo, const PagedOut& po,
+                                                     const PagedView& pv, const PagedWork& wk) {
   constexpr int QVT = 128, NT = 256, KT = 64;
   constexpr int T = HD / 16;           // steps over d for the scores
   constexpr int DT = HD / 32;          // 32-dim tiles of the output
@@ -513,7 +513,7 @@ __global__ void __launch_bounds__(256, 2) paged_attention_tall_mfma_kernel(const
   __shared__ int poison_s;
   const int g = blockIdx.x, GQ = pv.nh / pv.nkv, rpb = QVT / GQ;
   PagedItem it;
-  if (!paged_find<NT, KT, false, true>(pv, cu, start, max_new, GQ, lo, INT_MAX, rpb, wk.shift, PAGED_KEYS_TALL, blockIdx.y, it)) return;
+  if (!paged_find<NT, KT, false, true>(pv, cu, start, max_new, GQ, lo, INT_MAX, rpb, wk.shift, PAGED_KEYS_TALL, y, it)) return;
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), hi = lane >> 5;
   bf16_t* ring = (bf16_t*)paged_dyn_smem;                      // K, K, V^T, V^T
   const int QV = it.r * GQ, qv = 32 * w + (lane & 31), kb = it.kb, ke = it.ke;
@@ -801,6 +801,24 @@ __global__ void __launch_bounds__(256, 2) paged_attention_tall_mfma_kernel(const
       for (int q = 0; q < 4; ++q) *(f32x4*)(part + (size_t)qo * HD + 32 * t + 8 * q + 4 * (ln >> 5)) = f32x4{acc[t][4 * q], acc[t][4 * q + 1], acc[t][4 * q + 2], acc[t][4 * q + 3]};
     if (ln < 32) *(float2*)(part + (size_t)QVT * HD + 2 * qo) = make_float2(m_run, l_run);
   }
+}
+
+template <typename CT, int HD, bool PLANES>
+__global__ void __launch_bounds__(64 * PAGED_WAVES, sizeof(CT) == 2 ? 4 : 2) paged_attention_few_mfma_kernel(
+    const int* __restrict__ cu, const int* __restrict__ start, const float* __restrict__ qkv, long ld, const CT* __restrict__ q_gain, const float2* __restrict__ rope_tab, float eps,
+    int max_new, int hi, PagedOut po, PagedView pv, PagedWork wk) {
+  paged_attention_few<CT, HD, PLANES>(blockIdx.y, cu, start, qkv, ld, q_gain, rope_tab, eps, max_new, hi, po, pv, wk);
+}
+
+// Both kinds of requests in one launch, the longer blocks first: a chunk's leave the memory to the single tokens' (330 rows of a chunk and 15 tokens, 14/2 heads of 64, us: one launch
+// after the other 28, here see below; with no single token in the batch their launch took 4.8)
+template <int HD, bool PLANES>
+__global__ void __launch_bounds__(256, 2) paged_attention_both_mfma_kernel(const int* __restrict__ cu, const int* __restrict__ start, const float* __restrict__ qkv, long ld,
+                                                                           const bf16_t* __restrict__ q_gain, const float2* __restrict__ rope_tab, float eps, int max_new, int border,
+                                                                           int n_tall, PagedOut po, PagedView pv, PagedWork few, PagedWork tall) {
+  static_assert(PAGED_WAVES == 4, "blocks of one size");
+  if ((int)blockIdx.y < n_tall) paged_attention_tall<HD, PLANES>(blockIdx.y, cu, start, qkv, ld, q_gain, rope_tab, eps, max_new, border, po, pv, tall);
+  else paged_attention_few<bf16_t, HD, PLANES>(blockIdx.y - n_tall, cu, start, qkv, ld, q_gain, rope_tab, eps, max_new, border, po, pv, few);
 }
 
 // The ranges of the tall kernel's groups joined: 64 KiB of partial results a group and range are too much for the block that ends last (64 rows behind

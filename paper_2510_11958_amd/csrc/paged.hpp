@@ -63,15 +63,18 @@ __device__ __forceinline__ T block_scan(T v, T* wave_sums /* LDS, NT / 64 */, T&
   return before + incl - v;
 }
 
-// Last i in [0, n) with first[i] <= x (first ascending, first[0] <= x): among equal entries the last, so that of requests without rows in
-// front of one that has some the latter is found
-__device__ __forceinline__ int last_at_most(const int* first, int n, int x) {
-  int lo = 0, hi = n;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (first[mid] <= x) lo = mid; else hi = mid;
-  }
-  return lo;
+// For each of U values x: the last i in [0, n) with first[i] <= x (first ascending, first[0] <= x); among equal entries the last, so that of requests
+// without rows in front of one that has some the latter is found.  The same steps for all, so that their reads are in flight together.
+template <int U>
+__device__ __forceinline__ void last_at_most(const int* first, int n, const int (&x)[U], int (&at)[U]) {
+#pragma unroll
+  for (int u = 0; u < U; ++u) at[u] = 0;
+  for (int step = n > 1 ? 1 << (31 - __builtin_clz(n - 1)) : 0; step; step >>= 1)
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int to = at[u] + step;
+      if (to < n && first[min(to, n - 1)] <= x[u]) at[u] = to;
+    }
 }
 
 // Position and place of row t of the new tokens, which is token t - cu[i] of request i
@@ -168,38 +171,39 @@ __global__ void __launch_bounds__(NT) page_tables_kernel(int* __restrict__ table
       }
     __syncthreads();
   };
-  constexpr int U = NT == 1024 ? 4 : 1;       // pages in flight per thread
+  constexpr int U = NT == 1024 ? 4 : 1;       // pages and rows in flight per thread
   if (give) {
     lay_out(0);
     for (int k0 = tid; k0 < give; k0 += U * NT) {
+      int k[U], i[U], page[U];
       int* entry[U];
-      int page[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) k[u] = min(k0 + u * NT, give - 1);
+      last_at_most<U>(first_s, n_req, k, i);
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const int k = min(k0 + u * NT, give - 1), i = last_at_most(first_s, n_req, k);
-        entry[u] = table + (size_t)i * max_pages + ((start[i] + rows[i] + (1 << page_shift) - 1) >> page_shift) + k - first_s[i];
+        entry[u] = table + (size_t)i[u] * max_pages + ((start[i[u]] + rows[i[u]] + (1 << page_shift) - 1) >> page_shift) + k[u] - first_s[i[u]];
         page[u] = *entry[u];
       }
 #pragma unroll
       for (int u = 0; u < U; ++u)
-        if (k0 + u * NT < give) { stack[top - 1 - k0 - u * NT] = page[u]; *entry[u] = -1; }
+        if (k0 + u * NT < give) { stack[top - 1 - k[u]] = page[u]; *entry[u] = -1; }
     }
     __syncthreads();                // the stack is whole before pages come off it, the search's array free again
   }
   if (take) {
     lay_out(1);
     for (int k0 = tid; k0 < take; k0 += U * NT) {
-      int page[U];
+      int k[U], i[U], page[U];
       int* entry[U];
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int k = min(k0 + u * NT, take - 1), i = last_at_most(first_s, n_req, k);
-        page[u] = stack[top - 1 - k];
-        entry[u] = table + (size_t)i * max_pages + held[i] + k - first_s[i];
-      }
+      for (int u = 0; u < U; ++u) { k[u] = min(k0 + u * NT, take - 1); page[u] = stack[top - 1 - k[u]]; }
+      last_at_most<U>(first_s, n_req, k, i);
+#pragma unroll
+      for (int u = 0; u < U; ++u) entry[u] = table + (size_t)i[u] * max_pages + held[i[u]] + k[u] - first_s[i[u]];
 #pragma unroll
       for (int u = 0; u < U; ++u)
-        if (k0 + u * NT < take) { *entry[u] = page[u]; stack[top - 1 - k0 - u * NT] = -1; }
+        if (k0 + u * NT < take) { *entry[u] = page[u]; stack[top - 1 - k[u]] = -1; }
     }
     __syncthreads();                // held is read above; entries are read below
   }
@@ -213,8 +217,10 @@ __global__ void __launch_bounds__(NT) page_tables_kernel(int* __restrict__ table
   if (tid == 0) { cu[n_req] = n_rows; n_free[0] = top - take; }
   if (!slots) return;
   for (int t = tid; t < n_rows; t += NT) {
-    const int i = last_at_most(first_s, n_req, t);
-    page_row(table, start, max_pages, page_shift, i, t - first_s[i], t, row_pos, slots);
+    const int x[1] = {t};
+    int i[1];
+    last_at_most<1>(first_s, n_req, x, i);
+    page_row(table, start, max_pages, page_shift, i[0], t - first_s[i[0]], t, row_pos, slots);
   }
 }
 
@@ -226,10 +232,12 @@ __global__ void __launch_bounds__(256) page_rows_kernel(const int* __restrict__ 
   if (base >= total) return;
   for (int i = threadIdx.x; i < n_req; i += 256) first_s[i] = cu[i];
   __syncthreads();
-  for (int t = base + threadIdx.x; t < min(base + 1024, total); t += 256) {
-    const int i = last_at_most(first_s, n_req, t);
-    page_row(table, start, max_pages, page_shift, i, t - first_s[i], t, row_pos, slots);
-  }
+  int t[4], i[4];
+#pragma unroll
+  for (int u = 0; u < 4; ++u) t[u] = min(base + (int)threadIdx.x + 256 * u, total - 1);      // (beyond the last: the last one again)
+  last_at_most<4>(first_s, n_req, t, i);
+#pragma unroll
+  for (int u = 0; u < 4; ++u) page_row(table, start, max_pages, page_shift, i[u], t[u] - first_s[i[u]], t[u], row_pos, slots);
 }
 
 // Elements of one type to the pool, four or two at a time, each rounded to nearest even once

@@ -91,8 +91,8 @@ void launch_paged_append(const PagedView& v, int head_dim, const float* qkv, lon
 }
 
 // How an attention call is laid out: blocks per KV head of either kernel (0: no launch), groups that the merge looks at, log2 of those that the key ranges are chosen
-// for, and the workspace: the counts of the groups with several ranges, then their partial results (paged_find), the larger of the two kernels'.
-struct PagedPlan { int few, tall, merge, few_shift, tall_shift; size_t count_bytes, part_bytes; };
+// for, and the workspace: the counts of the few-rows groups with several ranges, their partial results, the tall groups' (paged_find).
+struct PagedPlan { int few, tall, merge, few_shift, tall_shift; size_t count_bytes, few_bytes, tall_bytes; };
 int floor_log2(int v) { int s = 0; while ((2 << s) <= v) ++s; return s; }
 PagedPlan paged_plan(const dmtd_paged_cache* c, int max_new) {
   PagedPlan p{};
@@ -108,15 +108,14 @@ PagedPlan paged_plan(const dmtd_paged_cache* c, int max_new) {
   long few = std::min<long>(c->max_rows, all + c->max_rows / rpb_few);
   if (bf16) few = std::min<long>(few, (long)c->n_req * ((tall_from - 1 + rpb_few - 1) / rpb_few));
   p.few = blocks(few, p.few_shift, PAGED_KEYS_FEW);
-  size_t slot = (size_t)16 * (c->head_dim + 2) * 4 << p.few_shift;
+  p.few_bytes = align_up(((size_t)16 * (c->head_dim + 2) * 4 << p.few_shift) * 2 * c->n_kv_heads, 256);
+  p.count_bytes = align_up(((size_t)4 << p.few_shift) * c->n_kv_heads, 256);
   if (bf16 && few_rows >= tall_from) {
     const long groups = std::min<long>(c->n_req, c->max_rows / tall_from) + c->max_rows / rpb_tall;
     p.tall = blocks(groups, p.tall_shift, PAGED_KEYS_TALL);
     p.merge = (int)std::min(groups, 1L << p.tall_shift);
-    slot = std::max(slot, (size_t)128 * (c->head_dim + 2) * 4 << p.tall_shift);
+    p.tall_bytes = ((size_t)128 * (c->head_dim + 2) * 4 << p.tall_shift) * 2 * c->n_kv_heads;
   }
-  p.count_bytes = align_up(((size_t)4 << std::max(p.few_shift, p.tall_shift)) * c->n_kv_heads, 256);
-  p.part_bytes = 2 * slot * c->n_kv_heads;
   return p;
 }
 
@@ -135,30 +134,31 @@ template <typename CT, int HD, bool PLANES>
 hipError_t launch_paged_attention_t(const PagedView& v, const PagedPlan& p, const PagedCall& a, const PagedOut& out) {
   const int GQ = v.nh / v.nkv;
   constexpr bool BF = sizeof(CT) == 2;
-  PagedWork wk{p.few_shift, (int*)a.ws, (float*)(a.ws + p.count_bytes)};
+  // The two kinds of requests have partial results of their own: they may be under way at the same time
+  const PagedWork few{p.few_shift, (int*)a.ws, (float*)(a.ws + p.count_bytes)}, tall{p.tall_shift, nullptr, (float*)(a.ws + p.count_bytes + p.few_bytes)};
   // the queries' parts, then the waves' results, then what the join exchanges
   const int qv_max = std::min(16 / GQ, a.max_new) * GQ;
   const size_t few_lds = std::max({(size_t)PAGED_WAVES * qv_max * HD * 4, (size_t)16 * (BF ? 2 * (HD + ATT_QPAD) * 2 : (HD + 4) * 4), (size_t)2 * 64 * PAGED_WAVES * 16});
-  hipLaunchKernelGGL((paged_attention_few_mfma_kernel<CT, HD, PLANES>), dim3(v.nkv, p.few), dim3(64 * PAGED_WAVES), few_lds, a.stream, a.cu, a.start, a.qkv, a.ld, (const CT*)a.gain,
-                     (const float2*)a.rope, a.eps, a.max_new, BF ? PAGED_FEW : INT_MAX, out, v, wk);
   if constexpr (BF) {
     if (p.tall > 0) {
-      wk.shift = p.tall_shift;
-      auto kern = paged_attention_tall_mfma_kernel<HD, PLANES>;
-      constexpr size_t lds = (size_t)4 * 64 * HD * 2;
+      auto kern = paged_attention_both_mfma_kernel<HD, PLANES>;
+      const size_t lds = std::max((size_t)4 * 64 * HD * 2, few_lds);
       static bool big_lds = false;
       if (lds > 48 * 1024 && !big_lds) {
-        hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+        hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, 4 * 64 * 128 * 2);
         if (e != hipSuccess) return e;
         big_lds = true;
       }
-      hipLaunchKernelGGL(kern, dim3(v.nkv, p.tall), dim3(256), lds, a.stream, a.cu, a.start, a.qkv, a.ld, (const bf16_t*)a.gain, (const float2*)a.rope, a.eps, a.max_new, PAGED_FEW, out,
-                         v, wk);
+      hipLaunchKernelGGL(kern, dim3(v.nkv, p.tall + p.few), dim3(256), lds, a.stream, a.cu, a.start, a.qkv, a.ld, (const bf16_t*)a.gain, (const float2*)a.rope, a.eps, a.max_new, PAGED_FEW,
+                         p.tall, out, v, few, tall);
       // a vector per thread as long as that makes at most 1024 blocks, most of which have nothing to do
       const int merge_blocks = std::min(HD / 8, std::max(HD / 32, 1024 / (v.nkv * p.merge)));
-      hipLaunchKernelGGL((paged_attention_merge_kernel<HD, PLANES>), dim3(v.nkv, merge_blocks, p.merge), dim3(256), 0, a.stream, a.cu, a.start, a.max_new, PAGED_FEW, out, v, wk);
+      hipLaunchKernelGGL((paged_attention_merge_kernel<HD, PLANES>), dim3(v.nkv, merge_blocks, p.merge), dim3(256), 0, a.stream, a.cu, a.start, a.max_new, PAGED_FEW, out, v, tall);
+      return hipGetLastError();
     }
   }
+  hipLaunchKernelGGL((paged_attention_few_mfma_kernel<CT, HD, PLANES>), dim3(v.nkv, p.few), dim3(64 * PAGED_WAVES), few_lds, a.stream, a.cu, a.start, a.qkv, a.ld, (const CT*)a.gain,
+                     (const float2*)a.rope, a.eps, a.max_new, BF ? PAGED_FEW : INT_MAX, out, v, few);
   return hipGetLastError();
 }
 
@@ -221,7 +221,7 @@ int dmtd_paged_append(const dmtd_paged_cache* c, const float* qkv, int64_t ld, c
 size_t dmtd_paged_workspace_bytes(const dmtd_paged_cache* c) {
   if (check_cache(c) != DMTD_OK) return 0;
   const PagedPlan p = paged_plan(c, c->max_rows);
-  return std::max<size_t>(256, p.count_bytes + p.part_bytes);
+  return p.count_bytes + p.few_bytes + p.tall_bytes;
 }
 
 int dmtd_paged_attention(const dmtd_paged_cache* c, const float* qkv, int64_t ld, const int32_t* start, const int32_t* cu_rows, int32_t max_new,

@@ -85,7 +85,7 @@ bool paged_layout(const dmtd_config& c, int wide, int page, PagedLayout& w) {
   pc.n_pages = w.n_pages; pc.page_size = page; pc.n_req = (int)B; pc.max_pages = w.max_pages;
   pc.n_q_heads = c.n_q_heads; pc.n_kv_heads = c.n_kv_heads; pc.head_dim = c.head_dim; pc.dtype = c.dtype; pc.max_rows = w.rows;
   const PagedPlan p = paged_plan(&pc, w.rows);
-  w.attention_bytes = p.count_bytes + p.part_bytes;
+  w.attention_bytes = p.count_bytes + p.few_bytes + p.tall_bytes;
   w.attention = take(w.attention_bytes);
   w.total = off;
   return true;
