@@ -87,157 +87,205 @@ __device__ __forceinline__ void page_row(const int* table, const int* start, int
 
 // Pages for a step.  Request i holds held[i] pages and needs ceil((start[i] + rows[i]) / page size) of them.  Its surplus goes onto the
 // pool's stack, what it lacks comes off the stack, in the order of the requests and of their pages.  The k-th page given back lies k below
-// the new top, so the next step takes it as its k-th: giving back what a step took restores the stack.
-// One block, whose threads hold up to RPT requests each: three prefix sums, and a search in one of them for each page that moves and for
-// each row.  Everything is checked before anything is written; a step that does not fit has no rows (cu all 0) and changes nothing.
-// Bound by latency: a chain of four round trips to memory (lengths; pages off the stack; their entries read for the rows' places; the last stores) and five
-// barriers.  us in a stream of calls: one request 2.9; 256, of which 19 grow by a page 6.2 with 1024 threads, three sums one after the other and
-// lengths read again, 22 for 200 prompts of 2000 tokens; as it stands see below.
-constexpr int PAGE_RPT = kPagedMaxRequests / 1024;
+// the new top, so the next step takes it as its k-th: giving back what a step took restores the stack.  It also means that the k-th page given back in a step is the
+// k-th taken in it: it goes straight from one table to the other, and every page moves by itself, in any order.
+//
+// page_sums: what the requests give back, take and bring, and where each one's begins among them.  Everything is
+// checked before anything is written; a step that does not fit has no rows (cu all 0) and changes nothing.
+// A small step is one block (page_tables_kernel): sums, pages, rows.  Its chain of four round trips to memory and four barriers is what bounds it.  Where rows may be many,
+// a search per page and row is too much for one CU (200 prompts of 2000 tokens, 18k pages, 280k rows: 20 us), so sums, pages and rows are a launch each: page_sums_kernel,
+// page_moves_kernel, page_rows_kernel.
+struct PageArgs {
+  int *table, *held, *stack, *n_free;
+  const int *start, *rows;
+  int n_req, max_pages, n_pages, page_shift, max_rows;
+  int *cu, *row_pos;
+  long long* slots;
+  int* status;
+  __device__ __forceinline__ int need(int i) const { return (start[i] + rows[i] + (1 << page_shift) - 1) >> page_shift; }
+};
+
+template <int NT> struct PageSums {
+  static constexpr int NWV = NT / 64;
+  int ipt, i0;                 // this thread's requests: i0 .. i0 + ipt - 1
+  int before[3], total[3];     // pages given back, pages taken, rows: in front of its first request, and in all
+  int top0, code, detail;
+  int h0, need0, r0;           // its first request's pages held and needed, and rows: mostly the only one
+  __device__ __forceinline__ int held(const PageArgs& a, int i) const { return i == i0 ? h0 : a.held[i]; }
+  __device__ __forceinline__ int need(const PageArgs& a, int i) const { return i == i0 ? need0 : a.need(i); }
+  __device__ __forceinline__ int rows(const PageArgs& a, int i) const { return i == i0 ? r0 : a.rows[i]; }
+};
+
 template <int NT>
-__global__ void __launch_bounds__(NT) page_tables_kernel(int* __restrict__ table, int* __restrict__ held, int* __restrict__ stack, int* __restrict__ n_free,
-                                                         const int* __restrict__ start, const int* __restrict__ rows, int n_req, int max_pages, int n_pages,
-                                                         int page_shift, int max_rows, int* __restrict__ cu, int* __restrict__ row_pos,
-                                                         long long* __restrict__ slots /* null: page_rows_kernel follows */, int* __restrict__ status) {
-  constexpr int NWV = NT / 64, RPT = NT == 1024 ? PAGE_RPT : 1;
-  __shared__ int first_s[NT * RPT];
+__device__ __forceinline__ PageSums<NT> page_sums(const PageArgs& a) {
+  constexpr int NWV = PageSums<NT>::NWV;
   __shared__ int sums_s[3][NWV];
   __shared__ float sizes_s[3][NWV];
   __shared__ int bad_s;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, ipt = (n_req + NT - 1) / NT, i0 = tid * ipt;
-  const int limit = max_pages << page_shift;             // at most 2^30
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  PageSums<NT> p;
+  p.ipt = (a.n_req + NT - 1) / NT;
+  p.i0 = tid * p.ipt;
+  const int limit = a.max_pages << a.page_shift;             // at most 2^30
   if (tid == 0) bad_s = INT_MAX;
-  const int top0 = n_free[0];
-  int s[RPT], r[RPT], h[RPT], need[RPT];
+  p.top0 = a.n_free[0];
+  p.h0 = p.need0 = p.r0 = 0;
+  // as integers, and as floats, which tell whether the integers have run over
+  int sum[3] = {0, 0, 0}, bad = INT_MAX;
+  float size[3] = {0.f, 0.f, 0.f};
+  for (int i = p.i0; i < min(p.i0 + p.ipt, a.n_req); ++i) {
+    const int s = a.start[i], r = a.rows[i], h = a.held[i];
+    if (s < 0 || r < 0 || h < 0 || h > a.max_pages || s > limit || r > limit - s) { bad = min(bad, i); continue; }
+    const int need = (s + r + (1 << a.page_shift) - 1) >> a.page_shift;
+    if (i == p.i0) { p.h0 = h; p.need0 = need; p.r0 = r; }
+    const int v[3] = {max(h - need, 0), max(need - h, 0), r};
 #pragma unroll
-  for (int j = 0; j < RPT; ++j) {
-    const bool on = j < ipt && i0 + j < n_req;
-    s[j] = on ? start[i0 + j] : 0;
-    r[j] = on ? rows[i0 + j] : 0;
-    h[j] = on ? held[i0 + j] : 0;
+    for (int k = 0; k < 3; ++k) { sum[k] += v[k]; size[k] += (float)v[k]; }
   }
   __syncthreads();
-  // pages given back, pages taken, rows: as integers, and as floats, which tell whether the integers have run over
-  int sum[3] = {0, 0, 0};
-  float size[3] = {0.f, 0.f, 0.f};
-#pragma unroll
-  for (int j = 0; j < RPT; ++j) {
-    const bool fits = s[j] >= 0 && r[j] >= 0 && h[j] >= 0 && h[j] <= max_pages && s[j] <= limit && r[j] <= limit - s[j];
-    if (!fits) atomicMin(&bad_s, i0 + j);
-    need[j] = fits ? (s[j] + r[j] + (1 << page_shift) - 1) >> page_shift : 0;
-    const int v[3] = {max(h[j] - need[j], 0), max(need[j] - h[j], 0), r[j]};
-#pragma unroll
-    for (int k = 0; k < 3; ++k) { sum[k] += fits ? v[k] : 0; size[k] += fits ? (float)v[k] : 0.f; }
-  }
-  int before[3], total[3] = {0, 0, 0};
-  float all[3] = {0.f, 0.f, 0.f};
+  if (bad != INT_MAX) atomicMin(&bad_s, bad);
 #pragma unroll
   for (int k = 0; k < 3; ++k) {
     const int incl = wave_scan(sum[k]);
-    before[k] = incl - sum[k];
+    p.before[k] = incl - sum[k];
     size[k] = wave_sum(size[k]);
     if (lane == 63) { sums_s[k][wave] = incl; sizes_s[k][wave] = size[k]; }
   }
   __syncthreads();
+  float all[3];
 #pragma unroll
-  for (int k = 0; k < 3; ++k)
-#pragma unroll
-    for (int w = 0; w < NWV; ++w) {
-      const int u = sums_s[k][w];
-      if (w < wave) before[k] += u;
-      total[k] += u;
-      all[k] += sizes_s[k][w];
-    }
+  for (int k = 0; k < 3; ++k) {
+    const int incl = wave_scan(lane < NWV ? sums_s[k][lane < NWV ? lane : 0] : 0);
+    p.total[k] = __builtin_amdgcn_readlane(incl, 63);
+    if (wave > 0) p.before[k] += __builtin_amdgcn_readlane(incl, wave - 1);
+    all[k] = wave_sum(lane < NWV ? sizes_s[k][lane < NWV ? lane : 0] : 0.f);
+  }
   const bool over[3] = {all[0] >= 1.1e9f, all[1] >= 1.1e9f, all[2] >= 1.1e9f};      // 2^30 and more
-  int code = 0, detail = 0;
-  if (top0 < 0 || top0 > n_pages) { code = -1; detail = -1; }
-  else if (bad_s != INT_MAX) { code = -1; detail = bad_s; }
-  else if (over[2] || total[2] > max_rows || over[0] || total[0] > n_pages - top0) { code = -1; detail = -1; }
-  else if (over[1] || total[1] > top0 + total[0]) { code = -3; detail = over[1] ? INT_MAX : total[1] - total[0] - top0; }
-  if (tid == 0) { status[0] = code; status[1] = detail; }
-  if (code) {
-    for (int i = tid; i <= n_req; i += NT) cu[i] = 0;
-    return;
+  p.code = p.detail = 0;
+  if (p.top0 < 0 || p.top0 > a.n_pages) { p.code = -1; p.detail = -1; }
+  else if (bad_s != INT_MAX) { p.code = -1; p.detail = bad_s; }
+  else if (over[2] || p.total[2] > a.max_rows || over[0] || p.total[0] > a.n_pages - p.top0) { p.code = -1; p.detail = -1; }
+  else if (over[1] || p.total[1] > p.top0 + p.total[0]) { p.code = -3; p.detail = over[1] ? INT_MAX : p.total[1] - p.total[0] - p.top0; }
+  return p;
+}
+
+// The pages that move, `step` threads side by side from number k0 on.  dyn: LDS, 4 n_req ints: the prefix sums of the pages given back and taken, and what leads from a
+// number in either to a column of its request's table.
+template <int NT, int U>
+__device__ __forceinline__ void page_moves(const PageArgs& a, const PageSums<NT>& p, int* dyn, int k0, int step) {
+  const int n = a.n_req, give = p.total[0], take = p.total[1], most = max(give, take), top = p.top0 + give;
+  if (most == 0) return;
+  int *give_s = dyn, *give_from = dyn + n, *take_s = dyn + 2 * n, *take_from = dyn + 3 * n;
+  int g = p.before[0], t = p.before[1];
+  for (int i = p.i0; i < min(p.i0 + p.ipt, n); ++i) {
+    const int h = p.held(a, i), need = p.need(a, i);
+    give_s[i] = g; give_from[i] = need - g;
+    take_s[i] = t; take_from[i] = h - t;
+    g += max(h - need, 0);
+    t += max(need - h, 0);
   }
-  const int give = total[0], take = total[1], n_rows = total[2], top = top0 + give;
-  // a prefix sum into LDS, for searches in it
-  auto lay_out = [&](int k) {
-    int at = before[k];
+  __syncthreads();
+  for (; k0 < most; k0 += U * step) {
+    int k[U], i[U], page[U];
 #pragma unroll
-    for (int j = 0; j < RPT; ++j)
-      if (j < ipt && i0 + j < n_req) {
-        first_s[i0 + j] = at;
-        at += k == 0 ? max(h[j] - need[j], 0) : k == 1 ? max(need[j] - h[j], 0) : r[j];
-      }
-    __syncthreads();
-  };
-  constexpr int U = NT == 1024 ? 4 : 1;       // pages and rows in flight per thread
-  if (give) {
-    lay_out(0);
-    for (int k0 = tid; k0 < give; k0 += U * NT) {
-      int k[U], i[U], page[U];
-      int* entry[U];
+    for (int u = 0; u < U; ++u) k[u] = min(k0 + u * step, most - 1);
+    // where it is: in the table of who gives it back, or on the stack
+    if (give) {
+      int kg[U];
 #pragma unroll
-      for (int u = 0; u < U; ++u) k[u] = min(k0 + u * NT, give - 1);
-      last_at_most<U>(first_s, n_req, k, i);
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        entry[u] = table + (size_t)i[u] * max_pages + ((start[i[u]] + rows[i[u]] + (1 << page_shift) - 1) >> page_shift) + k[u] - first_s[i[u]];
-        page[u] = *entry[u];
-      }
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (k0 + u * NT < give) { stack[top - 1 - k[u]] = page[u]; *entry[u] = -1; }
+      for (int u = 0; u < U; ++u) kg[u] = min(k[u], give - 1);
+      last_at_most<U>(give_s, n, kg, i);
     }
-    __syncthreads();                // the stack is whole before pages come off it, the search's array free again
-  }
-  if (take) {
-    lay_out(1);
-    for (int k0 = tid; k0 < take; k0 += U * NT) {
-      int k[U], i[U], page[U];
-      int* entry[U];
 #pragma unroll
-      for (int u = 0; u < U; ++u) { k[u] = min(k0 + u * NT, take - 1); page[u] = stack[top - 1 - k[u]]; }
-      last_at_most<U>(first_s, n_req, k, i);
-#pragma unroll
-      for (int u = 0; u < U; ++u) entry[u] = table + (size_t)i[u] * max_pages + held[i[u]] + k[u] - first_s[i[u]];
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (k0 + u * NT < take) { *entry[u] = page[u]; stack[top - 1 - k[u]] = -1; }
+    for (int u = 0; u < U; ++u) {
+      const bool back = k[u] < give;
+      int* from = back ? a.table + (size_t)i[u] * a.max_pages + give_from[i[u]] + k[u] : a.stack + top - 1 - k[u];
+      page[u] = *from;
     }
-    __syncthreads();                // held is read above; entries are read below
-  }
-  lay_out(2);
 #pragma unroll
-  for (int j = 0; j < RPT; ++j)
-    if (j < ipt && i0 + j < n_req) {
-      cu[i0 + j] = first_s[i0 + j];
-      if (need[j] != h[j]) held[i0 + j] = need[j];
+    for (int u = 0; u < U; ++u)
+      if (k0 + u * step < most) *(k[u] < give ? a.table + (size_t)i[u] * a.max_pages + give_from[i[u]] + k[u] : a.stack + top - 1 - k[u]) = -1;
+    // where it goes
+    if (take) {
+      int kt[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) kt[u] = min(k[u], take - 1);
+      last_at_most<U>(take_s, n, kt, i);
     }
-  if (tid == 0) { cu[n_req] = n_rows; n_free[0] = top - take; }
-  if (!slots) return;
-  for (int t = tid; t < n_rows; t += NT) {
-    const int x[1] = {t};
-    int i[1];
-    last_at_most<1>(first_s, n_req, x, i);
-    page_row(table, start, max_pages, page_shift, i[0], t - first_s[i[0]], t, row_pos, slots);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (k0 + u * step < most) *(k[u] < take ? a.table + (size_t)i[u] * a.max_pages + take_from[i[u]] + k[u] : a.stack + top - 1 - k[u]) = page[u];
   }
 }
 
-// Positions and places of the rows where they are many: a block per 1024 rows, the requests' first rows in LDS
-__global__ void __launch_bounds__(256) page_rows_kernel(const int* __restrict__ table, const int* __restrict__ start, int n_req, int max_pages, int page_shift,
-                                                        const int* __restrict__ cu, int* __restrict__ row_pos, long long* __restrict__ slots) {
-  __shared__ int first_s[kPagedMaxRequests];
-  const int total = cu[n_req], base = blockIdx.x * 1024;
+template <int NT>
+__global__ void __launch_bounds__(NT) page_tables_kernel(PageArgs a) {
+  extern __shared__ int page_dyn_smem[];
+  const PageSums<NT> p = page_sums<NT>(a);
+  const int tid = threadIdx.x, n = a.n_req;
+  if (tid == 0) { a.status[0] = p.code; a.status[1] = p.detail; }
+  if (p.code) {
+    for (int i = tid; i <= n; i += NT) a.cu[i] = 0;
+    return;
+  }
+  page_moves<NT, 1>(a, p, page_dyn_smem, tid, NT);
+  __syncthreads();                // the search's arrays are free, and entries written
+  int at = p.before[2];
+  for (int i = p.i0; i < min(p.i0 + p.ipt, n); ++i) {
+    page_dyn_smem[i] = at;
+    a.cu[i] = at;
+    at += p.rows(a, i);
+    if (p.need(a, i) != p.held(a, i)) a.held[i] = p.need(a, i);
+  }
+  if (tid == 0) { a.cu[n] = p.total[2]; a.n_free[0] = p.top0 + p.total[0] - p.total[1]; }
+  __syncthreads();
+  for (int t = tid; t < p.total[2]; t += NT) {
+    const int x[1] = {t};
+    int i[1];
+    last_at_most<1>(page_dyn_smem, n, x, i);
+    page_row(a.table, a.start, a.max_pages, a.page_shift, i[0], t - page_dyn_smem[i[0]], t, a.row_pos, a.slots);
+  }
+}
+
+__global__ void __launch_bounds__(1024) page_sums_kernel(PageArgs a) {
+  const PageSums<1024> p = page_sums<1024>(a);
+  if (threadIdx.x == 0) { a.status[0] = p.code; a.status[1] = p.detail; }
+  int at = p.before[2];
+  for (int i = p.i0; i < min(p.i0 + p.ipt, a.n_req); ++i) {
+    a.cu[i] = p.code ? 0 : at;
+    at += p.code ? 0 : p.rows(a, i);
+  }
+  if (threadIdx.x == 0) a.cu[a.n_req] = p.code ? 0 : p.total[2];
+}
+
+// (the sums once more in every block: nothing but the caller's arrays passes from launch to launch)
+__global__ void __launch_bounds__(256) page_moves_kernel(PageArgs a) {
+  extern __shared__ int page_dyn_smem[];
+  const PageSums<256> p = page_sums<256>(a);
+  if (p.code) return;
+  page_moves<256, 2>(a, p, page_dyn_smem, blockIdx.x * 256 + threadIdx.x, gridDim.x * 256);
+}
+
+// Positions and places: a block per 1024 rows, the requests' first rows in LDS.  The last block brings the pages held up to date.
+__global__ void __launch_bounds__(256) page_rows_kernel(PageArgs a) {
+  extern __shared__ int page_dyn_smem[];
+  const int total = a.cu[a.n_req], base = blockIdx.x * 1024;
+  if (blockIdx.x == gridDim.x - 1) {
+    const PageSums<256> p = page_sums<256>(a);
+    if (p.code) return;
+    for (int i = p.i0; i < min(p.i0 + p.ipt, a.n_req); ++i) a.held[i] = p.need(a, i);
+    if (threadIdx.x == 0) a.n_free[0] = p.top0 + p.total[0] - p.total[1];
+    return;
+  }
   if (base >= total) return;
-  for (int i = threadIdx.x; i < n_req; i += 256) first_s[i] = cu[i];
+  for (int i = threadIdx.x; i < a.n_req; i += 256) page_dyn_smem[i] = a.cu[i];
   __syncthreads();
   int t[4], i[4];
 #pragma unroll
   for (int u = 0; u < 4; ++u) t[u] = min(base + (int)threadIdx.x + 256 * u, total - 1);      // (beyond the last: the last one again)
-  last_at_most<4>(first_s, n_req, t, i);
+  last_at_most<4>(page_dyn_smem, a.n_req, t, i);
 #pragma unroll
-  for (int u = 0; u < 4; ++u) page_row(table, start, max_pages, page_shift, i[u], t[u] - first_s[i[u]], t[u], row_pos, slots);
+  for (int u = 0; u < 4; ++u) page_row(a.table, a.start, a.max_pages, a.page_shift, i[u], t[u] - page_dyn_smem[i[u]], t[u], a.row_pos, a.slots);
 }
 
 // Elements of one type to the pool, four or two at a time, each rounded to nearest even once

@@ -77,7 +77,7 @@ PagedView paged_view(const dmtd_paged_cache* c, const float* rope, int32_t rope_
   return v;
 }
 
-// Rows that the block of the bookkeeping places by itself; more go through page_rows_kernel's blocks
+// Rows up to which the bookkeeping is one block's
 constexpr int kTableRows = 2048;
 
 template <typename CT>
@@ -188,19 +188,29 @@ int dmtd_page_tables(const dmtd_page_pool* p, const int32_t* start, const int32_
   if (max_rows < 1 || max_rows > (1 << 24)) return paged_fail(DMTD_EINVAL, "max_rows must be in [1, 2^24]");
   const hipStream_t s = (hipStream_t)stream;
   if ((rc = check_stream_device(s)) != DMTD_OK) return rc;
-  const bool many = max_rows > kTableRows;
-  const int shift = log2_of(p->page_size);
-  auto launch = [&](auto nt_c) {
-    constexpr int NT = decltype(nt_c)::value;
-    hipLaunchKernelGGL(page_tables_kernel<NT>, dim3(1), dim3(NT), 0, s, p->block_table, p->held, p->free_pages, p->n_free, start, rows, p->n_req, p->max_pages,
-                       p->n_pages, shift, max_rows, cu_rows, row_pos, many ? (long long*)nullptr : (long long*)slots, status);
+  const PageArgs a{p->block_table, p->held, p->free_pages, p->n_free, start, rows, p->n_req, p->max_pages, p->n_pages, log2_of(p->page_size), max_rows, cu_rows, row_pos,
+                   (long long*)slots, status};
+  const size_t lds = (size_t)16 * p->n_req;          // of a block that moves pages
+  auto room = [&](auto kern, bool& done) {
+    if (lds <= 48 * 1024 || done) return hipSuccess;
+    done = true;
+    return hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, 16 * kPagedMaxRequests);
   };
-  if (p->n_req <= 64 && max_rows <= 256) launch(std::integral_constant<int, 64>());
-  else if (p->n_req <= 256 && max_rows <= 1024) launch(std::integral_constant<int, 256>());
-  else launch(std::integral_constant<int, 1024>());
-  if (many)
-    hipLaunchKernelGGL(page_rows_kernel, dim3((max_rows + 1023) / 1024), dim3(256), 0, s, (const int*)p->block_table, start, p->n_req, p->max_pages, shift,
-                       (const int*)cu_rows, row_pos, (long long*)slots);
+  static bool big_tables = false, big_moves = false;
+  hipError_t e = hipSuccess;
+  if (max_rows > kTableRows) {
+    if ((e = room(page_moves_kernel, big_moves)) != hipSuccess) return paged_fail(DMTD_EHIP, hipGetErrorString(e));
+    hipLaunchKernelGGL(page_sums_kernel, dim3(1), dim3(1024), 0, s, a);
+    hipLaunchKernelGGL(page_moves_kernel, dim3(64), dim3(256), lds, s, a);
+    hipLaunchKernelGGL(page_rows_kernel, dim3((max_rows + 1023) / 1024 + 1), dim3(256), (size_t)4 * p->n_req, s, a);
+  } else if (p->n_req <= 64 && max_rows <= 256) {
+    hipLaunchKernelGGL(page_tables_kernel<64>, dim3(1), dim3(64), lds, s, a);
+  } else if (p->n_req <= 256 && max_rows <= 1024) {
+    hipLaunchKernelGGL(page_tables_kernel<256>, dim3(1), dim3(256), lds, s, a);
+  } else {
+    if ((e = room(page_tables_kernel<1024>, big_tables)) != hipSuccess) return paged_fail(DMTD_EHIP, hipGetErrorString(e));
+    hipLaunchKernelGGL(page_tables_kernel<1024>, dim3(1), dim3(1024), lds, s, a);
+  }
   return paged_done();
 }
 
