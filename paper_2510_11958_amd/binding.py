@@ -408,6 +408,7 @@ class Engine:
         if nbytes == 0 or self.cfg.dry_run:
             self._check(self.lib.dmtd_paged_begin(self._h, page_size, None, 0))
         memory = torch.empty(nbytes, dtype=torch.uint8, device=self._workspace.device)
+        torch.cuda.current_stream(memory.device).synchronize()      # whatever that stream still does with the memory
         self._check(self.lib.dmtd_paged_begin(self._h, page_size, memory.data_ptr(), nbytes))
         self._paged_memory = memory
 

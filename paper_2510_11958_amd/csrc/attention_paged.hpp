@@ -68,7 +68,7 @@ __device__ __forceinline__ bool paged_find(const PagedView& pv, const int* cu, c
                                            int y, PagedItem& it) {
   auto keys_of = [&](unsigned long long total) {
     const unsigned long long per = (total + (1ull << shift) - 1) >> shift;
-    return (int)max((unsigned long long)min_keys, (per + STEP - 1) / STEP * STEP);
+    return (int)min(max((unsigned long long)min_keys, (per + STEP - 1) / STEP * STEP), 1ull << 30);      // no request is longer
   };
   int i, kps, splits, before, slots, multi;
   PagedReq q;
@@ -803,22 +803,26 @@ __device__ __forceinline__ void paged_attention_tall(int y, const int* __restric
   }
 }
 
+// Block of a KV head (x), through the grid's two other dimensions, which end at 65535 each
+__device__ __forceinline__ int paged_block() { return blockIdx.z * gridDim.y + blockIdx.y; }
+
 template <typename CT, int HD, bool PLANES>
 __global__ void __launch_bounds__(64 * PAGED_WAVES, sizeof(CT) == 2 ? 4 : 2) paged_attention_few_mfma_kernel(
     const int* __restrict__ cu, const int* __restrict__ start, const float* __restrict__ qkv, long ld, const CT* __restrict__ q_gain, const float2* __restrict__ rope_tab, float eps,
     int max_new, int hi, PagedOut po, PagedView pv, PagedWork wk) {
-  paged_attention_few<CT, HD, PLANES>(blockIdx.y, cu, start, qkv, ld, q_gain, rope_tab, eps, max_new, hi, po, pv, wk);
+  paged_attention_few<CT, HD, PLANES>(paged_block(), cu, start, qkv, ld, q_gain, rope_tab, eps, max_new, hi, po, pv, wk);
 }
 
 // Both kinds of requests in one launch, the longer blocks first: a chunk's leave the memory to the single tokens' (330 rows of a chunk and 15 tokens, 14/2 heads of 64, us: one launch
-// after the other 28, here see below; with no single token in the batch their launch took 4.8)
+// after the other 28, together 17; with no single token in the batch their launch took 4.8)
 template <int HD, bool PLANES>
 __global__ void __launch_bounds__(256, 2) paged_attention_both_mfma_kernel(const int* __restrict__ cu, const int* __restrict__ start, const float* __restrict__ qkv, long ld,
                                                                            const bf16_t* __restrict__ q_gain, const float2* __restrict__ rope_tab, float eps, int max_new, int border,
                                                                            int n_tall, PagedOut po, PagedView pv, PagedWork few, PagedWork tall) {
   static_assert(PAGED_WAVES == 4, "blocks of one size");
-  if ((int)blockIdx.y < n_tall) paged_attention_tall<HD, PLANES>(blockIdx.y, cu, start, qkv, ld, q_gain, rope_tab, eps, max_new, border, po, pv, tall);
-  else paged_attention_few<bf16_t, HD, PLANES>(blockIdx.y - n_tall, cu, start, qkv, ld, q_gain, rope_tab, eps, max_new, border, po, pv, few);
+  const int y = paged_block();
+  if (y < n_tall) paged_attention_tall<HD, PLANES>(y, cu, start, qkv, ld, q_gain, rope_tab, eps, max_new, border, po, pv, tall);
+  else paged_attention_few<bf16_t, HD, PLANES>(y - n_tall, cu, start, qkv, ld, q_gain, rope_tab, eps, max_new, border, po, pv, few);
 }
 
 // The ranges of the tall kernel's groups joined: 64 KiB of partial results a group and range are too much for the block that ends last (64 rows behind

@@ -15,6 +15,23 @@ bool aligned(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
 bool page_size_ok(int p) { return p == 16 || p == 32 || p == 64 || p == 128 || p == 256; }
 int log2_of(int p) { int s = 0; while ((1 << s) < p) ++s; return s; }
 
+// Lets the blocks of a kernel have up to `most` bytes of dynamic LDS on the current device, once for each device (done: the kernel's own)
+template <typename K>
+hipError_t lds_room(K kern, size_t bytes, size_t most, bool (&done)[kMaxDevices]) {
+  if (bytes <= 48 * 1024) return hipSuccess;
+  int dev = 0;
+  hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess || dev < 0 || dev >= kMaxDevices || done[dev]) return e;
+  e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)most);
+  done[dev] = e == hipSuccess;
+  return e;
+}
+// A grid of `blocks` blocks for each of nkv KV heads (paged_block)
+dim3 paged_grid(int nkv, int blocks) {
+  const int z = (blocks + 65534) / 65535;
+  return dim3(nkv, (blocks + z - 1) / z, z);
+}
+
 // A launch goes to the device that is current; on a stream of another one it would fail or, worse, read that one's addresses here
 int check_stream_device(hipStream_t s) {
   if (!s) return DMTD_OK;
@@ -48,7 +65,8 @@ int check_cache(const dmtd_paged_cache* c) {
   if (c->head_dim != 64 && c->head_dim != 128) return paged_fail(DMTD_EINVAL, "head_dim must be 64 or 128");
   if (c->n_kv_heads < 1 || c->n_kv_heads > 1024 || c->n_q_heads < 1 || c->n_q_heads % c->n_kv_heads || c->n_q_heads / c->n_kv_heads > QV_MAX)
     return paged_fail(DMTD_EINVAL, "n_q_heads must be a multiple of n_kv_heads (at most 1024), at most 16 times as many");
-  if (c->max_rows < 1 || c->max_rows > (1 << 24)) return paged_fail(DMTD_EINVAL, "max_rows must be in [1, 2^24]");
+  if (c->max_rows < 1 || c->max_rows > (1 << 24) || (long)c->max_rows * c->n_kv_heads > (1L << 27))
+    return paged_fail(DMTD_EINVAL, "max_rows must be in [1, 2^24], and at most 2^27 with the KV heads");
   if (!c->k || !c->v || !c->block_table) return paged_fail(DMTD_EINVAL, "null cache pointer");
   if (!aligned(c->k, 16) || !aligned(c->v, 16) || !aligned(c->block_table, 4)) return paged_fail(DMTD_EINVAL, "k and v must be 16-byte aligned");
   const long one = (long)c->n_kv_heads * c->page_size * c->head_dim;
@@ -143,13 +161,10 @@ hipError_t launch_paged_attention_t(const PagedView& v, const PagedPlan& p, cons
     if (p.tall > 0) {
       auto kern = paged_attention_both_mfma_kernel<HD, PLANES>;
       const size_t lds = std::max((size_t)4 * 64 * HD * 2, few_lds);
-      static bool big_lds = false;
-      if (lds > 48 * 1024 && !big_lds) {
-        hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, 4 * 64 * 128 * 2);
-        if (e != hipSuccess) return e;
-        big_lds = true;
-      }
-      hipLaunchKernelGGL(kern, dim3(v.nkv, p.tall + p.few), dim3(256), lds, a.stream, a.cu, a.start, a.qkv, a.ld, (const bf16_t*)a.gain, (const float2*)a.rope, a.eps, a.max_new, PAGED_FEW,
+      static bool big_lds[kMaxDevices];
+      const hipError_t e = lds_room(kern, lds, (size_t)4 * 64 * 128 * 2, big_lds);
+      if (e != hipSuccess) return e;
+      hipLaunchKernelGGL(kern, paged_grid(v.nkv, p.tall + p.few), dim3(256), lds, a.stream, a.cu, a.start, a.qkv, a.ld, (const bf16_t*)a.gain, (const float2*)a.rope, a.eps, a.max_new, PAGED_FEW,
                          p.tall, out, v, few, tall);
       // a vector per thread as long as that makes at most 1024 blocks, most of which have nothing to do
       const int merge_blocks = std::min(HD / 8, std::max(HD / 32, 1024 / (v.nkv * p.merge)));
@@ -157,7 +172,7 @@ hipError_t launch_paged_attention_t(const PagedView& v, const PagedPlan& p, cons
       return hipGetLastError();
     }
   }
-  hipLaunchKernelGGL((paged_attention_few_mfma_kernel<CT, HD, PLANES>), dim3(v.nkv, p.few), dim3(64 * PAGED_WAVES), few_lds, a.stream, a.cu, a.start, a.qkv, a.ld, (const CT*)a.gain,
+  hipLaunchKernelGGL((paged_attention_few_mfma_kernel<CT, HD, PLANES>), paged_grid(v.nkv, p.few), dim3(64 * PAGED_WAVES), few_lds, a.stream, a.cu, a.start, a.qkv, a.ld, (const CT*)a.gain,
                      (const float2*)a.rope, a.eps, a.max_new, BF ? PAGED_FEW : INT_MAX, out, v, few);
   return hipGetLastError();
 }
@@ -191,15 +206,10 @@ int dmtd_page_tables(const dmtd_page_pool* p, const int32_t* start, const int32_
   const PageArgs a{p->block_table, p->held, p->free_pages, p->n_free, start, rows, p->n_req, p->max_pages, p->n_pages, log2_of(p->page_size), max_rows, cu_rows, row_pos,
                    (long long*)slots, status};
   const size_t lds = (size_t)16 * p->n_req;          // of a block that moves pages
-  auto room = [&](auto kern, bool& done) {
-    if (lds <= 48 * 1024 || done) return hipSuccess;
-    done = true;
-    return hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, 16 * kPagedMaxRequests);
-  };
-  static bool big_tables = false, big_moves = false;
+  static bool big_tables[kMaxDevices], big_moves[kMaxDevices];
   hipError_t e = hipSuccess;
   if (max_rows > kTableRows) {
-    if ((e = room(page_moves_kernel, big_moves)) != hipSuccess) return paged_fail(DMTD_EHIP, hipGetErrorString(e));
+    if ((e = lds_room(page_moves_kernel, lds, 16 * kPagedMaxRequests, big_moves)) != hipSuccess) return paged_fail(DMTD_EHIP, hipGetErrorString(e));
     hipLaunchKernelGGL(page_sums_kernel, dim3(1), dim3(1024), 0, s, a);
     hipLaunchKernelGGL(page_moves_kernel, dim3(64), dim3(256), lds, s, a);
     hipLaunchKernelGGL(page_rows_kernel, dim3((max_rows + 1023) / 1024 + 1), dim3(256), (size_t)4 * p->n_req, s, a);
@@ -208,7 +218,7 @@ int dmtd_page_tables(const dmtd_page_pool* p, const int32_t* start, const int32_
   } else if (p->n_req <= 256 && max_rows <= 1024) {
     hipLaunchKernelGGL(page_tables_kernel<256>, dim3(1), dim3(256), lds, s, a);
   } else {
-    if ((e = room(page_tables_kernel<1024>, big_tables)) != hipSuccess) return paged_fail(DMTD_EHIP, hipGetErrorString(e));
+    if ((e = lds_room(page_tables_kernel<1024>, lds, 16 * kPagedMaxRequests, big_tables)) != hipSuccess) return paged_fail(DMTD_EHIP, hipGetErrorString(e));
     hipLaunchKernelGGL(page_tables_kernel<1024>, dim3(1), dim3(1024), lds, s, a);
   }
   return paged_done();

@@ -215,6 +215,10 @@ def test_attention(heads, page, start, rows, dtype):
     Setup(heads, dtype, page, start, rows, seed=len(start) + sum(rows)).check()
 
 
+def test_more_groups_than_a_grid_dimension_holds():
+    Setup((16, 1, 64), F32, 64, [0] * 128, [640] * 127 + [3], seed=22).check()
+
+
 def test_ranges_longer_than_a_wave_keeps_page_numbers_for():
     Setup((128, 128, 64), BF, 16, [8999], [1], seed=21).check()
 
@@ -337,6 +341,17 @@ def test_many_requests(dtype):
     rng = np.random.RandomState(3)
     for n in (65, 300, 1100):
         Setup(H4, dtype, 16, rng.randint(0, 40, n).tolist(), rng.randint(0, 3, n).tolist(), seed=n).check()
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_many_requests_of_all_kinds(dtype):
+    """More than a wave's lanes of them: single tokens, refills and chunks, behind short and long contexts, each over several key ranges."""
+    rng = np.random.RandomState(5)
+    start, rows = rng.randint(0, 700, 90), rng.randint(0, 5, 90)
+    start[[7, 50, 88]], rows[[7, 50, 88]] = [0, 900, 2100], [150, 77, 130]
+    s = Setup(H4, dtype, 32, start.tolist(), rows.tolist(), seed=23)
+    s.check()
+    assert torch.equal(s.attend(max_new=150), s.attend())
 
 
 def test_same_bits_every_time_and_on_every_stream():
