@@ -159,10 +159,14 @@ __device__ __forceinline__ bool paged_find(const PagedView& pv, const int* cu, c
 }
 
 // Partial results pass from block to block, maybe from die to die, whose L2 caches do not see each other's lines.  They are written through
-// those caches, 8 bytes at a time, by relaxed atomics of the device's scope, and only the block that joins them has its die's caches drop what is stale; a
-// fence on the writers' side would write a whole L2 back for each block (31 single tokens behind up to 2111 keys: 204 us with such fences, 26 without).
+// those caches and read past them, 8 bytes at a time, by relaxed atomics of the device's scope; a fence of that scope would write a whole L2 back for each block that
+// writes (31 single tokens behind up to 2111 keys: 204 us with such fences, 26 without) and empty it for each that joins (32 behind 2048, 14/2 heads of 64: 16.7, 13.5).
 __device__ __forceinline__ void put_through(float* p, float a, float b) {
   __hip_atomic_store((unsigned long long*)p, ((unsigned long long)__float_as_uint(b) << 32) | __float_as_uint(a), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float2 get_past(const float* p) {
+  const unsigned long long v = __hip_atomic_load((const unsigned long long*)p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  return make_float2(__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32)));
 }
 __device__ __forceinline__ void put_through4(float* p, const f32x4& v) { put_through(p, v.x, v.y); put_through(p + 2, v.z, v.w); }
 
@@ -176,7 +180,8 @@ struct PagedSum {
     o = f * o + f2 * o2;
     m = mn;
   }
-  // ranges s0, s0 + by, ... below n, of partial results `step` floats apart
+  // ranges s0, s0 + by, ... below n, of partial results `step` floats apart (PAST: put through by blocks of the same launch)
+  template <bool PAST>
   __device__ __forceinline__ void add_ranges(const float* ml, const float* po, size_t step, int s0, int n, int by) {
     constexpr int U = 8;                  // of them in flight
     for (; s0 < n; s0 += U * by) {
@@ -185,8 +190,14 @@ struct PagedSum {
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const size_t at = (size_t)min(s0 + u * by, n - 1) * step;
-        w[u] = *(const float2*)(ml + at);
-        x[u] = *(const f32x4*)(po + at);
+        if (PAST) {
+          const float2 a = get_past(po + at), b = get_past(po + at + 2);
+          w[u] = get_past(ml + at);
+          x[u] = f32x4{a.x, a.y, b.x, b.y};
+        } else {
+          w[u] = *(const float2*)(ml + at);
+          x[u] = *(const f32x4*)(po + at);
+        }
       }
 #pragma unroll
       for (int u = 0; u < U; ++u)
@@ -215,7 +226,6 @@ __device__ __forceinline__ void paged_join(const PagedWork& w, const PagedItem& 
   }
   __syncthreads();
   if (!last_s) return;
-  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");      // what this die's caches hold of the others' slots is stale
   constexpr size_t SLOT = (size_t)QVT * (HD + 2);
   const float* part = w.part + ((size_t)it.slot * nkv + g) * SLOT;
   const size_t step = (size_t)nkv * SLOT;
@@ -229,7 +239,7 @@ __device__ __forceinline__ void paged_join(const PagedWork& w, const PagedItem& 
     const bool on = turn < share && cell < cells;
     const int v = on ? cell / T4 : 0, d = on ? (cell % T4) * 4 : 0;
     PagedSum sum;
-    sum.add_ranges(part + (size_t)QVT * HD + 2 * v, part + (size_t)v * HD + d, step, on ? turn : it.n, it.n, share);
+    sum.add_ranges<true>(part + (size_t)QVT * HD + 2 * v, part + (size_t)v * HD + d, step, on ? turn : it.n, it.n, share);
     if (share > 1) {
       sums[tid] = sum.o;
       sums[NT + tid] = f32x4{sum.m, sum.l, 0.f, 0.f};
@@ -279,7 +289,7 @@ __device__ __forceinline__ void paged_attention_few(int y, const int* __restrict
   typedef unsigned int vraw_t __attribute__((ext_vector_type(VW)));
   typedef float fvec_t __attribute__((ext_vector_type(HL)));
   typedef unsigned short hvec_t __attribute__((ext_vector_type(HL)));
-  const int g = blockIdx.x, GQ = pv.nh / pv.nkv, rpb = QVT / GQ;
+  const int g = blockIdx.x, GQ = pv.gq, rpb = pv.rpb_few;
   PagedItem it;
   if (!paged_find<NT, 16 * NW, false>(pv, cu, start, max_new, GQ, 0, hi, rpb, wk.shift, PAGED_KEYS_FEW, y, it)) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), sl = lane & 15, kq = lane >> 4;
@@ -295,11 +305,22 @@ __device__ __forceinline__ void paged_attention_few(int y, const int* __restrict
   const int first = it.kb + 16 * wave;
   int pages = load_pages(first);
   // query vector tid / 16, 2 HL values a lane
+  static_assert(NT == 16 * QVT, "16 lanes to a query vector");
+  const int qv = tid >> 4, l16 = tid & 15, qr = pv.row_of(qv < QV ? qv : 0), qrow = it.row0 + qr, qhead = g * GQ + (qv < QV ? qv - qr * GQ : 0);
   fvec_t xa, xb;
-  const int qv = tid >> 4, l16 = tid & 15, qrow = it.row0 + (qv < QV ? qv / GQ : 0), qhead = g * GQ + (qv < QV ? qv % GQ : 0);
-  if (qv < QVT) {
+  float2 cs[HL];
+  CT g0[HL], g1[HL];
+  {
+    // what it needs is asked for in front of the keys, whose arrival it is made ready beside
     const float* src = qkv + (size_t)(it.first + qrow) * ld + (size_t)qhead * HD + HL * l16;
     xa = *(const fvec_t*)src; xb = *(const fvec_t*)(src + half);
+    const float2* rp = rope_tab + (size_t)(it.pos0 + qr) * half + HL * l16;
+#pragma unroll
+    for (int e = 0; e < HL; ++e) {
+      cs[e] = rope_tab ? rp[e] : make_float2(1.f, 0.f);
+      g0[e] = q_gain ? q_gain[HL * l16 + e] : CT(0);
+      g1[e] = q_gain ? q_gain[half + HL * l16 + e] : CT(0);
+    }
   }
   if (tid == 0) poison_s = INT_MAX;
   u32x4 kr[KS];
@@ -316,24 +337,21 @@ __device__ __forceinline__ void paged_attention_few(int y, const int* __restrict
     for (int m = 0; m < 4; ++m) vr[m] = __builtin_nontemporal_load((const vraw_t*)(vp + (4 * kq + m) * HD + DPL * sl));
   };
   if (first < ke) load_kv(first, __builtin_amdgcn_readlane(pages, 0));
-  if (qv < QVT) {
-    const int pos = it.pos0 + (qrow - it.row0);
+  {
     float x0[HL], x1[HL], ss = 0.f;
 #pragma unroll
     for (int e = 0; e < HL; ++e) { x0[e] = xa[e]; x1[e] = xb[e]; ss += x0[e] * x0[e] + x1[e] * x1[e]; }
     if (q_gain) {
       const float rs = rsqrtf(row16_sum(ss) / (float)HD + eps);
 #pragma unroll
-      for (int e = 0; e < HL; ++e) { x0[e] *= rs * Elem<CT>::to_f32(q_gain[HL * l16 + e]); x1[e] *= rs * Elem<CT>::to_f32(q_gain[half + HL * l16 + e]); }
+      for (int e = 0; e < HL; ++e) { x0[e] *= rs * Elem<CT>::to_f32(g0[e]); x1[e] *= rs * Elem<CT>::to_f32(g1[e]); }
     }
     if (rope_tab) {
-      const float2* rp = rope_tab + (size_t)pos * half + HL * l16;
 #pragma unroll
       for (int e = 0; e < HL; ++e) {
-        const float2 cs = rp[e];
         const float a = x0[e], b = x1[e];
-        x0[e] = a * cs.x - b * cs.y;
-        x1[e] = b * cs.x + a * cs.y;
+        x0[e] = a * cs[e].x - b * cs[e].y;
+        x1[e] = b * cs[e].x + a * cs[e].y;
       }
     }
     const float scale = rsqrtf((float)HD) * 1.4426950408889634f;
@@ -353,7 +371,7 @@ __device__ __forceinline__ void paged_attention_few(int y, const int* __restrict
     }
   }
   __syncthreads();
-  const int my_pos = it.pos0 + sl / GQ;
+  const int my_pos = it.pos0 + pv.row_of(sl);
   float m_run = -INFINITY, l_run = 0.f;
   f32x4 acc[DPL];
 #pragma unroll
@@ -459,7 +477,10 @@ __device__ __forceinline__ void paged_attention_few(int y, const int* __restrict
   __syncthreads();
   constexpr size_t SLOT = (size_t)QVT * (HD + 2);
   float* part = wk.part + ((size_t)(it.slot + it.split) * pv.nkv + g) * SLOT;
-  auto store = [&](int v, int d, const f32x4& x) { paged_store4<CT, PLANES>(po, it.first + it.row0 + v / GQ, (g * GQ + v % GQ) * HD + d, x); };
+  auto store = [&](int v, int d, const f32x4& x) {
+    const int r = pv.row_of(v);
+    paged_store4<CT, PLANES>(po, it.first + it.row0 + r, (g * GQ + v - r * GQ) * HD + d, x);
+  };
   for (int e = tid; e < QV * (HD / 4); e += NT) {
     const int v = e / (HD / 4), d = (e % (HD / 4)) * 4;
     float mm = wm[0][v];
@@ -474,7 +495,7 @@ __device__ __forceinline__ void paged_attention_few(int y, const int* __restrict
       o += fw * *(const f32x4*)(wacc + ((size_t)w * QV + v) * HD + d);
       l += fw * wl[w][v];
     }
-    if (it.pos0 + v / GQ >= poison_s) l = __uint_as_float(0x7FC00000u);
+    if (it.pos0 + pv.row_of(v) >= poison_s) l = __uint_as_float(0x7FC00000u);
     if (it.n == 1) {
       const float inv = l == 0.f ? 0.f : 1.0f / l;
       store(v, d, f32x4{o.x * inv, o.y * inv, o.z * inv, o.w * inv});
@@ -511,14 +532,14 @@ __device__ __forceinline__ void paged_attention_tall(int y, const int* __restric
   typedef unsigned int vraw_t __attribute__((ext_vector_type(DV / 2)));
   extern __shared__ float4 paged_dyn_smem[];
   __shared__ int poison_s;
-  const int g = blockIdx.x, GQ = pv.nh / pv.nkv, rpb = QVT / GQ;
+  const int g = blockIdx.x, GQ = pv.gq, rpb = pv.rpb_tall;
   PagedItem it;
   if (!paged_find<NT, KT, false, true>(pv, cu, start, max_new, GQ, lo, INT_MAX, rpb, wk.shift, PAGED_KEYS_TALL, y, it)) return;
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), hi = lane >> 5;
   bf16_t* ring = (bf16_t*)paged_dyn_smem;                      // K, K, V^T, V^T
   const int QV = it.r * GQ, qv = 32 * w + (lane & 31), kb = it.kb, ke = it.ke;
   const bool valid = qv < QV;
-  const int row = it.row0 + (valid ? qv / GQ : 0), head = g * GQ + (valid ? qv % GQ : 0), my_pos = it.pos0 + (row - it.row0);
+  const int qr = pv.row_of(valid ? qv : 0), row = it.row0 + qr, head = g * GQ + (valid ? qv - qr * GQ : 0), my_pos = it.pos0 + (row - it.row0);
   const int* trow = pv.table + (size_t)it.req * pv.max_pages;
   const int in_page = (1 << pv.page_shift) - 1;
 
@@ -779,8 +800,8 @@ __device__ __forceinline__ void paged_attention_tall(int y, const int* __restric
   // where the vector goes, worked out anew: kept through the loop it would be spilled
   int ln = lane;
   asm volatile("" : "+v"(ln));
-  const int qo = 32 * w + (ln & 31), ro = it.row0 + qo / GQ, co = (g * GQ + qo % GQ) * HD + 4 * (ln >> 5);
-  if (it.pos0 + qo / GQ >= poison) l_run = __uint_as_float(0x7FC00000u);
+  const int qo = 32 * w + (ln & 31), qor = pv.row_of(qo), ro = it.row0 + qor, co = (g * GQ + qo - qor * GQ) * HD + 4 * (ln >> 5);
+  if (it.pos0 + qor >= poison) l_run = __uint_as_float(0x7FC00000u);
   constexpr size_t SLOT = (size_t)QVT * (HD + 2);
   if (it.n == 1) {
     if (qo < QV) {
@@ -832,16 +853,17 @@ __global__ void __launch_bounds__(256) paged_attention_merge_kernel(const int* _
                                                                     PagedWork wk) {
   constexpr int QVT = 128, NT = 256, T4 = HD / 4;
   constexpr size_t SLOT = (size_t)QVT * (HD + 2);
-  const int g = blockIdx.x, GQ = pv.nh / pv.nkv;
+  const int g = blockIdx.x, GQ = pv.gq;
   PagedItem it;
-  if (!paged_find<NT, 64, true>(pv, cu, start, max_new, GQ, lo, INT_MAX, QVT / GQ, wk.shift, PAGED_KEYS_TALL, blockIdx.z, it)) return;
+  if (!paged_find<NT, 64, true>(pv, cu, start, max_new, GQ, lo, INT_MAX, pv.rpb_tall, wk.shift, PAGED_KEYS_TALL, blockIdx.z, it)) return;
   if (it.n < 2) return;      // the request's first range is all that the group sees: written
   const float* part = wk.part + ((size_t)it.slot * pv.nkv + g) * SLOT;
   const int d = (threadIdx.x % T4) * 4;
   for (int v = blockIdx.y * (NT / T4) + threadIdx.x / T4; v < it.r * GQ; v += gridDim.y * (NT / T4)) {      // one each, unless the groups are many
     PagedSum sum;
-    sum.add_ranges(part + (size_t)QVT * HD + 2 * v, part + (size_t)v * HD + d, (size_t)pv.nkv * SLOT, 0, it.n, 1);
-    paged_store4<bf16_t, PLANES>(po, it.first + it.row0 + v / GQ, (g * GQ + v % GQ) * HD + d, sum.result());
+    sum.add_ranges<false>(part + (size_t)QVT * HD + 2 * v, part + (size_t)v * HD + d, (size_t)pv.nkv * SLOT, 0, it.n, 1);
+    const int r = pv.row_of(v);
+    paged_store4<bf16_t, PLANES>(po, it.first + it.row0 + r, (g * GQ + v - r * GQ) * HD + d, sum.result());
   }
 }
 

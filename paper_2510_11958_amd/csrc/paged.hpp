@@ -22,6 +22,8 @@ struct PagedView {
   const int* table;                 // [n_req][max_pages]
   int n_pages, page_shift, n_req, max_pages, nh, nkv, max_rows;
   int limit;                        // positions a request may have: the block table's, or the rotary table's where that is shorter
+  int gq, gq_mul, rpb_few, rpb_tall;      // query heads per KV head, what a division by them is replaced by, rows of 16 and of 128 query vectors
+  __device__ __forceinline__ int row_of(int v) const { return (v * gq_mul) >> 16; }      // v / gq for v < 128: gq_mul = 2^16 / gq + 1 is off by less than 1 / gq for those
 };
 
 // Sums over the lanes up to and with this one, without LDS: within rows of 16, then the rows' last values onto the rows behind them

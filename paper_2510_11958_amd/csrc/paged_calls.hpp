@@ -91,6 +91,7 @@ PagedView paged_view(const dmtd_paged_cache* c, const float* rope, int32_t rope_
   v.n_pages = c->n_pages; v.page_shift = log2_of(c->page_size); v.n_req = c->n_req; v.max_pages = c->max_pages;
   v.nh = c->n_q_heads; v.nkv = c->n_kv_heads; v.max_rows = c->max_rows;
   v.limit = c->max_pages * c->page_size;
+  v.gq = v.nh / v.nkv; v.gq_mul = (1 << 16) / v.gq + 1; v.rpb_few = 16 / v.gq; v.rpb_tall = 128 / v.gq;
   if (rope && rope_len < v.limit) v.limit = rope_len;
   return v;
 }
