@@ -515,8 +515,8 @@ __device__ __forceinline__ void paged_attention_few(int y, const int* __restrict
 // K goes from the pages straight into LDS, a wave 16 keys of a tile (one page), rows' 16-byte chunks permuted by the key number; V through registers, transposed
 // on the way (4 keys x HD / 16 dims per thread; 8-byte pieces permuted by the dim).  Two buffers of each: the next tile's loads fly during
 // a tile, and a tile's page numbers are fetched a tile earlier still, one per 4 keys and lane.
-// The products run over whole tiles: keys behind the block's last row are that row's key again (its value is finite or poisoned), with probability 0.  Values of the
-// block's own positions may be infinite or NaN, which 0 does not silence: the block looks at them first; if one is not finite, it and its like behind
+// The products run over whole tiles, with probability 0 for keys that a row does not see.  Values behind the block's last key go into LDS as 0.  Values of its
+// own positions may be infinite or NaN, which 0 does not silence: the block looks at them first; if one is not finite, it and its like behind
 // it go into LDS as 0 and the rows that see it become NaN.
 template <int HD, bool PLANES>
 __device__ __forceinline__ void paged_attention_tall(int y, const int* __restrict__ cu, const int* __restrict__ start, const float* __restrict__ qkv, long ld,
@@ -536,7 +536,12 @@ __device__ __forceinline__ void paged_attention_tall(int y, const int* __restric
   PagedItem it;
   if (!paged_find<NT, KT, false, true>(pv, cu, start, max_new, GQ, lo, INT_MAX, rpb, wk.shift, PAGED_KEYS_TALL, y, it)) return;
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), hi = lane >> 5;
-  bf16_t* ring = (bf16_t*)paged_dyn_smem;                      // K, K, V^T, V^T
+  // LDS by byte address: K, K, V^T, V^T from a multiple of 1 KiB on, so that a permuted piece's address is the row's with bits exclusive-or'ed in
+  typedef __attribute__((address_space(3))) char lds_char;
+  typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
+  typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+  typedef __attribute__((address_space(3))) u32x2 lds_u32x2;
+  const uint32_t ring = ((uint32_t)(uintptr_t)(lds_char*)(char*)paged_dyn_smem + 1023u) & ~1023u;
   const int QV = it.r * GQ, qv = 32 * w + (lane & 31), kb = it.kb, ke = it.ke;
   const bool valid = qv < QV;
   const int qr = pv.row_of(valid ? qv : 0), row = it.row0 + qr, head = g * GQ + (valid ? qv - qr * GQ : 0), my_pos = it.pos0 + (row - it.row0);
@@ -552,38 +557,44 @@ __device__ __forceinline__ void paged_attention_tall(int y, const int* __restric
     const int pg = __builtin_amdgcn_readlane(page, 4 * w), k0 = ln / CH, c0 = (ln % CH) ^ k0, ki = (w * KI + i) * (64 / CH);
     const bf16_t* src = (const bf16_t*)pv.k + (size_t)(outside(pg) ? 0 : pg) * pv.page_stride + (((size_t)g << pv.page_shift) + ((base + 16 * w) & in_page)) * HD;
     __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(src + (uint32_t)((i * (64 / CH) + k0) * HD + (c0 ^ (ki & (CH - 1))) * 8)),
-                                     (__attribute__((address_space(3))) void*)(ring + buf * TILE + (w * KI + i) * 512), 16, 0, 0);
+                                     (__attribute__((address_space(3))) void*)(uintptr_t)(ring + (uint32_t)(buf * TILE + (w * KI + i) * 512) * 2), 16, 0, 0);
   };
-  const int kgp = lane & 15, dg = w * 4 + (lane >> 4), vslot = 2 * (kgp >> 2) + (kgp & 1), vhalf = ((kgp >> 1) & 1) * 4;
+  // V: 4 keys of a page, DV dims a thread; keys behind the range's last are whatever the page holds there
   vraw_t vr[4];
-  auto load_v = [&](int ln, int base, int page, int m) {
-    const int key = min(base + 4 * (ln & 15), ke - 1);
-    const bf16_t* src = (const bf16_t*)pv.v + (size_t)(outside(page) ? 0 : page) * pv.page_stride + (uint32_t)(((g << pv.page_shift) + (key & in_page)) * HD + (w * 4 + (ln >> 4)) * DV);
-    vr[m] = *(const vraw_t*)(src + min(m, ke - 1 - key) * HD);
+  const bf16_t* vsrc = nullptr;
+  auto aim_v = [&](int ln, int base, int page) {
+    vsrc = (const bf16_t*)pv.v + (size_t)(outside(page) ? 0 : page) * pv.page_stride +
+           (uint32_t)(((g << pv.page_shift) + ((base + 4 * (ln & 15)) & in_page)) * HD + (w * 4 + (ln >> 4)) * DV);
   };
-  // values of pages outside the pool become 0; so do those from poison_s on that are not finite
+  auto load_v = [&](int m) { vr[m] = *(const vraw_t*)(vsrc + m * HD); };
+  // values of pages outside the pool and of keys behind the last become 0; so do those from poison_s on that are not finite
+  auto needs_clean = [&](int base, int page, bool drop) { return drop || base + KT > ke || __any(outside(page)); };
   auto clean_v = [&](int base, int page, bool drop) {
 #pragma unroll
     for (int m = 0; m < 4; ++m) {
-      if (outside(page)) {
+      const int key = base + 4 * (lane & 15) + m;
+      if (outside(page) || key >= ke) {
 #pragma unroll
         for (int u = 0; u < DV / 2; ++u) vr[m][u] = 0u;
-      } else if (drop && min(base + 4 * kgp + m, ke - 1) >= poison_s) {
+      } else if (drop && key >= poison_s) {
 #pragma unroll
         for (int u = 0; u < DV / 2; ++u)
           vr[m][u] = ((vr[m][u] & 0x7F80u) == 0x7F80u ? 0u : vr[m][u] & 0xFFFFu) | ((vr[m][u] & 0x7F800000u) == 0x7F800000u ? 0u : vr[m][u] & 0xFFFF0000u);
       }
     }
   };
-  auto store_v = [&](int buf) {
+  // A V^T row is a dim; 16 keys' groups of 4 lie in it in the order 0, 2, 1, 3, so that the two groups a lane of the product needs are one 16-byte slot; slots
+  // permuted by the dim's pair, which for pair u of a thread is that of pair 0, exclusive-or u
+  static_assert((DV / 2 & (DV / 2 - 1)) == 0 && DV / 2 <= 8, "pairs of a thread: low bits of the permutation");
+  auto store_v = [&](int ln, int buf) {
+    const int kgp = ln & 15, dg = w * 4 + (ln >> 4);
+    const uint32_t at = ring + (uint32_t)((2 + buf) * TILE + dg * DV * KT) * 2 + (((2 * (kgp >> 2) + (kgp & 1)) ^ ((dg * (DV / 2)) & 7)) << 4) + (((kgp >> 1) & 1) << 3);
 #pragma unroll
     for (int u = 0; u < DV / 2; ++u)
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const int d = dg * DV + 2 * u + h;
         const unsigned int s = h ? 0x07060302u : 0x05040100u;
-        *(uint2*)(ring + (2 + buf) * TILE + d * KT + ((vslot ^ ((d >> 1) & 7)) * 8 + vhalf)) =
-            make_uint2(__builtin_amdgcn_perm(vr[1][u], vr[0][u], s), __builtin_amdgcn_perm(vr[3][u], vr[2][u], s));
+        *(lds_u32x2*)(uintptr_t)((at ^ (u << 4)) + (2 * u + h) * KT * 2) = u32x2{__builtin_amdgcn_perm(vr[1][u], vr[0][u], s), __builtin_amdgcn_perm(vr[3][u], vr[2][u], s)};
       }
   };
   const int n_tiles = (ke - kb + KT - 1) / KT;
@@ -604,8 +615,9 @@ __device__ __forceinline__ void paged_attention_tall(int y, const int* __restric
     }
 #pragma unroll
     for (int i = 0; i < KI; ++i) load_k(lane, kb, pages, 0, i);
+    aim_v(lane, kb, pages);
 #pragma unroll
-    for (int m = 0; m < 4; ++m) load_v(lane, kb, pages, m);
+    for (int m = 0; m < 4; ++m) load_v(m);
 #pragma unroll
     for (int t = 0; t < T; ++t)
 #pragma unroll
@@ -667,8 +679,8 @@ __device__ __forceinline__ void paged_attention_tall(int y, const int* __restric
   __syncthreads();
   const int poison = __builtin_amdgcn_readfirstlane(poison_s);
   const bool drop = poison != INT_MAX;
-  if (drop || __any(outside(pages))) clean_v(kb, pages, drop);
-  store_v(0);
+  if (needs_clean(kb, pages, drop)) clean_v(kb, pages, drop);
+  store_v(lane, 0);
   __syncthreads();
 
   for (int tl = 0; tl < n_tiles; ++tl) {
@@ -676,13 +688,14 @@ __device__ __forceinline__ void paged_attention_tall(int y, const int* __restric
     const bool more = tl + 1 < n_tiles;
     const unsigned long long missing = __ballot(outside(pages));
     const int pages_after = more ? load_pages(ahead + KT) : 0;
-    // Fragment offsets: chunk 2 t + hi of a K row and slot 2 q + hi of a V^T row, permuted, differ from chunk and slot hi by an exclusive or
-    int ko = (lane & 31) * HD + ((hi ^ (lane & (CH - 1))) << 3), vo = (lane & 31) * KT + ((hi ^ ((lane >> 1) & 7)) << 3), ln = lane;
-    asm volatile("" : "+v"(ko), "+v"(vo), "+v"(ln));
-    const bf16_t* kbuf = ring + buf * TILE;
-    const bf16_t* vbuf = ring + (2 + buf) * TILE;
-    auto read_k = [&](int k, int t) { return __builtin_bit_cast(bf16x8_t, *(const u32x4*)(kbuf + (ko ^ (t << 4)) + k * 32 * HD)); };
-    auto read_v = [&](int q, int t) { return __builtin_bit_cast(bf16x8_t, *(const u32x4*)(vbuf + (vo ^ (q << 4)) + t * 32 * KT)); };
+    // Fragment addresses: chunk 2 t + hi of a K row and slot 2 q + hi of a V^T row, permuted, differ from chunk and slot hi by an exclusive or
+    int ln = lane;
+    asm volatile("" : "+v"(ln));
+    const uint32_t ko = ring + (uint32_t)(buf * TILE * 2) + (ln & 31) * (HD * 2) + (((ln >> 5) ^ (ln & (CH - 1))) << 4);
+    const uint32_t vo = ring + (uint32_t)((2 + buf) * TILE * 2) + (ln & 31) * (KT * 2) + (((ln >> 5) ^ ((ln >> 1) & 7)) << 4);
+    auto read_k = [&](int k, int t) { return __builtin_bit_cast(bf16x8_t, *(const lds_u32x4*)(uintptr_t)((ko ^ (t << 5)) + k * 32 * HD * 2)); };
+    auto read_v = [&](int q, int t) { return __builtin_bit_cast(bf16x8_t, *(const lds_u32x4*)(uintptr_t)((vo ^ (q << 5)) + t * 32 * KT * 2)); };
+    if (more) aim_v(ln, ahead, pages_next);
     // scores (in units of log2) of keys base + 32 k + 8 (e / 4) + 4 hi + e % 4 for the lane's query
     f32x16 s[2];
 #pragma unroll
@@ -705,7 +718,7 @@ __device__ __forceinline__ void paged_attention_tall(int y, const int* __restric
 #pragma unroll
         for (int z = t * LD / T; z < (t + 1) * LD / T; ++z) {
           if (z < KI) load_k(ln, ahead, pages_next, buf ^ 1, z);
-          else load_v(ln, ahead, pages_next, z - KI);
+          else load_v(z - KI);
         }
         s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[t & 1][0], qh[t], s[0], 0, 0, 0);
         s[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[t & 1][1], qh[t], s[1], 0, 0, 0);
@@ -787,8 +800,8 @@ __device__ __forceinline__ void paged_attention_tall(int y, const int* __restric
       }
     }
     if (more) {
-      if (drop || __any(outside(pages_next))) clean_v(ahead, pages_next, drop);
-      store_v(buf ^ 1);
+      if (needs_clean(ahead, pages_next, drop)) clean_v(ahead, pages_next, drop);
+      store_v(ln, buf ^ 1);
     }
     pages = pages_next;
     pages_next = pages_after;

@@ -161,9 +161,9 @@ hipError_t launch_paged_attention_t(const PagedView& v, const PagedPlan& p, cons
   if constexpr (BF) {
     if (p.tall > 0) {
       auto kern = paged_attention_both_mfma_kernel<HD, PLANES>;
-      const size_t lds = std::max((size_t)4 * 64 * HD * 2, few_lds);
+      const size_t lds = std::max((size_t)4 * 64 * HD * 2 + 1024, few_lds);      // (the rings start at a multiple of 1 KiB)
       static bool big_lds[kMaxDevices];
-      const hipError_t e = lds_room(kern, lds, (size_t)4 * 64 * 128 * 2, big_lds);
+      const hipError_t e = lds_room(kern, lds, (size_t)4 * 64 * 128 * 2 + 1024, big_lds);
       if (e != hipSuccess) return e;
       hipLaunchKernelGGL(kern, paged_grid(v.nkv, p.tall + p.few), dim3(256), lds, a.stream, a.cu, a.start, a.qkv, a.ld, (const bf16_t*)a.gain, (const float2*)a.rope, a.eps, a.max_new, PAGED_FEW,
                          p.tall, out, v, few, tall);

@@ -96,12 +96,12 @@ dmtd_page_pool paged_pool(const dmtd_ctx* c, const PagedLayout& w) {
   return dmtd_page_pool{w.n_pages, w.page, c->cfg.max_batch, w.max_pages, (int*)(m + w.table), (int*)(m + w.held), (int*)(m + w.free_pages), (int*)(m + w.n_free)};
 }
 
-// Pages and places of pass `which` (0: the late layers' rows, 1: the front layers') from the uploaded lengths
-int paged_tables(dmtd_ctx* c, const PagedLayout& w, int which) {
+// Pages and places of pass `which` (0: the late layers' rows, 1: the front layers') of so many rows from the uploaded lengths
+int paged_tables(dmtd_ctx* c, const PagedLayout& w, int which, int rows) {
   char* m = c->paged.mem;
   const dmtd_page_pool pool = paged_pool(c, w);
   const int* up = (const int*)(m + w.up);
-  const int rc = dmtd_page_tables(&pool, up + w.start[which], up + w.count[which], w.rows, (int*)(m + w.cu[which]), (int*)(m + w.pos[which]), (int64_t*)(m + w.slots[which]),
+  const int rc = dmtd_page_tables(&pool, up + w.start[which], up + w.count[which], rows, (int*)(m + w.cu[which]), (int*)(m + w.pos[which]), (int64_t*)(m + w.slots[which]),
                                   (int*)(m + w.status) + 2 * which, c->stream);
   if (rc != DMTD_OK) c->err = g_create_error;
   return rc;
@@ -247,8 +247,8 @@ int dmtd_paged_step(dmtd_ctx* c, int32_t n, const int32_t* slots, const int32_t*
   std::vector<int32_t> next(n);
   auto run = [&]() -> int {
     HIP_TRY(c, hipMemcpyAsync(m + w.up, up.data(), up.size() * 4, hipMemcpyHostToDevice, c->stream));
-    int rc = paged_tables(c, w, 0);
-    if (rc == DMTD_OK && front_rows_n > 0 && F > 0 && !same) rc = paged_tables(c, w, 1);
+    int rc = paged_tables(c, w, 0, late_rows_n);
+    if (rc == DMTD_OK && front_rows_n > 0 && F > 0 && !same) rc = paged_tables(c, w, 1, front_rows_n);
     if (rc != DMTD_OK) return rc;
     Rows R = front_rows(c), last = late_rows(c);
     if (F > 0 && front_rows_n > 0) {
@@ -313,7 +313,7 @@ int dmtd_paged_release(dmtd_ctx* c, int32_t slot) try {
   std::vector<int32_t> up(2 * (size_t)c->cfg.max_batch, 0);          // lengths, no rows
   for (int s = 0; s < c->cfg.max_batch; ++s) up[s] = s == slot ? 0 : c->paged.seqs[s].n_tok;
   HIP_TRY(c, hipMemcpyAsync(c->paged.mem + w.up + w.start[0] * 4, up.data(), up.size() * 4, hipMemcpyHostToDevice, c->stream));
-  const int rc = paged_tables(c, w, 0);
+  const int rc = paged_tables(c, w, 0, 1);
   HIP_TRY(c, hipStreamSynchronize(c->stream));
   if (rc != DMTD_OK) { c->paged.failed = true; return rc; }
   c->paged.free_pages += (q.n_tok + w.page - 1) / w.page;
