@@ -435,6 +435,7 @@ class Engine:
 
     def reset(self):
         self._check(self.lib.dmtd_reset(self._h))
+        self._paged_memory = None
 
 
 # ------------------------------------------------------------------------------- paged key/value cache
@@ -511,9 +512,10 @@ class PageTables(_OnDevice):
 class PagedCache(_OnDevice):
     """One layer's keys and values in pages, ``k`` and ``v`` ``[n_pages, n_kv_heads, page_size, head_dim]`` (bfloat16 or float32; pages may lie apart,
     a page itself is contiguous), read and filled through ``block_table`` int32 ``[n_req, max_pages]`` (``dmtd_paged_append``, ``dmtd_paged_attention``) on
-    torch's current stream.  Steps have up to ``max_rows`` rows.  The handle holds the attention's workspace: calls of one handle must not overlap."""
+    torch's current stream.  Steps have up to ``max_rows`` rows.  The handle holds the attention's workspace: calls of one handle, and of those that
+    :meth:`layer` made from it, must not overlap."""
 
-    def __init__(self, k, v, block_table, n_q_heads: int, max_rows: int):
+    def __init__(self, k, v, block_table, n_q_heads: int, max_rows: int, _workspace_of=None):
         self._open(k)
         torch, dev = self._torch, self._index
         if k.dtype not in (torch.bfloat16, torch.float32) or v.dtype is not k.dtype:
@@ -535,11 +537,20 @@ class PagedCache(_OnDevice):
         self._ws_bytes = self._lib.dmtd_paged_workspace_bytes(self._p)
         if self._ws_bytes == 0:
             _raise(self._lib, DMTD_EINVAL)
+        if _workspace_of is not None:
+            if _workspace_of._ws_bytes < self._ws_bytes or _workspace_of.device != self.device:
+                raise ValueError("the other layer's caches must be laid out like these")
+            self._ws, self._ws_ptr, self._streams = _workspace_of._ws, _workspace_of._ws_ptr, _workspace_of._streams
+            return
         self._ws = torch.zeros(self._ws_bytes, dtype=torch.uint8, device=k.device)
         self._ws_ptr = self._ws.data_ptr()
         stream = torch.cuda.current_stream(k.device)
         stream.synchronize()              # zeroed, whichever stream the first call is on
         self._streams = {stream.cuda_stream}
+
+    def layer(self, k, v) -> "PagedCache":
+        """The handle of another layer's pools ``k`` and ``v``, with this one's block table and workspace."""
+        return PagedCache(k, v, self.block_table, self._q_heads[0], self.max_rows, _workspace_of=self)
 
     def _rows(self, qkv, cols, norm, rope):
         dev, shape = self._index, qkv.shape

@@ -43,7 +43,7 @@ def check_step(tables, model, start, rows, room):
 
 @pytest.mark.parametrize("n_req, page, max_pages, n_pages, room, most", [
     (1, 16, 4, 5, 16, 20), (3, 16, 6, 12, 64, 30), (64, 32, 5, 200, 64, 3), (65, 16, 9, 300, 2048, 60), (7, 256, 3, 15, 2049, 600), (300, 16, 40, 4000, 6000, 200),
-    (1025, 16, 4, 2500, 5000, 25), (8192, 16, 2, 9000, 9000, 3),
+    (1025, 16, 4, 2500, 5000, 25), (8192, 16, 2, 9000, 9000, 3), (8192, 32, 2, 8192, 2048, 1),
 ])
 def test_page_tables_over_many_steps(n_req, page, max_pages, n_pages, room, most):
     rng = np.random.RandomState(n_req * 31 + page)
@@ -363,6 +363,76 @@ def test_same_bits_every_time_and_on_every_stream():
         with torch.cuda.stream(side if turn % 2 else torch.cuda.current_stream()):
             assert torch.equal(s.attend(c), first)
         torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_steps_without_rows(dtype):
+    """A step that was refused, and one in which no request brings anything: nothing is stored, nothing comes out."""
+    s = Setup(H8, dtype, 16, [20, 3], [4, 1], seed=32)
+    c = s.cache()
+    tables = pkg.PageTables.empty(2, 16, 2, s.width, DEV)
+    for rows, status in (([40, 1], -3), ([0, 0], 0)):
+        m = Maps(2, s.room)
+        tables.build(ints([0, 0]), ints(rows), *m.all())
+        out = torch.full((s.room, s.nq, s.hd), 7.0, dtype=dtype, device=DEV)
+        c.append(s.qkv.to(DEV), m.cu, m.pos, m.slots, k_norm=s.dev(s.gain), rope=s.dev(s.rope))
+        c.attention(s.qkv.to(DEV), ints([0, 0]), m.cu, out, q_norm=s.dev(s.gain), rope=s.dev(s.rope))
+        assert m.status[0].item() == status and m.cu.tolist() == [0, 0, 0]
+        assert (out == 7.0).all()
+        for got, was in ((s.kd, s.k), (s.vd, s.v)):
+            assert torch.equal(got.cpu().view(torch.int16), was.view(torch.int16))
+
+
+def test_layers_share_a_block_table_and_a_workspace():
+    """Handles of several layers one after the other on a stream, and what they refuse."""
+    layers = [Setup(H8, BF, 32, [700, 0, 90], [1, 130, 3], seed=30) for _ in range(3)]
+    for i, s in enumerate(layers[1:], 1):          # the same tables, other keys and values
+        gen = torch.Generator().manual_seed(i)
+        for t in (s.k, s.v):
+            fresh = torch.randn(t.shape, generator=gen).to(BF)
+            t.copy_(torch.where(torch.isnan(t), t, fresh))
+    first = layers[0].cache()
+    handles = [first] + [first.layer(s.k.to(DEV), s.v.to(DEV)) for s in layers[1:]]
+    for _ in range(2):
+        for s, c in zip(layers, handles):
+            s.check(s.attend(c))
+    with pytest.raises(ValueError):
+        first.layer(layers[0].kd[:, :1].contiguous(), layers[0].vd)
+    with pytest.raises(pkg.DmtdError):
+        first.layer(layers[0].kd[:, :, :24].contiguous(), layers[0].vd[:, :, :24].contiguous())
+
+
+def test_the_handles_check_their_tensors():
+    s = Setup(H8, BF, 32, [40], [3], seed=31)
+    c = s.cache()
+    qkv, start, cu, out = s.qkv.to(DEV), ints(s.start), ints(s.cu), torch.zeros(s.room, 8, 128, dtype=BF, device=DEV)
+    pos, slots, gain, rope = ints(s.pos + [0] * (s.room - s.total)), ints(s.slots + [0] * (s.room - s.total), torch.int64), s.dev(s.gain), s.dev(s.rope)
+    for bad in (dict(qkv=qkv.bfloat16()), dict(qkv=qkv[:-1]), dict(qkv=qkv[:, :1000]), dict(qkv=qkv.t()), dict(start=start.long()), dict(start=ints([1, 2])), dict(cu=cu[:1]),
+                dict(cu=cu.cpu()), dict(out=out.float()), dict(out=out[:, :4]), dict(out=out[:2]), dict(q_norm=gain.float()), dict(q_norm=gain[:64]), dict(rope=rope.double()),
+                dict(rope=rope[:, :32])):
+        a = dict(dict(qkv=qkv, start=start, cu=cu, out=out, q_norm=gain, rope=rope), **bad)
+        with pytest.raises(ValueError):
+            c.attention(a["qkv"], a["start"], a["cu"], a["out"], q_norm=a["q_norm"], rope=a["rope"])
+    for bad in (dict(qkv=qkv[:, :1400]), dict(pos=pos[:-1]), dict(pos=pos.long()), dict(slots=slots.int()), dict(slots=slots[::2])):
+        a = dict(dict(qkv=qkv, cu=cu, pos=pos, slots=slots), **bad)
+        with pytest.raises(ValueError):
+            c.append(a["qkv"], a["cu"], a["pos"], a["slots"], k_norm=gain, rope=rope)
+    with pytest.raises(pkg.DmtdError):             # rows that are not 16-byte aligned
+        c.attention(torch.zeros(s.room, qkv.shape[1] + 1, device=DEV)[:, 1:], start, cu, out)
+    with pytest.raises(pkg.DmtdError):
+        c.attention(qkv, start, cu, out, max_new=s.room + 1)
+    with pytest.raises(ValueError):
+        pkg.PagedCache(s.kd.transpose(1, 2), s.vd.transpose(1, 2), c.block_table, 8, 8)
+    with pytest.raises(ValueError):
+        pkg.PagedCache(s.kd, s.vd.float(), c.block_table, 8, 8)
+    with pytest.raises(pkg.DmtdError):
+        pkg.PagedCache(s.kd, s.vd, c.block_table, 7, 8)
+    t = pkg.PageTables.empty(8, 16, 2, 4, DEV)
+    m = Maps(2, 16)
+    for bad in ((start, start) + m.all(), (ints([0, 0]).long(), ints([0, 0])) + m.all(), (ints([0, 0]), ints([0, 0]), m.cu, m.pos, m.slots[:8], m.status)):
+        with pytest.raises(ValueError):
+            t.build(*bad)
+    assert c.attention(qkv, start, cu, q_norm=gain, rope=rope).shape == (s.room, 8, 128)
 
 
 # ------------------------------------------------------------------------------------------ together
