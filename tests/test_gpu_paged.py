@@ -370,8 +370,8 @@ def test_steps_without_rows(dtype):
     """A step that was refused, and one in which no request brings anything: nothing is stored, nothing comes out."""
     s = Setup(H8, dtype, 16, [20, 3], [4, 1], seed=32)
     c = s.cache()
-    tables = pkg.PageTables.empty(2, 16, 2, s.width, DEV)
-    for rows, status in (([40, 1], -3), ([0, 0], 0)):
+    tables = pkg.PageTables.empty(1, 16, 2, s.width, DEV)
+    for rows, status in (([9, 1], -3), ([0, 0], 0)):
         m = Maps(2, s.room)
         tables.build(ints([0, 0]), ints(rows), *m.all())
         out = torch.full((s.room, s.nq, s.hd), 7.0, dtype=dtype, device=DEV)
