@@ -1,13 +1,13 @@
 // Attention of a step's new tokens over the paged cache of their requests (paged.hpp).  The new tokens' own keys and values are in the cache
 // already (paged_append_kernel); row t of request i, at position start[i] + t, sees the request's keys 0 .. start[i] + t.
 //
-// Two kernels for bf16 caches.  paged_attention_few_mfma_kernel takes the requests with few query vectors per KV head (rows x query heads that share
-// it, up to PAGED_FEW): blocks of 16 vectors, which read keys and values straight from the cache at the rate of the memory.
-// paged_attention_tall_mfma_kernel takes the others: blocks of 128 vectors, whose keys and values pass through LDS, bound by the matrix cores.
+// Two kinds of blocks for bf16 caches.  paged_attention_few takes the requests with few query vectors per KV head (rows x query heads that share it, up to
+// PAGED_FEW): blocks of 16 vectors, which read keys and values straight from the pages at the rate of the memory.  paged_attention_tall takes the
+// others: blocks of 128 vectors, whose keys and values pass through LDS, bound by the matrix cores.  A step that may have both kinds is one launch of both.
 // A block serves one KV head, one group of a request's rows and one range of its keys.  The ranges are found by every block itself from the
 // requests' lengths (paged_find): all of one length, such that the blocks fill the chip about once, whatever the lengths are.  Where a group has several
-// ranges, their partial results go through the workspace and the block that ends last joins them, in the order of the ranges: no second
-// launch, and the same bits whichever block that is.
+// ranges, their partial results go through the workspace and are joined in the order of the ranges: of few vectors by the block that ends
+// last, without a second launch, of many by paged_attention_merge_kernel.
 #pragma once
 #include "paged.hpp"
 #include "gemm_wide.hpp"
