@@ -539,7 +539,7 @@ class PagedCache(_OnDevice):
             _raise(self._lib, DMTD_EINVAL)
         if _workspace_of is not None:
             if _workspace_of._ws_bytes < self._ws_bytes or _workspace_of.device != self.device:
-                raise ValueError("the other layer's caches must be laid out like these")
+                raise ValueError("the workspace is too small for the other layer's caches, or on another GPU")
             self._ws, self._ws_ptr, self._streams = _workspace_of._ws, _workspace_of._ws_ptr, _workspace_of._streams
             return
         self._ws = torch.zeros(self._ws_bytes, dtype=torch.uint8, device=k.device)

@@ -112,6 +112,9 @@ void launch_paged_append(const PagedView& v, int head_dim, const float* qkv, lon
 // How an attention call is laid out: blocks per KV head of either kernel (0: no launch), groups that the merge looks at, log2 of those that the key ranges are chosen
 // for, and the workspace: the counts of the few-rows groups with several ranges, their partial results, the tall groups' (paged_find).
 struct PagedPlan { int few, tall, merge, few_shift, tall_shift; size_t count_bytes, few_bytes, tall_bytes; };
+// The counts' room is the same for all caches, so that nothing else is ever written there and caches of different layouts may use one workspace in turn: fewer than
+// 2^few_shift groups of each KV head count, which is at most 512 counts in all (1024 KV heads: none).
+constexpr size_t PAGED_COUNT_BYTES = 4096;
 int floor_log2(int v) { int s = 0; while ((2 << s) <= v) ++s; return s; }
 PagedPlan paged_plan(const dmtd_paged_cache* c, int max_new) {
   PagedPlan p{};
@@ -128,7 +131,7 @@ PagedPlan paged_plan(const dmtd_paged_cache* c, int max_new) {
   if (bf16) few = std::min<long>(few, (long)c->n_req * ((tall_from - 1 + rpb_few - 1) / rpb_few));
   p.few = blocks(few, p.few_shift, PAGED_KEYS_FEW);
   p.few_bytes = align_up(((size_t)16 * (c->head_dim + 2) * 4 << p.few_shift) * 2 * c->n_kv_heads, 256);
-  p.count_bytes = align_up(((size_t)4 << p.few_shift) * c->n_kv_heads, 256);
+  p.count_bytes = PAGED_COUNT_BYTES;
   if (bf16 && few_rows >= tall_from) {
     const long groups = std::min<long>(c->n_req, c->max_rows / tall_from) + c->max_rows / rpb_tall;
     p.tall = blocks(groups, p.tall_shift, PAGED_KEYS_TALL);

@@ -402,6 +402,16 @@ def test_layers_share_a_block_table_and_a_workspace():
         first.layer(layers[0].kd[:, :, :24].contiguous(), layers[0].vd[:, :, :24].contiguous())
 
 
+def test_layers_of_other_types_share_a_workspace():
+    """Pools of another type behind the same block table; the bfloat16 layer leaves partial results, and the float32 one has more groups in several key ranges than the other can count."""
+    layers = [Setup(H8, dtype, 32, [2000] + [300] * 150, [1] * 151, seed=33) for dtype in (BF, F32)]
+    first = layers[0].cache()
+    handles = [first, first.layer(layers[1].k.to(DEV), layers[1].v.to(DEV))]
+    for _ in range(2):
+        for s, c in zip(layers, handles):
+            s.check(s.attend(c))
+
+
 def test_the_handles_check_their_tensors():
     s = Setup(H8, BF, 32, [40], [3], seed=31)
     c = s.cache()
