@@ -139,6 +139,24 @@ def test_many_rows():
 
 
 @pytest.mark.gpu
+def test_many_requests():
+    """More requests than the tiled projections' rows: single tokens, and the head, in the wide layout of rows; the slots named out of order."""
+    n = 200
+    s = Server("bf16", n, 32, 16, 2)
+    for slot in range(n):
+        s.arrive(slot, 1 + slot % 3, 1 + slot % 4, 12, 100 + slot)
+    order = np.random.RandomState(3).permutation(n).tolist()
+    s.step([(slot, s.req[slot]["prompt"]) for slot in order])
+    for _ in range(3):
+        s.step([(slot, 1) for slot in order])
+    s.step([(slot, 1) for slot in order if slot % 50 != 7])          # 196 of them
+    for slot in order[:9]:
+        s.leave(slot)
+    s.step([(slot, 1) for slot in order[9:]])                        # 191
+    s.done()
+
+
+@pytest.mark.gpu
 def test_pool_and_slots_run_out():
     s = Server("fp32", 3, 64, 16, 2)                    # 12 pages
     eng = s.eng
