@@ -399,7 +399,7 @@ int dmtd_paged_begin(dmtd_ctx* ctx, int32_t page_size, void* memory_dev, size_t 
 int dmtd_paged_step(dmtd_ctx* ctx, int32_t n, const int32_t* slots, const int32_t* counts, const int32_t* tokens, const uint8_t* full, int32_t n_late,
                     int32_t* next_tokens);
 
-/* The request in a slot ends: its pages go back to the pool.  Errors: DMTD_EINVAL, DMTD_ESTATE, DMTD_EHIP. */
+/* The request in a slot ends: its pages go back to the pool.  Errors: DMTD_EINVAL, DMTD_ESTATE, DMTD_EHIP (only dmtd_reset is left). */
 int dmtd_paged_release(dmtd_ctx* ctx, int32_t slot);
 
 /* A slot's tokens in the late (n_tok) and front (n_front) layers' caches, and the pool's free pages.  Any pointer may be NULL.  Errors: DMTD_EINVAL (no dmtd_paged_begin, slot). */

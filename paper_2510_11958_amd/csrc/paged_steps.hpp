@@ -312,10 +312,15 @@ int dmtd_paged_release(dmtd_ctx* c, int32_t slot) try {
   PagedState::Seq& q = c->paged.seqs[slot];
   std::vector<int32_t> up(2 * (size_t)c->cfg.max_batch, 0);          // lengths, no rows
   for (int s = 0; s < c->cfg.max_batch; ++s) up[s] = s == slot ? 0 : c->paged.seqs[s].n_tok;
-  HIP_TRY(c, hipMemcpyAsync(c->paged.mem + w.up + w.start[0] * 4, up.data(), up.size() * 4, hipMemcpyHostToDevice, c->stream));
-  const int rc = paged_tables(c, w, 0, 1);
-  HIP_TRY(c, hipStreamSynchronize(c->stream));
-  if (rc != DMTD_OK) { c->paged.failed = true; return rc; }
+  auto run = [&]() -> int {
+    HIP_TRY(c, hipMemcpyAsync(c->paged.mem + w.up + w.start[0] * 4, up.data(), up.size() * 4, hipMemcpyHostToDevice, c->stream));
+    const int rc = paged_tables(c, w, 0, 1);
+    if (rc != DMTD_OK) return rc;
+    HIP_TRY(c, hipStreamSynchronize(c->stream));
+    return DMTD_OK;
+  };
+  const int rc = run();
+  if (rc != DMTD_OK) { c->paged.failed = true; (void)hipStreamSynchronize(c->stream); return rc; }
   c->paged.free_pages += (q.n_tok + w.page - 1) / w.page;
   q = PagedState::Seq{};
   return DMTD_OK;
