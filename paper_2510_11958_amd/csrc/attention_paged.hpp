@@ -14,6 +14,20 @@
 
 namespace dmtd {
 
+// bf16 parts in which a probability of a bf16 cache enters its products.  Rows of bf16: two, 16 of its 24 bits, twice what the output keeps (2048 rows behind 6144, 32/8 heads of 128:
+// 438 us, with three 516; 0.0017 off 64 bits with either, the output's rounding).  The planes that the projections read keep 16 bits: three, which add up to all 24, as
+// in the attention of the other calls (attention_mfma.hpp, attention_prefill.hpp); values that cancel would show the roundings of two.
+template <bool PLANES> constexpr int PAGED_PARTS = PLANES ? 3 : 2;
+
+// A pair of probabilities in three bf16 parts: the leading 8 bits, the next 8, the rest
+__device__ __forceinline__ void paged_split3(float a, float b, uint32_t& h, uint32_t& m, uint32_t& l) {
+  const float a1 = a - __uint_as_float(__float_as_uint(a) & 0xFFFF0000u), b1 = b - __uint_as_float(__float_as_uint(b) & 0xFFFF0000u);
+  const float a2 = a1 - __uint_as_float(__float_as_uint(a1) & 0xFFFF0000u), b2 = b1 - __uint_as_float(__float_as_uint(b1) & 0xFFFF0000u);
+  h = __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
+  m = __builtin_amdgcn_perm(__float_as_uint(b1), __float_as_uint(a1), 0x07060302u);
+  l = __builtin_amdgcn_perm(__float_as_uint(b2), __float_as_uint(a2), 0x07060302u);
+}
+
 // Blocks that the key ranges are chosen for.  bf16, few rows: one of four waves on each CU reads as fast as more do, and shorter ranges cost more joins (us, 32/8 heads of 128,
 // 256 / 512 / 1024 blocks: 3 rows of 8 requests behind 16384 86 / 95 / 107, one row behind 16384 20 / 23 / 28, 4 rows of 32 behind 1024 26 / 35 / 35).  fp32, whose
 // products weigh more: 512 (16/8 heads, 200 rows behind 1000 55 / 41 / 46).  Tall: half of the blocks that the chip holds (64 rows behind 4096 29, with 512 46).
@@ -271,17 +285,18 @@ __device__ __forceinline__ void paged_store4(const PagedOut& o, int row, int col
 // waves take groups of 16 keys in turn, which never leave a page, the next group's loads in flight.  Per group, in one wave (lane: sl = lane % 16, kq = lane / 16):
 //   scores   S^T[key, q] = sum_d K[key, d] Q[q, d], 16x16x32: K rows as they lie in the cache, the queries as two bf16 parts (16 bits);
 //   output   O[q, d] += sum_key P[q, key] V[key, d], 16x16x16: a lane's operand is 4 consecutive keys of one row or column, so nothing moves between
-//            lanes; a probability goes in as two bf16 parts.
+//            lanes; a probability goes in as PAGED_PARTS bf16 parts.
 // fp32 caches: 16x16x4 for both, the queries and probabilities as they are, any number of rows (a chunk's groups of 16 vectors find the keys in the L2).
 // Values are loaded past the L2, keys through it: a key's 256 bytes take four loads, which share cache lines (us, both through the caches / values past
 // them / both: 3 rows of 8 requests behind 16384 103 / 86 / 92, 31 ragged rows in pages of 16 tokens 24 / 26 / 30, out of cold memory 30 / 28 / 31, one row of 64
 // behind 1024 out of cold memory 53 / 49 / 48).
-// Bound by the memory: 8 KiB per wave and group against 2 x HD / 16 + 2 x HD / 32 products.
+// Bound by the memory: 8 KiB per wave and group against PAGED_PARTS x HD / 16 + 2 x HD / 32 products.
 template <typename CT, int HD, bool PLANES>
 __device__ __forceinline__ void paged_attention_few(int y, const int* __restrict__ cu, const int* __restrict__ start, const float* __restrict__ qkv, long ld,
                                                     const CT* __restrict__ q_gain, const float2* __restrict__ rope_tab, float eps, int max_new, int hi, const PagedOut& po,
                                                     const PagedView& pv, const PagedWork& wk) {
   constexpr bool BF = sizeof(CT) == 2;
+  constexpr int PARTS = PAGED_PARTS<PLANES>;
   constexpr int QVT = 16, NW = PAGED_WAVES, NT = 64 * NW, DPL = HD / 16, half = HD / 2, HL = HD / 32;
   constexpr int KS = BF ? HD / 32 : HD / 16;                 // 16-byte pieces of a key a lane carries
   constexpr int QLD = BF ? HD + ATT_QPAD : HD + 4;           // a query row in LDS
@@ -448,17 +463,23 @@ __device__ __forceinline__ void paged_attention_few(int y, const int* __restrict
 #pragma unroll
         for (int m = 0; m < 4; ++m) acc[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(p[m], __uint_as_float(va[m][e]), acc[e], 0, 0, 0);
     } else {
-    uint2 ph, pl;
-    ph.x = pack_bf16x2(p[0], p[1]);
-    ph.y = pack_bf16x2(p[2], p[3]);
-    pl.x = pack_bf16x2(p[0] - __uint_as_float(ph.x << 16), p[1] - __uint_as_float(ph.x & 0xFFFF0000u));
-    pl.y = pack_bf16x2(p[2] - __uint_as_float(ph.y << 16), p[3] - __uint_as_float(ph.y & 0xFFFF0000u));
+    uint2 pp[PARTS];
+    if constexpr (PARTS == 3) {
+      paged_split3(p[0], p[1], pp[0].x, pp[1].x, pp[2].x);
+      paged_split3(p[2], p[3], pp[0].y, pp[1].y, pp[2].y);
+    } else {
+      pp[0].x = pack_bf16x2(p[0], p[1]);
+      pp[0].y = pack_bf16x2(p[2], p[3]);
+      pp[1].x = pack_bf16x2(p[0] - __uint_as_float(pp[0].x << 16), p[1] - __uint_as_float(pp[0].x & 0xFFFF0000u));
+      pp[1].y = pack_bf16x2(p[2] - __uint_as_float(pp[0].y << 16), p[3] - __uint_as_float(pp[0].y & 0xFFFF0000u));
+    }
 #pragma unroll
     for (int e = 0; e < DPL; ++e) {
       const unsigned int sel = (e & 1) ? 0x07060302u : 0x05040100u;
       const uint2 v4 = make_uint2(__builtin_amdgcn_perm(va[1][e >> 1], va[0][e >> 1], sel), __builtin_amdgcn_perm(va[3][e >> 1], va[2][e >> 1], sel));
-      acc[e] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(bf16x4s_t, pl), __builtin_bit_cast(bf16x4s_t, v4), acc[e], 0, 0, 0);
-      acc[e] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(bf16x4s_t, ph), __builtin_bit_cast(bf16x4s_t, v4), acc[e], 0, 0, 0);
+#pragma unroll
+      for (int z = PARTS - 1; z >= 0; --z)
+        acc[e] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(bf16x4s_t, pp[z]), __builtin_bit_cast(bf16x4s_t, v4), acc[e], 0, 0, 0);
     }
     }
   }
@@ -511,7 +532,7 @@ __device__ __forceinline__ void paged_attention_few(int y, const int* __restrict
 // wave - and walks its range of keys in tiles of 64 through LDS.  Per tile and wave, with 32x32x16 products:
 //   scores   S^T[key, q]: K rows from LDS, the queries in registers as two bf16 parts; a lane ends up with 16 keys of one vector per 32 keys;
 //   output   O^T[d, q] += sum_key V^T[d, key] P^T[key, q]: a lane's own probabilities are the operand as they stand, V^T comes from LDS; a
-//            probability goes in as two bf16 parts (16 bits, as the planes that the O projection reads keep).
+//            probability goes in as PAGED_PARTS bf16 parts.
 // K goes from the pages straight into LDS, a wave 16 keys of a tile (one page), rows' 16-byte chunks permuted by the key number; V through registers, transposed
 // on the way (4 keys x HD / 16 dims per thread; 8-byte pieces permuted by the dim).  Two buffers of each: the next tile's loads fly during
 // a tile, and a tile's page numbers are fetched a tile earlier still, one per 4 keys and lane.
@@ -522,6 +543,7 @@ template <int HD, bool PLANES>
 __device__ __forceinline__ void paged_attention_tall(int y, const int* __restrict__ cu, const int* __restrict__ start, const float* __restrict__ qkv, long ld,
                                                      const bf16_t* __restrict__ q_gain, const float2* __restrict__ rope_tab, float eps, int max_new, int lo, const PagedOut& po,
                                                      const PagedView& pv, const PagedWork& wk) {
+  constexpr int PARTS = PAGED_PARTS<PLANES>;
   constexpr int QVT = 128, NT = 256, KT = 64;
   constexpr int T = HD / 16;           // steps over d for the scores
   constexpr int DT = HD / 32;          // 32-dim tiles of the output
@@ -759,25 +781,28 @@ __device__ __forceinline__ void paged_attention_tall(int y, const int* __restric
         for (int e = 0; e < 16; ++e) acc[t][e] *= f;
       m_run = m_new;
     }
-    // the 8 probabilities of a contraction step q as two bf16 parts, pair j of them in two pieces
-    uint32_t pp[2][2][4];
+    // the 8 probabilities of a contraction step q in bf16 parts, pair j of them in as many pieces
+    uint32_t pp[2][PARTS][4];
     auto piece = [&](int q, int j, int z) {
       const int e = 8 * (q & 1) + 2 * j;
       const float a = s[q >> 1][e], d = s[q >> 1][e + 1];
       if (z == 0) {
         s[q >> 1][e] = __builtin_amdgcn_exp2f(a - m_use);
         s[q >> 1][e + 1] = __builtin_amdgcn_exp2f(d - m_use);
+      } else if (z == 2) {
+        paged_split3(a, d, pp[q & 1][0][j], pp[q & 1][1][j], pp[q & 1][PARTS - 1][j]);
       } else {
         l_run += a;
         l_run += d;
+        if (PARTS == 3) return;
         const uint32_t h = pack_bf16x2(a, d);
         pp[q & 1][0][j] = h;
         pp[q & 1][1][j] = pack_bf16x2(a - __uint_as_float(h << 16), d - __uint_as_float(h & 0xFFFF0000u));
       }
     };
-    constexpr int PG = 4 / DT;          // pairs of the next step beside a V fragment's two products
+    constexpr int PG = 4 / DT;          // pairs of the next step beside a V fragment's products
 #pragma unroll
-    for (int z = 0; z < 2; ++z)
+    for (int z = 0; z < PARTS; ++z)
 #pragma unroll
       for (int j = 0; j < 4; ++j) piece(0, j, z);
     __builtin_amdgcn_sched_barrier(0);
@@ -788,8 +813,8 @@ __device__ __forceinline__ void paged_attention_tall(int y, const int* __restric
         const int n = q * DT + t;
         if (n + 1 < 4 * DT) vf[(n + 1) & 1] = read_v((n + 1) / DT, (n + 1) % DT);
 #pragma unroll
-        for (int z = 0; z < 2; ++z) {
-          const uint32_t* f = pp[q & 1][1 - z];
+        for (int z = 0; z < PARTS; ++z) {
+          const uint32_t* f = pp[q & 1][PARTS - 1 - z];
           acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[n & 1], __builtin_bit_cast(bf16x8_t, u32x4{f[0], f[1], f[2], f[3]}), acc[t], 0, 0, 0);
           if (q < 3) {
 #pragma unroll
