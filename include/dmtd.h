@@ -369,7 +369,7 @@ size_t dmtd_paged_workspace_bytes(const dmtd_paged_cache* cache);
  * out: DEVICE [max_rows, ldo] of dtype, n_q_heads heads of head_dim; 16-byte aligned, ldo a multiple of 8.
  * workspace: DEVICE, 256-byte aligned, zeroed once before its first use; calls leave it fit for the next, also of another cache.  Calls that may overlap need one each.
  * Requests whose lengths do not fit (negative, more than max_new rows, beyond max_rows, the block table or the rotary table) are left out, their rows of out
- * as they were.  Keys in pages outside the pool are left out; a row without any key, or whose scores are all minus infinity, comes out as 0.  Values that are not finite reach the rows that see them,
+ * as they were; where cu_rows descends, all of them are.  Keys in pages outside the pool are left out; a row without any key, or whose scores are all minus infinity, comes out as 0.  Values that are not finite reach the rows that see them,
  * as NaN or infinity in their own dim or as NaN in all, and no others.  Results do not depend on which workgroup ends first.
  * Errors: DMTD_EINVAL, DMTD_ECAPACITY (workspace too small), DMTD_EHIP. */
 int dmtd_paged_attention(const dmtd_paged_cache* cache, const float* qkv, int64_t ld, const int32_t* start, const int32_t* cu_rows, int32_t max_new,

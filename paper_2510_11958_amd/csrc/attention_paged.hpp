@@ -41,10 +41,13 @@ constexpr int PAGED_FEW = 64;
 // single tokens, 14/2 heads of 64, 33 / 35 / 45)
 constexpr int PAGED_KEYS_FEW = 128, PAGED_KEYS_TALL = 256;
 
-// Rows of a request as the kernels read them: none where the lengths do not fit the buffers or the tables
+// Rows of a request as the kernels read them: none where the lengths do not fit the buffers or the tables.  `descends` is set where cu does not ascend from 0 on: as
+// long as it does, requests share no rows, and what they bring together fits max_rows, which the grids and the workspace are made for.
 struct PagedReq { int first, n, start; };
-__device__ __forceinline__ PagedReq paged_req(const PagedView& pv, const int* cu, const int* start, int max_new, int i) {
-  PagedReq q{cu[i], cu[i + 1] - cu[i], start[i]};
+__device__ __forceinline__ PagedReq paged_req(const PagedView& pv, const int* cu, const int* start, int max_new, int i, bool& descends) {
+  const int first = cu[i], end = cu[i + 1];
+  descends |= first < 0 || end < first;
+  PagedReq q{first, (int)((unsigned)end - (unsigned)first), start[i]};
   if (q.first < 0 || q.n < 0 || q.n > max_new || q.first > pv.max_rows - q.n || q.start < 0 || q.start > pv.limit - q.n) q.n = 0;
   return q;
 }
@@ -89,7 +92,9 @@ __device__ __forceinline__ bool paged_find(const PagedView& pv, const int* cu, c
   if (pv.n_req <= 64) {       // a request per lane, every wave for itself
     const int lane = threadIdx.x & 63;
     q = PagedReq{0, 0, 0};
-    if (lane < pv.n_req) q = paged_req(pv, cu, start, max_new, lane);
+    bool descends = false;
+    if (lane < pv.n_req) q = paged_req(pv, cu, start, max_new, lane, descends);
+    if (__any(descends)) return false;
     const int gr = paged_groups(q, GQ, lo, hi, rpb);
     kps = keys_of(wave_reduce((unsigned long long)gr * (unsigned)(q.start + q.n), [](unsigned long long a, unsigned long long b) { return a + b; }));
     const int sp = (int)((unsigned)(q.start + q.n + kps - 1) / (unsigned)kps), items = GROUP ? (sp > 1 ? gr : 0) : gr * sp;
@@ -111,16 +116,19 @@ __device__ __forceinline__ bool paged_find(const PagedView& pv, const int* cu, c
     __shared__ int found_s[8];
     const int tid = threadIdx.x, ipt = (pv.n_req + NT - 1) / NT, i0 = min(tid * ipt, pv.n_req), i1 = min(i0 + ipt, pv.n_req);
     long long mine = 0, total;
+    bool descends = false;
     for (int j = i0; j < i1; ++j) {
-      const PagedReq r = paged_req(pv, cu, start, max_new, j);
+      const PagedReq r = paged_req(pv, cu, start, max_new, j, descends);
       mine += (long long)paged_groups(r, GQ, lo, hi, rpb) * (r.start + r.n);
     }
-    (void)block_scan<NT>(mine, sums_s, total);
+    // rows are at most 2^24, keys 2^30: a sum of 2^55 and more says that some thread saw cu descend
+    (void)block_scan<NT>(descends ? 1ll << 55 : mine, sums_s, total);
+    if ((unsigned long long)total >> 55) return false;
     kps = keys_of((unsigned long long)total);
     // items in the low half, those of groups with several ranges in the upper one, and such groups
     long long n_items = 0, n_multi = 0;
     auto share = [&](int j) {
-      const PagedReq r = paged_req(pv, cu, start, max_new, j);
+      const PagedReq r = paged_req(pv, cu, start, max_new, j, descends);
       return PagedShare{paged_groups(r, GQ, lo, hi, rpb), (int)((unsigned)(r.start + r.n + kps - 1) / (unsigned)kps)};
     };
     for (int j = i0; j < i1; ++j) {
@@ -147,7 +155,7 @@ __device__ __forceinline__ bool paged_find(const PagedView& pv, const int* cu, c
     __syncthreads();
     i = __builtin_amdgcn_readfirstlane(found_s[0]);
     splits = found_s[1]; before = found_s[2]; slots = found_s[3]; multi = found_s[4];
-    q = paged_req(pv, cu, start, max_new, i);
+    q = paged_req(pv, cu, start, max_new, i, descends);
   }
   // the same in every lane: in scalar registers from here on
   kps = __builtin_amdgcn_readfirstlane(kps);
