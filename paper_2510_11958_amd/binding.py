@@ -527,6 +527,8 @@ class PagedCache(_OnDevice):
         for t in (k, v):
             if any(n > 1 and a != b for n, a, b in zip(t.shape, t.stride(), stride)):
                 raise ValueError("pages must be contiguous, and k and v laid out alike")
+        if stride[0] < n_kv * page_size * hd:      # (0, as of an expanded page, would mean pages behind each other)
+            raise ValueError("pages must not overlap")
         n_req, max_pages = block_table.shape
         self.k, self.v, self.block_table, self.dtype, self.max_rows = k, v, block_table, k.dtype, int(max_rows)
         self._c = _PagedCache(k.data_ptr(), v.data_ptr(), stride[0], _want(block_table, "block_table", self._i32, dev, (n_req, max_pages)), n_pages, page_size, n_req, max_pages,

@@ -3,6 +3,7 @@ import pytest
 import torch
 
 import paged_util as pu
+import paper_2510_11958_amd as pkg
 from test_gpu_paged import BF, DEV, H8, Setup, ints
 
 pytestmark = pytest.mark.gpu
@@ -28,3 +29,15 @@ def test_rows_that_descend(n_req):
         assert ((attend(shorter, s.cu).double() - ref).abs() <= tol).all()
         s.check(attend(s.start, s.cu))
         assert (out == 77.0).all()
+
+
+def test_pages_that_overlap():
+    """One page expanded to many has a stride of 0, which the C call takes for pages that follow each other; others lie closer than a page is long."""
+    table = ints([[0, 1]])
+    for dtype in (BF, torch.float32):
+        page = torch.zeros(1, 2, 16, 64, dtype=dtype, device=DEV)
+        close = torch.zeros(9 * 1024 + 2048, dtype=dtype, device=DEV).as_strided((10, 2, 16, 64), (1024, 1024, 64, 1))
+        for k in (page.expand(10, 2, 16, 64), close):
+            with pytest.raises(ValueError):
+                pkg.PagedCache(k, k, table, 4, 8)
+        pkg.PagedCache(page, page, table, 4, 8)
