@@ -563,6 +563,8 @@ class PagedCache(_OnDevice):
         if rope is None:
             return qkv.data_ptr(), ld, gain, None, 0
         n = rope.shape[0]
+        if n < 1:                                  # (its address would be null: no rotation)
+            raise ValueError("rope must hold a position")
         return qkv.data_ptr(), ld, gain, _want(rope, "rope", self._f32, dev, (n, *self._angles)), n
 
     def append(self, qkv, cu_rows, row_pos, slots, k_norm=None, rope=None, eps: float = 1e-6):

@@ -41,3 +41,16 @@ def test_pages_that_overlap():
             with pytest.raises(ValueError):
                 pkg.PagedCache(k, k, table, 4, 8)
         pkg.PagedCache(page, page, table, 4, 8)
+
+
+def test_an_empty_rotary_table():
+    """Not "no rotation", although its address is null."""
+    s = Setup(H8, BF, 16, [20], [3], seed=42)
+    c, none = s.cache(), torch.zeros(0, s.hd // 2, 2, device=DEV)
+    qkv, cu, pad = s.qkv.to(DEV), ints(s.cu), s.room - s.total
+    with pytest.raises(ValueError):
+        c.attention(qkv, ints(s.start), cu, q_norm=s.dev(s.gain), rope=none)
+    with pytest.raises(ValueError):
+        c.append(qkv, cu, ints(s.pos + [-1] * pad), ints(s.slots + [-1] * pad, torch.int64), k_norm=s.dev(s.gain), rope=none)
+    torch.cuda.synchronize()
+    assert torch.equal(s.kd.cpu().view(torch.int16), s.k.view(torch.int16))
