@@ -240,7 +240,7 @@ struct dmtd_ctx {
   unsigned long long* amax = nullptr;
   float* gemm_part = nullptr;
   int part_rows = 0;          // rows per sequence the partials are laid out for (stride between ranges: part_rows * query heads per KV head)
-  int test_fail_step = -1;    // tests of the failure path: the next decode call reports a launch failure before this step (once)
+  int test_fail_step = -1;    // tests of the failure path: the next decode call reports a launch failure before this step (once); of paged calls, so many succeed before one fails midway
   char* static_scratch = nullptr;   // this device's copy of the library's own scratch array (address taken at create)
   PagedState paged;                 // requests that come and go
   const PagedPass* paged_pass = nullptr;      // run_layer: the rows are theirs
@@ -2551,6 +2551,8 @@ int dmtd_reset(dmtd_ctx* c) {
     hipLaunchKernelGGL(set_state_kernel, dim3(1), dim3(64), 0, c->stream, (DevState*)(c->ws + c->o.state), 0, 0, c->cfg.max_batch, sample_count(c));
     HIP_TRY(c, hipGetLastError());
     HIP_TRY(c, hipMemsetAsync(c->ws + c->o.state + kStateDeltaOff, 0, 12 * (size_t)c->cfg.max_batch, c->stream));
+    // selection keys: a step that failed behind its LM head has left some, which the next one's would be compared with
+    HIP_TRY(c, hipMemsetAsync(c->ws + c->o.amax, 0, (size_t)AMAX_CELLS * c->cfg.max_batch * 8, c->stream));
     HIP_TRY(c, hipStreamSynchronize(c->stream));
   }
   c->sched.reset();

@@ -129,6 +129,13 @@ hipError_t paged_layers(dmtd_ctx* c, const PagedLayout& w, int which, Rows& R, i
   return e;
 }
 
+// A failure injected from the host (DMTD_TEST_FAIL_STEP at create), midway in a paged call, the way a refused launch would fail it; what was enqueued completes normally
+bool paged_injected(dmtd_ctx* c) {
+  if (c->test_fail_step < 0 || c->test_fail_step-- > 0) return false;
+  c->err = "injected launch failure (DMTD_TEST_FAIL_STEP)";
+  return true;
+}
+
 // The host ran out of memory inside a call: what the device has done of it is not known
 int paged_no_memory(dmtd_ctx* c) {
   c->paged.failed = true;
@@ -275,6 +282,7 @@ int dmtd_paged_step(dmtd_ctx* c, int32_t n, const int32_t* slots, const int32_t*
     HIP_TRY(c, paged_layers(c, w, 0, R, late_rows_n, max_late, F, cf.n_layers));
     HIP_TRY(c, paged_rows(c, n, R.h, dev + w.last, nullptr, false, last, cf.n_layers));
     HIP_TRY(c, head_logits(c, last, n, (float*)(c->ws + c->o.logits), c->amax, cf.max_batch));
+    if (paged_injected(c)) return DMTD_EHIP;
     hipLaunchKernelGGL(paged_pick_kernel, dim3(n), dim3(64), 0, c->stream, c->amax, AMAX_CELLS, cf.max_batch, (int*)(m + w.emitted));
     HIP_TRY(c, hipGetLastError());
     HIP_TRY(c, hipMemcpyAsync(next.data(), m + w.emitted, (size_t)n * 4, hipMemcpyDeviceToHost, c->stream));
@@ -316,6 +324,7 @@ int dmtd_paged_release(dmtd_ctx* c, int32_t slot) try {
     HIP_TRY(c, hipMemcpyAsync(c->paged.mem + w.up + w.start[0] * 4, up.data(), up.size() * 4, hipMemcpyHostToDevice, c->stream));
     const int rc = paged_tables(c, w, 0, 1);
     if (rc != DMTD_OK) return rc;
+    if (paged_injected(c)) return DMTD_EHIP;
     HIP_TRY(c, hipStreamSynchronize(c->stream));
     return DMTD_OK;
   };

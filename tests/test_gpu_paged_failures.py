@@ -1,0 +1,65 @@
+"""Paged steps that fail midway (a launch failure injected from the host, DMTD_TEST_FAIL_STEP; every kernel that was enqueued completes), and what is left behind them."""
+import numpy as np
+import pytest
+
+import dmtd_inputs as di
+import paper_2510_11958_amd as pkg
+from parity_util import engine_config
+from test_gpu_paged_steps import SHAPES
+
+pytestmark = pytest.mark.gpu
+
+
+def failing_engine(cfg, blob, monkeypatch, after):
+    """An engine of whose paged calls `after` succeed before one fails."""
+    monkeypatch.setenv("DMTD_TEST_FAIL_STEP", str(after))
+    eng = pkg.Engine(cfg, blob)
+    monkeypatch.delenv("DMTD_TEST_FAIL_STEP")
+    return eng
+
+
+def fails(code, call):
+    with pytest.raises(pkg.DmtdError) as e:
+        call()
+    assert e.value.code == code
+    return str(e.value)
+
+
+@pytest.mark.parametrize("name", ["fp32", "bf16"])
+@pytest.mark.parametrize("fails_in", ["step", "release"])
+def test_only_a_reset_is_left_and_it_leaves_nothing_behind(name, fails_in, monkeypatch):
+    """A step fails behind its head and in front of its choice.  Behind the reset, paged steps, prefill and decoding are a fresh context's, bit for bit: where the failed
+    step's largest logits are above the next one's, its selection keys must not decide."""
+    sh = SHAPES[name]
+    blob = di.make_weight_blob(sh, seed=7)
+    prompt = di.make_prompts(sh.vocab, 2, 40, seed=8)
+    cfg = engine_config(sh, 128, 2)
+
+    def run(eng):
+        eng.paged_begin(32)
+        out = [eng.paged_step([1, 0], [prompt[0][:30], prompt[1][:9]], [1, 1], 2), eng.logits()]
+        for t in (3, 4, 5):
+            out += [eng.paged_step([0, 1], [[t], [t + 1]], [t == 5, 0], 2), eng.logits()]
+        eng.reset()
+        out += [eng.prefill(prompt), eng.logits(), eng.decode(3, 2, 7), eng.logits()]
+        eng.reset()
+        return out
+
+    want = run(pkg.Engine(cfg, blob))
+    for seed in range(6):
+        eng = failing_engine(cfg, blob, monkeypatch, 1)
+        eng.paged_begin(32)
+        text = di.make_prompts(sh.vocab, 2, 60, seed=90 + seed)
+        eng.paged_step([0, 1], [text[0][:20], text[1]], [1, 1], 2)
+        if fails_in == "step":
+            assert "injected" in fails(pkg.DMTD_EHIP, lambda: eng.paged_step([1, 0], [text[0][20:25], text[0][25:40]], [1, 0], 2))
+        else:
+            assert "injected" in fails(pkg.DMTD_EHIP, lambda: eng.paged_release(0))
+        for _ in range(2):
+            fails(pkg.DMTD_ESTATE, lambda: eng.paged_step([1], [[3]], [1], 2))
+            fails(pkg.DMTD_ESTATE, lambda: eng.paged_release(1))
+            fails(pkg.DMTD_ESTATE, lambda: eng.paged_begin(32))
+            fails(pkg.DMTD_ESTATE, lambda: eng.prefill(prompt))
+        eng.reset()
+        for a, b in zip(want, run(eng)):
+            assert np.array_equal(a, b)
