@@ -2275,6 +2275,7 @@ int dmtd_get_seq_state(const dmtd_ctx* c, int32_t b, int32_t* n_front, int32_t* 
 int dmtd_logits(dmtd_ctx* c, float* out, size_t out_elems) {
   if (!c) return DMTD_EINVAL;
   if (!out) { c->err = "null output pointer"; return DMTD_EINVAL; }
+  if (c->paged.on && c->paged.failed) { c->err = "a paged step failed midway; call dmtd_reset"; return DMTD_ESTATE; }
   const int rows = c->paged.on ? c->paged.last_n : c->sched.n_tok == 0 ? 0 : c->batch;
   if (rows == 0 || c->cfg.dry_run) { c->err = "no logits before prefill"; return DMTD_ESTATE; }
   const size_t need = (size_t)rows * c->cfg.vocab;

@@ -63,3 +63,18 @@ def test_only_a_reset_is_left_and_it_leaves_nothing_behind(name, fails_in, monke
         eng.reset()
         for a, b in zip(want, run(eng)):
             assert np.array_equal(a, b)
+
+
+def test_no_logits_behind_a_failed_step(monkeypatch):
+    """Those of the step before are overwritten, for other requests maybe."""
+    sh = SHAPES["bf16"]
+    eng = failing_engine(engine_config(sh, 64, 2), di.make_weight_blob(sh, seed=7), monkeypatch, 1)
+    eng.paged_begin(16)
+    eng.paged_step([0, 1], [[1, 2, 3], [4]], [1, 1], 2)
+    assert eng.logits().shape == (2, sh.vocab)
+    fails(pkg.DMTD_EHIP, lambda: eng.paged_step([1, 0], [[5], [6]], [0, 1], 2))
+    assert "reset" in fails(pkg.DMTD_ESTATE, eng.logits)
+    eng.reset()
+    fails(pkg.DMTD_ESTATE, eng.logits)
+    eng.prefill(np.array([[1, 2, 3]]))
+    assert eng.logits().shape == (1, sh.vocab)
