@@ -383,7 +383,7 @@ int dmtd_paged_attention(const dmtd_paged_cache* cache, const float* qkv, int64_
  *
  * dmtd_paged_begin: turns an empty context (fresh or reset) over to paged steps; dmtd_reset ends them.  Until then dmtd_prefill*, dmtd_masked_forward and dmtd_read_kv return
  * DMTD_ESTATE, decode calls as before prefill.  memory_dev: DEVICE, 256-byte aligned, dmtd_paged_step_bytes(cfg, page_size) bytes (0: invalid), the caller's and left alone by others until
- * then.  Errors: DMTD_EINVAL, DMTD_ESTATE (not empty, n_early > 0, dry run), DMTD_ECAPACITY (memory too small), DMTD_EHIP. */
+ * then (a step or release that finds its tables changed fails with DMTD_EHIP).  Errors: DMTD_EINVAL, DMTD_ESTATE (not empty, n_early > 0, dry run), DMTD_ECAPACITY (memory too small), DMTD_EHIP. */
 size_t dmtd_paged_step_bytes(const dmtd_config* cfg, int32_t page_size);
 int dmtd_paged_begin(dmtd_ctx* ctx, int32_t page_size, void* memory_dev, size_t memory_bytes);
 

@@ -47,7 +47,8 @@ hipError_t paged_rows(dmtd_ctx* c, int n, const float* src, const int* idx, cons
 // The DEVICE memory of a context's paged steps, in bytes from its start
 struct PagedLayout {
   int page, max_pages, n_pages, rows;
-  size_t table, held, free_pages, n_free, status, up, cu[2], pos[2], slots[2], emitted, attention, attention_bytes, total;
+  static constexpr int kStatus = 4;      // ints at `status`: what the tables of either pass say (paged_tables), which the tokens follow that a step emits
+  size_t table, held, free_pages, n_free, status, up, cu[2], pos[2], slots[2], attention, attention_bytes, total;
   // what a step uploads, in ints from `up`: per slot the lengths of the late layers' rows and of the front layers', tokens of either, the late rows' places
   // among the front rows, the requests' last rows
   size_t start[2], count[2], tokens[2], from, last, up_ints;
@@ -66,7 +67,6 @@ bool paged_layout(const dmtd_config& c, int wide, int page, PagedLayout& w) {
   w.held = take(B * 4);
   w.free_pages = take((size_t)w.n_pages * 4);
   w.n_free = take(4);
-  w.status = take(2 * 2 * 4);
   size_t up = 0;
   auto ints = [&](size_t n) { const size_t o = up; up += n; return o; };
   for (int i = 0; i < 2; ++i) { w.start[i] = ints(B); w.count[i] = ints(B); }
@@ -80,7 +80,7 @@ bool paged_layout(const dmtd_config& c, int wide, int page, PagedLayout& w) {
     w.pos[i] = take((size_t)w.rows * 4);
     w.slots[i] = take((size_t)w.rows * 8);
   }
-  w.emitted = take(B * 4);
+  w.status = take((w.kStatus + B) * 4);
   dmtd_paged_cache pc{};
   pc.n_pages = w.n_pages; pc.page_size = page; pc.n_req = (int)B; pc.max_pages = w.max_pages;
   pc.n_q_heads = c.n_q_heads; pc.n_kv_heads = c.n_kv_heads; pc.head_dim = c.head_dim; pc.dtype = c.dtype; pc.max_rows = w.rows;
@@ -105,6 +105,13 @@ int paged_tables(dmtd_ctx* c, const PagedLayout& w, int which, int rows) {
                                   (int*)(m + w.status) + 2 * which, c->stream);
   if (rc != DMTD_OK) c->err = g_create_error;
   return rc;
+}
+
+// The device's word on the tables of a pass: it refuses what does not fit the pool, and the host has checked that the step does
+int paged_status(dmtd_ctx* c, const int32_t* status) {
+  if (status[0] == 0) return DMTD_OK;
+  c->err = "the pool's tables on the device are not those of the steps so far: their memory was written to";
+  return DMTD_EHIP;
 }
 
 hipError_t paged_layers(dmtd_ctx* c, const PagedLayout& w, int which, Rows& R, int rows, int max_new, int first, int end) {
@@ -251,11 +258,12 @@ int dmtd_paged_step(dmtd_ctx* c, int32_t n, const int32_t* slots, const int32_t*
   const int F = cf.n_layers - n_late;
   const int* dev = (const int*)(m + w.up);
   const bool add = cf.full_pos_add_embed != 0;
-  std::vector<int32_t> next(n);
+  std::vector<int32_t> next(w.kStatus + n);
+  const bool front_tables = front_rows_n > 0 && F > 0 && !same;
   auto run = [&]() -> int {
     HIP_TRY(c, hipMemcpyAsync(m + w.up, up.data(), up.size() * 4, hipMemcpyHostToDevice, c->stream));
     int rc = paged_tables(c, w, 0, late_rows_n);
-    if (rc == DMTD_OK && front_rows_n > 0 && F > 0 && !same) rc = paged_tables(c, w, 1, front_rows_n);
+    if (rc == DMTD_OK && front_tables) rc = paged_tables(c, w, 1, front_rows_n);
     if (rc != DMTD_OK) return rc;
     Rows R = front_rows(c), last = late_rows(c);
     if (F > 0 && front_rows_n > 0) {
@@ -283,11 +291,12 @@ int dmtd_paged_step(dmtd_ctx* c, int32_t n, const int32_t* slots, const int32_t*
     HIP_TRY(c, paged_rows(c, n, R.h, dev + w.last, nullptr, false, last, cf.n_layers));
     HIP_TRY(c, head_logits(c, last, n, (float*)(c->ws + c->o.logits), c->amax, cf.max_batch));
     if (paged_injected(c)) return DMTD_EHIP;
-    hipLaunchKernelGGL(paged_pick_kernel, dim3(n), dim3(64), 0, c->stream, c->amax, AMAX_CELLS, cf.max_batch, (int*)(m + w.emitted));
+    hipLaunchKernelGGL(paged_pick_kernel, dim3(n), dim3(64), 0, c->stream, c->amax, AMAX_CELLS, cf.max_batch, (int*)(m + w.status) + w.kStatus);
     HIP_TRY(c, hipGetLastError());
-    HIP_TRY(c, hipMemcpyAsync(next.data(), m + w.emitted, (size_t)n * 4, hipMemcpyDeviceToHost, c->stream));
+    HIP_TRY(c, hipMemcpyAsync(next.data(), m + w.status, next.size() * 4, hipMemcpyDeviceToHost, c->stream));
     HIP_TRY(c, hipStreamSynchronize(c->stream));
-    return DMTD_OK;
+    if ((rc = paged_status(c, next.data())) == DMTD_OK && front_tables) rc = paged_status(c, next.data() + 2);
+    return rc;
   };
   const int rc = run();
   if (rc != DMTD_OK) { c->paged.failed = true; (void)hipStreamSynchronize(c->stream); return rc; }
@@ -306,7 +315,7 @@ int dmtd_paged_step(dmtd_ctx* c, int32_t n, const int32_t* slots, const int32_t*
   c->paged.free_pages -= take;
   c->paged.n_late = n_late;
   c->paged.last_n = n;
-  if (next_tokens) std::memcpy(next_tokens, next.data(), (size_t)n * 4);
+  if (next_tokens) std::memcpy(next_tokens, next.data() + w.kStatus, (size_t)n * 4);
   return DMTD_OK;
 } catch (const std::bad_alloc&) { return paged_no_memory(c); }
 
@@ -325,8 +334,10 @@ int dmtd_paged_release(dmtd_ctx* c, int32_t slot) try {
     const int rc = paged_tables(c, w, 0, 1);
     if (rc != DMTD_OK) return rc;
     if (paged_injected(c)) return DMTD_EHIP;
+    int32_t status[2] = {-1, -1};
+    HIP_TRY(c, hipMemcpyAsync(status, c->paged.mem + w.status, sizeof(status), hipMemcpyDeviceToHost, c->stream));
     HIP_TRY(c, hipStreamSynchronize(c->stream));
-    return DMTD_OK;
+    return paged_status(c, status);
   };
   const int rc = run();
   if (rc != DMTD_OK) { c->paged.failed = true; (void)hipStreamSynchronize(c->stream); return rc; }

@@ -1,6 +1,7 @@
 """Paged steps that fail midway (a launch failure injected from the host, DMTD_TEST_FAIL_STEP; every kernel that was enqueued completes), and what is left behind them."""
 import numpy as np
 import pytest
+import torch
 
 import dmtd_inputs as di
 import paper_2510_11958_amd as pkg
@@ -78,3 +79,25 @@ def test_no_logits_behind_a_failed_step(monkeypatch):
     fails(pkg.DMTD_ESTATE, eng.logits)
     eng.prefill(np.array([[1, 2, 3]]))
     assert eng.logits().shape == (1, sh.vocab)
+
+
+@pytest.mark.parametrize("name", ["fp32", "bf16"])
+def test_tables_that_others_wrote_to(name):
+    """The device refuses a step, or a release, that does not fit its tables: the call says so instead of returning tokens of rows that saw no keys, and a reset gives the context back."""
+    sh = SHAPES[name]
+    blob = di.make_weight_blob(sh, seed=7)
+    prompt = di.make_prompts(sh.vocab, 1, 40, seed=8)
+    want = pkg.Engine(engine_config(sh, 64, 2), blob)
+    first, logits = want.prefill(prompt), want.logits()
+    for wrong, call in ((0, lambda e: e.paged_step([1], [list(range(1, 18))], [1], 2)), (8, lambda e: e.paged_release(0)), (-1, lambda e: e.paged_step([0, 1], [[1], [2]], [0, 1], 2))):
+        eng = pkg.Engine(engine_config(sh, 64, 2), blob)
+        eng.paged_begin(16)
+        eng.paged_step([0, 1], [prompt[0, :20], prompt[0, 20:]], [1, 1], 2)          # 2 and 2 of the pool's 8 pages
+        n_free = eng._paged_memory.view(dtype=torch.int32)[3 * 64]                    # behind block table, pages held and free pages, each from a multiple of 256 bytes on
+        assert n_free.item() == 4 == eng.paged_state(0)["free_pages"]
+        n_free.fill_(wrong)
+        torch.cuda.synchronize()
+        assert "tables" in fails(pkg.DMTD_EHIP, lambda: call(eng))
+        assert "reset" in fails(pkg.DMTD_ESTATE, lambda: eng.paged_step([0], [[1]], [0], 2))
+        eng.reset()
+        assert np.array_equal(eng.prefill(prompt), first) and np.array_equal(eng.logits(), logits)
