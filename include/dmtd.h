@@ -394,8 +394,9 @@ int dmtd_paged_begin(dmtd_ctx* ctx, int32_t page_size, void* memory_dev, size_t 
  * next_tokens: HOST int32 [n] or NULL: greedy choice behind each request's last new token, whose logits dmtd_logits returns as float32 [n, vocab].
  * A request's results are those of the other calls for the same tokens and cycles (up to the rounding of other sums), whatever the other requests do.
  * Steps run kernel by kernel (use_graphs is ignored); dmtd_get_state and dmtd_get_trace do not follow them.  After DMTD_EHIP only dmtd_reset is left.
- * Errors: DMTD_EINVAL; DMTD_ESTATE (no dmtd_paged_begin; sampling on; n_late changed while tokens await refill); DMTD_ECAPACITY (max_seq_len; more new tokens, or more rows for
- * the front layers, than a pass carries: 2048 for a bf16 model, or as many as its workspace holds, at least 16 max_batch; too few free pages); DMTD_EHIP. */
+ * Errors: DMTD_EINVAL; DMTD_ESTATE (no dmtd_paged_begin; sampling on; n_late changed while tokens await refill); DMTD_ECAPACITY (max_seq_len; more new tokens than a pass
+ * carries: 2048 for a bf16 model, or as many as its workspace holds, 128 for an fp32 model, at least 16 max_batch; too few free pages); DMTD_EHIP.  Rows that the front layers
+ * take beyond that, of requests with many tokens that await their refill, go through them in several passes. */
 int dmtd_paged_step(dmtd_ctx* ctx, int32_t n, const int32_t* slots, const int32_t* counts, const int32_t* tokens, const uint8_t* full, int32_t n_late,
                     int32_t* next_tokens);
 

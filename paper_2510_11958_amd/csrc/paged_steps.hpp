@@ -143,6 +143,14 @@ bool paged_injected(dmtd_ctx* c) {
   return true;
 }
 
+// A pass of a step's front layers: per slot where its rows start and their number, the rows' tokens, which of them are new, the most of one slot
+struct PagedFront {
+  struct Run { int first, n; };
+  std::vector<int32_t> lengths, tokens;
+  std::vector<Run> kept;
+  int max_new = 0;
+};
+
 // The host ran out of memory inside a call: what the device has done of it is not known
 int paged_no_memory(dmtd_ctx* c) {
   c->paged.failed = true;
@@ -206,7 +214,7 @@ int dmtd_paged_step(dmtd_ctx* c, int32_t n, const int32_t* slots, const int32_t*
   std::vector<int> request(cf.max_batch, -1);          // of a slot
   std::vector<size_t> first_token(n);
   size_t n_tokens = 0;
-  int late_rows_n = 0, front_rows_n = 0, take = 0;
+  int late_rows_n = 0, take = 0;
   for (int j = 0; j < n; ++j) {
     if (slots[j] < 0 || slots[j] >= cf.max_batch) { c->err = "slot outside [0, max_batch)"; return DMTD_EINVAL; }
     if (request[slots[j]] >= 0) { c->err = "a slot is named twice"; return DMTD_EINVAL; }
@@ -216,11 +224,6 @@ int dmtd_paged_step(dmtd_ctx* c, int32_t n, const int32_t* slots, const int32_t*
     if (counts[j] > cf.max_seq_len - q.n_tok) { c->err = "a request would exceed max_seq_len"; return DMTD_ECAPACITY; }
     if (counts[j] > w.rows - late_rows_n) { c->err = "more rows than a pass carries"; return DMTD_ECAPACITY; }
     late_rows_n += counts[j];
-    if (full[j]) {
-      const int rows = (int)q.pending.size() + counts[j];
-      if (rows > w.rows - front_rows_n) { c->err = "more rows than a pass carries"; return DMTD_ECAPACITY; }
-      front_rows_n += rows;
-    }
     first_token[j] = n_tokens;
     for (int i = 0; i < counts[j]; ++i, ++n_tokens)
       if (tokens[n_tokens] < 0 || tokens[n_tokens] >= cf.vocab) { c->err = "token id outside the vocabulary"; return DMTD_EINVAL; }
@@ -230,55 +233,97 @@ int dmtd_paged_step(dmtd_ctx* c, int32_t n, const int32_t* slots, const int32_t*
   if (c->paged.n_late != 0 && c->paged.n_late != n_late)
     for (const PagedState::Seq& q : seqs)
       if (!q.pending.empty()) { c->err = "n_late changed while tokens await refill"; return DMTD_ESTATE; }
-  // the rows in the order of the slots
+  // The rows in the order of the slots.  The front layers' rows may take several passes: a request that the last pass does not hold whole begins one, and fills several where no pass holds it; behind its
+  // last part others follow.  Lengths say what pages a request holds, so the first of several parts gives back those of the later ones; nobody else takes or gives any until these, pass by
+  // pass, have taken them off the stack again, in their order.
+  const int F = cf.n_layers - n_late;
   std::vector<int32_t> up(w.up_ints, 0);
-  int late_at = 0, front_at = 0, max_late = 0, max_front = 0;
-  bool same = true;                    // the front layers' rows are the late layers'
+  std::vector<PagedFront> fronts;
+  auto new_front = [&]() {
+    fronts.emplace_back();
+    PagedFront& f = fronts.back();
+    f.lengths.resize(w.count[1] + cf.max_batch - w.start[1], 0);
+    for (int s = 0; s < cf.max_batch; ++s) f.lengths[s] = seqs[s].n_tok + (request[s] >= 0 ? counts[request[s]] : 0);       // (no rows: it keeps its pages)
+  };
+  std::vector<int32_t> from;           // where several passes leave their results at the new tokens: behind one another
+  int late_at = 0, kept_at = 0, max_late = 0;
+  bool same = true, any_full = false;                    // the front layers' rows are the late layers'
   for (int s = 0; s < cf.max_batch; ++s) {
     const PagedState::Seq& q = seqs[s];
     const int j = request[s], count = j >= 0 ? counts[j] : 0, rows = j >= 0 && full[j] ? (int)q.pending.size() + count : 0;
     up[w.start[0] + s] = q.n_tok;
     up[w.count[0] + s] = count;
-    up[w.start[1] + s] = rows ? q.n_front : q.n_tok + count;       // (no rows: it keeps its pages)
-    up[w.count[1] + s] = rows;
     same = same && rows == count;
-    if (rows)
-      for (int p : q.pending) up[w.tokens[1] + front_at++] = p;
+    any_full = any_full || rows;
+    if (F > 0)
+      for (int at = 0; at < rows;) {
+        if (fronts.empty() || (int)fronts.back().tokens.size() + (at ? 0 : std::min(rows, w.rows)) > w.rows) new_front();
+        PagedFront& f = fronts.back();
+        const int n_rows = std::min(rows - at, w.rows), pending = (int)q.pending.size();
+        f.lengths[s] = q.n_front + at;
+        f.lengths[w.count[1] - w.start[1] + s] = n_rows;
+        f.max_new = std::max(f.max_new, n_rows);
+        const int fresh = std::max(at, pending);
+        if (at + n_rows > fresh) f.kept.push_back({(int)f.tokens.size() + fresh - at, at + n_rows - fresh});
+        for (int i = at; i < at + n_rows; ++i) f.tokens.push_back(i < pending ? q.pending[i] : tokens[first_token[j] + i - pending]);
+        at += n_rows;
+        if (at < rows) new_front();
+      }
+    const int new_at = rows && F > 0 ? (int)fronts.back().tokens.size() - count : 0;      // in one pass: all rows are kept
     for (int i = 0; i < count; ++i) {
-      const int t = tokens[first_token[j] + i];
-      up[w.from + late_at] = rows ? front_at : -1;
-      up[w.tokens[0] + late_at++] = t;
-      if (rows) up[w.tokens[1] + front_at++] = t;
+      from.push_back(rows ? kept_at++ : -1);
+      up[w.from + late_at] = rows ? new_at + i : -1;
+      up[w.tokens[0] + late_at++] = tokens[first_token[j] + i];
     }
     if (j >= 0) up[w.last + j] = late_at - 1;
     max_late = std::max(max_late, count);
-    max_front = std::max(max_front, rows);
+  }
+  if (fronts.size() > 1) {
+    std::copy(from.begin(), from.end(), up.begin() + w.from);
+  } else if (!fronts.empty()) {
+    std::copy(fronts[0].lengths.begin(), fronts[0].lengths.end(), up.begin() + w.start[1]);
+    std::copy(fronts[0].tokens.begin(), fronts[0].tokens.end(), up.begin() + w.tokens[1]);
   }
   char* m = c->paged.mem;
-  const int F = cf.n_layers - n_late;
   const int* dev = (const int*)(m + w.up);
   const bool add = cf.full_pos_add_embed != 0;
   std::vector<int32_t> next(w.kStatus + n);
-  const bool front_tables = front_rows_n > 0 && F > 0 && !same;
+  const bool front_tables = !fronts.empty() && !same;
   auto run = [&]() -> int {
     HIP_TRY(c, hipMemcpyAsync(m + w.up, up.data(), up.size() * 4, hipMemcpyHostToDevice, c->stream));
     int rc = paged_tables(c, w, 0, late_rows_n);
-    if (rc == DMTD_OK && front_tables) rc = paged_tables(c, w, 1, front_rows_n);
     if (rc != DMTD_OK) return rc;
     Rows R = front_rows(c), last = late_rows(c);
-    if (F > 0 && front_rows_n > 0) {
-      HIP_TRY(c, paged_rows(c, front_rows_n, nullptr, nullptr, dev + w.tokens[1], false, R, 0));
-      HIP_TRY(c, paged_layers(c, w, same ? 0 : 1, R, front_rows_n, max_front, 0, F));
-      if (!same || add) {
-        float* kept = (float*)(c->ws + c->o.enc_tmp);
-        HIP_TRY(c, hipMemcpyAsync(kept, R.h, (size_t)front_rows_n * cf.hidden * 4, hipMemcpyDeviceToDevice, c->stream));
-        HIP_TRY(c, paged_rows(c, late_rows_n, kept, dev + w.from, dev + w.tokens[0], add, R, F));
+    float* kept = (float*)(c->ws + c->o.enc_tmp);        // the front layers' results at the new tokens
+    size_t n_kept = 0;
+    for (const PagedFront& f : fronts) {
+      const int rows = (int)f.tokens.size();
+      if (fronts.size() > 1) {
+        HIP_TRY(c, hipMemcpyAsync(m + w.up + w.start[1] * 4, f.lengths.data(), f.lengths.size() * 4, hipMemcpyHostToDevice, c->stream));
+        HIP_TRY(c, hipMemcpyAsync(m + w.up + w.tokens[1] * 4, f.tokens.data(), f.tokens.size() * 4, hipMemcpyHostToDevice, c->stream));
       }
+      if (front_tables && (rc = paged_tables(c, w, 1, rows)) != DMTD_OK) return rc;
+      HIP_TRY(c, paged_rows(c, rows, nullptr, nullptr, dev + w.tokens[1], false, R, 0));
+      HIP_TRY(c, paged_layers(c, w, same ? 0 : 1, R, rows, f.max_new, 0, F));
+      if (fronts.size() == 1) {
+        if (!same || add) HIP_TRY(c, hipMemcpyAsync(kept, R.h, (size_t)rows * cf.hidden * 4, hipMemcpyDeviceToDevice, c->stream));
+        continue;
+      }
+      for (const auto& k : f.kept) {
+        HIP_TRY(c, hipMemcpyAsync(kept + n_kept * cf.hidden, R.h + (size_t)k.first * cf.hidden, (size_t)k.n * cf.hidden * 4, hipMemcpyDeviceToDevice, c->stream));
+        n_kept += k.n;
+      }
+      int32_t status[2] = {-1, -1};                      // before the next pass's
+      HIP_TRY(c, hipMemcpyAsync(status, (int*)(m + w.status) + 2, sizeof(status), hipMemcpyDeviceToHost, c->stream));
+      HIP_TRY(c, hipStreamSynchronize(c->stream));
+      if ((rc = paged_status(c, status)) != DMTD_OK) return rc;
+    }
+    if (!fronts.empty()) {
+      if (!same || add) HIP_TRY(c, paged_rows(c, late_rows_n, kept, dev + w.from, dev + w.tokens[0], add, R, F));
     } else {
       HIP_TRY(c, paged_rows(c, late_rows_n, nullptr, nullptr, dev + w.tokens[0], false, R, F));
       // no front layers: the literal reading adds the embedding once more at full positions
-      if (add && F == 0 && front_rows_n > 0) {
-        float* kept = (float*)(c->ws + c->o.enc_tmp);
+      if (add && any_full) {
         HIP_TRY(c, hipMemcpyAsync(kept, R.h, (size_t)late_rows_n * cf.hidden * 4, hipMemcpyDeviceToDevice, c->stream));
         std::vector<int32_t> twice(late_rows_n);
         for (int i = 0; i < late_rows_n; ++i) twice[i] = up[w.from + i] >= 0 ? i : -1;
