@@ -65,10 +65,6 @@ struct PagedWork {
 // the range's number of n of its group; where partial results and the count lie (in slots of all KV heads)
 struct PagedItem { int req, first, row0, r, pos0, kb, ke, split, n, slot, group; };
 
-// Item y of the launch that takes requests with lo < rows x GQ <= hi in groups of rpb rows.  All ranges have kps keys: with T = sum of groups x
-// keys over the requests, kps >= T / 2^shift, so there are at most 2^shift + groups items; those of groups with several ranges (keys > kps, hence ceil(keys / kps) < 2
-// keys / kps) are fewer than 2^(shift + 1), and such groups fewer than 2^shift: what the workspace holds.  Called by whole blocks.  GROUP: y counts the
-// groups with several ranges instead (split and range of the result mean nothing).
 // The tall kernel's order of n items per KV head.  A chunk's later groups see more keys.  Up to PAGED_RESIDENT_TALL blocks are all resident from the start, two
 // on a CU: the first round of the CUs goes from the longest down, the second from the shortest up, and a CU's two come to about the same.
 // More blocks than that start as others end, longest first.
@@ -80,6 +76,10 @@ struct PagedShare { int groups, splits; };
 __device__ __forceinline__ int paged_groups(const PagedReq& q, int GQ, int lo, int hi, int rpb) {
   return q.n > 0 && q.n * GQ > lo && q.n * GQ <= hi ? (q.n + rpb - 1) / rpb : 0;
 }
+// Item y of the launch that takes requests with lo < rows x GQ <= hi in groups of rpb rows.  All ranges have kps keys: with T = sum of groups x
+// keys over the requests, kps >= T / 2^shift, so there are at most 2^shift + groups items; those of groups with several ranges (keys > kps, hence ceil(keys / kps) < 2
+// keys / kps) are fewer than 2^(shift + 1), and such groups fewer than 2^shift: what the workspace holds.  Called by whole blocks.  GROUP: y counts the
+// groups with several ranges instead (split and range of the result mean nothing).
 template <int NT, int STEP, bool GROUP, bool TALL = false>
 __device__ __forceinline__ bool paged_find(const PagedView& pv, const int* cu, const int* start, int max_new, int GQ, int lo, int hi, int rpb, int shift, int min_keys,
                                            int y, PagedItem& it) {
@@ -422,9 +422,9 @@ __device__ __forceinline__ void paged_attention_few(int y, const int* __restrict
         for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_16x16x4f32(k4[e], q4[e], s, 0, 0, 0);
         continue;
       } else {
-      const bf16x8_t ql = __builtin_bit_cast(bf16x8_t, *(const u32x4*)&qlo_s[sl][32 * t + 8 * kq]), qh = __builtin_bit_cast(bf16x8_t, *(const u32x4*)&qhi_s[sl][32 * t + 8 * kq]);
-      s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, ka[t]), ql, s, 0, 0, 0);
-      s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, ka[t]), qh, s, 0, 0, 0);
+        const bf16x8_t ql = __builtin_bit_cast(bf16x8_t, *(const u32x4*)&qlo_s[sl][32 * t + 8 * kq]), qh = __builtin_bit_cast(bf16x8_t, *(const u32x4*)&qhi_s[sl][32 * t + 8 * kq]);
+        s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, ka[t]), ql, s, 0, 0, 0);
+        s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, ka[t]), qh, s, 0, 0, 0);
       }
     }
     float sc[4] = {s.x, s.y, s.z, s.w};
@@ -471,24 +471,24 @@ __device__ __forceinline__ void paged_attention_few(int y, const int* __restrict
 #pragma unroll
         for (int m = 0; m < 4; ++m) acc[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(p[m], __uint_as_float(va[m][e]), acc[e], 0, 0, 0);
     } else {
-    uint2 pp[PARTS];
-    if constexpr (PARTS == 3) {
-      paged_split3(p[0], p[1], pp[0].x, pp[1].x, pp[2].x);
-      paged_split3(p[2], p[3], pp[0].y, pp[1].y, pp[2].y);
-    } else {
-      pp[0].x = pack_bf16x2(p[0], p[1]);
-      pp[0].y = pack_bf16x2(p[2], p[3]);
-      pp[1].x = pack_bf16x2(p[0] - __uint_as_float(pp[0].x << 16), p[1] - __uint_as_float(pp[0].x & 0xFFFF0000u));
-      pp[1].y = pack_bf16x2(p[2] - __uint_as_float(pp[0].y << 16), p[3] - __uint_as_float(pp[0].y & 0xFFFF0000u));
-    }
+      uint2 pp[PARTS];
+      if constexpr (PARTS == 3) {
+        paged_split3(p[0], p[1], pp[0].x, pp[1].x, pp[2].x);
+        paged_split3(p[2], p[3], pp[0].y, pp[1].y, pp[2].y);
+      } else {
+        pp[0].x = pack_bf16x2(p[0], p[1]);
+        pp[0].y = pack_bf16x2(p[2], p[3]);
+        pp[1].x = pack_bf16x2(p[0] - __uint_as_float(pp[0].x << 16), p[1] - __uint_as_float(pp[0].x & 0xFFFF0000u));
+        pp[1].y = pack_bf16x2(p[2] - __uint_as_float(pp[0].y << 16), p[3] - __uint_as_float(pp[0].y & 0xFFFF0000u));
+      }
 #pragma unroll
-    for (int e = 0; e < DPL; ++e) {
-      const unsigned int sel = (e & 1) ? 0x07060302u : 0x05040100u;
-      const uint2 v4 = make_uint2(__builtin_amdgcn_perm(va[1][e >> 1], va[0][e >> 1], sel), __builtin_amdgcn_perm(va[3][e >> 1], va[2][e >> 1], sel));
+      for (int e = 0; e < DPL; ++e) {
+        const unsigned int sel = (e & 1) ? 0x07060302u : 0x05040100u;
+        const uint2 v4 = make_uint2(__builtin_amdgcn_perm(va[1][e >> 1], va[0][e >> 1], sel), __builtin_amdgcn_perm(va[3][e >> 1], va[2][e >> 1], sel));
 #pragma unroll
-      for (int z = PARTS - 1; z >= 0; --z)
-        acc[e] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(bf16x4s_t, pp[z]), __builtin_bit_cast(bf16x4s_t, v4), acc[e], 0, 0, 0);
-    }
+        for (int z = PARTS - 1; z >= 0; --z)
+          acc[e] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(bf16x4s_t, pp[z]), __builtin_bit_cast(bf16x4s_t, v4), acc[e], 0, 0, 0);
+      }
     }
   }
   // the waves' results of a vector, 4 consecutive dims a thread

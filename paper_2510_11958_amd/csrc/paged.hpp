@@ -47,10 +47,6 @@ __device__ __forceinline__ T block_scan(T v, T* wave_sums /* LDS, NT / 64 */, T&
     const T u = __shfl_up(incl, o, 64);
     if (lane >= o) incl += u;
   }
-  if (NT == 64) {
-    total = __shfl(incl, 63, 64);
-    return incl - v;
-  }
   __syncthreads();                  // the sums of an earlier call have been read
   if (lane == 63) wave_sums[wave] = incl;
   __syncthreads();
