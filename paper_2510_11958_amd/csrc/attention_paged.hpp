@@ -29,16 +29,16 @@ __device__ __forceinline__ void paged_split3(float a, float b, uint32_t& h, uint
 }
 
 // Blocks that the key ranges are chosen for.  bf16, few rows: one of four waves on each CU reads as fast as more do, and shorter ranges cost more joins (us, 32/8 heads of 128,
-// 256 / 512 / 1024 blocks: 3 rows of 8 requests behind 16384 86 / 95 / 107, one row behind 16384 20 / 23 / 28, 4 rows of 32 behind 1024 26 / 35 / 35).  fp32, whose
-// products weigh more: 512 (16/8 heads, 200 rows behind 1000 55 / 41 / 46).  Tall: half of the blocks that the chip holds (64 rows behind 4096 29, with 512 46).
+// 256 / 512 / 1024 blocks: 3 rows of 8 requests behind 16384 84 / 85 / 95, one row behind 16384 19 / 22 / 27, 4 rows of 32 behind 1024 27 / 31 / 36).  fp32, whose
+// products weigh more: 512 (16/8 heads, 200 rows behind 1000 55 / 40 / 44).  Tall: half of the blocks that the chip holds (64 rows behind 4096 27, with 512 33).
 constexpr int PAGED_SLOTS_FEW = 256, PAGED_SLOTS_FP32 = 512, PAGED_SLOTS_TALL = 256;
 constexpr int PAGED_RESIDENT_TALL = 512;                           // blocks of the tall kernel that the chip holds
 constexpr int PAGED_WAVES = 4;                                     // waves of a block of the few-rows kernel
-// Query vectors per KV head of a request that the few-rows kernel takes, which reads its keys once per 16 of them (us, few / tall: 64 vectors behind 4096 18 / 24, of 16
-// requests behind 2000 43 / 51; 128 vectors 22 / 26 and 78 / 57).
+// Query vectors per KV head of a request that the few-rows kernel takes, which reads its keys once per 16 of them (us, few / tall: 64 vectors behind 4096 17 / 21, of 16
+// requests behind 2000 49 / 49; 128 vectors 22 / 23 and 88 / 55).
 constexpr int PAGED_FEW = 64;
-// Shortest key ranges (few, us at 64 / 128 / 256: one row behind 100 8.2 / 6.6 / 6.6, behind 1024 10.6 / 9.7 / 10.9; tall, at 256 / 512 / 1024: a chunk of 330 rows beside
-// single tokens, 14/2 heads of 64, 33 / 35 / 45)
+// Shortest key ranges (few, us at 64 / 128 / 256: one row behind 100 8.2 / 6.7 / 6.7, behind 1024 10.2 / 9.2 / 10.3; tall, at 256 / 512 / 1024: a chunk of 316 rows beside
+// 14 single tokens, 14/2 heads of 64, 22 / 24 / 34, 64 rows behind 4096 27 / 30 / 43)
 constexpr int PAGED_KEYS_FEW = 128, PAGED_KEYS_TALL = 256;
 
 // Rows of a request as the kernels read them: none where the lengths do not fit the buffers or the tables.  `descends` is set where cu does not ascend from 0 on: as
@@ -296,8 +296,8 @@ __device__ __forceinline__ void paged_store4(const PagedOut& o, int row, int col
 //            lanes; a probability goes in as PAGED_PARTS bf16 parts.
 // fp32 caches: 16x16x4 for both, the queries and probabilities as they are, any number of rows (a chunk's groups of 16 vectors find the keys in the L2).
 // Values are loaded past the L2, keys through it: a key's 256 bytes take four loads, which share cache lines (us, both through the caches / values past
-// them / both: 3 rows of 8 requests behind 16384 103 / 86 / 92, 31 ragged rows in pages of 16 tokens 24 / 26 / 30, out of cold memory 30 / 28 / 31, one row of 64
-// behind 1024 out of cold memory 53 / 49 / 48).
+// them / both: 3 rows of 8 requests behind 16384 102 / 84 / 91, 31 ragged rows in pages of 16 tokens 23 / 25 / 30, out of cold memory 29 / 28 / 30, one row of 64
+// behind 1024 out of cold memory 54 / 49 / 48).
 // Bound by the memory: 8 KiB per wave and group against PAGED_PARTS x HD / 16 + 2 x HD / 32 products.
 template <typename CT, int HD, bool PLANES>
 __device__ __forceinline__ void paged_attention_few(int y, const int* __restrict__ cu, const int* __restrict__ start, const float* __restrict__ qkv, long ld,
@@ -880,8 +880,8 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, sizeof(CT) == 2 ? 4 : 2) pag
   paged_attention_few<CT, HD, PLANES>(paged_block(), cu, start, qkv, ld, q_gain, rope_tab, eps, max_new, hi, po, pv, wk);
 }
 
-// Both kinds of requests in one launch, the longer blocks first: a chunk's leave the memory to the single tokens' (330 rows of a chunk and 15 tokens, 14/2 heads of 64, us: one launch
-// after the other 28, together 17; with no single token in the batch their launch took 4.8)
+// Both kinds of requests in one launch, the longer blocks first: a chunk's leave the memory to the single tokens' (316 rows of a chunk and 14 tokens, 14/2 heads of 64: 17.5 us; when
+// both ways stood side by side one launch after the other took 28, and where no single token was in the batch their launch 4.8)
 template <int HD, bool PLANES>
 __global__ void __launch_bounds__(256, 2) paged_attention_both_mfma_kernel(const int* __restrict__ cu, const int* __restrict__ start, const float* __restrict__ qkv, long ld,
                                                                            const bf16_t* __restrict__ q_gain, const float2* __restrict__ rope_tab, float eps, int max_new, int border,
@@ -893,7 +893,7 @@ __global__ void __launch_bounds__(256, 2) paged_attention_both_mfma_kernel(const
 }
 
 // The ranges of the tall kernel's groups joined: 64 KiB of partial results a group and range are too much for the block that ends last (64 rows behind
-// 4096, 32/8 heads: 87 us by it, 41 with this launch).
+// 4096, 32/8 heads: 87 us by it against 41 with this launch when both were tried, 27 since; the launch is 4.8 of them, with nothing to join too).
 template <int HD, bool PLANES>
 __global__ void __launch_bounds__(256) paged_attention_merge_kernel(const int* __restrict__ cu, const int* __restrict__ start, int max_new, int lo, PagedOut po, PagedView pv,
                                                                     PagedWork wk) {
