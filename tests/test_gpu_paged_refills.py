@@ -26,9 +26,10 @@ class Requests:
         self.eng.paged_begin(page)
 
     def step(self, work, full):
-        """work: (slot, new tokens); full: of all of them.  A first step is a prompt's."""
+        """work: (slot, new tokens); full: of all of them, or the slots of which.  A first step is a prompt's."""
+        fulls = [bool(full) if isinstance(full, bool) else s in full for s, _ in work]
         toks = [self.text[s][self.at[s]:self.at[s] + n] for s, n in work]
-        self.eng.paged_step([s for s, _ in work], toks, [int(full)] * len(work), self.n_late)
+        self.eng.paged_step([s for s, _ in work], toks, [int(f) for f in fulls], self.n_late)
         z = self.eng.logits()
         for j, (s, n) in enumerate(work):
             o = self.orcs[s]
@@ -36,8 +37,8 @@ class Requests:
                 o.prefill(toks[j], self.n_late)
             else:
                 for i, t in enumerate(toks[j]):          # tau 1: a full step; a cycle without end: a late-only one
-                    o.decode_cycle(1 if full else 1 << 20, self.n_late, max_new=1, forced=[int(t)])
-                    assert not full or n == 1
+                    o.decode_cycle(1 if fulls[j] else 1 << 20, self.n_late, max_new=1, forced=[int(t)])
+                    assert not fulls[j] or n == 1
             self.at[s] += n
             self.worst = max(self.worst, norm_err(z[j], o.last_logits.astype(np.float64)))
             state = self.eng.paged_state(s)
@@ -87,3 +88,21 @@ def test_a_refill_of_one_long_request(literal):
     r.step([(0, 1), (1, 1)], True)
     r.step([(0, 1), (1, 1)], False)
     r.step([(1, 1), (0, 1)], True)
+
+
+@pytest.mark.parametrize("literal", [False, True])
+@pytest.mark.parametrize("name", ["fp32", "bf16"])
+def test_refills_beside_late_only_rows(name, literal):
+    """Late-only rows of some requests, in front of, between and behind those whose refills take several passes; n_late = all layers: none take any."""
+    room, most = (400, 100) if name == "fp32" else (700, 600)          # a pass: 128 rows, 2048
+    for n_late in (2, SHAPES[name].n_layers):
+        r = Requests(name, [room] * 6, 16, n_late, literal)
+        r.step([(s, 5 + s) for s in range(6)], True)
+        for s in range(6):
+            r.step([(s, most)], False)
+        if name == "fp32":
+            r.step([(1, 90)], False)
+        r.step([(0, 2), (1, 1), (2, 3), (3, 1), (4, 1), (5, 4)], {1, 3, 4})
+        r.step([(5, 1), (4, 1), (2, 1), (0, 1)], {5, 0, 2})
+        r.step([(s, 1) for s in range(6)], False)
+        r.step([(s, 1) for s in range(6)], True)
