@@ -53,6 +53,7 @@ extern "C" {
 
 #define DMTD_DTYPE_F32   0
 #define DMTD_DTYPE_BF16  1
+#define DMTD_DTYPE_E4M3  3   /* of dmtd_paged_cache only: 8-bit codes with a power of two per row */
 
 typedef struct dmtd_ctx dmtd_ctx;   /* opaque host object owned by the library */
 
@@ -344,12 +345,18 @@ typedef struct dmtd_paged_cache {
   const int32_t* block_table;
   int32_t  n_pages, page_size, n_req, max_pages;
   int32_t  n_q_heads;      /* a multiple of n_kv_heads, at most 16 times as many */
-  int32_t  n_kv_heads, head_dim /* 64 or 128 */, dtype /* DMTD_DTYPE_* of k, v, gains and output */;
+  int32_t  n_kv_heads, head_dim /* 64 or 128 */, dtype /* DMTD_DTYPE_* of k, v, gains and output; DMTD_DTYPE_E4M3: of k and v, gains and output are bf16 */;
   int32_t  max_rows;       /* rows there is room for, at most 2^24; times n_kv_heads at most 2^27 */
+  /* DMTD_DTYPE_E4M3 only (not read otherwise): k and v hold e4m3 codes (page_stride a multiple of 16), and each head_dim of them a power of two, here as its biased
+   * exponent e: a value is code * 2^(e - 127), which is a bf16 value (e = 255: NaN). */
+  uint8_t* k_scale;        /* DEVICE [n_pages][n_kv_heads][page_size], 16-byte aligned */
+  uint8_t* v_scale;        /* DEVICE, as k_scale */
+  int64_t  scale_stride;   /* bytes from one page's scales to the next's, a multiple of 16; 0: pages follow each other */
 } dmtd_paged_cache;
 
 /* The new tokens' keys and values into their places: a head's key is normalised (RMS norm with gain k_norm, DEVICE [head_dim] of dtype; NULL: not),
- * rotated by the angles of its position, and rounded to dtype; values are rounded as they are.
+ * rotated by the angles of its position, and rounded to dtype; values are rounded as they are.  DMTD_DTYPE_E4M3: a row of head_dim values gets the least
+ * power of two s >= 2^-111 with max |x| <= 448 s, and the codes of x / s, rounded to nearest even; values that are not finite have no say in s and become NaN.
  * qkv: DEVICE float32 [max_rows, ld], the fused projection's rows: n_q_heads query heads, then n_kv_heads keys, then n_kv_heads values, of head_dim
  * each; 16-byte aligned, ld a multiple of 4.  cu_rows, row_pos, slots: of dmtd_page_tables (of cu_rows only the last entry is read).
  * rope: DEVICE float32 [rope_len][head_dim / 2][2], (cos, sin) of the pair (i, i + head_dim / 2) at each position; NULL: no rotation.
@@ -358,12 +365,18 @@ typedef struct dmtd_paged_cache {
 int dmtd_paged_append(const dmtd_paged_cache* cache, const float* qkv, int64_t ld, const int32_t* cu_rows, const int32_t* row_pos, const int64_t* slots,
                       const void* k_norm, float eps, const float* rope, int32_t rope_len, void* stream);
 
+/* Keys and values out of given places: rows t = 0 .. n - 1 of k_out and v_out, DEVICE [n, ldo] of dtype (DMTD_DTYPE_E4M3: of bf16, the values that the codes stand for, without
+ * rounding), n_kv_heads heads of head_dim, 16-byte aligned, ldo a multiple of 8, are what lies in place slots[t] (DEVICE int64 [n], as dmtd_page_tables numbers them, in any order, the same one
+ * any number of times).  Rows whose place is outside the pool stay as they were.  n: HOST; 0: nothing is done.  block_table and max_rows are not used.
+ * Errors: DMTD_EINVAL, DMTD_EHIP. */
+int dmtd_paged_read(const dmtd_paged_cache* cache, const int64_t* slots, int32_t n, void* k_out, void* v_out, int64_t ldo, void* stream);
+
 /* Bytes of DEVICE workspace dmtd_paged_attention needs; 0 if the cache is invalid (its pointers are checked too). */
 size_t dmtd_paged_workspace_bytes(const dmtd_paged_cache* cache);
 
 /* Attention of a step's rows over their requests' pages: out[t, h] = sum_j p_j v_j with p = softmax(q_t,h . k_j / sqrt(head_dim)) over the keys
  * j = 0 .. position of row t of its request, whose own key is in the cache already; queries are normalised (q_norm, eps) and rotated (rope) as the keys
- * were by dmtd_paged_append.  Softmax and sums in float32; products of bf16 caches on the matrix cores, queries and probabilities as two bf16 parts each.
+ * were by dmtd_paged_append.  Softmax and sums in float32; products of bf16 and e4m3 caches on the matrix cores, queries and probabilities as two bf16 parts each.
  * qkv: as above; only its query heads are read (ld >= n_q_heads * head_dim).  start: DEVICE int32 [n_req].  cu_rows: DEVICE int32 [n_req + 1], ascending from 0 on.
  * max_new: HOST, the most rows that one request brings (0: max_rows): a launch of many rows per request is left out where none has them.
  * out: DEVICE [max_rows, ldo] of dtype, n_q_heads heads of head_dim; 16-byte aligned, ldo a multiple of 8.

@@ -34,7 +34,8 @@ class _PagePool(C.Structure):
 
 class _PagedCache(C.Structure):
     _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("page_stride", C.c_int64), ("block_table", C.c_void_p)] + [
-        (n, C.c_int32) for n in ("n_pages", "page_size", "n_req", "max_pages", "n_q_heads", "n_kv_heads", "head_dim", "dtype", "max_rows")]
+        (n, C.c_int32) for n in ("n_pages", "page_size", "n_req", "max_pages", "n_q_heads", "n_kv_heads", "head_dim", "dtype", "max_rows")] + [
+        ("k_scale", C.c_void_p), ("v_scale", C.c_void_p), ("scale_stride", C.c_int64)]
 
 
 class DmtdError(RuntimeError):
@@ -121,6 +122,8 @@ def load_library():
     lib.dmtd_paged_append.restype = C.c_int
     lib.dmtd_paged_append.argtypes = [P(_PagedCache), C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_float,
                                       C.c_void_p, C.c_int32, C.c_void_p]
+    lib.dmtd_paged_read.restype = C.c_int
+    lib.dmtd_paged_read.argtypes = [P(_PagedCache), C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p]
     lib.dmtd_paged_workspace_bytes.restype = C.c_size_t
     lib.dmtd_paged_workspace_bytes.argtypes = [P(_PagedCache)]
     lib.dmtd_paged_attention.restype = C.c_int
@@ -510,16 +513,18 @@ class PageTables(_OnDevice):
 
 
 class PagedCache(_OnDevice):
-    """One layer's keys and values in pages, ``k`` and ``v`` ``[n_pages, n_kv_heads, page_size, head_dim]`` (bfloat16 or float32; pages may lie apart,
+    """One layer's keys and values in pages, ``k`` and ``v`` ``[n_pages, n_kv_heads, page_size, head_dim]`` (bfloat16, float32 or float8_e4m3fn; pages may lie apart,
     a page itself is contiguous), read and filled through ``block_table`` int32 ``[n_req, max_pages]`` (``dmtd_paged_append``, ``dmtd_paged_attention``) on
-    torch's current stream.  Steps have up to ``max_rows`` rows.  The handle holds the attention's workspace: calls of one handle, and of those that
+    torch's current stream.  Steps have up to ``max_rows`` rows.  8-bit caches come with ``k_scale`` and ``v_scale``, uint8 ``[n_pages, n_kv_heads, page_size]``: a value is its code
+    times ``2 ** (scale - 127)``; norms' gains, outputs and what :meth:`read` returns are then bfloat16.  The handle holds the attention's workspace: calls of one handle, and of those that
     :meth:`layer` made from it, must not overlap."""
 
-    def __init__(self, k, v, block_table, n_q_heads: int, max_rows: int, _workspace_of=None):
+    def __init__(self, k, v, block_table, n_q_heads: int, max_rows: int, k_scale=None, v_scale=None, _workspace_of=None):
         self._open(k)
         torch, dev = self._torch, self._index
-        if k.dtype not in (torch.bfloat16, torch.float32) or v.dtype is not k.dtype:
-            raise ValueError("k and v must be bfloat16 or float32, both alike")
+        code = {torch.float32: 0, torch.bfloat16: 1, torch.float8_e4m3fn: 3}.get(k.dtype)
+        if code is None or v.dtype is not k.dtype:
+            raise ValueError("k and v must be bfloat16, float32 or float8_e4m3fn, both alike")
         n_pages, n_kv, page_size, hd = k.shape
         if v.shape != k.shape or v.device != k.device:
             raise ValueError("k and v must have one shape and lie on one GPU")
@@ -530,12 +535,19 @@ class PagedCache(_OnDevice):
         if stride[0] < n_kv * page_size * hd:      # (0, as of an expanded page, would mean pages behind each other)
             raise ValueError("pages must not overlap")
         n_req, max_pages = block_table.shape
-        self.k, self.v, self.block_table, self.dtype, self.max_rows = k, v, block_table, k.dtype, int(max_rows)
+        scales = (None, None, 0)
+        if code == 3:
+            scales = self._scales(k_scale, v_scale, (n_pages, n_kv, page_size))
+        elif k_scale is not None or v_scale is not None:
+            raise ValueError("only float8_e4m3fn caches have scales")
+        self.k, self.v, self.k_scale, self.v_scale, self.block_table, self.max_rows = k, v, k_scale, v_scale, block_table, int(max_rows)
+        self.dtype = torch.bfloat16 if code == 3 else k.dtype      # of gains and outputs
         self._c = _PagedCache(k.data_ptr(), v.data_ptr(), stride[0], _want(block_table, "block_table", self._i32, dev, (n_req, max_pages)), n_pages, page_size, n_req, max_pages,
-                              n_q_heads, n_kv, hd, 1 if k.dtype is torch.bfloat16 else 0, max_rows)
+                              n_q_heads, n_kv, hd, code, max_rows, *scales)
         self._p = C.byref(self._c)
         self._q_heads, self._q_cols, self._cols = (n_q_heads, hd), n_q_heads * hd, (n_q_heads + 2 * n_kv) * hd
         self._per_req, self._per_end, self._per_row, self._gain, self._angles = (n_req,), (n_req + 1,), (self.max_rows,), (hd,), (hd // 2, 2)
+        self._kv_heads = (n_kv, hd)
         self._ws_bytes = self._lib.dmtd_paged_workspace_bytes(self._p)
         if self._ws_bytes == 0:
             _raise(self._lib, DMTD_EINVAL)
@@ -550,9 +562,21 @@ class PagedCache(_OnDevice):
         stream.synchronize()              # zeroed, whichever stream the first call is on
         self._streams = {stream.cuda_stream}
 
-    def layer(self, k, v) -> "PagedCache":
+    def _scales(self, k_scale, v_scale, shape):
+        """The addresses of an 8-bit cache's scales, and the bytes from page to page."""
+        stride = None
+        for name, t in (("k_scale", k_scale), ("v_scale", v_scale)):
+            if t is None or t.dtype is not self._torch.uint8 or t.get_device() != self._index or t.shape != shape:
+                raise ValueError(f"a float8_e4m3fn cache needs {name}, uint8 {shape} on GPU {self._index}")
+            apart = t.stride(0) if shape[0] > 1 else shape[1] * shape[2]
+            if any(n > 1 and a != b for n, a, b in zip(shape[1:], t.stride()[1:], (shape[2], 1))) or apart < shape[1] * shape[2] or stride not in (None, apart):
+                raise ValueError("a page's scales must be contiguous, not overlap the next one's, and k_scale and v_scale be laid out alike")
+            stride = apart
+        return k_scale.data_ptr(), v_scale.data_ptr(), stride
+
+    def layer(self, k, v, k_scale=None, v_scale=None) -> "PagedCache":
         """The handle of another layer's pools ``k`` and ``v``, with this one's block table and workspace."""
-        return PagedCache(k, v, self.block_table, self._q_heads[0], self.max_rows, _workspace_of=self)
+        return PagedCache(k, v, self.block_table, self._q_heads[0], self.max_rows, k_scale, v_scale, _workspace_of=self)
 
     def _rows(self, qkv, cols, norm, rope):
         dev, shape = self._index, qkv.shape
@@ -574,6 +598,21 @@ class PagedCache(_OnDevice):
         i32, dev = self._i32, self._index
         self._call(self._lib.dmtd_paged_append, self._p, x, ld, _want(cu_rows, "cu_rows", i32, dev, self._per_end), _want(row_pos, "row_pos", i32, dev, self._per_row),
                    _want(slots, "slots", self._i64, dev, self._per_row), gain, eps, tab, n_tab)
+
+    def read(self, slots, k_out=None, v_out=None):
+        """Keys and values out of the places ``slots`` (int64 ``[n]``, as :meth:`PageTables.build` numbers them; in any order), into ``k_out`` and ``v_out``
+        ``[n, n_kv_heads, head_dim]`` of the cache's type, bfloat16 for 8-bit caches (made if not given).  Rows whose place is outside the pool are not written."""
+        n = slots.shape[0] if len(slots.shape) == 1 and slots.shape[0] <= 1 << 30 else -1
+        where = _want(slots, "slots", self._i64, self._index, (max(n, 0),))
+        shape = (n, *self._kv_heads)
+        if k_out is None:
+            k_out = self._torch.empty(shape, dtype=self.dtype, device=self.device)
+        if v_out is None:
+            v_out = self._torch.empty(shape, dtype=self.dtype, device=self.device)
+        to_k, to_v = _want(k_out, "k_out", self.dtype, self._index, shape), _want(v_out, "v_out", self.dtype, self._index, shape)
+        if n:
+            self._call(self._lib.dmtd_paged_read, self._p, where, n, to_k, to_v, shape[1] * shape[2])
+        return k_out, v_out
 
     def attention(self, qkv, start, cu_rows, out=None, q_norm=None, rope=None, eps: float = 1e-6, max_new: int = 0):
         """The rows' queries over their requests' pages, into ``out`` ``[max_rows, n_q_heads, head_dim]`` of the cache's type (made if not given; rows behind

@@ -171,6 +171,14 @@ __device__ __forceinline__ float row16_sum(float v) {
   v += lane_dpp<0x121>(v);
   return v;
 }
+// The same for the maximum
+__device__ __forceinline__ float row16_max(float v) {
+  v = fmaxf(v, lane_dpp<0x128>(v));
+  v = fmaxf(v, lane_dpp<0x124>(v));
+  v = fmaxf(v, lane_dpp<0x122>(v));
+  v = fmaxf(v, lane_dpp<0x121>(v));
+  return v;
+}
 
 // QK-RMSNorm + RoPE + KV append as a launch of its own, for passes that carry more rows per sequence than an attention
 // block keeps in LDS (prefill, the whole-sequence forward): per-head RMSNorm and rotation of the rows' keys, and their

@@ -301,15 +301,18 @@ __device__ __forceinline__ void paged_store4(const PagedOut& o, int row, int col
 // Bound by the memory: 8 KiB per wave and group against PAGED_PARTS x HD / 16 + 2 x HD / 32 products.
 template <typename CT, int HD, bool PLANES>
 __device__ __forceinline__ void paged_attention_few(int y, const int* __restrict__ cu, const int* __restrict__ start, const float* __restrict__ qkv, long ld,
-                                                    const CT* __restrict__ q_gain, const float2* __restrict__ rope_tab, float eps, int max_new, int hi, const PagedOut& po,
+                                                    const typename PagedWide<CT>::type* __restrict__ q_gain, const float2* __restrict__ rope_tab, float eps, int max_new, int hi, const PagedOut& po,
                                                     const PagedView& pv, const PagedWork& wk) {
-  constexpr bool BF = sizeof(CT) == 2;
+  typedef typename PagedWide<CT>::type GT;
+  constexpr bool BF = sizeof(GT) == 2, Q8 = sizeof(CT) == 1;
   constexpr int PARTS = PAGED_PARTS<PLANES>;
   constexpr int QVT = 16, NW = PAGED_WAVES, NT = 64 * NW, DPL = HD / 16, half = HD / 2, HL = HD / 32;
-  constexpr int KS = BF ? HD / 32 : HD / 16;                 // 16-byte pieces of a key a lane carries
+  constexpr int KS = HD * (int)sizeof(CT) / 64;              // 16-byte pieces of a key a lane carries
+  constexpr int G = Q8 ? 2 : 1;                              // groups of 16 keys that a wave loads together
   constexpr int QLD = BF ? HD + ATT_QPAD : HD + 4;           // a query row in LDS
-  constexpr int VW = DPL * sizeof(CT) / 4;                   // 32-bit words of a value a lane carries: its DPL dims
-  typedef unsigned int vraw_t __attribute__((ext_vector_type(VW)));
+  constexpr int KW = BF ? HD / 32 : HD / 16;                 // pieces of a key in the products: KS, or 8-bit ones widened
+  constexpr int VW = DPL * sizeof(GT) / 4;                   // 32-bit words of a value in the products: its DPL dims that a lane carries
+  typedef unsigned int vraw_t __attribute__((ext_vector_type(Q8 ? VW / 2 : VW)));
   typedef float fvec_t __attribute__((ext_vector_type(HL)));
   typedef unsigned short hvec_t __attribute__((ext_vector_type(HL)));
   const int g = blockIdx.x, GQ = pv.gq, rpb = pv.rpb_few;
@@ -321,7 +324,7 @@ __device__ __forceinline__ void paged_attention_few(int y, const int* __restrict
   __shared__ int poison_s;
   extern __shared__ float4 paged_dyn_smem[];
   float* wacc = (float*)paged_dyn_smem;                       // [NW][QV][HD], in the place of the queries' two parts when these are done with
-  CT (*qhi_s)[QLD] = (CT (*)[QLD])paged_dyn_smem, (*qlo_s)[QLD] = qhi_s + QVT;      // (fp32: one part)
+  GT (*qhi_s)[QLD] = (GT (*)[QLD])paged_dyn_smem, (*qlo_s)[QLD] = qhi_s + QVT;      // (fp32: one part)
   // pages of this wave's next 64 groups, one a lane
   const int* trow = pv.table + (size_t)it.req * pv.max_pages;
   auto load_pages = [&](int base) { return base + 16 * NW * lane < ke ? trow[(base + 16 * NW * lane) >> pv.page_shift] : 0; };
@@ -332,7 +335,7 @@ __device__ __forceinline__ void paged_attention_few(int y, const int* __restrict
   const int qv = tid >> 4, l16 = tid & 15, qr = pv.row_of(qv < QV ? qv : 0), qrow = it.row0 + qr, qhead = g * GQ + (qv < QV ? qv - qr * GQ : 0);
   fvec_t xa, xb;
   float2 cs[HL];
-  CT g0[HL], g1[HL];
+  GT g0[HL], g1[HL];
   {
     // what it needs is asked for in front of the keys, whose arrival it is made ready beside
     const float* src = qkv + (size_t)(it.first + qrow) * ld + (size_t)qhead * HD + HL * l16;
@@ -341,25 +344,40 @@ __device__ __forceinline__ void paged_attention_few(int y, const int* __restrict
 #pragma unroll
     for (int e = 0; e < HL; ++e) {
       cs[e] = rope_tab ? rp[e] : make_float2(1.f, 0.f);
-      g0[e] = q_gain ? q_gain[HL * l16 + e] : CT(0);
-      g1[e] = q_gain ? q_gain[half + HL * l16 + e] : CT(0);
+      g0[e] = q_gain ? q_gain[HL * l16 + e] : GT(0);
+      g1[e] = q_gain ? q_gain[half + HL * l16 + e] : GT(0);
     }
   }
   if (tid == 0) poison_s = INT_MAX;
-  u32x4 kr[KS];
-  vraw_t vr[4];
-  bool ok;
-  auto load_kv = [&](int base, int page) {
-    ok = page >= 0 && page < pv.n_pages;
-    const size_t at = (size_t)(ok ? page : 0) * pv.page_stride + (((size_t)g << pv.page_shift) + (base & ((1 << pv.page_shift) - 1))) * HD;
+  u32x4 kr[G][KS];
+  vraw_t vr[G][4];
+  bool ok[G];
+  uint32_t ksr[G], vsr[G];                                    // 8 bits: the scale of the lane's key, those of its four values
+  auto load_kv = [&](int base, int page, int u) {
+    ok[u] = page >= 0 && page < pv.n_pages;
+    const size_t row = ((size_t)g << pv.page_shift) + (base & ((1 << pv.page_shift) - 1));
+    const size_t at = (size_t)(ok[u] ? page : 0) * pv.page_stride + row * HD;
     const CT* kp = (const CT*)pv.k + at;
     const CT* vp = (const CT*)pv.v + at;
 #pragma unroll
-    for (int t = 0; t < KS; ++t) kr[t] = *(const u32x4*)(kp + sl * HD + (HD / KS) * t + (16 / (int)sizeof(CT)) * kq);
+    for (int t = 0; t < KS; ++t) kr[u][t] = *(const u32x4*)(kp + sl * HD + (HD / KS) * t + (16 / (int)sizeof(CT)) * kq);
 #pragma unroll
-    for (int m = 0; m < 4; ++m) vr[m] = __builtin_nontemporal_load((const vraw_t*)(vp + (4 * kq + m) * HD + DPL * sl));
+    for (int m = 0; m < 4; ++m) vr[u][m] = __builtin_nontemporal_load((const vraw_t*)(vp + (4 * kq + m) * HD + DPL * sl));
+    if constexpr (Q8) {
+      const size_t sc = (size_t)(ok[u] ? page : 0) * pv.scale_stride + row;
+      ksr[u] = pv.ks[sc + sl];
+      vsr[u] = *(const uint32_t*)(pv.vs + sc + 4 * kq);
+    }
   };
-  if (first < ke) load_kv(first, __builtin_amdgcn_readlane(pages, 0));
+  // groups j .. j + G - 1 of this wave's (load_pages(base) has been called for 64 of them)
+  auto load_groups = [&](int base, int j) {
+#pragma unroll
+    for (int u = 0; u < G; ++u) {
+      ok[u] = false;
+      if (base + 16 * NW * u < ke) load_kv(base + 16 * NW * u, __builtin_amdgcn_readlane(pages, (j + u) & 63), u);
+    }
+  };
+  if (first < ke) load_groups(first, 0);
   {
     float x0[HL], x1[HL], ss = 0.f;
 #pragma unroll
@@ -367,7 +385,7 @@ __device__ __forceinline__ void paged_attention_few(int y, const int* __restrict
     if (q_gain) {
       const float rs = rsqrtf(row16_sum(ss) / (float)HD + eps);
 #pragma unroll
-      for (int e = 0; e < HL; ++e) { x0[e] *= rs * Elem<CT>::to_f32(g0[e]); x1[e] *= rs * Elem<CT>::to_f32(g1[e]); }
+      for (int e = 0; e < HL; ++e) { x0[e] *= rs * Elem<GT>::to_f32(g0[e]); x1[e] *= rs * Elem<GT>::to_f32(g1[e]); }
     }
     if (rope_tab) {
 #pragma unroll
@@ -399,30 +417,66 @@ __device__ __forceinline__ void paged_attention_few(int y, const int* __restrict
   f32x4 acc[DPL];
 #pragma unroll
   for (int e = 0; e < DPL; ++e) acc[e] = f32x4{0.f, 0.f, 0.f, 0.f};
-  for (int base = first, j = 0; base < ke; base += 16 * NW, ++j) {
-    u32x4 ka[KS];
-    vraw_t va[4];
-    const bool here = ok;
+  for (int from = first, j = 0; from < ke; from += 16 * NW * G, j += G) {
+    u32x4 kc[G][KS];
+    vraw_t vc[G][4];
+    bool here[G];
+    uint32_t ksc[G], vsc[G];
 #pragma unroll
-    for (int t = 0; t < KS; ++t) ka[t] = kr[t];
+    for (int u = 0; u < G; ++u) {
+      here[u] = ok[u];
 #pragma unroll
-    for (int m = 0; m < 4; ++m) va[m] = vr[m];
-    const int next = base + 16 * NW;
-    if (next < ke) {
-      if ((j & 63) == 63) pages = load_pages(next);
-      load_kv(next, __builtin_amdgcn_readlane(pages, (j + 1) & 63));
+      for (int t = 0; t < KS; ++t) kc[u][t] = kr[u][t];
+#pragma unroll
+      for (int m = 0; m < 4; ++m) vc[u][m] = vr[u][m];
+      if constexpr (Q8) { ksc[u] = ksr[u]; vsc[u] = vsr[u]; }
     }
-    if (!here) continue;                                      // a page outside the pool
+    const int next = from + 16 * NW * G;
+    if (next < ke) {
+      if (((j + G) & 63) == 0) pages = load_pages(next);
+      load_groups(next, j + G);
+    }
+#pragma unroll
+    for (int u = 0; u < G; ++u) {
+    if (!here[u]) continue;                                   // a page outside the pool, or behind the last key
+    const int base = from + 16 * NW * u;
+    uint32_t va[4][VW];                                       // the values, as bf16 or fp32
+    u32x4 ka[KW];
+    if constexpr (Q8) {
+      const float sk = e8m0_scale(ksc[u]);
+#pragma unroll
+      for (int t = 0; t < KS; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          ka[2 * t + (e >> 1)][2 * (e & 1)] = e4m3_pair<false>(kc[u][t][e], sk);
+          ka[2 * t + (e >> 1)][2 * (e & 1) + 1] = e4m3_pair<true>(kc[u][t][e], sk);
+        }
+#pragma unroll
+      for (int m = 0; m < 4; ++m) {
+        const float sv = e8m0_scale((vsc[u] >> (8 * m)) & 0xFFu);
+#pragma unroll
+        for (int e = 0; e < VW / 2; ++e) { va[m][2 * e] = e4m3_pair<false>(vc[u][m][e], sv); va[m][2 * e + 1] = e4m3_pair<true>(vc[u][m][e], sv); }
+      }
+    } else {
+#pragma unroll
+      for (int t = 0; t < KS; ++t) ka[t] = kc[u][t];
+#pragma unroll
+      for (int m = 0; m < 4; ++m)
+#pragma unroll
+        for (int e = 0; e < VW; ++e) va[m][e] = vc[u][m][e];
+    }
     f32x4 s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int t = 0; t < KS; ++t) {
+    for (int t = 0; t < KW; ++t) {
       if constexpr (!BF) {
         const f32x4 k4 = __builtin_bit_cast(f32x4, ka[t]), q4 = *(const f32x4*)&qhi_s[sl][16 * t + 4 * kq];
 #pragma unroll
         for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_16x16x4f32(k4[e], q4[e], s, 0, 0, 0);
         continue;
       } else {
-        const bf16x8_t ql = __builtin_bit_cast(bf16x8_t, *(const u32x4*)&qlo_s[sl][32 * t + 8 * kq]), qh = __builtin_bit_cast(bf16x8_t, *(const u32x4*)&qhi_s[sl][32 * t + 8 * kq]);
+        // (8 bits: a lane's 16 codes of a piece are consecutive dims, and the products' eight go by that)
+        const int d0 = Q8 ? 64 * (t >> 1) + 16 * kq + 8 * (t & 1) : 32 * t + 8 * kq;
+        const bf16x8_t ql = __builtin_bit_cast(bf16x8_t, *(const u32x4*)&qlo_s[sl][d0]), qh = __builtin_bit_cast(bf16x8_t, *(const u32x4*)&qhi_s[sl][d0]);
         s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, ka[t]), ql, s, 0, 0, 0);
         s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, ka[t]), qh, s, 0, 0, 0);
       }
@@ -490,6 +544,7 @@ __device__ __forceinline__ void paged_attention_few(int y, const int* __restrict
           acc[e] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(bf16x4s_t, pp[z]), __builtin_bit_cast(bf16x4s_t, v4), acc[e], 0, 0, 0);
       }
     }
+    }
   }
   // the waves' results of a vector, 4 consecutive dims a thread
   l_run = column_sum(l_run);
@@ -508,7 +563,7 @@ __device__ __forceinline__ void paged_attention_few(int y, const int* __restrict
   float* part = wk.part + ((size_t)(it.slot + it.split) * pv.nkv + g) * SLOT;
   auto store = [&](int v, int d, const f32x4& x) {
     const int r = pv.row_of(v);
-    paged_store4<CT, PLANES>(po, it.first + it.row0 + r, (g * GQ + v - r * GQ) * HD + d, x);
+    paged_store4<GT, PLANES>(po, it.first + it.row0 + r, (g * GQ + v - r * GQ) * HD + d, x);
   };
   for (int e = tid; e < QV * (HD / 4); e += NT) {
     const int v = e / (HD / 4), d = (e % (HD / 4)) * 4;
@@ -547,7 +602,7 @@ __device__ __forceinline__ void paged_attention_few(int y, const int* __restrict
 // The products run over whole tiles, with probability 0 for keys that a row does not see.  Values behind the block's last key go into LDS as 0.  Values of its
 // own positions may be infinite or NaN, which 0 does not silence: the block looks at them first; if one is not finite, it and its like behind
 // it go into LDS as 0 and the rows that see it become NaN.
-template <int HD, bool PLANES>
+template <typename CT, int HD, bool PLANES>
 __device__ __forceinline__ void paged_attention_tall(int y, const int* __restrict__ cu, const int* __restrict__ start, const float* __restrict__ qkv, long ld,
                                                      const bf16_t* __restrict__ q_gain, const float2* __restrict__ rope_tab, float eps, int max_new, int lo, const PagedOut& po,
                                                      const PagedView& pv, const PagedWork& wk) {
@@ -557,9 +612,11 @@ __device__ __forceinline__ void paged_attention_tall(int y, const int* __restric
   constexpr int DT = HD / 32;          // 32-dim tiles of the output
   constexpr int DV = HD / 16;          // dims of V a thread carries
   constexpr int CH = HD / 8;           // 16-byte chunks of a K row
-  constexpr int KI = KT * CH / 256;    // K pieces (16 bytes per lane) per wave and tile
+  constexpr bool Q8 = sizeof(CT) == 1;
+  constexpr int KI = KT * CH / 256 / (Q8 ? 2 : 1);      // K pieces (16 bytes per lane) per wave and tile
   constexpr int TILE = KT * HD;
-  typedef unsigned int vraw_t __attribute__((ext_vector_type(DV / 2)));
+  constexpr int VR = Q8 ? DV / 4 : DV / 2;              // words of a value as they come from the pool
+  typedef unsigned int vraw_t __attribute__((ext_vector_type(VR)));
   extern __shared__ float4 paged_dyn_smem[];
   __shared__ int poison_s;
   const int g = blockIdx.x, GQ = pv.gq, rpb = pv.rpb_tall;
@@ -582,21 +639,61 @@ __device__ __forceinline__ void paged_attention_tall(int y, const int* __restric
   auto load_pages = [&](int base) { return trow[min(base + 4 * (lane & 15), ke - 1) >> pv.page_shift]; };
   auto outside = [&](int page) { return page < 0 || page >= pv.n_pages; };
   // K: piece i of the wave's 16 keys holds 64 / CH of them, a chunk of one per lane, permuted by the key number
+  u32x4 kraw[Q8 ? KI : 1];
+  uint32_t kscale[Q8 ? KI : 1], vscale = 0;
   auto load_k = [&](int ln, int base, int page, int buf, int i) {
-    static_assert(64 / CH <= CH && KI * (64 / CH) == 16, "a wave's pieces are 16 keys, and a piece's permutation is that of piece 0, exclusive-or its first key");
+    if constexpr (Q8) {      // codes: into registers, 16 of one key a lane; store_k widens them into LDS
+      const int pg = __builtin_amdgcn_readlane(page, 4 * w), key = (i * 64 + ln) / (HD / 16);
+      const size_t p = outside(pg) ? 0 : pg;
+      const uint32_t row = (g << pv.page_shift) + ((base + 16 * w) & in_page) + key;
+      kraw[i] = *(const u32x4*)((const unsigned char*)pv.k + p * pv.page_stride + (size_t)row * HD + (ln % (HD / 16)) * 16);
+      kscale[i] = pv.ks[p * pv.scale_stride + row];
+      return;
+    }
+    static_assert(64 / CH <= CH && (Q8 ? 2 : 1) * KI * (64 / CH) == 16, "a wave's pieces are 16 keys, and a piece's permutation is that of piece 0, exclusive-or its first key");
     const int pg = __builtin_amdgcn_readlane(page, 4 * w), k0 = ln / CH, c0 = (ln % CH) ^ k0, ki = (w * KI + i) * (64 / CH);
     const bf16_t* src = (const bf16_t*)pv.k + (size_t)(outside(pg) ? 0 : pg) * pv.page_stride + (((size_t)g << pv.page_shift) + ((base + 16 * w) & in_page)) * HD;
     __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(src + (uint32_t)((i * (64 / CH) + k0) * HD + (c0 ^ (ki & (CH - 1))) * 8)),
                                      (__attribute__((address_space(3))) void*)(uintptr_t)(ring + (uint32_t)(buf * TILE + (w * KI + i) * 512) * 2), 16, 0, 0);
   };
   // V: 4 keys of a page, DV dims a thread; keys behind the range's last are whatever the page holds there
-  vraw_t vr[4];
-  const bf16_t* vsrc = nullptr;
+  vraw_t vraw[4];
+  uint32_t vr[4][DV / 2];
+  const CT* vsrc = nullptr;
   auto aim_v = [&](int ln, int base, int page) {
-    vsrc = (const bf16_t*)pv.v + (size_t)(outside(page) ? 0 : page) * pv.page_stride +
+    if constexpr (Q8)
+      vscale = *(const uint32_t*)(pv.vs + (size_t)(outside(page) ? 0 : page) * pv.scale_stride + (uint32_t)((g << pv.page_shift) + ((base + 4 * (ln & 15)) & in_page)));
+    vsrc = (const CT*)pv.v + (size_t)(outside(page) ? 0 : page) * pv.page_stride +
            (uint32_t)(((g << pv.page_shift) + ((base + 4 * (ln & 15)) & in_page)) * HD + (w * 4 + (ln >> 4)) * DV);
   };
-  auto load_v = [&](int m) { vr[m] = *(const vraw_t*)(vsrc + m * HD); };
+  auto load_v = [&](int m) { vraw[m] = *(const vraw_t*)(vsrc + m * HD); };
+  // what has been loaded, as bf16: the values in registers, 8-bit keys in LDS, as the direct loads of bf16 keys leave them
+  auto widen = [&](int ln, int buf) {
+    if constexpr (Q8) {
+#pragma unroll
+      for (int i = 0; i < KI; ++i) {
+        const int key = 16 * w + (i * 64 + ln) / (HD / 16), c = 2 * (ln % (HD / 16));
+        const float sk = e8m0_scale(kscale[i]);
+        const uint32_t at = ring + (uint32_t)(buf * TILE + key * HD) * 2;
+        uint32_t x[8];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) { x[2 * e] = e4m3_pair<false>(kraw[i][e], sk); x[2 * e + 1] = e4m3_pair<true>(kraw[i][e], sk); }
+        *(lds_u32x4*)(uintptr_t)(at + ((c ^ (key & (CH - 1))) << 4)) = u32x4{x[0], x[1], x[2], x[3]};
+        *(lds_u32x4*)(uintptr_t)(at + (((c + 1) ^ (key & (CH - 1))) << 4)) = u32x4{x[4], x[5], x[6], x[7]};
+      }
+#pragma unroll
+      for (int m = 0; m < 4; ++m) {
+        const float sv = e8m0_scale((vscale >> (8 * m)) & 0xFFu);
+#pragma unroll
+        for (int u = 0; u < VR; ++u) { vr[m][2 * u] = e4m3_pair<false>(vraw[m][u], sv); vr[m][2 * u + 1] = e4m3_pair<true>(vraw[m][u], sv); }
+      }
+    } else {
+#pragma unroll
+      for (int m = 0; m < 4; ++m)
+#pragma unroll
+        for (int u = 0; u < DV / 2; ++u) vr[m][u] = vraw[m][u];
+    }
+  };
   // values of pages outside the pool and of keys behind the last become 0; so do those from poison_s on that are not finite
   auto needs_clean = [&](int base, int page, bool drop) { return drop || base + KT > ke || __any(outside(page)); };
   auto clean_v = [&](int base, int page, bool drop) {
@@ -700,15 +797,25 @@ __device__ __forceinline__ void paged_attention_tall(int y, const int* __restric
   for (int c = tid; c < (ke - max(it.pos0 + 1, kb)) * CH; c += NT) {
     const int key = max(it.pos0 + 1, kb) + c / CH, page = trow[key >> pv.page_shift];
     if (outside(page)) continue;
-    const u32x4 v = *(const u32x4*)((const bf16_t*)pv.v + (size_t)page * pv.page_stride + (((size_t)g << pv.page_shift) + (key & in_page)) * HD + c % CH * 8);
     bool bad = false;
+    const size_t row = ((size_t)g << pv.page_shift) + (key & in_page);
+    if constexpr (Q8) {
+      const uint2 codes = *(const uint2*)((const unsigned char*)pv.v + (size_t)page * pv.page_stride + row * HD + c % CH * 8);
+      const float sv = e8m0_scale(pv.vs[(size_t)page * pv.scale_stride + row]);
+      const uint32_t v[4] = {e4m3_pair<false>(codes.x, sv), e4m3_pair<true>(codes.x, sv), e4m3_pair<false>(codes.y, sv), e4m3_pair<true>(codes.y, sv)};
 #pragma unroll
-    for (int u = 0; u < 4; ++u) bad |= (v[u] & 0x7F80u) == 0x7F80u || (v[u] & 0x7F800000u) == 0x7F800000u;
+      for (int u = 0; u < 4; ++u) bad |= (v[u] & 0x7F80u) == 0x7F80u || (v[u] & 0x7F800000u) == 0x7F800000u;
+    } else {
+      const u32x4 v = *(const u32x4*)((const bf16_t*)pv.v + (size_t)page * pv.page_stride + row * HD + c % CH * 8);
+#pragma unroll
+      for (int u = 0; u < 4; ++u) bad |= (v[u] & 0x7F80u) == 0x7F80u || (v[u] & 0x7F800000u) == 0x7F800000u;
+    }
     if (bad) atomicMin(&poison_s, key);
   }
   __syncthreads();
   const int poison = __builtin_amdgcn_readfirstlane(poison_s);
   const bool drop = poison != INT_MAX;
+  widen(lane, 0);
   if (needs_clean(kb, pages, drop)) clean_v(kb, pages, drop);
   store_v(lane, 0);
   __syncthreads();
@@ -833,6 +940,7 @@ __device__ __forceinline__ void paged_attention_tall(int y, const int* __restric
       }
     }
     if (more) {
+      widen(ln, buf ^ 1);
       if (needs_clean(ahead, pages_next, drop)) clean_v(ahead, pages_next, drop);
       store_v(ln, buf ^ 1);
     }
@@ -875,21 +983,21 @@ __device__ __forceinline__ int paged_block() { return blockIdx.z * gridDim.y + b
 
 template <typename CT, int HD, bool PLANES>
 __global__ void __launch_bounds__(64 * PAGED_WAVES, sizeof(CT) == 2 ? 4 : 2) paged_attention_few_mfma_kernel(
-    const int* __restrict__ cu, const int* __restrict__ start, const float* __restrict__ qkv, long ld, const CT* __restrict__ q_gain, const float2* __restrict__ rope_tab, float eps,
+    const int* __restrict__ cu, const int* __restrict__ start, const float* __restrict__ qkv, long ld, const typename PagedWide<CT>::type* __restrict__ q_gain, const float2* __restrict__ rope_tab, float eps,
     int max_new, int hi, PagedOut po, PagedView pv, PagedWork wk) {
   paged_attention_few<CT, HD, PLANES>(paged_block(), cu, start, qkv, ld, q_gain, rope_tab, eps, max_new, hi, po, pv, wk);
 }
 
 // Both kinds of requests in one launch, the longer blocks first: a chunk's leave the memory to the single tokens' (316 rows of a chunk and 14 tokens, 14/2 heads of 64: 17.5 us; when
 // both ways stood side by side one launch after the other took 28, and where no single token was in the batch their launch 4.8)
-template <int HD, bool PLANES>
+template <typename CT, int HD, bool PLANES>
 __global__ void __launch_bounds__(256, 2) paged_attention_both_mfma_kernel(const int* __restrict__ cu, const int* __restrict__ start, const float* __restrict__ qkv, long ld,
                                                                            const bf16_t* __restrict__ q_gain, const float2* __restrict__ rope_tab, float eps, int max_new, int border,
                                                                            int n_tall, PagedOut po, PagedView pv, PagedWork few, PagedWork tall) {
   static_assert(PAGED_WAVES == 4, "blocks of one size");
   const int y = paged_block();
-  if (y < n_tall) paged_attention_tall<HD, PLANES>(y, cu, start, qkv, ld, q_gain, rope_tab, eps, max_new, border, po, pv, tall);
-  else paged_attention_few<bf16_t, HD, PLANES>(y - n_tall, cu, start, qkv, ld, q_gain, rope_tab, eps, max_new, border, po, pv, few);
+  if (y < n_tall) paged_attention_tall<CT, HD, PLANES>(y, cu, start, qkv, ld, q_gain, rope_tab, eps, max_new, border, po, pv, tall);
+  else paged_attention_few<CT, HD, PLANES>(y - n_tall, cu, start, qkv, ld, q_gain, rope_tab, eps, max_new, border, po, pv, few);
 }
 
 // The ranges of the tall kernel's groups joined: 64 KiB of partial results a group and range are too much for the block that ends last (64 rows behind

@@ -3,7 +3,8 @@
 // share; the attention itself is in attention_paged.hpp.
 //
 // Pool: K and V each [n_pages][n_kv_heads][page_size][head_dim], so that the keys of one head in one page are one contiguous run of
-// page_size * head_dim elements (4 KiB at 16 keys of 128 bf16 values).  Page sizes are powers of two from 16 to 256: a group of 16 keys,
+// page_size * head_dim elements (4 KiB at 16 keys of 128 bf16 values).  8-bit pools hold e4m3 codes, and beside each pool a power of two per row of head_dim
+// codes, as its biased exponent: [n_pages][n_kv_heads][page_size] bytes.  Page sizes are powers of two from 16 to 256: a group of 16 keys,
 // which is what a wave of the attention kernels loads together, never leaves its page.
 #pragma once
 #include <limits.h>
@@ -15,10 +16,30 @@ namespace dmtd {
 
 constexpr int kPagedMaxRequests = 8192;      // requests of a call: their prefix sums lie in LDS
 
+// An element of an 8-bit pool: an e4m3 code (sign, 4 bits of exponent, 3 of fraction; 0x7F is NaN, there is no infinity).  A code times its row's power of two is a bf16
+// value without rounding (4 significant bits, and PAGED_LEAST_SCALE keeps the smallest normal), so the matrix cores see exactly what is stored, and the chip's
+// conversion multiplies by the power on the way.
+struct e4m3_t { unsigned char code; };
+// What the kernels compute with, and gains and outputs have, beside a pool's type
+template <typename CT> struct PagedWide { typedef CT type; };
+template <> struct PagedWide<e4m3_t> { typedef bf16_t type; };
+constexpr int PAGED_LEAST_SCALE = 16;      // biased: 2^-111.  Rows of smaller magnitude than 448 times that keep fewer bits.
+constexpr float E4M3_MAX = 448.f;
+
+// Two codes of a word (the low or the high ones) times 2^(e - 127), as two bf16 values.  A scale byte of 255 (append writes none) is NaN.
+template <bool HIGH> __device__ __forceinline__ uint32_t e4m3_pair(uint32_t codes, float scale) {
+  typedef __bf16 bf2_t __attribute__((ext_vector_type(2)));
+  const bf2_t v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, scale, HIGH);
+  return __builtin_bit_cast(uint32_t, v);
+}
+__device__ __forceinline__ float e8m0_scale(uint32_t e) { return __uint_as_float(e << 23); }
+
 // What the append and the attention know of the cache
 struct PagedView {
   void *k, *v;
   long page_stride;                 // elements from page to page
+  unsigned char *ks, *vs;           // 8-bit pools: the rows' scales, biased exponents
+  long scale_stride;                // bytes from page to page of these
   const int* table;                 // [n_req][max_pages]
   int n_pages, page_shift, n_req, max_pages, nh, nkv, max_rows;
   int limit;                        // positions a request may have: the block table's, or the rotary table's where that is shorter
@@ -296,14 +317,45 @@ template <int N> __device__ __forceinline__ void store_elems(bf16_t* p, const fl
   for (int e = 0; e < N; e += 2) *(uint32_t*)(p + e) = pack_bf16x2(x[e], x[e + 1]);
 }
 
+// A row of 16 lanes' values as codes: N consecutive ones from p on and as many from p + half on.  Returns the row's scale.
+template <int N> __device__ __forceinline__ uint32_t store_codes(unsigned char* p, int half, const float (&x0)[N], const float (&x1)[N]) {
+  float most = 0.f;
+#pragma unroll
+  for (int e = 0; e < N; ++e) {
+    const float a = fabsf(x0[e]), b = fabsf(x1[e]);
+    if (a < INFINITY) most = fmaxf(most, a);      // (false for NaN too)
+    if (b < INFINITY) most = fmaxf(most, b);
+  }
+  most = row16_max(most);
+  // 448 = 1.75 x 2^8: the exponent less 8, one more where the fraction is above 1.75
+  const uint32_t e = (uint32_t)max((int)((__float_as_uint(most) + 0x1FFFFFu) >> 23) - 8, PAGED_LEAST_SCALE);
+  const float inv = __uint_as_float((254u - e) << 23);
+  auto code = [&](float x) { return fabsf(x) < INFINITY ? x * inv : __uint_as_float(0x7FC00000u); };
+  if constexpr (N == 4) {
+    int a = __builtin_amdgcn_cvt_pk_fp8_f32(code(x0[0]), code(x0[1]), 0, false), b = __builtin_amdgcn_cvt_pk_fp8_f32(code(x1[0]), code(x1[1]), 0, false);
+    a = __builtin_amdgcn_cvt_pk_fp8_f32(code(x0[2]), code(x0[3]), a, true);
+    b = __builtin_amdgcn_cvt_pk_fp8_f32(code(x1[2]), code(x1[3]), b, true);
+    *(int*)p = a;
+    *(int*)(p + half) = b;
+  } else {
+    static_assert(N == 2, "head dims 64 and 128");
+    *(unsigned short*)p = (unsigned short)__builtin_amdgcn_cvt_pk_fp8_f32(code(x0[0]), code(x0[1]), 0, false);
+    *(unsigned short*)(p + half) = (unsigned short)__builtin_amdgcn_cvt_pk_fp8_f32(code(x1[0]), code(x1[1]), 0, false);
+  }
+  return e;
+}
+
 // The new tokens' keys - RMS norm with gain (k_gain null: none), then the rotation of the pairs (i, i + HD/2) by the angles of the token's
 // position (rope_tab null: none) - and values, rounded to the pool's type and stored in their places.  16 lanes take one (row, KV head):
 // its key and its value, HD/32 pairs a lane, so that a wave's loads are runs of 256 bytes and the norm's sum stays inside a DPP row.  Rows at
 // and behind cu[n_req], and rows whose place or position is out of range, are not stored.
+// 8-bit pools: the 16 lanes' largest finite magnitude a gives the row's power of two, the least with a <= 448 times it; values that are not finite become NaN, with no
+// say in the power.  Codes are rounded to nearest even, once.
 template <typename CT, int HD>
 __global__ void __launch_bounds__(256) paged_append_kernel(const float* __restrict__ qkv, long ld, const int* __restrict__ cu, const int* __restrict__ row_pos,
-                                                           const long long* __restrict__ slots, const CT* __restrict__ k_gain, const float2* __restrict__ rope_tab,
-                                                           float eps, PagedView pv) {
+                                                           const long long* __restrict__ slots, const typename PagedWide<CT>::type* __restrict__ k_gain,
+                                                           const float2* __restrict__ rope_tab, float eps, PagedView pv) {
+  typedef typename PagedWide<CT>::type GT;
   constexpr int half = HD / 2, HL = AttRow<HD>::HL;
   const int l = threadIdx.x & 15;
   const long v = (long)blockIdx.x * 16 + (threadIdx.x >> 4);
@@ -321,7 +373,7 @@ __global__ void __launch_bounds__(256) paged_append_kernel(const float* __restri
   if (k_gain) {
     const float rs = rsqrtf(row16_sum(ss) / (float)HD + eps);
 #pragma unroll
-    for (int e = 0; e < HL; ++e) { x0[e] *= rs * Elem<CT>::to_f32(k_gain[HL * l + e]); x1[e] *= rs * Elem<CT>::to_f32(k_gain[half + HL * l + e]); }
+    for (int e = 0; e < HL; ++e) { x0[e] *= rs * Elem<GT>::to_f32(k_gain[HL * l + e]); x1[e] *= rs * Elem<GT>::to_f32(k_gain[half + HL * l + e]); }
   }
   if (rope_tab) {
     const float2* rp = rope_tab + (size_t)pos * half + HL * l;
@@ -333,13 +385,61 @@ __global__ void __launch_bounds__(256) paged_append_kernel(const float* __restri
       x1[e] = b * cs.x + a * cs.y;
     }
   }
-  const size_t at = (size_t)(slot >> pv.page_shift) * pv.page_stride + (((size_t)g << pv.page_shift) + (size_t)(slot & ((1 << pv.page_shift) - 1))) * HD + HL * l;
+  const size_t row = ((size_t)g << pv.page_shift) + (size_t)(slot & ((1 << pv.page_shift) - 1));
+  const size_t at = (size_t)(slot >> pv.page_shift) * pv.page_stride + row * HD + HL * l;
+  if constexpr (sizeof(CT) == 1) {
+    const size_t sc = (size_t)(slot >> pv.page_shift) * pv.scale_stride + row;
+    const uint32_t ek = store_codes<HL>((unsigned char*)pv.k + at, half, x0, x1);
+#pragma unroll
+    for (int e = 0; e < HL; ++e) { x0[e] = w.a[e]; x1[e] = w.b[e]; }
+    const uint32_t ev = store_codes<HL>((unsigned char*)pv.v + at, half, x0, x1);
+    if (l == 0) { pv.ks[sc] = (unsigned char)ek; pv.vs[sc] = (unsigned char)ev; }
+    return;
+  } else {
   store_elems<HL>((CT*)pv.k + at, x0);
   store_elems<HL>((CT*)pv.k + at + half, x1);
 #pragma unroll
   for (int e = 0; e < HL; ++e) { x0[e] = w.a[e]; x1[e] = w.b[e]; }
   store_elems<HL>((CT*)pv.v + at, x0);
   store_elems<HL>((CT*)pv.v + at + half, x1);
+  }
+}
+
+// Keys and values at given places (n of them), as rows [nkv][HD] of the wide type, `ldo` elements apart: 16 lanes a (row, KV head), HD / 16 elements of either a lane.  Rows whose
+// place is outside the pool stay as they were.  Bound by the memory, if the rows are many.
+template <typename CT, int HD>
+__global__ void __launch_bounds__(256) paged_read_kernel(const long long* __restrict__ slots, int n, typename PagedWide<CT>::type* __restrict__ k_out,
+                                                         typename PagedWide<CT>::type* __restrict__ v_out, long ldo, PagedView pv) {
+  typedef typename PagedWide<CT>::type GT;
+  constexpr int N = HD / 16;
+  const int l = threadIdx.x & 15;
+  const long v = (long)blockIdx.x * 16 + (threadIdx.x >> 4);
+  const long t = v / pv.nkv;
+  const int g = (int)(v - t * pv.nkv);
+  if (t >= n) return;
+  const long long slot = slots[t];
+  if (slot < 0 || slot >= ((long long)pv.n_pages << pv.page_shift)) return;
+  const size_t row = ((size_t)g << pv.page_shift) + (size_t)(slot & ((1 << pv.page_shift) - 1)), page = (size_t)(slot >> pv.page_shift);
+  const size_t at = page * pv.page_stride + row * HD + N * l, to = (size_t)t * ldo + (size_t)g * HD + N * l;
+  if constexpr (sizeof(CT) == 1) {
+    typedef uint32_t codes_t __attribute__((ext_vector_type(N / 4)));
+    typedef uint32_t vals_t __attribute__((ext_vector_type(N / 2)));
+    const codes_t ck = *(const codes_t*)((const unsigned char*)pv.k + at), cv = *(const codes_t*)((const unsigned char*)pv.v + at);
+    const float sk = e8m0_scale(pv.ks[page * pv.scale_stride + row]), sv = e8m0_scale(pv.vs[page * pv.scale_stride + row]);
+    vals_t xk, xv;
+#pragma unroll
+    for (int e = 0; e < N / 4; ++e) {
+      xk[2 * e] = e4m3_pair<false>(ck[e], sk); xk[2 * e + 1] = e4m3_pair<true>(ck[e], sk);
+      xv[2 * e] = e4m3_pair<false>(cv[e], sv); xv[2 * e + 1] = e4m3_pair<true>(cv[e], sv);
+    }
+    *(vals_t*)(k_out + to) = xk;
+    *(vals_t*)(v_out + to) = xv;
+  } else {
+    typedef GT vals_t __attribute__((ext_vector_type(N)));
+    const vals_t xk = *(const vals_t*)((const GT*)pv.k + at), xv = *(const vals_t*)((const GT*)pv.v + at);
+    *(vals_t*)(k_out + to) = xk;
+    *(vals_t*)(v_out + to) = xv;
+  }
 }
 
 }  // namespace dmtd

@@ -61,7 +61,8 @@ int check_cache(const dmtd_paged_cache* c) {
   if (!c) return paged_fail(DMTD_EINVAL, "null cache");
   const int rc = check_table(c->n_req, c->max_pages, c->n_pages, c->page_size);
   if (rc != DMTD_OK) return rc;
-  if (c->dtype != DMTD_DTYPE_F32 && c->dtype != DMTD_DTYPE_BF16) return paged_fail(DMTD_EINVAL, "unknown dtype");
+  const bool q8 = c->dtype == DMTD_DTYPE_E4M3;
+  if (c->dtype != DMTD_DTYPE_F32 && c->dtype != DMTD_DTYPE_BF16 && !q8) return paged_fail(DMTD_EINVAL, "unknown dtype");
   if (c->head_dim != 64 && c->head_dim != 128) return paged_fail(DMTD_EINVAL, "head_dim must be 64 or 128");
   if (c->n_kv_heads < 1 || c->n_kv_heads > 1024 || c->n_q_heads < 1 || c->n_q_heads % c->n_kv_heads || c->n_q_heads / c->n_kv_heads > QV_MAX)
     return paged_fail(DMTD_EINVAL, "n_q_heads must be a multiple of n_kv_heads (at most 1024), at most 16 times as many");
@@ -70,7 +71,11 @@ int check_cache(const dmtd_paged_cache* c) {
   if (!c->k || !c->v || !c->block_table) return paged_fail(DMTD_EINVAL, "null cache pointer");
   if (!aligned(c->k, 16) || !aligned(c->v, 16) || !aligned(c->block_table, 4)) return paged_fail(DMTD_EINVAL, "k and v must be 16-byte aligned");
   const long one = (long)c->n_kv_heads * c->page_size * c->head_dim;
-  if (c->page_stride != 0 && (c->page_stride < one || c->page_stride % 8)) return paged_fail(DMTD_EINVAL, "page_stride must be 0 or a multiple of 8 that holds a page");
+  if (c->page_stride != 0 && (c->page_stride < one || c->page_stride % (q8 ? 16 : 8))) return paged_fail(DMTD_EINVAL, "page_stride must be 0 or a multiple of 8 (e4m3: 16) that holds a page");
+  if (!q8) return DMTD_OK;      // (callers of the other types may not know of the fields behind max_rows)
+  if (!c->k_scale || !c->v_scale || !aligned(c->k_scale, 16) || !aligned(c->v_scale, 16)) return paged_fail(DMTD_EINVAL, "an e4m3 cache needs 16-byte aligned k_scale and v_scale");
+  const long scales = (long)c->n_kv_heads * c->page_size;
+  if (c->scale_stride != 0 && (c->scale_stride < scales || c->scale_stride % 16)) return paged_fail(DMTD_EINVAL, "scale_stride must be 0 or a multiple of 16 that holds a page's scales");
   return DMTD_OK;
 }
 
@@ -88,6 +93,10 @@ PagedView paged_view(const dmtd_paged_cache* c, const float* rope, int32_t rope_
   PagedView v{};
   v.k = c->k; v.v = c->v; v.table = c->block_table;
   v.page_stride = c->page_stride ? c->page_stride : (long)c->n_kv_heads * c->page_size * c->head_dim;
+  if (c->dtype == DMTD_DTYPE_E4M3) {
+    v.ks = (unsigned char*)c->k_scale; v.vs = (unsigned char*)c->v_scale;
+    v.scale_stride = c->scale_stride ? c->scale_stride : (long)c->n_kv_heads * c->page_size;
+  }
   v.n_pages = c->n_pages; v.page_shift = log2_of(c->page_size); v.n_req = c->n_req; v.max_pages = c->max_pages;
   v.nh = c->n_q_heads; v.nkv = c->n_kv_heads; v.max_rows = c->max_rows;
   v.limit = c->max_pages * c->page_size;
@@ -104,9 +113,17 @@ void launch_paged_append(const PagedView& v, int head_dim, const float* qkv, lon
                          float eps, const float* rope, hipStream_t s) {
   const dim3 grid((unsigned)(((long)v.max_rows * v.nkv + 15) / 16));
   if (head_dim == 128)
-    hipLaunchKernelGGL((paged_append_kernel<CT, 128>), grid, dim3(256), 0, s, qkv, ld, cu, row_pos, (const long long*)slots, (const CT*)gain, (const float2*)rope, eps, v);
+    hipLaunchKernelGGL((paged_append_kernel<CT, 128>), grid, dim3(256), 0, s, qkv, ld, cu, row_pos, (const long long*)slots, (const typename PagedWide<CT>::type*)gain, (const float2*)rope, eps, v);
   else
-    hipLaunchKernelGGL((paged_append_kernel<CT, 64>), grid, dim3(256), 0, s, qkv, ld, cu, row_pos, (const long long*)slots, (const CT*)gain, (const float2*)rope, eps, v);
+    hipLaunchKernelGGL((paged_append_kernel<CT, 64>), grid, dim3(256), 0, s, qkv, ld, cu, row_pos, (const long long*)slots, (const typename PagedWide<CT>::type*)gain, (const float2*)rope, eps, v);
+}
+
+template <typename CT>
+void launch_paged_read(const PagedView& v, int head_dim, const int64_t* slots, int n, void* k_out, void* v_out, long ldo, hipStream_t s) {
+  typedef typename PagedWide<CT>::type GT;
+  const dim3 grid((unsigned)(((long)n * v.nkv + 15) / 16));
+  if (head_dim == 128) hipLaunchKernelGGL((paged_read_kernel<CT, 128>), grid, dim3(256), 0, s, (const long long*)slots, n, (GT*)k_out, (GT*)v_out, ldo, v);
+  else hipLaunchKernelGGL((paged_read_kernel<CT, 64>), grid, dim3(256), 0, s, (const long long*)slots, n, (GT*)k_out, (GT*)v_out, ldo, v);
 }
 
 // How an attention call is laid out: blocks per KV head of either kernel (0: no launch), groups that the merge looks at, log2 of those that the key ranges are chosen
@@ -120,7 +137,7 @@ PagedPlan paged_plan(const dmtd_paged_cache* c, int max_new) {
   PagedPlan p{};
   const int GQ = c->n_q_heads / c->n_kv_heads;
   const long limit = (long)c->max_pages * c->page_size;
-  const bool bf16 = c->dtype == DMTD_DTYPE_BF16;
+  const bool bf16 = c->dtype != DMTD_DTYPE_F32;      // bf16 products
   p.few_shift = floor_log2(std::max((bf16 ? PAGED_SLOTS_FEW : PAGED_SLOTS_FP32) / c->n_kv_heads, 1));
   p.tall_shift = floor_log2(std::max(PAGED_SLOTS_TALL / c->n_kv_heads, 1));
   auto blocks = [&](long groups, int shift, int min_keys) { return (int)std::min((1L << shift) + groups, groups * ((limit + min_keys - 1) / min_keys)); };
@@ -155,7 +172,8 @@ struct PagedCall {
 template <typename CT, int HD, bool PLANES>
 hipError_t launch_paged_attention_t(const PagedView& v, const PagedPlan& p, const PagedCall& a, const PagedOut& out) {
   const int GQ = v.nh / v.nkv;
-  constexpr bool BF = sizeof(CT) == 2;
+  typedef typename PagedWide<CT>::type GT;
+  constexpr bool BF = sizeof(GT) == 2;
   // The two kinds of requests have partial results of their own: they may be under way at the same time
   const PagedWork few{p.few_shift, (int*)a.ws, (float*)(a.ws + p.count_bytes)}, tall{p.tall_shift, nullptr, (float*)(a.ws + p.count_bytes + p.few_bytes)};
   // the queries' parts, then the waves' results, then what the join exchanges
@@ -163,7 +181,7 @@ hipError_t launch_paged_attention_t(const PagedView& v, const PagedPlan& p, cons
   const size_t few_lds = std::max({(size_t)PAGED_WAVES * qv_max * HD * 4, (size_t)16 * (BF ? 2 * (HD + ATT_QPAD) * 2 : (HD + 4) * 4), (size_t)2 * 64 * PAGED_WAVES * 16});
   if constexpr (BF) {
     if (p.tall > 0) {
-      auto kern = paged_attention_both_mfma_kernel<HD, PLANES>;
+      auto kern = paged_attention_both_mfma_kernel<CT, HD, PLANES>;
       const size_t lds = std::max((size_t)4 * 64 * HD * 2 + 1024, few_lds);      // (the rings start at a multiple of 1 KiB)
       static bool big_lds[kMaxDevices];
       const hipError_t e = lds_room(kern, lds, (size_t)4 * 64 * 128 * 2 + 1024, big_lds);
@@ -176,7 +194,7 @@ hipError_t launch_paged_attention_t(const PagedView& v, const PagedPlan& p, cons
       return hipGetLastError();
     }
   }
-  hipLaunchKernelGGL((paged_attention_few_mfma_kernel<CT, HD, PLANES>), paged_grid(v.nkv, p.few), dim3(64 * PAGED_WAVES), few_lds, a.stream, a.cu, a.start, a.qkv, a.ld, (const CT*)a.gain,
+  hipLaunchKernelGGL((paged_attention_few_mfma_kernel<CT, HD, PLANES>), paged_grid(v.nkv, p.few), dim3(64 * PAGED_WAVES), few_lds, a.stream, a.cu, a.start, a.qkv, a.ld, (const GT*)a.gain,
                      (const float2*)a.rope, a.eps, a.max_new, BF ? PAGED_FEW : INT_MAX, out, v, few);
   return hipGetLastError();
 }
@@ -186,6 +204,7 @@ hipError_t launch_paged_attention(const dmtd_paged_cache* c, const PagedView& v,
   const PagedPlan p = paged_plan(c, a.max_new);
   if (c->dtype == DMTD_DTYPE_BF16 && out.lo) return c->head_dim == 128 ? launch_paged_attention_t<bf16_t, 128, true>(v, p, a, out) : launch_paged_attention_t<bf16_t, 64, true>(v, p, a, out);
   if (c->dtype == DMTD_DTYPE_BF16) return c->head_dim == 128 ? launch_paged_attention_t<bf16_t, 128, false>(v, p, a, out) : launch_paged_attention_t<bf16_t, 64, false>(v, p, a, out);
+  if (c->dtype == DMTD_DTYPE_E4M3) return c->head_dim == 128 ? launch_paged_attention_t<e4m3_t, 128, false>(v, p, a, out) : launch_paged_attention_t<e4m3_t, 64, false>(v, p, a, out);
   return c->head_dim == 128 ? launch_paged_attention_t<float, 128, false>(v, p, a, out) : launch_paged_attention_t<float, 64, false>(v, p, a, out);
 }
 
@@ -238,7 +257,25 @@ int dmtd_paged_append(const dmtd_paged_cache* c, const float* qkv, int64_t ld, c
   if ((rc = check_stream_device(s)) != DMTD_OK) return rc;
   const PagedView v = paged_view(c, rope, rope_len);
   if (c->dtype == DMTD_DTYPE_BF16) launch_paged_append<bf16_t>(v, c->head_dim, qkv, ld, cu_rows, row_pos, slots, k_norm, eps, rope, s);
+  else if (c->dtype == DMTD_DTYPE_E4M3) launch_paged_append<e4m3_t>(v, c->head_dim, qkv, ld, cu_rows, row_pos, slots, k_norm, eps, rope, s);
   else launch_paged_append<float>(v, c->head_dim, qkv, ld, cu_rows, row_pos, slots, k_norm, eps, rope, s);
+  return paged_done();
+}
+
+int dmtd_paged_read(const dmtd_paged_cache* c, const int64_t* slots, int32_t n, void* k_out, void* v_out, int64_t ldo, void* stream) {
+  int rc = check_cache(c);
+  if (rc != DMTD_OK) return rc;
+  if (n < 0 || (long)n * c->n_kv_heads > (1L << 30)) return paged_fail(DMTD_EINVAL, "n must not be negative, and at most 2^30 with the KV heads");
+  if (!slots || !aligned(slots, 8)) return paged_fail(DMTD_EINVAL, "slots must be an 8-byte aligned pointer");
+  if (!k_out || !v_out || !aligned(k_out, 16) || !aligned(v_out, 16)) return paged_fail(DMTD_EINVAL, "k_out and v_out must be 16-byte aligned pointers");
+  if (ldo < (int64_t)c->n_kv_heads * c->head_dim || ldo % 8 || ldo > (1 << 24)) return paged_fail(DMTD_EINVAL, "ldo must be a multiple of 8 that holds a row");
+  const hipStream_t s = (hipStream_t)stream;
+  if ((rc = check_stream_device(s)) != DMTD_OK) return rc;
+  if (n == 0) return DMTD_OK;
+  const PagedView v = paged_view(c, nullptr, 0);
+  if (c->dtype == DMTD_DTYPE_BF16) launch_paged_read<bf16_t>(v, c->head_dim, slots, n, k_out, v_out, (long)ldo, s);
+  else if (c->dtype == DMTD_DTYPE_E4M3) launch_paged_read<e4m3_t>(v, c->head_dim, slots, n, k_out, v_out, (long)ldo, s);
+  else launch_paged_read<float>(v, c->head_dim, slots, n, k_out, v_out, (long)ldo, s);
   return paged_done();
 }
 
