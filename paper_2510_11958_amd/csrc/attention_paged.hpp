@@ -313,6 +313,7 @@ __device__ __forceinline__ void paged_attention_few(int y, const int* __restrict
   constexpr int KW = BF ? HD / 32 : HD / 16;                 // pieces of a key in the products: KS, or 8-bit ones widened
   constexpr int VW = DPL * sizeof(GT) / 4;                   // 32-bit words of a value in the products: its DPL dims that a lane carries
   typedef unsigned int vraw_t __attribute__((ext_vector_type(Q8 ? VW / 2 : VW)));
+  typedef unsigned int vwide_t __attribute__((ext_vector_type(VW)));
   typedef float fvec_t __attribute__((ext_vector_type(HL)));
   typedef unsigned short hvec_t __attribute__((ext_vector_type(HL)));
   const int g = blockIdx.x, GQ = pv.gq, rpb = pv.rpb_few;
@@ -389,10 +390,10 @@ __device__ __forceinline__ void paged_attention_few(int y, const int* __restrict
     }
     if (rope_tab) {
 #pragma unroll
-      for (int e = 0; e < HL; ++e) {
+      for (int e = 0; e < HL; ++e) {      // (which product is the rounded one is written out: the compiler's own choice differs from one instantiation to the next)
         const float a = x0[e], b = x1[e];
-        x0[e] = a * cs[e].x - b * cs[e].y;
-        x1[e] = b * cs[e].x + a * cs[e].y;
+        x0[e] = __builtin_fmaf(a, cs[e].x, -(b * cs[e].y));
+        x1[e] = __builtin_fmaf(a, cs[e].y, b * cs[e].x);
       }
     }
     const float scale = rsqrtf((float)HD) * 1.4426950408889634f;
@@ -440,7 +441,7 @@ __device__ __forceinline__ void paged_attention_few(int y, const int* __restrict
     for (int u = 0; u < G; ++u) {
     if (!here[u]) continue;                                   // a page outside the pool, or behind the last key
     const int base = from + 16 * NW * u;
-    uint32_t va[4][VW];                                       // the values, as bf16 or fp32
+    vwide_t va[4];                                            // the values, as bf16 or fp32
     u32x4 ka[KW];
     if constexpr (Q8) {
       const float sk = e8m0_scale(ksc[u]);
@@ -461,9 +462,7 @@ __device__ __forceinline__ void paged_attention_few(int y, const int* __restrict
 #pragma unroll
       for (int t = 0; t < KS; ++t) ka[t] = kc[u][t];
 #pragma unroll
-      for (int m = 0; m < 4; ++m)
-#pragma unroll
-        for (int e = 0; e < VW; ++e) va[m][e] = vc[u][m][e];
+      for (int m = 0; m < 4; ++m) va[m] = vc[u][m];
     }
     f32x4 s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -617,6 +616,7 @@ __device__ __forceinline__ void paged_attention_tall(int y, const int* __restric
   constexpr int TILE = KT * HD;
   constexpr int VR = Q8 ? DV / 4 : DV / 2;              // words of a value as they come from the pool
   typedef unsigned int vraw_t __attribute__((ext_vector_type(VR)));
+  typedef unsigned int vwide_t __attribute__((ext_vector_type(DV / 2)));
   extern __shared__ float4 paged_dyn_smem[];
   __shared__ int poison_s;
   const int g = blockIdx.x, GQ = pv.gq, rpb = pv.rpb_tall;
@@ -657,8 +657,8 @@ __device__ __forceinline__ void paged_attention_tall(int y, const int* __restric
                                      (__attribute__((address_space(3))) void*)(uintptr_t)(ring + (uint32_t)(buf * TILE + (w * KI + i) * 512) * 2), 16, 0, 0);
   };
   // V: 4 keys of a page, DV dims a thread; keys behind the range's last are whatever the page holds there
-  vraw_t vraw[4];
-  uint32_t vr[4][DV / 2];
+  vraw_t vraw[Q8 ? 4 : 1];
+  vwide_t vr[4];
   const CT* vsrc = nullptr;
   auto aim_v = [&](int ln, int base, int page) {
     if constexpr (Q8)
@@ -666,8 +666,11 @@ __device__ __forceinline__ void paged_attention_tall(int y, const int* __restric
     vsrc = (const CT*)pv.v + (size_t)(outside(page) ? 0 : page) * pv.page_stride +
            (uint32_t)(((g << pv.page_shift) + ((base + 4 * (ln & 15)) & in_page)) * HD + (w * 4 + (ln >> 4)) * DV);
   };
-  auto load_v = [&](int m) { vraw[m] = *(const vraw_t*)(vsrc + m * HD); };
-  // what has been loaded, as bf16: the values in registers, 8-bit keys in LDS, as the direct loads of bf16 keys leave them
+  auto load_v = [&](int m) {
+    if constexpr (Q8) vraw[m] = *(const vraw_t*)(vsrc + m * HD);
+    else vr[m] = *(const vwide_t*)(vsrc + m * HD);
+  };
+  // 8-bit pools: what has been loaded, as bf16: the values in registers, the keys in LDS, as the direct loads of bf16 keys leave them
   auto widen = [&](int ln, int buf) {
     if constexpr (Q8) {
 #pragma unroll
@@ -687,11 +690,6 @@ __device__ __forceinline__ void paged_attention_tall(int y, const int* __restric
 #pragma unroll
         for (int u = 0; u < VR; ++u) { vr[m][2 * u] = e4m3_pair<false>(vraw[m][u], sv); vr[m][2 * u + 1] = e4m3_pair<true>(vraw[m][u], sv); }
       }
-    } else {
-#pragma unroll
-      for (int m = 0; m < 4; ++m)
-#pragma unroll
-        for (int u = 0; u < DV / 2; ++u) vr[m][u] = vraw[m][u];
     }
   };
   // values of pages outside the pool and of keys behind the last become 0; so do those from poison_s on that are not finite
