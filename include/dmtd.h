@@ -338,6 +338,12 @@ typedef struct dmtd_page_pool {
 int dmtd_page_tables(const dmtd_page_pool* pool, const int32_t* start, const int32_t* rows, int32_t max_rows, int32_t* cu_rows, int32_t* row_pos,
                      int64_t* slots, int32_t* status, void* stream);
 
+/* The same where requests share pages: shared[i] (DEVICE int32 [n_req]; NULL: as dmtd_page_tables) is the number of pages at the front of request i's table that another one holds and that
+ * request i reads only.  The caller writes them into the table, counted in held[i]; they are never given back by request i, which keeps at least these: start = rows = 0 gives back
+ * the others.  A shared[i] that is negative or above held[i]: status as for lengths that do not fit, DMTD_EINVAL and i.  Whoever holds the pages for good (shared 0) keeps them as long as another reads them. */
+int dmtd_page_tables_shared(const dmtd_page_pool* pool, const int32_t* start, const int32_t* rows, const int32_t* shared, int32_t max_rows, int32_t* cu_rows,
+                            int32_t* row_pos, int64_t* slots, int32_t* status, void* stream);
+
 typedef struct dmtd_paged_cache {
   void*    k;              /* DEVICE [n_pages][n_kv_heads][page_size][head_dim] of dtype, 16-byte aligned */
   void*    v;              /* DEVICE, as k */
@@ -388,6 +394,40 @@ size_t dmtd_paged_workspace_bytes(const dmtd_paged_cache* cache);
 int dmtd_paged_attention(const dmtd_paged_cache* cache, const float* qkv, int64_t ld, const int32_t* start, const int32_t* cu_rows, int32_t max_new,
                          const void* q_norm, float eps, const float* rope, int32_t rope_len, void* out, int64_t ldo, void* workspace,
                          size_t workspace_bytes, void* stream);
+
+/* ---- Shared prefixes ----
+ * Attention of a step where groups of requests start with the same pages (a system prompt, a document that many ask about): each shared key and value is read once for many rows of the group
+ * instead of once per request.  Block tables, lengths, rows, positions and places are those of the calls above, and so are the results, up to the rounding of other sums: a
+ * request's table holds all of its pages, the shared ones in front.  dmtd_shared_plan_build once a step, then dmtd_paged_attention_shared per layer. */
+
+typedef struct dmtd_shared_plan {
+  int32_t n_groups;        /* groups, at most 8192 */
+  int32_t positions;       /* angles in the rotary table, which positions are then kept below; 0: as many as the block table has places for */
+  void*   plan;            /* DEVICE, 256-byte aligned, dmtd_shared_plan_bytes; zeroed once before its first use (of a plan that holds nothing the attention does nothing) */
+  size_t  plan_bytes;
+  void*   workspace;       /* DEVICE, 256-byte aligned, dmtd_shared_workspace_bytes; any content.  Attention calls that may overlap need one each */
+  size_t  workspace_bytes;
+} dmtd_shared_plan;
+
+/* Bytes of either; 0 if the cache (its pointers are checked too) or n_groups is invalid. */
+size_t dmtd_shared_plan_bytes(const dmtd_paged_cache* cache, int32_t n_groups);
+size_t dmtd_shared_workspace_bytes(const dmtd_paged_cache* cache);
+
+/* Lays out a step's attention in plan->plan, for all caches of one layout (block table, heads, page size, max_rows; bf16 and e4m3 caches are alike, fp32 ones are not).
+ * start: DEVICE int32 [n_req]; cu_rows: DEVICE int32 [n_req + 1], ascending from 0 on; as in dmtd_paged_attention.
+ * group: DEVICE int32 [n_req], a request's group, or any number outside [0, n_groups): none.  Requests of a group may stand in any order among others.
+ * prefix_pages: DEVICE int32 [n_groups], the pages that the tables of all of a group's requests start with.  A request with fewer cached tokens than these pages hold (start[i] < prefix_pages * page_size)
+ * goes by itself, as one without a group does; so do the requests of a group whose prefix_pages does not fit the block table.  The table of any one of the others is read for all of them.
+ * The plan holds until it is built again; it does not follow changes of start, cu_rows, group or prefix_pages (of the pages in block_table it does).
+ * Errors: DMTD_EINVAL, DMTD_ECAPACITY, DMTD_EHIP. */
+int dmtd_shared_plan_build(const dmtd_paged_cache* cache, const dmtd_shared_plan* plan, const int32_t* start, const int32_t* cu_rows, const int32_t* group, const int32_t* prefix_pages,
+                           void* stream);
+
+/* The attention of a plan's step: qkv, q_norm, eps, rope, out and what is said of rows, requests and values there as for dmtd_paged_attention; rope_len at least plan->positions (or the block
+ * table's places).  A plan of another layout leaves out as it was.  Results do not depend on the order in which workgroups run.
+ * Errors: DMTD_EINVAL, DMTD_ECAPACITY, DMTD_EHIP. */
+int dmtd_paged_attention_shared(const dmtd_paged_cache* cache, const dmtd_shared_plan* plan, const float* qkv, int64_t ld, const void* q_norm, float eps, const float* rope, int32_t rope_len,
+                                void* out, int64_t ldo, void* stream);
 
 /* ---- Paged steps of a context ----
  * Requests that come and go, over a context's model: the memory of its caches (max_batch x max_seq_len positions a layer) becomes a pool of pages, and each step takes

@@ -38,6 +38,10 @@ class _PagedCache(C.Structure):
         ("k_scale", C.c_void_p), ("v_scale", C.c_void_p), ("scale_stride", C.c_int64)]
 
 
+class _SharedPlan(C.Structure):
+    _fields_ = [("n_groups", C.c_int32), ("positions", C.c_int32), ("plan", C.c_void_p), ("plan_bytes", C.c_size_t), ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t)]
+
+
 class DmtdError(RuntimeError):
     def __init__(self, code: int, msg: str):
         super().__init__(f"{_CODES.get(code, code)}: {msg}")
@@ -119,6 +123,16 @@ def load_library():
     lib.dmtd_paged_get_state.argtypes = [C.c_void_p, C.c_int32, P(C.c_int32), P(C.c_int32), P(C.c_int32)]
     lib.dmtd_page_tables.restype = C.c_int
     lib.dmtd_page_tables.argtypes = [P(_PagePool), C.c_void_p, C.c_void_p, C.c_int32] + [C.c_void_p] * 5
+    lib.dmtd_page_tables_shared.restype = C.c_int
+    lib.dmtd_page_tables_shared.argtypes = [P(_PagePool), C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32] + [C.c_void_p] * 5
+    lib.dmtd_shared_plan_bytes.restype = C.c_size_t
+    lib.dmtd_shared_plan_bytes.argtypes = [P(_PagedCache), C.c_int32]
+    lib.dmtd_shared_workspace_bytes.restype = C.c_size_t
+    lib.dmtd_shared_workspace_bytes.argtypes = [P(_PagedCache)]
+    lib.dmtd_shared_plan_build.restype = C.c_int
+    lib.dmtd_shared_plan_build.argtypes = [P(_PagedCache), P(_SharedPlan)] + [C.c_void_p] * 5
+    lib.dmtd_paged_attention_shared.restype = C.c_int
+    lib.dmtd_paged_attention_shared.argtypes = [P(_PagedCache), P(_SharedPlan), C.c_void_p, C.c_int64, C.c_void_p, C.c_float, C.c_void_p, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p]
     lib.dmtd_paged_append.restype = C.c_int
     lib.dmtd_paged_append.argtypes = [P(_PagedCache), C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_float,
                                       C.c_void_p, C.c_int32, C.c_void_p]
@@ -502,13 +516,15 @@ class PageTables(_OnDevice):
         return cls(torch.full((n_req, max_pages), -1, dtype=torch.int32, device=device), torch.zeros(n_req, dtype=torch.int32, device=device), free,
                    torch.full((1,), n_pages, dtype=torch.int32, device=device), page_size)
 
-    def build(self, start, rows, cu_rows, row_pos, slots, status):
+    def build(self, start, rows, cu_rows, row_pos, slots, status, shared=None):
         """Pages and places for a step: request i has ``start[i]`` tokens and brings ``rows[i]``.  Writes ``cu_rows`` int32 ``[n_req + 1]``, ``row_pos`` int32
-        ``[max_rows]``, ``slots`` int64 ``[max_rows]`` and ``status`` int32 ``[2]`` (0, or why the step has no rows: see the header)."""
+        ``[max_rows]``, ``slots`` int64 ``[max_rows]`` and ``status`` int32 ``[2]`` (0, or why the step has no rows: see the header).  ``shared`` int32 ``[n_req]``: the pages at the
+        front of each request's table that another one holds (``dmtd_page_tables_shared``): they stay where they are, and are not given back."""
         i32, dev = self._i32, self._index
         room = row_pos.shape
-        self._call(self._lib.dmtd_page_tables, self._p, _want(start, "start", i32, dev, self._per_req), _want(rows, "rows", i32, dev, self._per_req), room[0] if len(room) == 1 else 0,
-                   _want(cu_rows, "cu_rows", i32, dev, self._per_end), _want(row_pos, "row_pos", i32, dev, room), _want(slots, "slots", self._i64, dev, room),
+        front = None if shared is None else _want(shared, "shared", i32, dev, self._per_req)
+        self._call(self._lib.dmtd_page_tables_shared, self._p, _want(start, "start", i32, dev, self._per_req), _want(rows, "rows", i32, dev, self._per_req), front,
+                   room[0] if len(room) == 1 else 0, _want(cu_rows, "cu_rows", i32, dev, self._per_end), _want(row_pos, "row_pos", i32, dev, room), _want(slots, "slots", self._i64, dev, room),
                    _want(status, "status", i32, dev, (2,)))
 
 
@@ -591,6 +607,21 @@ class PagedCache(_OnDevice):
             raise ValueError("rope must hold a position")
         return qkv.data_ptr(), ld, gain, _want(rope, "rope", self._f32, dev, (n, *self._angles)), n
 
+    def _out(self, out):
+        """The output rows, made if they are not given, and the elements from one to the next."""
+        if out is None:
+            out = self._torch.empty(self.max_rows, *self._q_heads, dtype=self.dtype, device=self.device)
+        shape = out.shape
+        if (len(shape) != 3 or shape[1:] != self._q_heads or shape[0] < self.max_rows or out.dtype is not self.dtype or out.get_device() != self._index or
+                out.stride(2) != 1 or (shape[1] > 1 and out.stride(1) != shape[2])):
+            raise ValueError(f"out must be {self.dtype} [at least {self.max_rows}, {self._q_heads[0]}, {self._q_heads[1]}] on GPU {self._index} with contiguous rows")
+        return out, out.stride(0) if shape[0] > 1 else self._q_cols
+
+    def _layout(self):
+        """What a plan of shared prefixes depends on."""
+        c = self._c
+        return (self._index, c.n_req, c.max_pages, c.page_size, c.n_q_heads, c.n_kv_heads, c.head_dim, c.dtype == 0, c.max_rows)
+
     def append(self, qkv, cu_rows, row_pos, slots, k_norm=None, rope=None, eps: float = 1e-6):
         """Keys (normalised with ``k_norm``, rotated by ``rope`` [positions, head_dim / 2, (cos, sin)]) and values of the fused projection's rows
         ``qkv`` into the places that :meth:`PageTables.build` gave them."""
@@ -619,15 +650,56 @@ class PagedCache(_OnDevice):
         the last one are not written).  ``max_new``: the most rows one request brings, if known."""
         x, ld, gain, tab, n_tab = self._rows(qkv, self._q_cols, q_norm, rope)
         i32, dev = self._i32, self._index
-        if out is None:
-            out = self._torch.empty(self.max_rows, *self._q_heads, dtype=self.dtype, device=self.device)
-        shape = out.shape
-        if (len(shape) != 3 or shape[1:] != self._q_heads or shape[0] < self.max_rows or out.dtype is not self.dtype or out.get_device() != dev or
-                out.stride(2) != 1 or (shape[1] > 1 and out.stride(1) != shape[2])):
-            raise ValueError(f"out must be {self.dtype} [at least {self.max_rows}, {self._q_heads[0]}, {self._q_heads[1]}] on GPU {dev} with contiguous rows")
+        out, ldo = self._out(out)
         stream = self._call(self._lib.dmtd_paged_attention, self._p, x, ld, _want(start, "start", i32, dev, self._per_req), _want(cu_rows, "cu_rows", i32, dev, self._per_end),
-                            max_new, gain, eps, tab, n_tab, out.data_ptr(), out.stride(0) if shape[0] > 1 else self._q_cols, self._ws_ptr, self._ws_bytes)
+                            max_new, gain, eps, tab, n_tab, out.data_ptr(), ldo, self._ws_ptr, self._ws_bytes)
         if stream not in self._streams:
             self._streams.add(stream)
             self._ws.record_stream(self._torch.cuda.current_stream(self._index))      # the workspace is not reused before this stream's work has ended
         return out
+
+    def attention_shared(self, plan, qkv, out=None, q_norm=None, rope=None, eps: float = 1e-6):
+        """The attention of the step that ``plan`` (:class:`SharedPlan`, of this handle's layout) was built for; ``qkv``, ``out``, ``q_norm``, ``rope`` and ``eps`` as for
+        :meth:`attention`."""
+        if plan._layout != self._layout():
+            raise ValueError("the plan was made for caches of another layout, or on another GPU")
+        x, ld, gain, tab, n_tab = self._rows(qkv, self._q_cols, q_norm, rope)
+        out, ldo = self._out(out)
+        stream = self._call(self._lib.dmtd_paged_attention_shared, self._p, plan._p, x, ld, gain, eps, tab, n_tab, out.data_ptr(), ldo)
+        plan._used_on(stream)
+        return out
+
+
+class SharedPlan(_OnDevice):
+    """How a step's attention is laid out where groups of requests start with the same pages (``dmtd_shared_plan_build``), for ``cache`` and all handles of its layout (those of the
+    other layers; bfloat16 and 8-bit caches are alike).  ``n_groups``: the most groups; ``positions``: how many the rotary table has angles for, if they are fewer than the block
+    table's places.  Holds the memory of the plan and of the attention's partial results: attention calls that use it must not overlap, nor overlap :meth:`build`."""
+
+    def __init__(self, cache: PagedCache, n_groups: int, positions: int = 0):
+        self._open(cache.k)
+        torch, lib = self._torch, self._lib
+        self._layout, self._cache, self.n_groups = cache._layout(), cache, int(n_groups)
+        nbytes, room = lib.dmtd_shared_plan_bytes(cache._p, self.n_groups), lib.dmtd_shared_workspace_bytes(cache._p)
+        if nbytes == 0 or room == 0:
+            _raise(lib, DMTD_EINVAL)
+        if positions < 0:
+            raise ValueError("positions must not be negative")
+        self._memory, self._ws = torch.zeros(nbytes, dtype=torch.uint8, device=self.device), torch.empty(room, dtype=torch.uint8, device=self.device)
+        self._c = _SharedPlan(self.n_groups, int(positions), self._memory.data_ptr(), nbytes, self._ws.data_ptr(), room)
+        self._p = C.byref(self._c)
+        stream = torch.cuda.current_stream(self.device)
+        stream.synchronize()              # zeroed, whichever stream the first call is on
+        self._streams = {stream.cuda_stream}
+
+    def _used_on(self, stream):
+        if stream not in self._streams:
+            self._streams.add(stream)
+            for t in (self._memory, self._ws):
+                t.record_stream(self._torch.cuda.current_stream(self._index))      # not reused before this stream's work has ended
+
+    def build(self, start, cu_rows, group, prefix_pages):
+        """A step's plan: ``start`` int32 ``[n_req]`` and ``cu_rows`` int32 ``[n_req + 1]`` as for :meth:`PagedCache.attention`, ``group`` int32 ``[n_req]`` (outside ``[0, n_groups)``: none),
+        ``prefix_pages`` int32 ``[n_groups]``, the pages that the tables of a group's requests start with."""
+        c, i32, dev = self._cache, self._i32, self._index
+        self._used_on(self._call(self._lib.dmtd_shared_plan_build, c._p, self._p, _want(start, "start", i32, dev, c._per_req), _want(cu_rows, "cu_rows", i32, dev, c._per_end),
+                                 _want(group, "group", i32, dev, c._per_req), _want(prefix_pages, "prefix_pages", i32, dev, (self.n_groups,))))

@@ -65,6 +65,18 @@ struct PagedWork {
 // the range's number of n of its group; where partial results and the count lie (in slots of all KV heads)
 struct PagedItem { int req, first, row0, r, pos0, kb, ke, split, n, slot, group; };
 
+// A block's share of a step with shared prefixes, as its plan holds it (attention_shared.hpp): keys kb .. ke - 1 of the table of request `req`; the rows list[row0] .. list[row0 + r - 1],
+// each (row, position); row j sees the keys up to pos0 + j (step 1) or all of them up to pos0 (step 0).  unit: where row 0's partial results go, -1: to the output.
+struct SharedItem { int req, row0, r, pos0, kb, ke, unit, step; };
+// What the blocks of such a step share: the rows' list, and room for partial results: per unit the sums of all query heads, then their (maximum, sum of weights)
+struct SharedParts {
+  const int2* list;
+  float* part;
+  long unit_floats;
+  __device__ __forceinline__ float* sums(int unit, int head, int hd) const { return part + (size_t)unit * unit_floats + (size_t)head * hd; }
+  __device__ __forceinline__ float* weights(int unit, int nh, int head, int hd) const { return part + (size_t)unit * unit_floats + (size_t)nh * hd + 2 * head; }
+};
+
 // The tall kernel's order of n items per KV head.  A chunk's later groups see more keys.  Up to PAGED_RESIDENT_TALL blocks are all resident from the start, two
 // on a CU: the first round of the CUs goes from the longest down, the second from the shortest up, and a CU's two come to about the same.
 // More blocks than that start as others end, longest first.
@@ -299,10 +311,10 @@ __device__ __forceinline__ void paged_store4(const PagedOut& o, int row, int col
 // them / both: 3 rows of 8 requests behind 16384 102 / 84 / 91, 31 ragged rows in pages of 16 tokens 23 / 25 / 30, out of cold memory 29 / 28 / 30, one row of 64
 // behind 1024 out of cold memory 54 / 49 / 48).
 // Bound by the memory: 8 KiB per wave and group against PAGED_PARTS x HD / 16 + 2 x HD / 32 products.
-template <typename CT, int HD, bool PLANES>
-__device__ __forceinline__ void paged_attention_few(int y, const int* __restrict__ cu, const int* __restrict__ start, const float* __restrict__ qkv, long ld,
-                                                    const typename PagedWide<CT>::type* __restrict__ q_gain, const float2* __restrict__ rope_tab, float eps, int max_new, int hi, const PagedOut& po,
-                                                    const PagedView& pv, const PagedWork& wk) {
+// SHARED: `it` is a SharedItem, and partial results go where it says.
+template <typename CT, int HD, bool PLANES, bool SHARED, typename ITEM>
+__device__ __forceinline__ void paged_few_item(const ITEM& it, int g, const int tid, const float* __restrict__ qkv, long ld, const typename PagedWide<CT>::type* __restrict__ q_gain,
+                                               const float2* __restrict__ rope_tab, float eps, const PagedOut& po, const PagedView& pv, const PagedWork& wk, const SharedParts& sp) {
   typedef typename PagedWide<CT>::type GT;
   constexpr bool BF = sizeof(GT) == 2, Q8 = sizeof(CT) == 1;
   constexpr int PARTS = PAGED_PARTS<PLANES>;
@@ -316,10 +328,8 @@ __device__ __forceinline__ void paged_attention_few(int y, const int* __restrict
   typedef unsigned int vwide_t __attribute__((ext_vector_type(VW)));
   typedef float fvec_t __attribute__((ext_vector_type(HL)));
   typedef unsigned short hvec_t __attribute__((ext_vector_type(HL)));
-  const int g = blockIdx.x, GQ = pv.gq, rpb = pv.rpb_few;
-  PagedItem it;
-  if (!paged_find<NT, 16 * NW, false>(pv, cu, start, max_new, GQ, 0, hi, rpb, wk.shift, PAGED_KEYS_FEW, y, it)) return;
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), sl = lane & 15, kq = lane >> 4;
+  const int GQ = pv.gq;
+  const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), sl = lane & 15, kq = lane >> 4;
   const int QV = it.r * GQ, ke = it.ke;
   __shared__ float wm[NW][QVT], wl[NW][QVT];
   __shared__ int poison_s;
@@ -339,9 +349,12 @@ __device__ __forceinline__ void paged_attention_few(int y, const int* __restrict
   GT g0[HL], g1[HL];
   {
     // what it needs is asked for in front of the keys, whose arrival it is made ready beside
-    const float* src = qkv + (size_t)(it.first + qrow) * ld + (size_t)qhead * HD + HL * l16;
+    int row, pos;
+    if constexpr (SHARED) { const int2 rp = sp.list[qrow]; row = rp.x; pos = rp.y; }
+    else { row = it.first + qrow; pos = it.pos0 + qr; }
+    const float* src = qkv + (size_t)row * ld + (size_t)qhead * HD + HL * l16;
     xa = *(const fvec_t*)src; xb = *(const fvec_t*)(src + half);
-    const float2* rp = rope_tab + (size_t)(it.pos0 + qr) * half + HL * l16;
+    const float2* rp = rope_tab + (size_t)pos * half + HL * l16;
 #pragma unroll
     for (int e = 0; e < HL; ++e) {
       cs[e] = rope_tab ? rp[e] : make_float2(1.f, 0.f);
@@ -413,7 +426,8 @@ __device__ __forceinline__ void paged_attention_few(int y, const int* __restrict
     }
   }
   __syncthreads();
-  const int my_pos = it.pos0 + pv.row_of(sl);
+  int my_pos = it.pos0 + pv.row_of(sl);
+  if constexpr (SHARED) my_pos = it.step ? my_pos : it.pos0;
   float m_run = -INFINITY, l_run = 0.f;
   f32x4 acc[DPL];
 #pragma unroll
@@ -559,10 +573,20 @@ __device__ __forceinline__ void paged_attention_few(int y, const int* __restrict
   }
   __syncthreads();
   constexpr size_t SLOT = (size_t)QVT * (HD + 2);
-  float* part = wk.part + ((size_t)(it.slot + it.split) * pv.nkv + g) * SLOT;
+  float* part = nullptr;
+  bool whole;
+  if constexpr (SHARED) {
+    whole = it.unit < 0;
+  } else {
+    part = wk.part + ((size_t)(it.slot + it.split) * pv.nkv + g) * SLOT;
+    whole = it.n == 1;
+  }
   auto store = [&](int v, int d, const f32x4& x) {
     const int r = pv.row_of(v);
-    paged_store4<GT, PLANES>(po, it.first + it.row0 + r, (g * GQ + v - r * GQ) * HD + d, x);
+    int row;
+    if constexpr (SHARED) row = sp.list[it.row0 + r].x;
+    else row = it.first + it.row0 + r;
+    paged_store4<GT, PLANES>(po, row, (g * GQ + v - r * GQ) * HD + d, x);
   };
   for (int e = tid; e < QV * (HD / 4); e += NT) {
     const int v = e / (HD / 4), d = (e % (HD / 4)) * 4;
@@ -579,15 +603,31 @@ __device__ __forceinline__ void paged_attention_few(int y, const int* __restrict
       l += fw * wl[w][v];
     }
     if (it.pos0 + pv.row_of(v) >= poison_s) l = __uint_as_float(0x7FC00000u);
-    if (it.n == 1) {
+    if (whole) {
       const float inv = l == 0.f ? 0.f : 1.0f / l;
       store(v, d, f32x4{o.x * inv, o.y * inv, o.z * inv, o.w * inv});
+    } else if constexpr (SHARED) {
+      const int r = pv.row_of(v), head = g * GQ + v - r * GQ;
+      *(f32x4*)(sp.sums(it.unit + r, head, HD) + d) = o;
+      if (d == 0) *(float2*)sp.weights(it.unit + r, pv.nh, head, HD) = make_float2(mm, l);
     } else {
       put_through4(part + (size_t)v * HD + d, o);
       if (d == 0) put_through(part + (size_t)QVT * HD + 2 * v, mm, l);
     }
   }
-  if (it.n > 1) paged_join<HD, QVT, NT>(wk, it, pv.nkv, g, QV, (f32x4*)paged_dyn_smem, store);
+  if constexpr (!SHARED) {
+    if (it.n > 1) paged_join<HD, QVT, NT>(wk, it, pv.nkv, g, QV, (f32x4*)paged_dyn_smem, store);
+  }
+}
+
+template <typename CT, int HD, bool PLANES>
+__device__ __forceinline__ void paged_attention_few(int y, const int* __restrict__ cu, const int* __restrict__ start, const float* __restrict__ qkv, long ld,
+                                                    const typename PagedWide<CT>::type* __restrict__ q_gain, const float2* __restrict__ rope_tab, float eps, int max_new, int hi, const PagedOut& po,
+                                                    const PagedView& pv, const PagedWork& wk) {
+  constexpr int NW = PAGED_WAVES, NT = 64 * NW;
+  PagedItem it;
+  if (!paged_find<NT, 16 * NW, false>(pv, cu, start, max_new, pv.gq, 0, hi, pv.rpb_few, wk.shift, PAGED_KEYS_FEW, y, it)) return;
+  paged_few_item<CT, HD, PLANES, false>(it, blockIdx.x, threadIdx.x, qkv, ld, q_gain, rope_tab, eps, po, pv, wk, SharedParts{});
 }
 
 // Requests with many query vectors (chunks of a prompt).  A block takes 128 vectors of one KV head - 128 / GQ rows x the GQ query heads that share it, 32 per
@@ -601,10 +641,9 @@ __device__ __forceinline__ void paged_attention_few(int y, const int* __restrict
 // The products run over whole tiles, with probability 0 for keys that a row does not see.  Values behind the block's last key go into LDS as 0.  Values of its
 // own positions may be infinite or NaN, which 0 does not silence: the block looks at them first; if one is not finite, it and its like behind
 // it go into LDS as 0 and the rows that see it become NaN.
-template <typename CT, int HD, bool PLANES>
-__device__ __forceinline__ void paged_attention_tall(int y, const int* __restrict__ cu, const int* __restrict__ start, const float* __restrict__ qkv, long ld,
-                                                     const bf16_t* __restrict__ q_gain, const float2* __restrict__ rope_tab, float eps, int max_new, int lo, const PagedOut& po,
-                                                     const PagedView& pv, const PagedWork& wk) {
+template <typename CT, int HD, bool PLANES, bool SHARED, typename ITEM>
+__device__ __forceinline__ void paged_tall_item(const ITEM& it, int g, const int tid, const float* __restrict__ qkv, long ld, const bf16_t* __restrict__ q_gain,
+                                                const float2* __restrict__ rope_tab, float eps, const PagedOut& po, const PagedView& pv, const PagedWork& wk, const SharedParts& sp) {
   constexpr int PARTS = PAGED_PARTS<PLANES>;
   constexpr int QVT = 128, NT = 256, KT = 64;
   constexpr int T = HD / 16;           // steps over d for the scores
@@ -619,10 +658,8 @@ __device__ __forceinline__ void paged_attention_tall(int y, const int* __restric
   typedef unsigned int vwide_t __attribute__((ext_vector_type(DV / 2)));
   extern __shared__ float4 paged_dyn_smem[];
   __shared__ int poison_s;
-  const int g = blockIdx.x, GQ = pv.gq, rpb = pv.rpb_tall;
-  PagedItem it;
-  if (!paged_find<NT, KT, false, true>(pv, cu, start, max_new, GQ, lo, INT_MAX, rpb, wk.shift, PAGED_KEYS_TALL, y, it)) return;
-  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), hi = lane >> 5;
+  const int GQ = pv.gq;
+  const int lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), hi = lane >> 5;
   // LDS by byte address: K, K, V^T, V^T from a multiple of 1 KiB on, so that a permuted piece's address is the row's with bits exclusive-or'ed in
   typedef __attribute__((address_space(3))) char lds_char;
   typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
@@ -631,7 +668,17 @@ __device__ __forceinline__ void paged_attention_tall(int y, const int* __restric
   const uint32_t ring = ((uint32_t)(uintptr_t)(lds_char*)(char*)paged_dyn_smem + 1023u) & ~1023u;
   const int QV = it.r * GQ, qv = 32 * w + (lane & 31), kb = it.kb, ke = it.ke;
   const bool valid = qv < QV;
-  const int qr = pv.row_of(valid ? qv : 0), row = it.row0 + qr, head = g * GQ + (valid ? qv - qr * GQ : 0), my_pos = it.pos0 + (row - it.row0);
+  const int qr = pv.row_of(valid ? qv : 0), row = it.row0 + qr, head = g * GQ + (valid ? qv - qr * GQ : 0);
+  int my_pos = it.pos0 + (row - it.row0), qkv_row, rope_pos;
+  if constexpr (SHARED) {
+    const int2 rp = sp.list[row];
+    qkv_row = rp.x;
+    rope_pos = rp.y;
+    my_pos = it.step ? my_pos : it.pos0;
+  } else {
+    qkv_row = it.first + row;
+    rope_pos = my_pos;
+  }
   const int* trow = pv.table + (size_t)it.req * pv.max_pages;
   const int in_page = (1 << pv.page_shift) - 1;
 
@@ -640,14 +687,13 @@ __device__ __forceinline__ void paged_attention_tall(int y, const int* __restric
   auto outside = [&](int page) { return page < 0 || page >= pv.n_pages; };
   // K: piece i of the wave's 16 keys holds 64 / CH of them, a chunk of one per lane, permuted by the key number
   u32x4 kraw[Q8 ? KI : 1];
-  uint32_t kscale[Q8 ? KI : 1], vscale = 0;
+  uint32_t kscale = 0, vscale = 0;      // 8 bits: the scales of keys 4 (lane % 16) .. + 3 of the tile
   auto load_k = [&](int ln, int base, int page, int buf, int i) {
     if constexpr (Q8) {      // codes: into registers, 16 of one key a lane; store_k widens them into LDS
       const int pg = __builtin_amdgcn_readlane(page, 4 * w), key = (i * 64 + ln) / (HD / 16);
       const size_t p = outside(pg) ? 0 : pg;
       const uint32_t row = (g << pv.page_shift) + ((base + 16 * w) & in_page) + key;
       kraw[i] = *(const u32x4*)((const unsigned char*)pv.k + p * pv.page_stride + (size_t)row * HD + (ln % (HD / 16)) * 16);
-      kscale[i] = pv.ks[p * pv.scale_stride + row];
       return;
     }
     static_assert(64 / CH <= CH && (Q8 ? 2 : 1) * KI * (64 / CH) == 16, "a wave's pieces are 16 keys, and a piece's permutation is that of piece 0, exclusive-or its first key");
@@ -661,8 +707,11 @@ __device__ __forceinline__ void paged_attention_tall(int y, const int* __restric
   vwide_t vr[4];
   const CT* vsrc = nullptr;
   auto aim_v = [&](int ln, int base, int page) {
-    if constexpr (Q8)
-      vscale = *(const uint32_t*)(pv.vs + (size_t)(outside(page) ? 0 : page) * pv.scale_stride + (uint32_t)((g << pv.page_shift) + ((base + 4 * (ln & 15)) & in_page)));
+    if constexpr (Q8) {
+      const size_t sc = (size_t)(outside(page) ? 0 : page) * pv.scale_stride + (uint32_t)((g << pv.page_shift) + ((base + 4 * (ln & 15)) & in_page));
+      kscale = *(const uint32_t*)(pv.ks + sc);
+      vscale = *(const uint32_t*)(pv.vs + sc);
+    }
     vsrc = (const CT*)pv.v + (size_t)(outside(page) ? 0 : page) * pv.page_stride +
            (uint32_t)(((g << pv.page_shift) + ((base + 4 * (ln & 15)) & in_page)) * HD + (w * 4 + (ln >> 4)) * DV);
   };
@@ -676,7 +725,7 @@ __device__ __forceinline__ void paged_attention_tall(int y, const int* __restric
 #pragma unroll
       for (int i = 0; i < KI; ++i) {
         const int key = 16 * w + (i * 64 + ln) / (HD / 16), c = 2 * (ln % (HD / 16));
-        const float sk = e8m0_scale(kscale[i]);
+        const float sk = e8m0_scale(((uint32_t)__shfl((int)kscale, key >> 2, 64) >> (8 * (key & 3))) & 0xFFu);
         const uint32_t at = ring + (uint32_t)(buf * TILE + key * HD) * 2;
         uint32_t x[8];
 #pragma unroll
@@ -730,7 +779,7 @@ __device__ __forceinline__ void paged_attention_tall(int y, const int* __restric
   bf16x8_t qh[T], ql[T];
   {
     float x[T][8];
-    const float* src = qkv + (size_t)(it.first + row) * ld + (size_t)head * HD + 8 * hi;
+    const float* src = qkv + (size_t)qkv_row * ld + (size_t)head * HD + 8 * hi;
     float ss = 0.f;
 #pragma unroll
     for (int t = 0; t < T; ++t) {
@@ -760,7 +809,7 @@ __device__ __forceinline__ void paged_attention_tall(int y, const int* __restric
       }
     }
     if (rope_tab) {
-      const float2* rp = rope_tab + (size_t)my_pos * (HD / 2) + 8 * hi;
+      const float2* rp = rope_tab + (size_t)rope_pos * (HD / 2) + 8 * hi;
 #pragma unroll
       for (int t = 0; t < T / 2; ++t)
 #pragma unroll
@@ -952,8 +1001,26 @@ __device__ __forceinline__ void paged_attention_tall(int y, const int* __restric
   // where the vector goes, worked out anew: kept through the loop it would be spilled
   int ln = lane;
   asm volatile("" : "+v"(ln));
-  const int qo = 32 * w + (ln & 31), qor = pv.row_of(qo), ro = it.row0 + qor, co = (g * GQ + qo - qor * GQ) * HD + 4 * (ln >> 5);
+  const int qo = 32 * w + (ln & 31), qor = pv.row_of(qo), ro = it.row0 + qor, ho = g * GQ + qo - qor * GQ, co = ho * HD + 4 * (ln >> 5);
   if (it.pos0 + qor >= poison) l_run = __uint_as_float(0x7FC00000u);
+  if constexpr (SHARED) {
+    if (qo < QV && it.unit >= 0) {
+      float* sums = sp.sums(it.unit + qor, ho, HD) + 4 * (ln >> 5);
+#pragma unroll
+      for (int t = 0; t < DT; ++t)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) *(f32x4*)(sums + 32 * t + 8 * q) = f32x4{acc[t][4 * q], acc[t][4 * q + 1], acc[t][4 * q + 2], acc[t][4 * q + 3]};
+      if (ln < 32) *(float2*)sp.weights(it.unit + qor, pv.nh, ho, HD) = make_float2(m_run, l_run);
+    } else if (qo < QV) {
+      const float inv = l_run == 0.f ? 0.f : 1.0f / l_run;
+      const int to = sp.list[ro].x;
+#pragma unroll
+      for (int t = 0; t < DT; ++t)
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          paged_store4<bf16_t, PLANES>(po, to, co + 32 * t + 8 * q, f32x4{acc[t][4 * q] * inv, acc[t][4 * q + 1] * inv, acc[t][4 * q + 2] * inv, acc[t][4 * q + 3] * inv});
+    }
+  } else {
   constexpr size_t SLOT = (size_t)QVT * (HD + 2);
   if (it.n == 1) {
     if (qo < QV) {
@@ -974,6 +1041,16 @@ __device__ __forceinline__ void paged_attention_tall(int y, const int* __restric
       for (int q = 0; q < 4; ++q) *(f32x4*)(part + (size_t)qo * HD + 32 * t + 8 * q + 4 * (ln >> 5)) = f32x4{acc[t][4 * q], acc[t][4 * q + 1], acc[t][4 * q + 2], acc[t][4 * q + 3]};
     if (ln < 32) *(float2*)(part + (size_t)QVT * HD + 2 * qo) = make_float2(m_run, l_run);
   }
+  }
+}
+
+template <typename CT, int HD, bool PLANES>
+__device__ __forceinline__ void paged_attention_tall(int y, const int* __restrict__ cu, const int* __restrict__ start, const float* __restrict__ qkv, long ld,
+                                                     const bf16_t* __restrict__ q_gain, const float2* __restrict__ rope_tab, float eps, int max_new, int lo, const PagedOut& po,
+                                                     const PagedView& pv, const PagedWork& wk) {
+  PagedItem it;
+  if (!paged_find<256, 64, false, true>(pv, cu, start, max_new, pv.gq, lo, INT_MAX, pv.rpb_tall, wk.shift, PAGED_KEYS_TALL, y, it)) return;
+  paged_tall_item<CT, HD, PLANES, false>(it, blockIdx.x, threadIdx.x, qkv, ld, q_gain, rope_tab, eps, po, pv, wk, SharedParts{});
 }
 
 // Block of a KV head (x), through the grid's two other dimensions, which end at 65535 each

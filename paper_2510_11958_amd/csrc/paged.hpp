@@ -104,7 +104,7 @@ __device__ __forceinline__ void page_row(const int* table, const int* start, int
   slots[t] = ((long long)table[(size_t)i * max_pages + (pos >> page_shift)] << page_shift) + (pos & ((1 << page_shift) - 1));
 }
 
-// Pages for a step.  Request i holds held[i] pages and needs ceil((start[i] + rows[i]) / page size) of them.  Its surplus goes onto the
+// Pages for a step.  Request i holds held[i] pages and needs ceil((start[i] + rows[i]) / page size) of them, at least those it shares.  Its surplus goes onto the
 // pool's stack, what it lacks comes off the stack, in the order of the requests and of their pages.  The k-th page given back lies k below
 // the new top, so the next step takes it as its k-th: giving back what a step took restores the stack.  It also means that the k-th page given back in a step is the
 // k-th taken in it: it goes straight from one table to the other, and every page moves by itself, in any order.
@@ -116,12 +116,12 @@ __device__ __forceinline__ void page_row(const int* table, const int* start, int
 // page_moves_kernel, page_rows_kernel.
 struct PageArgs {
   int *table, *held, *stack, *n_free;
-  const int *start, *rows;
+  const int *start, *rows, *shared;      // shared (null: none): pages at the front of a request's table that are not its own, and stay where they are
   int n_req, max_pages, n_pages, page_shift, max_rows;
   int *cu, *row_pos;
   long long* slots;
   int* status;
-  __device__ __forceinline__ int need(int i) const { return (start[i] + rows[i] + (1 << page_shift) - 1) >> page_shift; }
+  __device__ __forceinline__ int need(int i) const { return max((start[i] + rows[i] + (1 << page_shift) - 1) >> page_shift, shared ? shared[i] : 0); }
 };
 
 template <int NT> struct PageSums {
@@ -154,8 +154,9 @@ __device__ __forceinline__ PageSums<NT> page_sums(const PageArgs& a) {
   float size[3] = {0.f, 0.f, 0.f};
   for (int i = p.i0; i < min(p.i0 + p.ipt, a.n_req); ++i) {
     const int s = a.start[i], r = a.rows[i], h = a.held[i];
-    if (s < 0 || r < 0 || h < 0 || h > a.max_pages || s > limit || r > limit - s) { bad = min(bad, i); continue; }
-    const int need = (s + r + (1 << a.page_shift) - 1) >> a.page_shift;
+    const int front = a.shared ? a.shared[i] : 0;
+    if (s < 0 || r < 0 || h < 0 || h > a.max_pages || s > limit || r > limit - s || front < 0 || front > h) { bad = min(bad, i); continue; }
+    const int need = max((s + r + (1 << a.page_shift) - 1) >> a.page_shift, front);
     if (i == p.i0) { p.h0 = h; p.need0 = need; p.r0 = r; }
     const int v[3] = {max(h - need, 0), max(need - h, 0), r};
 #pragma unroll

@@ -2,6 +2,7 @@
 // Part of dmtd.hip: a failure's message goes where dmtd_last_error(NULL) finds it.
 #pragma once
 #include "attention_paged.hpp"
+#include "attention_shared.hpp"
 
 namespace {
 
@@ -208,25 +209,114 @@ hipError_t launch_paged_attention(const dmtd_paged_cache* c, const PagedView& v,
   return c->head_dim == 128 ? launch_paged_attention_t<float, 128, false>(v, p, a, out) : launch_paged_attention_t<float, 64, false>(v, p, a, out);
 }
 
+// ---- shared prefixes ----
+
+// How a step with shared prefixes is laid out: log2 of the blocks per KV head that the key ranges are chosen for, the most items there can be, a unit of partial results, and the sizes.
+struct SharedPlanSizes { int few_shift, tall_shift, few_max; long items, units, unit_floats; size_t list, recs, reqs, groups, plan_bytes; };
+SharedPlanSizes shared_sizes(const dmtd_paged_cache* c, int n_groups) {
+  SharedPlanSizes z{};
+  const int GQ = c->n_q_heads / c->n_kv_heads, rpb_few = 16 / GQ, rpb_tall = 128 / GQ;
+  const bool bf16 = c->dtype != DMTD_DTYPE_F32;
+  z.few_shift = floor_log2(std::max((bf16 ? PAGED_SLOTS_FEW : PAGED_SLOTS_FP32) / c->n_kv_heads, 1));
+  z.tall_shift = floor_log2(std::max(PAGED_SLOTS_TALL / c->n_kv_heads, 1));
+  z.few_max = bf16 ? PAGED_FEW : INT_MAX;
+  // entries are the requests and the groups of two and more; one of n rows has ceil(n / rows of a tile) tiles, and the ranges of all come to a tile's first and at most 2^shift more of either kind
+  const long R = c->max_rows, reqs = std::min<long>(c->n_req, R);
+  z.items = reqs + std::min<long>(n_groups, reqs / 2) + 2 * (R / rpb_few) + (1L << z.few_shift) + (1L << z.tall_shift);
+  z.units = 2 * R + ((long)rpb_few << z.few_shift) + ((long)rpb_tall << z.tall_shift);
+  z.unit_floats = (long)c->n_q_heads * c->head_dim + (2 * c->n_q_heads + 3) / 4 * 4;
+  size_t off = SHARE_HEADER * 4 + (size_t)z.items * 32;
+  auto take = [&](size_t bytes) { const size_t o = off; off += align_up(bytes, 16); return o; };
+  z.list = take((size_t)R * 16);
+  z.recs = take((size_t)R * 32);
+  z.reqs = take((size_t)c->n_req * 16);
+  z.groups = take((size_t)n_groups * 16);
+  z.plan_bytes = align_up(off, 256);
+  return z;
+}
+SharePlan share_plan(const SharedPlanSizes& z, void* at) {
+  char* p = (char*)at;
+  return SharePlan{(int*)p, (int4*)(p + SHARE_HEADER * 4), (int2*)(p + z.list), (int4*)(p + z.recs), (int4*)(p + z.reqs), (int4*)(p + z.groups)};
+}
+// What a plan is laid out for; the attention does nothing with a plan of another sign
+int shared_sign(const dmtd_paged_cache* c, int n_groups, int positions) {
+  uint32_t h = 2166136261u;
+  for (int v : {c->n_req, c->max_pages, c->page_size, c->n_q_heads, c->n_kv_heads, c->head_dim, (int)(c->dtype == DMTD_DTYPE_F32), c->max_rows, n_groups, positions})
+    for (int b = 0; b < 32; b += 8) h = (h ^ (((uint32_t)v >> b) & 0xFFu)) * 16777619u;
+  return (int)(h | 1u);
+}
+int check_shared(const dmtd_paged_cache* c, const dmtd_shared_plan* p) {
+  const int rc = check_cache(c);
+  if (rc != DMTD_OK) return rc;
+  if (!p) return paged_fail(DMTD_EINVAL, "null plan");
+  if (p->n_groups < 1 || p->n_groups > kShareMaxGroups) return paged_fail(DMTD_EINVAL, "n_groups must be in [1, 8192]");
+  if (p->positions < 0) return paged_fail(DMTD_EINVAL, "positions must not be negative");
+  if (!p->plan || !aligned(p->plan, 256)) return paged_fail(DMTD_EINVAL, "the plan's memory must be 256-byte aligned");
+  if (!p->workspace || !aligned(p->workspace, 256)) return paged_fail(DMTD_EINVAL, "workspace must be a 256-byte aligned pointer");
+  if (p->plan_bytes < dmtd_shared_plan_bytes(c, p->n_groups)) return paged_fail(DMTD_ECAPACITY, "the plan's memory is too small");
+  if (p->workspace_bytes < dmtd_shared_workspace_bytes(c)) return paged_fail(DMTD_ECAPACITY, "workspace too small");
+  return DMTD_OK;
+}
+
+struct SharedCall {
+  SharePlan plan;
+  int sign;
+  const float* qkv; long ld;
+  const void* gain;
+  float eps;
+  const float* rope;
+  hipStream_t stream;
+};
+
+template <typename CT, int HD>
+hipError_t launch_shared_t(const PagedView& v, long items, const SharedCall& a, const PagedOut& out, const SharedParts& sp) {
+  typedef typename PagedWide<CT>::type GT;
+  constexpr bool BF = sizeof(GT) == 2;
+  const size_t few_lds = std::max((size_t)PAGED_WAVES * (16 / v.gq) * v.gq * HD * 4, (size_t)16 * (BF ? 2 * (HD + ATT_QPAD) * 2 : (HD + 4) * 4));
+  const long want = items * v.nkv;
+  if (BF && (long)v.max_rows * v.gq > PAGED_FEW) {
+    if constexpr (BF) {
+      auto kern = paged_shared_mfma_kernel<CT, HD, true>;
+      const size_t lds = std::max((size_t)4 * 64 * HD * 2 + 1024, few_lds);
+      static bool big_lds[kMaxDevices];
+      const hipError_t e = lds_room(kern, lds, (size_t)4 * 64 * 128 * 2 + 1024, big_lds);
+      if (e != hipSuccess) return e;
+      hipLaunchKernelGGL(kern, dim3((unsigned)std::min<long>(want, PAGED_RESIDENT_TALL)), dim3(256), lds, a.stream, a.plan, a.sign, a.qkv, a.ld, (const GT*)a.gain, (const float2*)a.rope, a.eps, out, v, sp);
+    }
+  } else {
+    constexpr int resident = sizeof(CT) == 2 ? 768 : 512;
+    hipLaunchKernelGGL((paged_shared_mfma_kernel<CT, HD, false>), dim3((unsigned)std::min<long>(want, resident)), dim3(256), few_lds, a.stream, a.plan, a.sign, a.qkv, a.ld, (const GT*)a.gain,
+                       (const float2*)a.rope, a.eps, out, v, sp);
+  }
+  const long cells = (long)v.max_rows * v.nh * (HD / 4);
+  hipLaunchKernelGGL((paged_shared_join_kernel<GT, HD>), dim3((unsigned)std::min<long>((cells + 255) / 256, 2048)), dim3(256), 0, a.stream, a.plan, a.sign, out, v, sp);
+  return hipGetLastError();
+}
+
 }  // namespace
 
 extern "C" {
 
 int dmtd_page_tables(const dmtd_page_pool* p, const int32_t* start, const int32_t* rows, int32_t max_rows, int32_t* cu_rows, int32_t* row_pos,
                      int64_t* slots, int32_t* status, void* stream) {
+  return dmtd_page_tables_shared(p, start, rows, nullptr, max_rows, cu_rows, row_pos, slots, status, stream);
+}
+
+int dmtd_page_tables_shared(const dmtd_page_pool* p, const int32_t* start, const int32_t* rows, const int32_t* shared, int32_t max_rows, int32_t* cu_rows,
+                            int32_t* row_pos, int64_t* slots, int32_t* status, void* stream) {
   if (!p) return paged_fail(DMTD_EINVAL, "null pool");
   int rc = check_table(p->n_req, p->max_pages, p->n_pages, p->page_size);
   if (rc != DMTD_OK) return rc;
   if (!p->block_table || !p->held || !p->free_pages || !p->n_free || !start || !rows || !cu_rows || !row_pos || !slots || !status)
     return paged_fail(DMTD_EINVAL, "null pointer");
   for (const void* q : {(const void*)p->block_table, (const void*)p->held, (const void*)p->free_pages, (const void*)p->n_free, (const void*)start, (const void*)rows,
-                        (const void*)cu_rows, (const void*)row_pos, (const void*)status})
+                        (const void*)shared, (const void*)cu_rows, (const void*)row_pos, (const void*)status})
     if (!aligned(q, 4)) return paged_fail(DMTD_EINVAL, "int32 arrays must be 4-byte aligned");
   if (!aligned(slots, 8)) return paged_fail(DMTD_EINVAL, "slots must be 8-byte aligned");
   if (max_rows < 1 || max_rows > (1 << 24)) return paged_fail(DMTD_EINVAL, "max_rows must be in [1, 2^24]");
   const hipStream_t s = (hipStream_t)stream;
   if ((rc = check_stream_device(s)) != DMTD_OK) return rc;
-  const PageArgs a{p->block_table, p->held, p->free_pages, p->n_free, start, rows, p->n_req, p->max_pages, p->n_pages, log2_of(p->page_size), max_rows, cu_rows, row_pos,
+  const PageArgs a{p->block_table, p->held, p->free_pages, p->n_free, start, rows, shared, p->n_req, p->max_pages, p->n_pages, log2_of(p->page_size), max_rows, cu_rows, row_pos,
                    (long long*)slots, status};
   const size_t lds = (size_t)16 * p->n_req;          // of a block that moves pages
   static bool big_tables[kMaxDevices], big_moves[kMaxDevices];
@@ -302,6 +392,66 @@ int dmtd_paged_attention(const dmtd_paged_cache* c, const float* qkv, int64_t ld
   const PagedView v = paged_view(c, rope, rope_len);
   if (max_new == 0) max_new = c->max_rows;
   const hipError_t e = launch_paged_attention(c, v, PagedCall{qkv, (long)ld, start, cu_rows, max_new, q_norm, eps, rope, (char*)workspace, s}, PagedOut{out, nullptr, (long)ldo, 0});
+  return e == hipSuccess ? DMTD_OK : paged_fail(DMTD_EHIP, hipGetErrorString(e));
+}
+
+size_t dmtd_shared_plan_bytes(const dmtd_paged_cache* c, int32_t n_groups) {
+  if (check_cache(c) != DMTD_OK) return 0;
+  if (n_groups < 1 || n_groups > kShareMaxGroups) { paged_fail(DMTD_EINVAL, "n_groups must be in [1, 8192]"); return 0; }
+  return shared_sizes(c, n_groups).plan_bytes;
+}
+
+size_t dmtd_shared_workspace_bytes(const dmtd_paged_cache* c) {
+  if (check_cache(c) != DMTD_OK) return 0;
+  const SharedPlanSizes z = shared_sizes(c, 1);
+  return (size_t)z.units * z.unit_floats * 4;
+}
+
+int dmtd_shared_plan_build(const dmtd_paged_cache* c, const dmtd_shared_plan* p, const int32_t* start, const int32_t* cu_rows, const int32_t* group, const int32_t* prefix_pages,
+                           void* stream) {
+  int rc = check_shared(c, p);
+  if (rc != DMTD_OK) return rc;
+  for (const void* q : {(const void*)start, (const void*)cu_rows, (const void*)group, (const void*)prefix_pages})
+    if (!q || !aligned(q, 4)) return paged_fail(DMTD_EINVAL, "start, cu_rows, group and prefix_pages must be 4-byte aligned pointers");
+  const hipStream_t s = (hipStream_t)stream;
+  if ((rc = check_stream_device(s)) != DMTD_OK) return rc;
+  PagedView v = paged_view(c, nullptr, 0);
+  if (p->positions && p->positions < v.limit) v.limit = p->positions;
+  const SharedPlanSizes z = shared_sizes(c, p->n_groups);
+  const ShareArgs a{start, cu_rows, group, prefix_pages, p->n_groups, z.few_shift, z.tall_shift, z.few_max, shared_sign(c, p->n_groups, p->positions), share_plan(z, p->plan)};
+  const size_t lds = (size_t)8 * std::max(c->n_req, p->n_groups);
+  static bool big_lds[kMaxDevices];
+  if (c->n_req <= 256 && p->n_groups <= 256 && c->max_rows <= 1024) {
+    hipLaunchKernelGGL(share_plan_kernel<256>, dim3(1), dim3(256), lds, s, a, v);
+  } else {
+    const hipError_t e = lds_room(share_plan_kernel<1024>, lds, 8 * kShareMaxRequests, big_lds);
+    if (e != hipSuccess) return paged_fail(DMTD_EHIP, hipGetErrorString(e));
+    hipLaunchKernelGGL(share_plan_kernel<1024>, dim3(1), dim3(1024), lds, s, a, v);
+  }
+  return paged_done();
+}
+
+int dmtd_paged_attention_shared(const dmtd_paged_cache* c, const dmtd_shared_plan* p, const float* qkv, int64_t ld, const void* q_norm, float eps, const float* rope, int32_t rope_len,
+                                void* out, int64_t ldo, void* stream) {
+  int rc = check_shared(c, p);
+  if (rc == DMTD_OK) rc = check_rows(qkv, ld, (int64_t)c->n_q_heads * c->head_dim, q_norm, eps, rope, rope_len);
+  if (rc != DMTD_OK) return rc;
+  if (!out || !aligned(out, 16)) return paged_fail(DMTD_EINVAL, "out must be a 16-byte aligned pointer");
+  if (ldo < (int64_t)c->n_q_heads * c->head_dim || ldo % 8 || ldo > (1 << 24)) return paged_fail(DMTD_EINVAL, "ldo must be a multiple of 8 that holds a row");
+  PagedView v = paged_view(c, nullptr, 0);
+  if (p->positions && p->positions < v.limit) v.limit = p->positions;
+  if (rope && rope_len < v.limit) return paged_fail(DMTD_EINVAL, "the rotary table is shorter than the positions that the plan is made for");
+  const hipStream_t s = (hipStream_t)stream;
+  if ((rc = check_stream_device(s)) != DMTD_OK) return rc;
+  const SharedPlanSizes z = shared_sizes(c, p->n_groups);
+  const SharePlan plan = share_plan(z, p->plan);
+  const SharedCall a{plan, shared_sign(c, p->n_groups, p->positions), qkv, (long)ld, q_norm, eps, rope, s};
+  const PagedOut to{out, nullptr, (long)ldo, 0};
+  const SharedParts sp{plan.list, (float*)p->workspace, z.unit_floats};
+  hipError_t e;
+  if (c->dtype == DMTD_DTYPE_BF16) e = c->head_dim == 128 ? launch_shared_t<bf16_t, 128>(v, z.items, a, to, sp) : launch_shared_t<bf16_t, 64>(v, z.items, a, to, sp);
+  else if (c->dtype == DMTD_DTYPE_E4M3) e = c->head_dim == 128 ? launch_shared_t<e4m3_t, 128>(v, z.items, a, to, sp) : launch_shared_t<e4m3_t, 64>(v, z.items, a, to, sp);
+  else e = c->head_dim == 128 ? launch_shared_t<float, 128>(v, z.items, a, to, sp) : launch_shared_t<float, 64>(v, z.items, a, to, sp);
   return e == hipSuccess ? DMTD_OK : paged_fail(DMTD_EHIP, hipGetErrorString(e));
 }
 
