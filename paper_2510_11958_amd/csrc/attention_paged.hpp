@@ -65,14 +65,16 @@ struct PagedWork {
 // the range's number of n of its group; where partial results and the count lie (in slots of all KV heads)
 struct PagedItem { int req, first, row0, r, pos0, kb, ke, split, n, slot, group; };
 
-// A block's share of a step with shared prefixes, as its plan holds it (attention_shared.hpp): keys kb .. ke - 1 of the table of request `req`; the rows list[row0] .. list[row0 + r - 1],
-// each (row, position); row j sees the keys up to pos0 + j (step 1) or all of them up to pos0 (step 0).  unit: where row 0's partial results go, -1: to the output.
+// A block's share of a step with shared prefixes, as its plan holds it (attention_shared.hpp): keys kb .. ke - 1 of the table of request `req`; step 1: the rows row0 .. row0 + r - 1, of which
+// row j is at position pos0 + j and sees the keys up to there; step 0: the rows list[row0] .. list[row0 + r - 1], each (row, position), which see all keys up to pos0.
+// unit: where row 0's partial results go, -1: to the output.
 struct SharedItem { int req, row0, r, pos0, kb, ke, unit, step; };
 // What the blocks of such a step share: the rows' list, and room for partial results: per unit the sums of all query heads, then their (maximum, sum of weights)
 struct SharedParts {
   const int2* list;
   float* part;
   long unit_floats;
+  __device__ __forceinline__ int2 row(const SharedItem& it, int j) const { return it.step ? make_int2(it.row0 + j, it.pos0 + j) : list[it.row0 + j]; }
   __device__ __forceinline__ float* sums(int unit, int head, int hd) const { return part + (size_t)unit * unit_floats + (size_t)head * hd; }
   __device__ __forceinline__ float* weights(int unit, int nh, int head, int hd) const { return part + (size_t)unit * unit_floats + (size_t)nh * hd + 2 * head; }
 };
@@ -301,6 +303,9 @@ __device__ __forceinline__ void paged_store4(const PagedOut& o, int row, int col
   }
 }
 
+// Groups of 16 keys that a wave has under way, and weighs with one maximum: 8 KiB of bf16, and twice that where a wave works alone, with fewer of them on a CU.
+template <typename CT, bool SHARED> __host__ __device__ constexpr int paged_few_groups() { return sizeof(CT) == 4 ? 1 : (sizeof(CT) == 1 ? 2 : 1) * (SHARED ? 2 : 1); }
+
 // Requests with few query vectors.  16 vectors of one KV head are the 16 columns of the matrix tiles, so a block reads each key and value once; its 4
 // waves take groups of 16 keys in turn, which never leave a page, the next group's loads in flight.  Per group, in one wave (lane: sl = lane % 16, kq = lane / 16):
 //   scores   S^T[key, q] = sum_d K[key, d] Q[q, d], 16x16x32: K rows as they lie in the cache, the queries as two bf16 parts (16 bits);
@@ -311,16 +316,17 @@ __device__ __forceinline__ void paged_store4(const PagedOut& o, int row, int col
 // them / both: 3 rows of 8 requests behind 16384 102 / 84 / 91, 31 ragged rows in pages of 16 tokens 23 / 25 / 30, out of cold memory 29 / 28 / 30, one row of 64
 // behind 1024 out of cold memory 54 / 49 / 48).
 // Bound by the memory: 8 KiB per wave and group against PAGED_PARTS x HD / 16 + 2 x HD / 32 products.
-// SHARED: `it` is a SharedItem, and partial results go where it says.
+// SHARED: `it` is a SharedItem, a wave's alone (`slot`: its number in the block, tid its lane): no barriers, and the wave's own result is the item's, to go where it says.
 template <typename CT, int HD, bool PLANES, bool SHARED, typename ITEM>
-__device__ __forceinline__ void paged_few_item(const ITEM& it, int g, const int tid, const float* __restrict__ qkv, long ld, const typename PagedWide<CT>::type* __restrict__ q_gain,
+__device__ __forceinline__ void paged_few_item(const ITEM& it, int g, const int tid, int slot, const float* __restrict__ qkv, long ld, const typename PagedWide<CT>::type* __restrict__ q_gain,
                                                const float2* __restrict__ rope_tab, float eps, const PagedOut& po, const PagedView& pv, const PagedWork& wk, const SharedParts& sp) {
   typedef typename PagedWide<CT>::type GT;
   constexpr bool BF = sizeof(GT) == 2, Q8 = sizeof(CT) == 1;
   constexpr int PARTS = PAGED_PARTS<PLANES>;
-  constexpr int QVT = 16, NW = PAGED_WAVES, NT = 64 * NW, DPL = HD / 16, half = HD / 2, HL = HD / 32;
+  constexpr int QVT = 16, NW = SHARED ? 1 : PAGED_WAVES, NT = 64 * NW, DPL = HD / 16, half = HD / 2, HL = HD / 32;
+  constexpr int QI = 16 * QVT / NT;                          // query vectors that 16 lanes make ready
   constexpr int KS = HD * (int)sizeof(CT) / 64;              // 16-byte pieces of a key a lane carries
-  constexpr int G = Q8 ? 2 : 1;                              // groups of 16 keys that a wave loads together
+  constexpr int G = paged_few_groups<CT, SHARED>();          // groups of 16 keys that a wave loads and weighs together
   constexpr int QLD = BF ? HD + ATT_QPAD : HD + 4;           // a query row in LDS
   constexpr int KW = BF ? HD / 32 : HD / 16;                 // pieces of a key in the products: KS, or 8-bit ones widened
   constexpr int VW = DPL * sizeof(GT) / 4;                   // 32-bit words of a value in the products: its DPL dims that a lane carries
@@ -329,40 +335,44 @@ __device__ __forceinline__ void paged_few_item(const ITEM& it, int g, const int 
   typedef float fvec_t __attribute__((ext_vector_type(HL)));
   typedef unsigned short hvec_t __attribute__((ext_vector_type(HL)));
   const int GQ = pv.gq;
-  const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), sl = lane & 15, kq = lane >> 4;
+  const int lane = tid & 63, wave = SHARED ? 0 : __builtin_amdgcn_readfirstlane(tid >> 6), sl = lane & 15, kq = lane >> 4;
   const int QV = it.r * GQ, ke = it.ke;
   __shared__ float wm[NW][QVT], wl[NW][QVT];
   __shared__ int poison_s;
   extern __shared__ float4 paged_dyn_smem[];
   float* wacc = (float*)paged_dyn_smem;                       // [NW][QV][HD], in the place of the queries' two parts when these are done with
-  GT (*qhi_s)[QLD] = (GT (*)[QLD])paged_dyn_smem, (*qlo_s)[QLD] = qhi_s + QVT;      // (fp32: one part)
+  GT (*qhi_s)[QLD] = (GT (*)[QLD])paged_dyn_smem + slot * (BF ? 2 : 1) * QVT, (*qlo_s)[QLD] = qhi_s + QVT;      // (fp32: one part)
   // pages of this wave's next 64 groups, one a lane
   const int* trow = pv.table + (size_t)it.req * pv.max_pages;
   auto load_pages = [&](int base) { return base + 16 * NW * lane < ke ? trow[(base + 16 * NW * lane) >> pv.page_shift] : 0; };
   const int first = it.kb + 16 * wave;
   int pages = load_pages(first);
-  // query vector tid / 16, 2 HL values a lane
-  static_assert(NT == 16 * QVT, "16 lanes to a query vector");
-  const int qv = tid >> 4, l16 = tid & 15, qr = pv.row_of(qv < QV ? qv : 0), qrow = it.row0 + qr, qhead = g * GQ + (qv < QV ? qv - qr * GQ : 0);
-  fvec_t xa, xb;
-  float2 cs[HL];
+  // query vectors tid / 16 + 4 i, 2 HL values a lane
+  const int l16 = tid & 15;
+  fvec_t xa[QI], xb[QI];
+  float2 cs[QI][HL];
   GT g0[HL], g1[HL];
-  {
+#pragma unroll
+  for (int e = 0; e < HL; ++e) {
+    g0[e] = q_gain ? q_gain[HL * l16 + e] : GT(0);
+    g1[e] = q_gain ? q_gain[half + HL * l16 + e] : GT(0);
+  }
+#pragma unroll
+  for (int i = 0; i < QI; ++i) {
     // what it needs is asked for in front of the keys, whose arrival it is made ready beside
+    if (i > 0 && i * NT / 16 >= QV) break;
+    const int qv = (tid >> 4) + i * (NT / 16), qr = pv.row_of(qv < QV ? qv : 0), qrow = it.row0 + qr, qhead = g * GQ + (qv < QV ? qv - qr * GQ : 0);
     int row, pos;
-    if constexpr (SHARED) { const int2 rp = sp.list[qrow]; row = rp.x; pos = rp.y; }
+    if constexpr (SHARED) { const int2 rp = sp.row(it, qr); row = rp.x; pos = rp.y; }
     else { row = it.first + qrow; pos = it.pos0 + qr; }
     const float* src = qkv + (size_t)row * ld + (size_t)qhead * HD + HL * l16;
-    xa = *(const fvec_t*)src; xb = *(const fvec_t*)(src + half);
+    xa[i] = *(const fvec_t*)src; xb[i] = *(const fvec_t*)(src + half);
     const float2* rp = rope_tab + (size_t)pos * half + HL * l16;
 #pragma unroll
-    for (int e = 0; e < HL; ++e) {
-      cs[e] = rope_tab ? rp[e] : make_float2(1.f, 0.f);
-      g0[e] = q_gain ? q_gain[HL * l16 + e] : GT(0);
-      g1[e] = q_gain ? q_gain[half + HL * l16 + e] : GT(0);
-    }
+    for (int e = 0; e < HL; ++e) cs[i][e] = rope_tab ? rp[e] : make_float2(1.f, 0.f);
   }
-  if (tid == 0) poison_s = INT_MAX;
+  int poison = INT_MAX;      // SHARED: the least key of this lane's whose value is not finite, among those that some row does not see
+  if (!SHARED && tid == 0) poison_s = INT_MAX;
   u32x4 kr[G][KS];
   vraw_t vr[G][4];
   bool ok[G];
@@ -392,10 +402,13 @@ __device__ __forceinline__ void paged_few_item(const ITEM& it, int g, const int 
     }
   };
   if (first < ke) load_groups(first, 0);
-  {
+#pragma unroll
+  for (int i = 0; i < QI; ++i) {
+    if (i > 0 && i * NT / 16 >= QV) break;      // (columns of the products behind the last vector hold whatever lies there)
+    const int qv = (tid >> 4) + i * (NT / 16);
     float x0[HL], x1[HL], ss = 0.f;
 #pragma unroll
-    for (int e = 0; e < HL; ++e) { x0[e] = xa[e]; x1[e] = xb[e]; ss += x0[e] * x0[e] + x1[e] * x1[e]; }
+    for (int e = 0; e < HL; ++e) { x0[e] = xa[i][e]; x1[e] = xb[i][e]; ss += x0[e] * x0[e] + x1[e] * x1[e]; }
     if (q_gain) {
       const float rs = rsqrtf(row16_sum(ss) / (float)HD + eps);
 #pragma unroll
@@ -405,8 +418,8 @@ __device__ __forceinline__ void paged_few_item(const ITEM& it, int g, const int 
 #pragma unroll
       for (int e = 0; e < HL; ++e) {      // (which product is the rounded one is written out: the compiler's own choice differs from one instantiation to the next)
         const float a = x0[e], b = x1[e];
-        x0[e] = __builtin_fmaf(a, cs[e].x, -(b * cs[e].y));
-        x1[e] = __builtin_fmaf(a, cs[e].y, b * cs[e].x);
+        x0[e] = __builtin_fmaf(a, cs[i][e].x, -(b * cs[i][e].y));
+        x1[e] = __builtin_fmaf(a, cs[i][e].y, b * cs[i][e].x);
       }
     }
     const float scale = rsqrtf((float)HD) * 1.4426950408889634f;
@@ -425,7 +438,12 @@ __device__ __forceinline__ void paged_few_item(const ITEM& it, int g, const int 
       for (int e = 0; e < HL; ++e) { qhi_s[qv][HL * l16 + e] = qv < QV ? x0[e] * scale : 0.f; qhi_s[qv][half + HL * l16 + e] = qv < QV ? x1[e] * scale : 0.f; }
     }
   }
-  __syncthreads();
+  if constexpr (SHARED) {      // a wave's LDS accesses are in order: only the compiler has to keep them so
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  } else {
+    __syncthreads();
+  }
   int my_pos = it.pos0 + pv.row_of(sl);
   if constexpr (SHARED) my_pos = it.step ? my_pos : it.pos0;
   float m_run = -INFINITY, l_run = 0.f;
@@ -451,11 +469,22 @@ __device__ __forceinline__ void paged_few_item(const ITEM& it, int g, const int 
       if (((j + G) & 63) == 0) pages = load_pages(next);
       load_groups(next, j + G);
     }
+    bool some = false;
+#pragma unroll
+    for (int u = 0; u < G; ++u) some |= here[u];
+    if (!some) continue;                                      // pages outside the pool
+    // scores of all groups, then one maximum for them
+    float sc[G][4];
+    bool masked[G];
 #pragma unroll
     for (int u = 0; u < G; ++u) {
-    if (!here[u]) continue;                                   // a page outside the pool, or behind the last key
+    masked[u] = false;
+    if (!here[u]) {                                           // a page outside the pool, or behind the last key
+#pragma unroll
+      for (int m = 0; m < 4; ++m) sc[u][m] = -INFINITY;
+      continue;
+    }
     const int base = from + 16 * NW * u;
-    vwide_t va[4];                                            // the values, as bf16 or fp32
     u32x4 ka[KW];
     if constexpr (Q8) {
       const float sk = e8m0_scale(ksc[u]);
@@ -466,17 +495,9 @@ __device__ __forceinline__ void paged_few_item(const ITEM& it, int g, const int 
           ka[2 * t + (e >> 1)][2 * (e & 1)] = e4m3_pair<false>(kc[u][t][e], sk);
           ka[2 * t + (e >> 1)][2 * (e & 1) + 1] = e4m3_pair<true>(kc[u][t][e], sk);
         }
-#pragma unroll
-      for (int m = 0; m < 4; ++m) {
-        const float sv = e8m0_scale((vsc[u] >> (8 * m)) & 0xFFu);
-#pragma unroll
-        for (int e = 0; e < VW / 2; ++e) { va[m][2 * e] = e4m3_pair<false>(vc[u][m][e], sv); va[m][2 * e + 1] = e4m3_pair<true>(vc[u][m][e], sv); }
-      }
     } else {
 #pragma unroll
       for (int t = 0; t < KS; ++t) ka[t] = kc[u][t];
-#pragma unroll
-      for (int m = 0; m < 4; ++m) va[m] = vc[u][m];
     }
     f32x4 s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -494,34 +515,27 @@ __device__ __forceinline__ void paged_few_item(const ITEM& it, int g, const int 
         s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, ka[t]), qh, s, 0, 0, 0);
       }
     }
-    float sc[4] = {s.x, s.y, s.z, s.w};
-    if (base + 16 > it.pos0 + 1) {
-      // Keys that some row does not see: their scores are out; values behind the last key are whatever lies there, and values of the group's own
-      // positions may be infinite or NaN, which a probability of 0 would not silence: both go in as 0, and the rows that see such a one become NaN
+    sc[u][0] = s.x; sc[u][1] = s.y; sc[u][2] = s.z; sc[u][3] = s.w;
+    masked[u] = base + 16 > it.pos0 + 1;
+    if (masked[u]) {                                          // keys that some row does not see: their scores are out
 #pragma unroll
       for (int m = 0; m < 4; ++m) {
         const int key = base + 4 * kq + m;
-        if (key > my_pos || key >= ke) sc[m] = -INFINITY;
-        if (key > it.pos0) {
-          bool bad = false;
-#pragma unroll
-          for (int u = 0; u < VW; ++u) bad |= (BF && (va[m][u] & 0x7F80u) == 0x7F80u) || (va[m][u] & 0x7F800000u) == 0x7F800000u;
-          if (bad && key < ke) atomicMin(&poison_s, key);
-          if (bad || key >= ke) {
-#pragma unroll
-            for (int u = 0; u < VW; ++u) va[m][u] = 0u;
-          }
-        }
+        if (key > my_pos || key >= ke) sc[u][m] = -INFINITY;
       }
     }
-    float mx = fmaxf(fmaxf(sc[0], sc[1]), fmaxf(sc[2], sc[3]));
+    }
+    float mx = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < G; ++u) mx = fmaxf(mx, fmaxf(fmaxf(sc[u][0], sc[u][1]), fmaxf(sc[u][2], sc[u][3])));
     mx = column_max(mx);
     const float m_new = fmaxf(m_run, mx), m_use = m_new == -INFINITY ? 0.f : m_new;
     const float f = __builtin_amdgcn_exp2f(m_run - m_use);
-    float p[4];
     float psum = 0.f;
 #pragma unroll
-    for (int m = 0; m < 4; ++m) { p[m] = __builtin_amdgcn_exp2f(sc[m] - m_use); psum += p[m]; }
+    for (int u = 0; u < G; ++u)
+#pragma unroll
+      for (int m = 0; m < 4; ++m) { sc[u][m] = __builtin_amdgcn_exp2f(sc[u][m] - m_use); psum += sc[u][m]; }      // probabilities from here on
     l_run = l_run * f + psum;
     if (__any(m_new > m_run)) {                               // the sums this lane holds are those of queries 4 kq + j
 #pragma unroll
@@ -532,6 +546,44 @@ __device__ __forceinline__ void paged_few_item(const ITEM& it, int g, const int 
       }
     }
     m_run = m_new;
+#pragma unroll
+    for (int u = 0; u < G; ++u) {
+    if (!here[u]) continue;
+    const int base = from + 16 * NW * u;
+    const float (&p)[4] = sc[u];
+    vwide_t va[4];                                            // the values, as bf16 or fp32
+    if constexpr (Q8) {
+#pragma unroll
+      for (int m = 0; m < 4; ++m) {
+        const float sv = e8m0_scale((vsc[u] >> (8 * m)) & 0xFFu);
+#pragma unroll
+        for (int e = 0; e < VW / 2; ++e) { va[m][2 * e] = e4m3_pair<false>(vc[u][m][e], sv); va[m][2 * e + 1] = e4m3_pair<true>(vc[u][m][e], sv); }
+      }
+    } else {
+#pragma unroll
+      for (int m = 0; m < 4; ++m) va[m] = vc[u][m];
+    }
+    if (masked[u]) {
+      // values behind the last key are whatever lies there, and values of the item's own positions may be infinite or NaN, which a probability of 0 would not
+      // silence: both go in as 0, and the rows that see such a one become NaN
+#pragma unroll
+      for (int m = 0; m < 4; ++m) {
+        const int key = base + 4 * kq + m;
+        if (key > it.pos0) {
+          bool bad = false;
+#pragma unroll
+          for (int x = 0; x < VW; ++x) bad |= (BF && (va[m][x] & 0x7F80u) == 0x7F80u) || (va[m][x] & 0x7F800000u) == 0x7F800000u;
+          if (bad && key < ke) {
+            if constexpr (SHARED) poison = min(poison, key);
+            else atomicMin(&poison_s, key);
+          }
+          if (bad || key >= ke) {
+#pragma unroll
+            for (int x = 0; x < VW; ++x) va[m][x] = 0u;
+          }
+        }
+      }
+    }
     if constexpr (!BF) {
 #pragma unroll
       for (int e = 0; e < DPL; ++e)
@@ -559,8 +611,33 @@ __device__ __forceinline__ void paged_few_item(const ITEM& it, int g, const int 
     }
     }
   }
-  // the waves' results of a vector, 4 consecutive dims a thread
   l_run = column_sum(l_run);
+  if constexpr (SHARED) {
+    poison = wave_reduce((uint32_t)poison, [](uint32_t a, uint32_t b) { return a < b ? a : b; });
+    if (it.pos0 + pv.row_of(sl) >= poison) l_run = __uint_as_float(0x7FC00000u);
+    const float inv = l_run == 0.f ? 0.f : 1.0f / l_run;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int v = 4 * kq + q, r = pv.row_of(v), head = g * GQ + v - r * GQ;
+      const float inv_q = __shfl(inv, v, 64);
+      if (v >= QV) continue;
+      if (it.unit < 0) {
+        const int row = sp.row(it, r).x;
+#pragma unroll
+        for (int e = 0; e < DPL; e += 4) paged_store4<GT, PLANES>(po, row, head * HD + DPL * sl + e, f32x4{acc[e][q] * inv_q, acc[e + 1][q] * inv_q, acc[e + 2][q] * inv_q, acc[e + 3][q] * inv_q});
+      } else {
+        float* sums = sp.sums(it.unit + r, head, HD) + DPL * sl;
+#pragma unroll
+        for (int e = 0; e < DPL; e += 4) *(f32x4*)(sums + e) = f32x4{acc[e][q], acc[e + 1][q], acc[e + 2][q], acc[e + 3][q]};
+      }
+    }
+    if (it.unit >= 0 && kq == 0 && sl < QV) {
+      const int r = pv.row_of(sl);
+      *(float2*)sp.weights(it.unit + r, pv.nh, g * GQ + sl - r * GQ, HD) = make_float2(m_run, l_run);
+    }
+    return;
+  } else {
+  // the waves' results of a vector, 4 consecutive dims a thread
   __syncthreads();
   if (kq == 0 && sl < QV) { wm[wave][sl] = m_run; wl[wave][sl] = l_run; }
 #pragma unroll
@@ -573,20 +650,10 @@ __device__ __forceinline__ void paged_few_item(const ITEM& it, int g, const int 
   }
   __syncthreads();
   constexpr size_t SLOT = (size_t)QVT * (HD + 2);
-  float* part = nullptr;
-  bool whole;
-  if constexpr (SHARED) {
-    whole = it.unit < 0;
-  } else {
-    part = wk.part + ((size_t)(it.slot + it.split) * pv.nkv + g) * SLOT;
-    whole = it.n == 1;
-  }
+  float* part = wk.part + ((size_t)(it.slot + it.split) * pv.nkv + g) * SLOT;
   auto store = [&](int v, int d, const f32x4& x) {
     const int r = pv.row_of(v);
-    int row;
-    if constexpr (SHARED) row = sp.list[it.row0 + r].x;
-    else row = it.first + it.row0 + r;
-    paged_store4<GT, PLANES>(po, row, (g * GQ + v - r * GQ) * HD + d, x);
+    paged_store4<GT, PLANES>(po, it.first + it.row0 + r, (g * GQ + v - r * GQ) * HD + d, x);
   };
   for (int e = tid; e < QV * (HD / 4); e += NT) {
     const int v = e / (HD / 4), d = (e % (HD / 4)) * 4;
@@ -603,20 +670,15 @@ __device__ __forceinline__ void paged_few_item(const ITEM& it, int g, const int 
       l += fw * wl[w][v];
     }
     if (it.pos0 + pv.row_of(v) >= poison_s) l = __uint_as_float(0x7FC00000u);
-    if (whole) {
+    if (it.n == 1) {
       const float inv = l == 0.f ? 0.f : 1.0f / l;
       store(v, d, f32x4{o.x * inv, o.y * inv, o.z * inv, o.w * inv});
-    } else if constexpr (SHARED) {
-      const int r = pv.row_of(v), head = g * GQ + v - r * GQ;
-      *(f32x4*)(sp.sums(it.unit + r, head, HD) + d) = o;
-      if (d == 0) *(float2*)sp.weights(it.unit + r, pv.nh, head, HD) = make_float2(mm, l);
     } else {
       put_through4(part + (size_t)v * HD + d, o);
       if (d == 0) put_through(part + (size_t)QVT * HD + 2 * v, mm, l);
     }
   }
-  if constexpr (!SHARED) {
-    if (it.n > 1) paged_join<HD, QVT, NT>(wk, it, pv.nkv, g, QV, (f32x4*)paged_dyn_smem, store);
+  if (it.n > 1) paged_join<HD, QVT, NT>(wk, it, pv.nkv, g, QV, (f32x4*)paged_dyn_smem, store);
   }
 }
 
@@ -627,7 +689,7 @@ __device__ __forceinline__ void paged_attention_few(int y, const int* __restrict
   constexpr int NW = PAGED_WAVES, NT = 64 * NW;
   PagedItem it;
   if (!paged_find<NT, 16 * NW, false>(pv, cu, start, max_new, pv.gq, 0, hi, pv.rpb_few, wk.shift, PAGED_KEYS_FEW, y, it)) return;
-  paged_few_item<CT, HD, PLANES, false>(it, blockIdx.x, threadIdx.x, qkv, ld, q_gain, rope_tab, eps, po, pv, wk, SharedParts{});
+  paged_few_item<CT, HD, PLANES, false>(it, blockIdx.x, threadIdx.x, 0, qkv, ld, q_gain, rope_tab, eps, po, pv, wk, SharedParts{});
 }
 
 // Requests with many query vectors (chunks of a prompt).  A block takes 128 vectors of one KV head - 128 / GQ rows x the GQ query heads that share it, 32 per
@@ -671,7 +733,7 @@ __device__ __forceinline__ void paged_tall_item(const ITEM& it, int g, const int
   const int qr = pv.row_of(valid ? qv : 0), row = it.row0 + qr, head = g * GQ + (valid ? qv - qr * GQ : 0);
   int my_pos = it.pos0 + (row - it.row0), qkv_row, rope_pos;
   if constexpr (SHARED) {
-    const int2 rp = sp.list[row];
+    const int2 rp = sp.row(it, qr);
     qkv_row = rp.x;
     rope_pos = rp.y;
     my_pos = it.step ? my_pos : it.pos0;
@@ -1013,7 +1075,7 @@ __device__ __forceinline__ void paged_tall_item(const ITEM& it, int g, const int
       if (ln < 32) *(float2*)sp.weights(it.unit + qor, pv.nh, ho, HD) = make_float2(m_run, l_run);
     } else if (qo < QV) {
       const float inv = l_run == 0.f ? 0.f : 1.0f / l_run;
-      const int to = sp.list[ro].x;
+      const int to = sp.row(it, qor).x;
 #pragma unroll
       for (int t = 0; t < DT; ++t)
 #pragma unroll

@@ -15,16 +15,17 @@
 namespace dmtd {
 
 constexpr int SHARE_HEADER = 16;      // ints in front of the items: sign, tall items, items, rows
-constexpr int kShareMaxRequests = kPagedMaxRequests, kShareMaxGroups = kPagedMaxRequests;
+constexpr int SHARE_SLOTS_FEW = 1024;      // items of single waves that the key ranges are chosen for
+constexpr int kShareMaxGroups = kPagedMaxRequests;
+constexpr int SHARE_LDS_ENTRIES = 1024;      // requests, and groups, up to which a plan is worked out in LDS
 
 // A plan in the caller's memory
 struct SharePlan {
   int* head;            // SHARE_HEADER ints
   int4* items;          // two each: (req, row0, r, pos0), (kb, ke, unit, step)
-  int2* list;           // [max_rows] (row, position) of the step's rows, then [max_rows] of the rows that see a prefix, group by group
+  int2* list;           // [max_rows] (row, position) of the rows that see a prefix, group by group
   int4* recs;           // [max_rows][2]: unit of the row's first own part, parts, units from one to the next, 0; the same of its prefix
-  int4* reqs;           // [n_req]: tokens of the prefix, its place among the group's rows, first own unit, 0
-  int4* groups;         // [n_groups]: rows, a request of the group, first unit, first place in the list
+  int* scratch;         // what a plan of many requests is worked out in
 };
 
 struct ShareArgs {
@@ -34,247 +35,279 @@ struct ShareArgs {
   SharePlan plan;
 };
 
-// What the ranges of an entry (the rows of a request, or of a group) come to
-struct ShareEntry { int rows, keys, rpb, kps; bool tall; };
+// What a plan knows of its requests and groups: rows, keys (of a request: behind its prefix) and where its first unit, item and place in the list are
+struct ShareTables {
+  int *first, *n, *start, *group, *prefix, *place, *unit, *tall, *few;      // of the requests; first: [n_req + 1]
+  int *g_n, *g_head, *g_keys, *g_unit, *g_list, *g_tall, *g_few;            // of the groups
+  static constexpr int REQ = 9, GROUP = 7;
+  static __host__ __device__ long ints(int n_req, int n_groups) { return (long)REQ * n_req + 1 + (long)GROUP * n_groups; }
+  __device__ __forceinline__ ShareTables(int* at, int n_req, int n_groups) {
+    int** r[REQ] = {&n, &start, &group, &prefix, &place, &unit, &tall, &few, &first};
+#pragma unroll
+    for (int k = 0; k < REQ; ++k) *r[k] = at + (long)k * n_req;
+    int** g[GROUP] = {&g_n, &g_head, &g_keys, &g_unit, &g_list, &g_tall, &g_few};
+#pragma unroll
+    for (int k = 0; k < GROUP; ++k) *g[k] = at + (long)REQ * n_req + 1 + (long)k * n_groups;
+  }
+};
 
 // The plan of a step, in one block.  Own entries are the requests, with the keys behind their prefix; prefix entries are the groups of two requests and more that have rows.  A request
 // takes part in its group if its tokens reach beyond the prefix, and goes by itself over its whole table otherwise.  Its place among the group's rows is given out by an atomic add: where a
 // row stands in its tile has no influence on its results.  All ranges of a kind have kps keys, chosen as in paged_find.
-// A chain of round trips to memory and barriers is what bounds it.
-template <int NT>
+// Bound by its chain of round trips and barriers: three of the former, the tables being in LDS (57 requests, 750 items: 4.6 us; with the tables in memory 11.8).
+// LDS false: more requests or groups than that; the tables are in the plan's scratch, the groups' counts still in LDS.
+template <int NT, bool LDS>
 __global__ void __launch_bounds__(NT) share_plan_kernel(ShareArgs a, PagedView pv) {
   extern __shared__ int share_dyn_smem[];
-  __shared__ long long sums_s[NT / 64];
-  const int tid = threadIdx.x, n_req = pv.n_req, n_groups = a.n_groups, longest = max(n_req, n_groups);
-  int *first_s = share_dyn_smem, *head_s = share_dyn_smem + longest;      // rows of the groups and a request of each; later an entry's first item or row
+  __shared__ unsigned long long total_s[2][NT / 64];
+  __shared__ int scan_s[7][NT / 64];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n_req = pv.n_req, n_groups = a.n_groups;
   const SharePlan& P = a.plan;
-  for (int g = tid; g < n_groups; g += NT) { first_s[g] = 0; head_s[g] = INT_MAX; }
-  __syncthreads();
+  ShareTables T(LDS ? share_dyn_smem : P.scratch, n_req, n_groups);
+  if (!LDS) { T.g_n = share_dyn_smem; T.g_head = share_dyn_smem + n_groups; }
   const int ipr = (n_req + NT - 1) / NT, r0 = min(tid * ipr, n_req), r1 = min(r0 + ipr, n_req);
   const int ipg = (n_groups + NT - 1) / NT, g0 = min(tid * ipg, n_groups), g1 = min(g0 + ipg, n_groups);
+  const int end_of_all = a.cu[n_req];
+#pragma unroll 1
+  for (int g = g0; g < g1; ++g) {
+    const int pages = a.pages[g];
+    T.g_n[g] = 0;
+    T.g_head[g] = INT_MAX;
+    T.g_keys[g] = pages > 0 && pages <= pv.max_pages ? pages << pv.page_shift : 0;
+  }
   bool descends = false;
 #pragma unroll 1
   for (int i = r0; i < r1; ++i) {
     const PagedReq q = paged_req(pv, a.cu, a.start, INT_MAX, i, descends);
-    const int g = a.group[i], pages = g >= 0 && g < n_groups ? a.pages[g] : 0;
-    int prefix = 0, place = 0;
-    if (q.n > 0 && pages > 0 && pages <= pv.max_pages && (pages << pv.page_shift) <= q.start) {
-      prefix = pages << pv.page_shift;
-      place = atomicAdd(&first_s[g], q.n);
-      atomicMin(&head_s[g], i);
-    }
-    P.reqs[i] = make_int4(prefix, place, 0, 0);
+    T.first[i] = q.first;
+    T.n[i] = q.n;
+    T.start[i] = q.start;
+    T.group[i] = a.group[i];
   }
   if (__syncthreads_or(descends)) {
     if (tid == 0) { P.head[0] = a.sign; P.head[1] = P.head[2] = P.head[3] = 0; }
     return;
   }
-  auto rows_of_group = [&](int g) {      // 0 where the group is one request: that one goes by itself
-    const int n = first_s[g], h = head_s[g];
-    return n > 0 && a.cu[h + 1] - a.cu[h] < n ? n : 0;
-  };
-  auto own = [&](int i, PagedReq& q, int& prefix) {
-    bool d = false;
-    q = paged_req(pv, a.cu, a.start, INT_MAX, i, d);
-    prefix = P.reqs[i].x;
-    if (prefix && rows_of_group(a.group[i]) == 0) prefix = 0;
-    const bool tall = q.n * pv.gq > a.few_max;
-    return ShareEntry{q.n, q.start + q.n - prefix, tall ? pv.rpb_tall : pv.rpb_few, 0, tall};
-  };
-  auto shared = [&](int g) {
-    const int n = rows_of_group(g);
-    const bool tall = (long)n * pv.gq > a.few_max;
-    return ShareEntry{n, n ? a.pages[g] << pv.page_shift : 0, tall ? pv.rpb_tall : pv.rpb_few, 0, tall};
-  };
+#pragma unroll 1
+  for (int i = r0; i < r1; ++i) {
+    const int g = T.group[i], keys = g >= 0 && g < n_groups ? T.g_keys[g] : 0;
+    const bool in = T.n[i] > 0 && keys > 0 && keys <= T.start[i];
+    T.prefix[i] = in ? keys : 0;
+    if (in) {
+      T.place[i] = atomicAdd(&T.g_n[g], T.n[i]);
+      atomicMin(&T.g_head[g], i);
+    }
+  }
+  __syncthreads();
+  auto tall_of = [&](int n) { return (long)n * pv.gq > a.few_max; };
+  auto rpb_of = [&](bool tall) { return tall ? pv.rpb_tall : pv.rpb_few; };
+  auto tiles_of = [&](int n, bool tall) { return (int)((unsigned)(n + rpb_of(tall) - 1) / (unsigned)rpb_of(tall)); };
+  // a group that is one request goes by itself
+  unsigned long long sum[2] = {0, 0};
+#pragma unroll 1
+  for (int i = r0; i < r1; ++i) {
+    const int n = T.n[i], g = T.group[i];
+    if (T.prefix[i] && T.g_n[g] == n) T.prefix[i] = 0;
+    const bool tall = tall_of(n);
+    sum[tall] += (unsigned long long)tiles_of(n, tall) * (unsigned)(T.start[i] + n - T.prefix[i]);
+  }
+#pragma unroll 1
+  for (int g = g0; g < g1; ++g) {
+    const int n = T.g_n[g], h = T.g_head[g];
+    if (n == 0) continue;
+    if (T.n[h] == n) { T.g_keys[g] = 0; continue; }      // (no rows of it below either)
+    const bool tall = tall_of(n);
+    sum[tall] += (unsigned long long)tiles_of(n, tall) * (unsigned)T.g_keys[g];
+  }
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    sum[k] = wave_reduce(sum[k], [](unsigned long long x, unsigned long long y) { return x + y; });
+    if (lane == 0) total_s[k][wave] = sum[k];
+  }
+  __syncthreads();
   // keys of a range of either kind: rows are at most 2^24, keys 2^30
-  long long mine[2] = {0, 0}, total[2];
-  PagedReq q;
-  int prefix;
+  int kps[2];
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    unsigned long long all = 0;
+    for (int w = 0; w < NT / 64; ++w) all += total_s[k][w];
+    const int shift = k ? a.tall_shift : a.few_shift;
+    const unsigned long long per = (all + (1ull << shift) - 1) >> shift;
+    kps[k] = (int)min(max((unsigned long long)(k ? PAGED_KEYS_TALL : PAGED_KEYS_FEW), (per + 63) / 64 * 64), 1ull << 30);
+  }
+  auto ranges_of = [&](int keys, bool tall) { return (int)((unsigned)(keys + kps[tall] - 1) / (unsigned)kps[tall]); };
+  // tall and few items of the requests and of the groups, units of either, places in the list: of this thread, in front of it, and of all
+  int v[7] = {0, 0, 0, 0, 0, 0, 0}, all[7];
 #pragma unroll 1
   for (int i = r0; i < r1; ++i) {
-    const ShareEntry e = own(i, q, prefix);
-    if (e.rows) mine[e.tall] += (long long)((e.rows + e.rpb - 1) / e.rpb) * e.keys;
+    const int n = T.n[i];
+    if (!n) continue;
+    const bool tall = tall_of(n);
+    const int parts = ranges_of(T.start[i] + n - T.prefix[i], tall), count = tiles_of(n, tall) * parts;
+    v[0] += tall ? count : 0;
+    v[1] += tall ? 0 : count;
+    v[2] += T.prefix[i] || parts > 1 ? n * parts : 0;
   }
 #pragma unroll 1
   for (int g = g0; g < g1; ++g) {
-    const ShareEntry e = shared(g);
-    mine[e.tall] += (long long)((e.rows + e.rpb - 1) / e.rpb) * e.keys;
+    const int n = T.g_keys[g] ? T.g_n[g] : 0;
+    if (!n) continue;
+    const bool tall = tall_of(n);
+    const int parts = ranges_of(T.g_keys[g], tall), count = tiles_of(n, tall) * parts;
+    v[3] += tall ? count : 0;
+    v[4] += tall ? 0 : count;
+    v[5] += n * parts;
+    v[6] += n;
   }
-  for (int k = 0; k < 2; ++k) (void)block_scan<NT>(mine[k], sums_s, total[k]);
-  auto keys_of = [&](long long t, int shift, int least) {
-    const long long per = (t + (1ll << shift) - 1) >> shift;
-    return (int)min(max((long long)least, (per + 63) / 64 * 64), 1ll << 30);
-  };
-  const int kps[2] = {keys_of(total[0], a.few_shift, PAGED_KEYS_FEW), keys_of(total[1], a.tall_shift, PAGED_KEYS_TALL)};
-  auto ranges = [&](const ShareEntry& e) { return (int)((unsigned)(e.keys + kps[e.tall] - 1) / (unsigned)kps[e.tall]); };
-  auto tiles = [&](const ShareEntry& e) { return (int)((unsigned)(e.rows + e.rpb - 1) / (unsigned)e.rpb); };
-  // items of either kind (tall ones in the upper half), units and places in the list, in front of each thread's entries
-  long long items_own = 0, items_shared = 0, units_own = 0, units_shared = 0;      // (units_shared: places from bit 36 on)
-#pragma unroll 1
-  for (int i = r0; i < r1; ++i) {
-    const ShareEntry e = own(i, q, prefix);
-    if (!e.rows) continue;
-    const int n = ranges(e);
-    items_own += (long long)(tiles(e) * n) << (e.tall ? 32 : 0);
-    units_own += prefix || n > 1 ? (long long)e.rows * n : 0;
+#pragma unroll
+  for (int k = 0; k < 7; ++k) {
+    const int incl = wave_scan(v[k]);
+    if (lane == 63) scan_s[k][wave] = incl;
+    v[k] = incl - v[k];
   }
-#pragma unroll 1
-  for (int g = g0; g < g1; ++g) {
-    const ShareEntry e = shared(g);
-    if (!e.rows) continue;
-    const int n = ranges(e);
-    items_shared += (long long)(tiles(e) * n) << (e.tall ? 32 : 0);
-    units_shared += ((long long)e.rows << 36) + (long long)e.rows * n;
-  }
-  long long all_own, all_shared, all_units, none;
-  const long long at_own = block_scan<NT>(items_own, sums_s, all_own), at_shared = block_scan<NT>(items_shared, sums_s, all_shared);
-  long long unit_own = block_scan<NT>(units_own, sums_s, all_units), unit_shared = block_scan<NT>(units_shared, sums_s, none);
-  const long long low = (1ll << 36) - 1;
-#pragma unroll 1
-  for (int i = r0; i < r1; ++i) {
-    const ShareEntry e = own(i, q, prefix);
-    const int n = e.rows ? ranges(e) : 0;
-    P.reqs[i] = make_int4(prefix, P.reqs[i].y, (int)unit_own, 0);
-    unit_own += prefix || n > 1 ? (long long)e.rows * n : 0;
-  }
-#pragma unroll 1
-  for (int g = g0; g < g1; ++g) {
-    const ShareEntry e = shared(g);
-    P.groups[g] = make_int4(e.rows, head_s[g], (int)(all_units + (unit_shared & low)), (int)(unit_shared >> 36));
-    if (e.rows) unit_shared += ((long long)e.rows << 36) + (long long)e.rows * ranges(e);
-  }
-  const int n_rows = min(max(a.cu[n_req], 0), pv.max_rows);
-  const int tall_shared = (int)(all_shared >> 32), tall_own = (int)(all_own >> 32), few_shared = (int)(all_shared & 0xFFFFFFFF), few_own = (int)(all_own & 0xFFFFFFFF);
-  if (tid == 0) { P.head[0] = a.sign; P.head[1] = tall_shared + tall_own; P.head[2] = tall_shared + tall_own + few_shared + few_own; P.head[3] = n_rows; }
-  __syncthreads();          // the groups' rows are in P.groups now; the requests' and groups' records are written
-  // items, section by section: an entry's first item in LDS, then an item a thread
-  int base = 0;
-#pragma unroll 1
-  for (int sec = 0; sec < 4; ++sec) {
-    const bool tall = sec < 2, is_shared = (sec & 1) == 0;
-    const int count = sec == 0 ? tall_shared : sec == 1 ? tall_own : sec == 2 ? few_shared : few_own;
-    if (count == 0) continue;
-    auto of = [&](int i, int& pre) {
-      if (is_shared) {
-        const int n = P.groups[i].x;
-        const bool t = (long)n * pv.gq > a.few_max;
-        pre = 0;
-        return ShareEntry{n, n ? a.pages[i] << pv.page_shift : 0, t ? pv.rpb_tall : pv.rpb_few, 0, t};
-      }
-      bool d = false;
-      q = paged_req(pv, a.cu, a.start, INT_MAX, i, d);
-      pre = P.reqs[i].x;
-      const bool t = q.n * pv.gq > a.few_max;
-      return ShareEntry{q.n, q.start + q.n - pre, t ? pv.rpb_tall : pv.rpb_few, 0, t};
-    };
-    __syncthreads();        // the section before has been searched
-    const long long from = is_shared ? at_shared : at_own;
-    int at = tall ? (int)(from >> 32) : (int)(from & 0xFFFFFFFF);
-    for (int i = is_shared ? g0 : r0; i < (is_shared ? g1 : r1); ++i) {
-      int pre;
-      const ShareEntry e = of(i, pre);
-      first_s[i] = at;
-      if (e.rows && e.tall == tall) at += tiles(e) * ranges(e);
-    }
-    __syncthreads();
-#pragma unroll 1
-    for (int y = tid; y < count; y += NT) {
-      const int x[1] = {y};
-      int i[1], pre;
-      last_at_most<1>(first_s, is_shared ? n_groups : n_req, x, i);
-      const ShareEntry e = of(i[0], pre);
-      const int n = ranges(e), rel = y - first_s[i[0]], tile = (int)((unsigned)rel / (unsigned)n), k = rel - tile * n, row0 = tile * e.rpb, r = min(e.rpb, e.rows - row0), len = kps[tall];
-      int4 u, v;
-      if (is_shared) {
-        const int4 g = P.groups[i[0]];
-        u = make_int4(g.y, pv.max_rows + g.w + row0, r, e.keys - 1);
-        v = make_int4(k * len, min(e.keys, k * len + len), g.z + k * e.rows + row0, 0);
-      } else {
-        const int pos0 = q.start + row0, end = pos0 + r;
-        const bool whole = pre == 0 && end <= len;
-        u = make_int4(i[0], q.first + row0, r, pos0);
-        v = make_int4(pre + k * len, min(end, pre + k * len + len), whole ? -1 : P.reqs[i[0]].z + k * e.rows + row0, 1);
-      }
-      P.items[2 * (base + y)] = u;
-      P.items[2 * (base + y) + 1] = v;
-    }
-    base += count;
-  }
-  // rows
   __syncthreads();
-  for (int i = tid; i < n_req; i += NT) first_s[i] = a.cu[i];
+#pragma unroll
+  for (int k = 0; k < 7; ++k) {
+    all[k] = 0;
+    for (int w = 0; w < NT / 64; ++w) {
+      const int x = scan_s[k][w];
+      v[k] += w < wave ? x : 0;
+      all[k] += x;
+    }
+  }
+#pragma unroll 1
+  for (int i = r0; i < r1; ++i) {
+    T.tall[i] = v[0];
+    T.few[i] = v[1];
+    T.unit[i] = v[2];
+    const int n = T.n[i];
+    if (!n) continue;
+    const bool tall = tall_of(n);
+    const int parts = ranges_of(T.start[i] + n - T.prefix[i], tall), count = tiles_of(n, tall) * parts;
+    v[0] += tall ? count : 0;
+    v[1] += tall ? 0 : count;
+    v[2] += T.prefix[i] || parts > 1 ? n * parts : 0;
+  }
+#pragma unroll 1
+  for (int g = g0; g < g1; ++g) {
+    T.g_tall[g] = v[3];
+    T.g_few[g] = v[4];
+    T.g_unit[g] = all[2] + v[5];
+    T.g_list[g] = v[6];
+    const int n = T.g_keys[g] ? T.g_n[g] : 0;
+    if (!n) continue;
+    const bool tall = tall_of(n);
+    const int parts = ranges_of(T.g_keys[g], tall), count = tiles_of(n, tall) * parts;
+    v[3] += tall ? count : 0;
+    v[4] += tall ? 0 : count;
+    v[5] += n * parts;
+    v[6] += n;
+  }
+  const int n_rows = min(max(end_of_all, 0), pv.max_rows), n_tall = all[3] + all[0], n_items = n_tall + all[4] + all[1];
+  if (tid == 0) { P.head[0] = a.sign; P.head[1] = n_tall; P.head[2] = n_items; P.head[3] = n_rows; }
   __syncthreads();
+  // items: the groups' tall ones, the requests', then the few-rows ones likewise
+#pragma unroll 1
+  for (int y = tid; y < n_items; y += NT) {
+    const bool tall = y < n_tall;
+    const int in_kind = tall ? y : y - n_tall, shared_ones = tall ? all[3] : all[4], len = kps[tall], rpb = rpb_of(tall);
+    const bool shared = in_kind < shared_ones;
+    const int x[1] = {shared ? in_kind : in_kind - shared_ones};
+    int at[1];
+    const int* first = shared ? (tall ? T.g_tall : T.g_few) : (tall ? T.tall : T.few);
+    last_at_most<1>(first, shared ? n_groups : n_req, x, at);
+    const int i = at[0], rel = x[0] - first[i], n = shared ? T.g_n[i] : T.n[i], keys = shared ? T.g_keys[i] : T.start[i] + n - T.prefix[i];
+    const int parts = ranges_of(keys, tall), tile = (int)((unsigned)rel / (unsigned)parts), k = rel - tile * parts, row0 = tile * rpb, r = min(rpb, n - row0);
+    int4 u, w;
+    if (shared) {
+      u = make_int4(T.g_head[i], T.g_list[i] + row0, r, keys - 1);
+      w = make_int4(k * len, min(keys, k * len + len), T.g_unit[i] + k * n + row0, 0);
+    } else {
+      const int front = T.prefix[i], pos0 = T.start[i] + row0, end = pos0 + r;
+      const bool whole = front == 0 && end <= len;
+      u = make_int4(i, T.first[i] + row0, r, pos0);
+      w = make_int4(front + k * len, min(end, front + k * len + len), whole ? -1 : T.unit[i] + k * n + row0, 1);
+    }
+    P.items[2 * y] = u;
+    P.items[2 * y + 1] = w;
+  }
 #pragma unroll 1
   for (int t = tid; t < n_rows; t += NT) {
     const int x[1] = {t};
-    int i[1];
-    last_at_most<1>(first_s, n_req, x, i);
-    bool d = false;
-    q = paged_req(pv, a.cu, a.start, INT_MAX, i[0], d);
-    const int j = t - q.first;
-    int4 u = make_int4(0, 0, 0, 0), v = u;
-    if (j >= 0 && j < q.n) {
-      const int4 rec = P.reqs[i[0]];
-      const bool tall = q.n * pv.gq > a.few_max;
-      const int rpb = tall ? pv.rpb_tall : pv.rpb_few, end = q.start + min(j / rpb * rpb + rpb, q.n) - rec.x, n = (int)((unsigned)(end + kps[tall] - 1) / (unsigned)kps[tall]);
-      P.list[t] = make_int2(t, q.start + j);
-      if (rec.x || n > 1) u = make_int4(rec.z + j, n, q.n, 0);
-      if (rec.x) {
-        const int4 g = P.groups[a.group[i[0]]];
-        const int len = kps[(long)g.x * pv.gq > a.few_max], place = rec.y + j;
-        P.list[pv.max_rows + g.w + place] = make_int2(t, q.start + j);
-        v = make_int4(g.z + place, (int)((unsigned)(rec.x + len - 1) / (unsigned)len), g.x, 0);
+    int at[1];
+    last_at_most<1>(T.first, n_req, x, at);
+    const int i = at[0], j = t - T.first[i], n = T.n[i];
+    int4 u = make_int4(0, 0, 0, 0), w = u;
+    if (j >= 0 && j < n) {
+      const bool tall = tall_of(n);
+      const int rpb = rpb_of(tall), front = T.prefix[i], seen = T.start[i] + min((int)((unsigned)j / (unsigned)rpb) * rpb + rpb, n) - front, parts = ranges_of(seen, tall);
+      if (front || parts > 1) u = make_int4(T.unit[i] + j, parts, n, 0);
+      if (front) {
+        const int g = T.group[i], place = T.place[i] + j;
+        P.list[T.g_list[g] + place] = make_int2(t, T.start[i] + j);
+        w = make_int4(T.g_unit[g] + place, ranges_of(front, tall_of(T.g_n[g])), T.g_n[g], 0);
       }
     }
     P.recs[2 * t] = u;
-    P.recs[2 * t + 1] = v;
+    P.recs[2 * t + 1] = w;
   }
 }
 
-// The items of a plan, head by head, over a grid that the chip holds.  With 8 KV heads (or a multiple) a block's heads are those of its die, and a head's keys pass one L2.
+// The items of a plan, head by head, over a grid of blocks that the chip holds.  Tall ones are a block's: with 8 KV heads (or a multiple) block b's are of one head, whose keys stay in
+// the L2 of the block's die.  Then the others, a wave's each: those of the blocks with fewer tall ones come first.
 template <typename CT, int HD, bool TALL>
-__global__ void __launch_bounds__(256, !TALL && sizeof(CT) == 2 ? 3 : 2) paged_shared_mfma_kernel(SharePlan plan, int sign, const float* __restrict__ qkv, long ld,
-                                                                                             const typename PagedWide<CT>::type* __restrict__ q_gain, const float2* __restrict__ rope_tab,
-                                                                                             float eps, PagedOut po, PagedView pv, SharedParts sp) {
+__global__ void __launch_bounds__(256, 2) paged_shared_mfma_kernel(SharePlan plan, int sign, const float* __restrict__ qkv, long ld, const typename PagedWide<CT>::type* __restrict__ q_gain,
+                                                                   const float2* __restrict__ rope_tab, float eps, PagedOut po, PagedView pv, SharedParts sp) {
   if (plan.head[0] != sign) return;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int n_tall = TALL ? plan.head[1] : 0, total = plan.head[2] * pv.nkv;
-  for (int y = blockIdx.x; y < total; y += gridDim.x) {
-    const int item = (int)((unsigned)y / (unsigned)pv.nkv), g = y - item * pv.nkv;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), grid = gridDim.x;
+  const int n_tall = TALL ? plan.head[1] : 0, all_tall = n_tall * pv.nkv, all_few = plan.head[2] * pv.nkv - all_tall;
+  auto item_at = [&](int item) {
     const int4 u = plan.items[2 * item], v = plan.items[2 * item + 1];
-    const SharedItem it{__builtin_amdgcn_readfirstlane(u.x), __builtin_amdgcn_readfirstlane(u.y), __builtin_amdgcn_readfirstlane(u.z), __builtin_amdgcn_readfirstlane(u.w),
-                        __builtin_amdgcn_readfirstlane(v.x), __builtin_amdgcn_readfirstlane(v.y), __builtin_amdgcn_readfirstlane(v.z), __builtin_amdgcn_readfirstlane(v.w)};
-    if (it.kb >= it.ke) continue;             // keys that the tile's rows do not reach
-    // the thread's number and what follows from it are worked out anew for each item: kept through the loop they would be spilled
+    return SharedItem{__builtin_amdgcn_readfirstlane(u.x), __builtin_amdgcn_readfirstlane(u.y), __builtin_amdgcn_readfirstlane(u.z), __builtin_amdgcn_readfirstlane(u.w),
+                      __builtin_amdgcn_readfirstlane(v.x), __builtin_amdgcn_readfirstlane(v.y), __builtin_amdgcn_readfirstlane(v.z), __builtin_amdgcn_readfirstlane(v.w)};
+  };
+  // the lane's number and what follows from it are worked out anew for each item: kept through the loop they would be spilled
+  auto lane_now = [&] {
     unsigned zero = 0;
     asm volatile("" : "+v"(zero));
-    const int tid = 64 * wave + (int)__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, zero));
-    if constexpr (TALL) {
-      if (item < n_tall) paged_tall_item<CT, HD, false, true>(it, g, tid, qkv, ld, q_gain, rope_tab, eps, po, pv, PagedWork{}, sp);
-      else paged_few_item<CT, HD, false, true>(it, g, tid, qkv, ld, q_gain, rope_tab, eps, po, pv, PagedWork{}, sp);
-    } else {
-      paged_few_item<CT, HD, false, true>(it, g, tid, qkv, ld, q_gain, rope_tab, eps, po, pv, PagedWork{}, sp);
+    return (int)__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, zero));
+  };
+  if constexpr (TALL) {
+    for (int y = blockIdx.x; y < all_tall; y += grid) {
+      const int item = (int)((unsigned)y / (unsigned)pv.nkv), g = y - item * pv.nkv;
+      const SharedItem it = item_at(item);
+      if (it.kb < it.ke) paged_tall_item<CT, HD, false, true>(it, g, 64 * wave + lane_now(), qkv, ld, q_gain, rope_tab, eps, po, pv, PagedWork{}, sp);      // (or keys that the tile's rows do not reach)
+      __syncthreads();                          // the item's LDS is free
     }
-    __syncthreads();                          // the item's LDS is free
+  }
+  const int more = all_tall % grid, fewer = grid - more, rank = (int)blockIdx.x >= more ? blockIdx.x - more : fewer + blockIdx.x;
+  for (int y = rank < fewer ? wave * fewer + rank : 4 * fewer + wave * more + rank - fewer; y < all_few; y += 4 * grid) {
+    const int item = (int)((unsigned)y / (unsigned)pv.nkv), g = y - item * pv.nkv;
+    const SharedItem it = item_at(n_tall + item);
+    if (it.kb < it.ke) paged_few_item<CT, HD, false, true>(it, g, lane_now(), wave, qkv, ld, q_gain, rope_tab, eps, po, pv, PagedWork{}, sp);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");      // the item's LDS is free
+    __builtin_amdgcn_wave_barrier();
   }
 }
 
-// A row's parts joined, first the prefix's, then its own, each in the order of the keys: 4 dims of a head a thread.  Rows with one part have been written.
+// A row's parts joined, first the prefix's, then its own, each in the order of the keys: 4 dims of a head a thread, and as many threads as a wave has for it share the parts.  Rows with one part have been written.
 template <typename GT, int HD>
 __global__ void __launch_bounds__(256) paged_shared_join_kernel(SharePlan plan, int sign, PagedOut po, PagedView pv, SharedParts sp) {
   if (plan.head[0] != sign) return;
-  constexpr int T4 = HD / 4;
-  const int n_rows = plan.head[3];
-  const unsigned per_row = (unsigned)pv.nh * T4;
-  const long total = (long)n_rows * per_row;
-  for (long e = (long)blockIdx.x * 256 + threadIdx.x; e < total; e += (long)gridDim.x * 256) {
-    const int t = (int)(e / per_row), c = (int)(e - (long)t * per_row), head = c / T4, d = (c % T4) * 4;
+  constexpr int T4 = HD / 4, SHARE = 64 / T4;
+  const int n_rows = plan.head[3], turn = (threadIdx.x & 63) / T4, d = (threadIdx.x % T4) * 4;
+  const long total = (long)n_rows * pv.nh;
+  for (long e = (long)blockIdx.x * 4 + (threadIdx.x >> 6); e < total; e += (long)gridDim.x * 4) {
+    const int t = (int)(e / pv.nh), head = (int)(e - (long)t * pv.nh);
     const int4 u = plan.recs[2 * t], v = plan.recs[2 * t + 1];
     if (u.y == 0) continue;
     PagedSum sum;
-    if (v.y) sum.add_ranges<false>(sp.weights(v.x, pv.nh, head, HD), sp.sums(v.x, head, HD) + d, (size_t)v.z * sp.unit_floats, 0, v.y, 1);
-    sum.add_ranges<false>(sp.weights(u.x, pv.nh, head, HD), sp.sums(u.x, head, HD) + d, (size_t)u.z * sp.unit_floats, 0, u.y, 1);
-    paged_store4<GT, false>(po, t, head * HD + d, sum.result());
+    if (v.y) sum.add_ranges<false>(sp.weights(v.x, pv.nh, head, HD), sp.sums(v.x, head, HD) + d, (size_t)v.z * sp.unit_floats, turn, v.y, SHARE);
+    sum.add_ranges<false>(sp.weights(u.x, pv.nh, head, HD), sp.sums(u.x, head, HD) + d, (size_t)u.z * sp.unit_floats, turn, u.y, SHARE);
+#pragma unroll
+    for (int o = T4; o < 64; o *= 2)
+      sum.add(__shfl_xor(sum.m, o, 64), __shfl_xor(sum.l, o, 64), f32x4{__shfl_xor(sum.o.x, o, 64), __shfl_xor(sum.o.y, o, 64), __shfl_xor(sum.o.z, o, 64), __shfl_xor(sum.o.w, o, 64)});
+    if (turn == 0) paged_store4<GT, false>(po, t, head * HD + d, sum.result());
   }
 }
 

@@ -212,12 +212,12 @@ hipError_t launch_paged_attention(const dmtd_paged_cache* c, const PagedView& v,
 // ---- shared prefixes ----
 
 // How a step with shared prefixes is laid out: log2 of the blocks per KV head that the key ranges are chosen for, the most items there can be, a unit of partial results, and the sizes.
-struct SharedPlanSizes { int few_shift, tall_shift, few_max; long items, units, unit_floats; size_t list, recs, reqs, groups, plan_bytes; };
+struct SharedPlanSizes { int few_shift, tall_shift, few_max; long items, units, unit_floats; size_t list, recs, scratch, plan_bytes; };
 SharedPlanSizes shared_sizes(const dmtd_paged_cache* c, int n_groups) {
   SharedPlanSizes z{};
   const int GQ = c->n_q_heads / c->n_kv_heads, rpb_few = 16 / GQ, rpb_tall = 128 / GQ;
   const bool bf16 = c->dtype != DMTD_DTYPE_F32;
-  z.few_shift = floor_log2(std::max((bf16 ? PAGED_SLOTS_FEW : PAGED_SLOTS_FP32) / c->n_kv_heads, 1));
+  z.few_shift = floor_log2(std::max(SHARE_SLOTS_FEW / c->n_kv_heads, 1));
   z.tall_shift = floor_log2(std::max(PAGED_SLOTS_TALL / c->n_kv_heads, 1));
   z.few_max = bf16 ? PAGED_FEW : INT_MAX;
   // entries are the requests and the groups of two and more; one of n rows has ceil(n / rows of a tile) tiles, and the ranges of all come to a tile's first and at most 2^shift more of either kind
@@ -227,16 +227,15 @@ SharedPlanSizes shared_sizes(const dmtd_paged_cache* c, int n_groups) {
   z.unit_floats = (long)c->n_q_heads * c->head_dim + (2 * c->n_q_heads + 3) / 4 * 4;
   size_t off = SHARE_HEADER * 4 + (size_t)z.items * 32;
   auto take = [&](size_t bytes) { const size_t o = off; off += align_up(bytes, 16); return o; };
-  z.list = take((size_t)R * 16);
+  z.list = take((size_t)R * 8);
   z.recs = take((size_t)R * 32);
-  z.reqs = take((size_t)c->n_req * 16);
-  z.groups = take((size_t)n_groups * 16);
+  z.scratch = take((size_t)ShareTables::ints(c->n_req, n_groups) * 4);
   z.plan_bytes = align_up(off, 256);
   return z;
 }
 SharePlan share_plan(const SharedPlanSizes& z, void* at) {
   char* p = (char*)at;
-  return SharePlan{(int*)p, (int4*)(p + SHARE_HEADER * 4), (int2*)(p + z.list), (int4*)(p + z.recs), (int4*)(p + z.reqs), (int4*)(p + z.groups)};
+  return SharePlan{(int*)p, (int4*)(p + SHARE_HEADER * 4), (int2*)(p + z.list), (int4*)(p + z.recs), (int*)(p + z.scratch)};
 }
 // What a plan is laid out for; the attention does nothing with a plan of another sign
 int shared_sign(const dmtd_paged_cache* c, int n_groups, int positions) {
@@ -272,7 +271,7 @@ template <typename CT, int HD>
 hipError_t launch_shared_t(const PagedView& v, long items, const SharedCall& a, const PagedOut& out, const SharedParts& sp) {
   typedef typename PagedWide<CT>::type GT;
   constexpr bool BF = sizeof(GT) == 2;
-  const size_t few_lds = std::max((size_t)PAGED_WAVES * (16 / v.gq) * v.gq * HD * 4, (size_t)16 * (BF ? 2 * (HD + ATT_QPAD) * 2 : (HD + 4) * 4));
+  const size_t few_lds = (size_t)4 * 16 * (BF ? 2 * (HD + ATT_QPAD) * 2 : (HD + 4) * 4);      // the queries of each wave
   const long want = items * v.nkv;
   if (BF && (long)v.max_rows * v.gq > PAGED_FEW) {
     if constexpr (BF) {
@@ -284,12 +283,12 @@ hipError_t launch_shared_t(const PagedView& v, long items, const SharedCall& a, 
       hipLaunchKernelGGL(kern, dim3((unsigned)std::min<long>(want, PAGED_RESIDENT_TALL)), dim3(256), lds, a.stream, a.plan, a.sign, a.qkv, a.ld, (const GT*)a.gain, (const float2*)a.rope, a.eps, out, v, sp);
     }
   } else {
-    constexpr int resident = sizeof(CT) == 2 ? 768 : 512;
-    hipLaunchKernelGGL((paged_shared_mfma_kernel<CT, HD, false>), dim3((unsigned)std::min<long>(want, resident)), dim3(256), few_lds, a.stream, a.plan, a.sign, a.qkv, a.ld, (const GT*)a.gain,
+    constexpr int resident = 512;
+    hipLaunchKernelGGL((paged_shared_mfma_kernel<CT, HD, false>), dim3((unsigned)std::min<long>((want + 3) / 4, resident)), dim3(256), few_lds, a.stream, a.plan, a.sign, a.qkv, a.ld, (const GT*)a.gain,
                        (const float2*)a.rope, a.eps, out, v, sp);
   }
-  const long cells = (long)v.max_rows * v.nh * (HD / 4);
-  hipLaunchKernelGGL((paged_shared_join_kernel<GT, HD>), dim3((unsigned)std::min<long>((cells + 255) / 256, 2048)), dim3(256), 0, a.stream, a.plan, a.sign, out, v, sp);
+  const long waves = (long)v.max_rows * v.nh;
+  hipLaunchKernelGGL((paged_shared_join_kernel<GT, HD>), dim3((unsigned)std::min<long>((waves + 3) / 4, 2048)), dim3(256), 0, a.stream, a.plan, a.sign, out, v, sp);
   return hipGetLastError();
 }
 
@@ -419,15 +418,21 @@ int dmtd_shared_plan_build(const dmtd_paged_cache* c, const dmtd_shared_plan* p,
   if (p->positions && p->positions < v.limit) v.limit = p->positions;
   const SharedPlanSizes z = shared_sizes(c, p->n_groups);
   const ShareArgs a{start, cu_rows, group, prefix_pages, p->n_groups, z.few_shift, z.tall_shift, z.few_max, shared_sign(c, p->n_groups, p->positions), share_plan(z, p->plan)};
-  const size_t lds = (size_t)8 * std::max(c->n_req, p->n_groups);
-  static bool big_lds[kMaxDevices];
-  if (c->n_req <= 256 && p->n_groups <= 256 && c->max_rows <= 1024) {
-    hipLaunchKernelGGL(share_plan_kernel<256>, dim3(1), dim3(256), lds, s, a, v);
+  const size_t tables = (size_t)ShareTables::ints(c->n_req, p->n_groups) * 4;
+  static bool big_tables[kMaxDevices], big_counts[kMaxDevices];
+  const int most = std::max(c->n_req, p->n_groups);
+  hipError_t e = hipSuccess;
+  if (most <= 256 && c->max_rows <= 1024) {
+    hipLaunchKernelGGL((share_plan_kernel<256, true>), dim3(1), dim3(256), tables, s, a, v);
+  } else if (most <= SHARE_LDS_ENTRIES) {
+    e = lds_room(share_plan_kernel<1024, true>, tables, (size_t)ShareTables::ints(SHARE_LDS_ENTRIES, SHARE_LDS_ENTRIES) * 4, big_tables);
+    if (e == hipSuccess) hipLaunchKernelGGL((share_plan_kernel<1024, true>), dim3(1), dim3(1024), tables, s, a, v);
   } else {
-    const hipError_t e = lds_room(share_plan_kernel<1024>, lds, 8 * kShareMaxRequests, big_lds);
-    if (e != hipSuccess) return paged_fail(DMTD_EHIP, hipGetErrorString(e));
-    hipLaunchKernelGGL(share_plan_kernel<1024>, dim3(1), dim3(1024), lds, s, a, v);
+    const size_t lds = (size_t)8 * p->n_groups;
+    e = lds_room(share_plan_kernel<1024, false>, lds, (size_t)8 * kShareMaxGroups, big_counts);
+    if (e == hipSuccess) hipLaunchKernelGGL((share_plan_kernel<1024, false>), dim3(1), dim3(1024), lds, s, a, v);
   }
+  if (e != hipSuccess) return paged_fail(DMTD_EHIP, hipGetErrorString(e));
   return paged_done();
 }
 

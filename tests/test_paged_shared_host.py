@@ -82,7 +82,7 @@ def test_the_memory_holds_every_plan(seed):
         nkv, gq, f32 = rng.choice([1, 2, 3, 8, 16, 128]), rng.choice([1, 2, 4, 5, 7, 16]), rng.random() < 0.3
         page, n_req, n_groups = rng.choice([16, 32, 256]), rng.choice([1, 2, 5, 40, 300]), rng.choice([1, 2, 7, 40])
         few, tall = 16 // gq, 128 // gq
-        slots = [1 << floor_log2(max((512 if f32 else 256) // nkv, 1)), 1 << floor_log2(max(256 // nkv, 1))]
+        slots = [1 << floor_log2(max(1024 // nkv, 1)), 1 << floor_log2(max(256 // nkv, 1))]
         rows = [rng.choice([0, 1, 1, 1, 2, 3, rng.randint(0, 400)]) for _ in range(n_req)]
         room = sum(rows) + rng.choice([0, 0, 3, 100]) or 1
         pages = [rng.choice([0, 1, rng.randint(1, 600)]) for _ in range(n_groups)]
@@ -101,8 +101,8 @@ def test_the_memory_holds_every_plan(seed):
         units = sum(n * ceil(length, keys[t]) for (n, length, apart), t in zip(entries, kind) if apart or ceil(length, keys[t]) > 1)
         c = cache(page_size=page, n_req=n_req, max_pages=2000, n_q_heads=nkv * gq, n_kv_heads=nkv, dtype=0 if f32 else 1, max_rows=room)
         lib = pkg.load_library()
-        # behind a header of 64 bytes: 32 an item; a place and two records a row, 48; 16 a request and a group
-        assert 64 + 32 * items + 48 * room + 16 * (n_req + n_groups) <= lib.dmtd_shared_plan_bytes(C.byref(c), n_groups)
+        # behind a header of 64 bytes: 32 an item; a place and two records a row, 40; nine numbers a request and one more, seven a group
+        assert 64 + 32 * items + 40 * room + 4 * (9 * n_req + 1 + 7 * n_groups) <= lib.dmtd_shared_plan_bytes(C.byref(c), n_groups)
         assert units * (nkv * gq * 64 + ceil(2 * nkv * gq, 4) * 4) * 4 <= lib.dmtd_shared_workspace_bytes(C.byref(c))
 
 
