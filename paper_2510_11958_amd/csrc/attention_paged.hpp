@@ -303,8 +303,14 @@ __device__ __forceinline__ void paged_store4(const PagedOut& o, int row, int col
   }
 }
 
+// A pair of probabilities in two bf16 parts
+__device__ __forceinline__ void paged_split2(float a, float b, uint32_t& h, uint32_t& l) {
+  h = pack_bf16x2(a, b);
+  l = pack_bf16x2(a - __uint_as_float(h << 16), b - __uint_as_float(h & 0xFFFF0000u));
+}
+
 // Groups of 16 keys that a wave has under way, and weighs with one maximum: 8 KiB of bf16, and twice that where a wave works alone, with fewer of them on a CU.
-template <typename CT, bool SHARED> __host__ __device__ constexpr int paged_few_groups() { return sizeof(CT) == 4 ? 1 : (sizeof(CT) == 1 ? 2 : 1) * (SHARED ? 2 : 1); }
+template <typename CT, bool SHARED> __host__ __device__ constexpr int paged_few_groups() { return sizeof(CT) == 4 ? 1 : sizeof(CT) == 1 || SHARED ? 2 : 1; }
 
 // Requests with few query vectors.  16 vectors of one KV head are the 16 columns of the matrix tiles, so a block reads each key and value once; its 4
 // waves take groups of 16 keys in turn, which never leave a page, the next group's loads in flight.  Per group, in one wave (lane: sl = lane % 16, kq = lane / 16):
@@ -397,8 +403,9 @@ __device__ __forceinline__ void paged_few_item(const ITEM& it, int g, const int 
   auto load_groups = [&](int base, int j) {
 #pragma unroll
     for (int u = 0; u < G; ++u) {
-      ok[u] = false;
-      if (base + 16 * NW * u < ke) load_kv(base + 16 * NW * u, __builtin_amdgcn_readlane(pages, (j + u) & 63), u);
+      const bool in = u == 0 || base + 16 * NW * u < ke;      // (in place of one behind the last key the first one again, which counts for nothing)
+      load_kv(in ? base + 16 * NW * u : base, __builtin_amdgcn_readlane(pages, (in ? j + u : j) & 63), u);
+      ok[u] &= in;
     }
   };
   if (first < ke) load_groups(first, 0);
@@ -450,140 +457,78 @@ __device__ __forceinline__ void paged_few_item(const ITEM& it, int g, const int 
   f32x4 acc[DPL];
 #pragma unroll
   for (int e = 0; e < DPL; ++e) acc[e] = f32x4{0.f, 0.f, 0.f, 0.f};
-  for (int from = first, j = 0; from < ke; from += 16 * NW * G, j += G) {
-    u32x4 kc[G][KS];
-    vraw_t vc[G][4];
-    bool here[G];
-    uint32_t ksc[G], vsc[G];
+  auto rescale = [&](float f) {                               // the sums this lane holds are those of queries 4 kq + j
 #pragma unroll
-    for (int u = 0; u < G; ++u) {
-      here[u] = ok[u];
+    for (int q = 0; q < 4; ++q) {
+      const float fq = __shfl(f, 4 * kq + q, 64);
 #pragma unroll
-      for (int t = 0; t < KS; ++t) kc[u][t] = kr[u][t];
-#pragma unroll
-      for (int m = 0; m < 4; ++m) vc[u][m] = vr[u][m];
-      if constexpr (Q8) { ksc[u] = ksr[u]; vsc[u] = vsr[u]; }
+      for (int e = 0; e < DPL; ++e) acc[e][q] *= fq;
     }
-    const int next = from + 16 * NW * G;
+  };
+  auto not_finite = [&](const vwide_t& v) {
+    bool bad = false;
+#pragma unroll
+    for (int u = 0; u < VW; ++u) bad |= (BF && (v[u] & 0x7F80u) == 0x7F80u) || (v[u] & 0x7F800000u) == 0x7F800000u;
+    return bad;
+  };
+  if constexpr (G == 1) {
+  for (int base = first, j = 0; base < ke; base += 16 * NW, ++j) {
+    u32x4 ka[KS];
+    vwide_t va[4];
+    const bool here = ok[0];
+#pragma unroll
+    for (int t = 0; t < KS; ++t) ka[t] = kr[0][t];
+#pragma unroll
+    for (int m = 0; m < 4; ++m) va[m] = __builtin_bit_cast(vwide_t, vr[0][m]);
+    const int next = base + 16 * NW;
     if (next < ke) {
-      if (((j + G) & 63) == 0) pages = load_pages(next);
-      load_groups(next, j + G);
+      if ((j & 63) == 63) pages = load_pages(next);
+      load_groups(next, j + 1);
     }
-    bool some = false;
-#pragma unroll
-    for (int u = 0; u < G; ++u) some |= here[u];
-    if (!some) continue;                                      // pages outside the pool
-    // scores of all groups, then one maximum for them
-    float sc[G][4];
-    bool masked[G];
-#pragma unroll
-    for (int u = 0; u < G; ++u) {
-    masked[u] = false;
-    if (!here[u]) {                                           // a page outside the pool, or behind the last key
-#pragma unroll
-      for (int m = 0; m < 4; ++m) sc[u][m] = -INFINITY;
-      continue;
-    }
-    const int base = from + 16 * NW * u;
-    u32x4 ka[KW];
-    if constexpr (Q8) {
-      const float sk = e8m0_scale(ksc[u]);
-#pragma unroll
-      for (int t = 0; t < KS; ++t)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          ka[2 * t + (e >> 1)][2 * (e & 1)] = e4m3_pair<false>(kc[u][t][e], sk);
-          ka[2 * t + (e >> 1)][2 * (e & 1) + 1] = e4m3_pair<true>(kc[u][t][e], sk);
-        }
-    } else {
-#pragma unroll
-      for (int t = 0; t < KS; ++t) ka[t] = kc[u][t];
-    }
+    if (!here) continue;                                      // a page outside the pool
     f32x4 s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int t = 0; t < KW; ++t) {
+    for (int t = 0; t < KS; ++t) {
       if constexpr (!BF) {
         const f32x4 k4 = __builtin_bit_cast(f32x4, ka[t]), q4 = *(const f32x4*)&qhi_s[sl][16 * t + 4 * kq];
 #pragma unroll
         for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_16x16x4f32(k4[e], q4[e], s, 0, 0, 0);
         continue;
       } else {
-        // (8 bits: a lane's 16 codes of a piece are consecutive dims, and the products' eight go by that)
-        const int d0 = Q8 ? 64 * (t >> 1) + 16 * kq + 8 * (t & 1) : 32 * t + 8 * kq;
-        const bf16x8_t ql = __builtin_bit_cast(bf16x8_t, *(const u32x4*)&qlo_s[sl][d0]), qh = __builtin_bit_cast(bf16x8_t, *(const u32x4*)&qhi_s[sl][d0]);
+        const bf16x8_t ql = __builtin_bit_cast(bf16x8_t, *(const u32x4*)&qlo_s[sl][32 * t + 8 * kq]), qh = __builtin_bit_cast(bf16x8_t, *(const u32x4*)&qhi_s[sl][32 * t + 8 * kq]);
         s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, ka[t]), ql, s, 0, 0, 0);
         s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, ka[t]), qh, s, 0, 0, 0);
       }
     }
-    sc[u][0] = s.x; sc[u][1] = s.y; sc[u][2] = s.z; sc[u][3] = s.w;
-    masked[u] = base + 16 > it.pos0 + 1;
-    if (masked[u]) {                                          // keys that some row does not see: their scores are out
+    float sc[4] = {s.x, s.y, s.z, s.w};
+    if (base + 16 > it.pos0 + 1) {
+      // Keys that some row does not see: their scores are out; values behind the last key are whatever lies there, and values of the item's own
+      // positions may be infinite or NaN, which a probability of 0 would not silence: both go in as 0, and the rows that see such a one become NaN
 #pragma unroll
       for (int m = 0; m < 4; ++m) {
         const int key = base + 4 * kq + m;
-        if (key > my_pos || key >= ke) sc[u][m] = -INFINITY;
-      }
-    }
-    }
-    float mx = -INFINITY;
-#pragma unroll
-    for (int u = 0; u < G; ++u) mx = fmaxf(mx, fmaxf(fmaxf(sc[u][0], sc[u][1]), fmaxf(sc[u][2], sc[u][3])));
-    mx = column_max(mx);
-    const float m_new = fmaxf(m_run, mx), m_use = m_new == -INFINITY ? 0.f : m_new;
-    const float f = __builtin_amdgcn_exp2f(m_run - m_use);
-    float psum = 0.f;
-#pragma unroll
-    for (int u = 0; u < G; ++u)
-#pragma unroll
-      for (int m = 0; m < 4; ++m) { sc[u][m] = __builtin_amdgcn_exp2f(sc[u][m] - m_use); psum += sc[u][m]; }      // probabilities from here on
-    l_run = l_run * f + psum;
-    if (__any(m_new > m_run)) {                               // the sums this lane holds are those of queries 4 kq + j
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const float fq = __shfl(f, 4 * kq + q, 64);
-#pragma unroll
-        for (int e = 0; e < DPL; ++e) acc[e][q] *= fq;
-      }
-    }
-    m_run = m_new;
-#pragma unroll
-    for (int u = 0; u < G; ++u) {
-    if (!here[u]) continue;
-    const int base = from + 16 * NW * u;
-    const float (&p)[4] = sc[u];
-    vwide_t va[4];                                            // the values, as bf16 or fp32
-    if constexpr (Q8) {
-#pragma unroll
-      for (int m = 0; m < 4; ++m) {
-        const float sv = e8m0_scale((vsc[u] >> (8 * m)) & 0xFFu);
-#pragma unroll
-        for (int e = 0; e < VW / 2; ++e) { va[m][2 * e] = e4m3_pair<false>(vc[u][m][e], sv); va[m][2 * e + 1] = e4m3_pair<true>(vc[u][m][e], sv); }
-      }
-    } else {
-#pragma unroll
-      for (int m = 0; m < 4; ++m) va[m] = vc[u][m];
-    }
-    if (masked[u]) {
-      // values behind the last key are whatever lies there, and values of the item's own positions may be infinite or NaN, which a probability of 0 would not
-      // silence: both go in as 0, and the rows that see such a one become NaN
-#pragma unroll
-      for (int m = 0; m < 4; ++m) {
-        const int key = base + 4 * kq + m;
+        if (key > my_pos || key >= ke) sc[m] = -INFINITY;
         if (key > it.pos0) {
-          bool bad = false;
-#pragma unroll
-          for (int x = 0; x < VW; ++x) bad |= (BF && (va[m][x] & 0x7F80u) == 0x7F80u) || (va[m][x] & 0x7F800000u) == 0x7F800000u;
+          const bool bad = not_finite(va[m]);
           if (bad && key < ke) {
             if constexpr (SHARED) poison = min(poison, key);
             else atomicMin(&poison_s, key);
           }
-          if (bad || key >= ke) {
-#pragma unroll
-            for (int x = 0; x < VW; ++x) va[m][x] = 0u;
-          }
+          if (bad || key >= ke) va[m] = vwide_t(0u);
         }
       }
     }
+    float mx = fmaxf(fmaxf(sc[0], sc[1]), fmaxf(sc[2], sc[3]));
+    mx = column_max(mx);
+    const float m_new = fmaxf(m_run, mx), m_use = m_new == -INFINITY ? 0.f : m_new;
+    const float f = __builtin_amdgcn_exp2f(m_run - m_use);
+    float p[4];
+    float psum = 0.f;
+#pragma unroll
+    for (int m = 0; m < 4; ++m) { p[m] = __builtin_amdgcn_exp2f(sc[m] - m_use); psum += p[m]; }
+    l_run = l_run * f + psum;
+    if (__any(m_new > m_run)) rescale(f);
+    m_run = m_new;
     if constexpr (!BF) {
 #pragma unroll
       for (int e = 0; e < DPL; ++e)
@@ -595,10 +540,8 @@ __device__ __forceinline__ void paged_few_item(const ITEM& it, int g, const int 
         paged_split3(p[0], p[1], pp[0].x, pp[1].x, pp[2].x);
         paged_split3(p[2], p[3], pp[0].y, pp[1].y, pp[2].y);
       } else {
-        pp[0].x = pack_bf16x2(p[0], p[1]);
-        pp[0].y = pack_bf16x2(p[2], p[3]);
-        pp[1].x = pack_bf16x2(p[0] - __uint_as_float(pp[0].x << 16), p[1] - __uint_as_float(pp[0].x & 0xFFFF0000u));
-        pp[1].y = pack_bf16x2(p[2] - __uint_as_float(pp[0].y << 16), p[3] - __uint_as_float(pp[0].y & 0xFFFF0000u));
+        paged_split2(p[0], p[1], pp[0].x, pp[1].x);
+        paged_split2(p[2], p[3], pp[0].y, pp[1].y);
       }
 #pragma unroll
       for (int e = 0; e < DPL; ++e) {
@@ -609,7 +552,135 @@ __device__ __forceinline__ void paged_few_item(const ITEM& it, int g, const int 
           acc[e] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(bf16x4s_t, pp[z]), __builtin_bit_cast(bf16x4s_t, v4), acc[e], 0, 0, 0);
       }
     }
+  }
+  } else if constexpr (BF) {
+  // G groups at once: the queries stay in registers, the groups' scores are chains that do not wait for each other, one maximum serves all, and the values enter by pairs of groups
+  // (16x16x32: a lane's eight keys are four of either).  8-bit pieces are 16 consecutive dims of a key a lane, and the products' eight go by that.
+  static_assert(PARTS == 2 && G % 2 == 0, "two parts of a probability, pairs of groups");
+  bf16x8_t qh[KW], ql[KW];
+#pragma unroll
+  for (int t = 0; t < KW; ++t) {
+    const int d0 = Q8 ? 64 * (t >> 1) + 16 * kq + 8 * (t & 1) : 32 * t + 8 * kq;
+    qh[t] = __builtin_bit_cast(bf16x8_t, *(const u32x4*)&qhi_s[sl][d0]);
+    ql[t] = __builtin_bit_cast(bf16x8_t, *(const u32x4*)&qlo_s[sl][d0]);
+  }
+  for (int from = first, j = 0; from < ke; from += 16 * NW * G, j += G) {
+    u32x4 kc[G][KS];
+    vraw_t vc[G][4];
+    bool here[G], all = true, some = false;
+    uint32_t ksc[G], vsc[G];
+#pragma unroll
+    for (int u = 0; u < G; ++u) {
+      here[u] = ok[u];
+      all &= ok[u];
+      some |= ok[u];
+#pragma unroll
+      for (int t = 0; t < KS; ++t) kc[u][t] = kr[u][t];
+#pragma unroll
+      for (int m = 0; m < 4; ++m) vc[u][m] = vr[u][m];
+      if constexpr (Q8) { ksc[u] = ksr[u]; vsc[u] = vsr[u]; }
     }
+    const int next = from + 16 * NW * G;
+    if (next < ke) {
+      if (((j + G) & 63) == 0) pages = load_pages(next);
+      load_groups(next, j + G);
+    }
+    if (!some) continue;                                      // pages outside the pool
+    f32x4 s[G];
+#pragma unroll
+    for (int u = 0; u < G; ++u) s[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int t = 0; t < KS; ++t) {
+      constexpr int STEPS = Q8 ? 2 : 1;
+      bf16x8_t k8[G][STEPS];
+#pragma unroll
+      for (int u = 0; u < G; ++u) {
+        if constexpr (Q8) {
+          const float sk = e8m0_scale(ksc[u]);
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+            k8[u][h] = __builtin_bit_cast(bf16x8_t, u32x4{e4m3_pair<false>(kc[u][t][2 * h], sk), e4m3_pair<true>(kc[u][t][2 * h], sk), e4m3_pair<false>(kc[u][t][2 * h + 1], sk),
+                                                          e4m3_pair<true>(kc[u][t][2 * h + 1], sk)});
+        } else {
+          k8[u][0] = __builtin_bit_cast(bf16x8_t, kc[u][t]);
+        }
+      }
+#pragma unroll
+      for (int h = 0; h < STEPS; ++h) {
+#pragma unroll
+        for (int u = 0; u < G; ++u) s[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k8[u][h], ql[STEPS * t + h], s[u], 0, 0, 0);
+#pragma unroll
+        for (int u = 0; u < G; ++u) s[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k8[u][h], qh[STEPS * t + h], s[u], 0, 0, 0);
+      }
+    }
+    const bool edge = next > it.pos0 + 1;                     // keys that some row does not see
+    if (edge || !all) {
+#pragma unroll
+      for (int u = 0; u < G; ++u)
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {
+          const int key = from + 16 * NW * u + 4 * kq + m;
+          if (!here[u] || key > my_pos || key >= ke) s[u][m] = -INFINITY;
+        }
+    }
+    float mx = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < G; ++u) mx = fmaxf(mx, fmaxf(fmaxf(s[u][0], s[u][1]), fmaxf(s[u][2], s[u][3])));
+    mx = column_max(mx);
+    const float m_new = fmaxf(m_run, mx), m_use = m_new == -INFINITY ? 0.f : m_new;
+    const float f = __builtin_amdgcn_exp2f(m_run - m_use);
+    float psum = 0.f;
+    uint32_t ph[G][2], pl[G][2];
+#pragma unroll
+    for (int u = 0; u < G; ++u) {
+      float p[4];
+#pragma unroll
+      for (int m = 0; m < 4; ++m) { p[m] = __builtin_amdgcn_exp2f(s[u][m] - m_use); psum += p[m]; }
+      paged_split2(p[0], p[1], ph[u][0], pl[u][0]);
+      paged_split2(p[2], p[3], ph[u][1], pl[u][1]);
+    }
+    l_run = l_run * f + psum;
+    if (__any(m_new > m_run)) rescale(f);
+    m_run = m_new;
+#pragma unroll
+    for (int u0 = 0; u0 < G; u0 += 2) {
+      vwide_t va[2][4];
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {
+          if constexpr (Q8) {
+            const float sv = e8m0_scale((vsc[u0 + i] >> (8 * m)) & 0xFFu);
+#pragma unroll
+            for (int e = 0; e < VW / 2; ++e) { va[i][m][2 * e] = e4m3_pair<false>(vc[u0 + i][m][e], sv); va[i][m][2 * e + 1] = e4m3_pair<true>(vc[u0 + i][m][e], sv); }
+          } else {
+            va[i][m] = __builtin_bit_cast(vwide_t, vc[u0 + i][m]);
+          }
+        }
+      if (edge || !all) {                                     // (what is silenced here, and why: as above)
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int m = 0; m < 4; ++m) {
+            const int key = from + 16 * NW * (u0 + i) + 4 * kq + m;
+            const bool bad = key > it.pos0 && not_finite(va[i][m]);
+            if (bad && here[u0 + i] && key < ke) {
+              if constexpr (SHARED) poison = min(poison, key);
+              else atomicMin(&poison_s, key);
+            }
+            if (bad || !here[u0 + i] || key >= ke) va[i][m] = vwide_t(0u);
+          }
+      }
+#pragma unroll
+      for (int e = 0; e < DPL; ++e) {
+        const unsigned int sel = (e & 1) ? 0x07060302u : 0x05040100u;
+        const bf16x8_t v8 = __builtin_bit_cast(bf16x8_t, u32x4{__builtin_amdgcn_perm(va[0][1][e >> 1], va[0][0][e >> 1], sel), __builtin_amdgcn_perm(va[0][3][e >> 1], va[0][2][e >> 1], sel),
+                                                               __builtin_amdgcn_perm(va[1][1][e >> 1], va[1][0][e >> 1], sel), __builtin_amdgcn_perm(va[1][3][e >> 1], va[1][2][e >> 1], sel)});
+        acc[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, u32x4{pl[u0][0], pl[u0][1], pl[u0 + 1][0], pl[u0 + 1][1]}), v8, acc[e], 0, 0, 0);
+        acc[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, u32x4{ph[u0][0], ph[u0][1], ph[u0 + 1][0], ph[u0 + 1][1]}), v8, acc[e], 0, 0, 0);
+      }
+    }
+  }
   }
   l_run = column_sum(l_run);
   if constexpr (SHARED) {
