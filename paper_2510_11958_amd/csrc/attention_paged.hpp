@@ -94,6 +94,7 @@ __device__ __forceinline__ int paged_groups(const PagedReq& q, int GQ, int lo, i
 // keys over the requests, kps >= T / 2^shift, so there are at most 2^shift + groups items; those of groups with several ranges (keys > kps, hence ceil(keys / kps) < 2
 // keys / kps) are fewer than 2^(shift + 1), and such groups fewer than 2^shift: what the workspace holds.  Called by whole blocks.  GROUP: y counts the
 // groups with several ranges instead (split and range of the result mean nothing).
+// The few-rows kernel has a group's last ranges, which may be short, behind all others (LAST_APART): where its blocks are somewhat more than the CUs, the short ones share.
 template <int NT, int STEP, bool GROUP, bool TALL = false>
 __device__ __forceinline__ bool paged_find(const PagedView& pv, const int* cu, const int* start, int max_new, int GQ, int lo, int hi, int rpb, int shift, int min_keys,
                                            int y, PagedItem& it) {
@@ -101,6 +102,8 @@ __device__ __forceinline__ bool paged_find(const PagedView& pv, const int* cu, c
     const unsigned long long per = (total + (1ull << shift) - 1) >> shift;
     return (int)min(max((unsigned long long)min_keys, (per + STEP - 1) / STEP * STEP), 1ull << 30);      // no request is longer
   };
+  constexpr bool LAST_APART = !GROUP && !TALL;
+  bool last = false;
   int i, kps, splits, before, slots, multi;
   PagedReq q;
   if (pv.n_req <= 64) {       // a request per lane, every wave for itself
@@ -111,9 +114,19 @@ __device__ __forceinline__ bool paged_find(const PagedView& pv, const int* cu, c
     if (__any(descends)) return false;
     const int gr = paged_groups(q, GQ, lo, hi, rpb);
     kps = keys_of(wave_reduce((unsigned long long)gr * (unsigned)(q.start + q.n), [](unsigned long long a, unsigned long long b) { return a + b; }));
-    const int sp = (int)((unsigned)(q.start + q.n + kps - 1) / (unsigned)kps), items = GROUP ? (sp > 1 ? gr : 0) : gr * sp;
-    const int incl = wave_scan(items);
+    const int sp = (int)((unsigned)(q.start + q.n + kps - 1) / (unsigned)kps);
+    int items = GROUP ? (sp > 1 ? gr : 0) : LAST_APART ? gr * (sp - 1) : gr * sp;
+    int incl = wave_scan(items);
     if (TALL) y = paged_turn(y, __builtin_amdgcn_readlane(incl, 63), pv.nkv);
+    if (LAST_APART) {
+      const int whole = __builtin_amdgcn_readlane(incl, 63);
+      if (y >= whole) {
+        y -= whole;
+        last = true;
+        items = gr;
+        incl = wave_scan(items);
+      }
+    }
     const unsigned long long behind = __ballot(incl > y);
     if (!behind) return false;
     i = __builtin_ctzll(behind);
@@ -147,17 +160,25 @@ __device__ __forceinline__ bool paged_find(const PagedView& pv, const int* cu, c
     };
     for (int j = i0; j < i1; ++j) {
       const PagedShare s = share(j);
-      n_items += GROUP ? (s.splits > 1 ? s.groups : 0) : (long long)s.groups * s.splits;
+      n_items += GROUP ? (s.splits > 1 ? s.groups : 0) : LAST_APART ? ((long long)s.groups << 32) + s.groups * (s.splits - 1) : (long long)s.groups * s.splits;
       if (s.splits > 1) n_multi += ((long long)s.groups << 32) | (unsigned)(s.groups * s.splits);
     }
     long long all, all_multi;
     long long at = block_scan<NT>(n_items, sums_s, all), at_multi = block_scan<NT>(n_multi, sums_s, all_multi);
     if (TALL) y = paged_turn(y, (int)all, pv.nkv);
+    if (LAST_APART) {      // (the ranges in the low half, the last ones in the upper half)
+      const int whole = (int)(all & 0xFFFFFFFF);
+      last = y >= whole;
+      y -= last ? whole : 0;
+      all = last ? all >> 32 : whole;
+      at = last ? at >> 32 : at & 0xFFFFFFFF;
+      n_items = last ? n_items >> 32 : n_items & 0xFFFFFFFF;
+    }
     if (y >= all) return false;
     if (at <= y && y < at + n_items) {
       for (int j = i0; j < i1; ++j) {
         const PagedShare s = share(j);
-        const int n = GROUP ? (s.splits > 1 ? s.groups : 0) : s.groups * s.splits;
+        const int n = GROUP ? (s.splits > 1 ? s.groups : 0) : LAST_APART ? s.groups * (last ? 1 : s.splits - 1) : s.groups * s.splits;
         if (y < at + n) {
           found_s[0] = j; found_s[1] = s.splits; found_s[2] = (int)at; found_s[3] = (int)(at_multi & 0xFFFFFFFF); found_s[4] = (int)(at_multi >> 32);
           break;
@@ -178,13 +199,14 @@ __device__ __forceinline__ bool paged_find(const PagedView& pv, const int* cu, c
   slots = __builtin_amdgcn_readfirstlane(slots);
   multi = __builtin_amdgcn_readfirstlane(multi);
   q = PagedReq{__builtin_amdgcn_readfirstlane(q.first), __builtin_amdgcn_readfirstlane(q.n), __builtin_amdgcn_readfirstlane(q.start)};
-  const int rel = y - before, group = GROUP ? rel : (int)((unsigned)rel / (unsigned)splits);
+  const int per_group = LAST_APART ? (last ? 1 : splits - 1) : splits;
+  const int rel = y - before, group = GROUP ? rel : (int)((unsigned)rel / (unsigned)per_group);
   it.req = i;
   it.first = q.first;
   it.row0 = group * rpb;
   it.r = min(rpb, q.n - it.row0);
   it.pos0 = q.start + it.row0;
-  it.split = GROUP ? 0 : rel - group * splits;
+  it.split = GROUP ? 0 : LAST_APART && last ? splits - 1 : rel - group * per_group;
   it.kb = it.split * kps;
   const int end = it.pos0 + it.r;                   // the group's last row sees the keys in front of this
   it.ke = min(end, it.kb + kps);
