@@ -942,11 +942,26 @@ __device__ __forceinline__ void paged_tall_item(const ITEM& it, int g, const int
 #pragma unroll
       for (int e = 0; e < 4; ++e) { x[t][e] = a[e]; x[t][4 + e] = c[e]; }
     }
+    // gains and angles are asked for together with the row, in front of the keys: one latency instead of three (4.6 us to here without, of a block's 18 with 256 keys)
+    f32x4 turn[T / 2][4];
+    u32x4 gains[T];
+    if (q_gain) {
+#pragma unroll
+      for (int t = 0; t < T; ++t) gains[t] = *(const u32x4*)(q_gain + 16 * t + 8 * hi);
+    }
+    if (rope_tab) {
+      const f32x4* rp = (const f32x4*)(rope_tab + (size_t)rope_pos * (HD / 2) + 8 * hi);
+#pragma unroll
+      for (int t = 0; t < T / 2; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) turn[t][e] = rp[8 * t + e];
+    }
 #pragma unroll
     for (int i = 0; i < KI; ++i) load_k(lane, kb, pages, 0, i);
     aim_v(lane, kb, pages);
 #pragma unroll
     for (int m = 0; m < 4; ++m) load_v(m);
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int t = 0; t < T; ++t)
 #pragma unroll
@@ -958,18 +973,17 @@ __device__ __forceinline__ void paged_tall_item(const ITEM& it, int g, const int
 #pragma unroll
       for (int t = 0; t < T; ++t) {
         float gn[8];
-        Elem<bf16_t>::unpack(*(const u32x4*)(q_gain + 16 * t + 8 * hi), gn);
+        Elem<bf16_t>::unpack(gains[t], gn);
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[t][e] *= rs * gn[e];
       }
     }
     if (rope_tab) {
-      const float2* rp = rope_tab + (size_t)rope_pos * (HD / 2) + 8 * hi;
 #pragma unroll
       for (int t = 0; t < T / 2; ++t)
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const float2 cs = rp[16 * t + e];
+          const float2 cs = make_float2(turn[t][e / 2][2 * (e & 1)], turn[t][e / 2][2 * (e & 1) + 1]);
           const float a = x[t][e], b = x[t + T / 2][e];
           x[t][e] = a * cs.x - b * cs.y;
           x[t + T / 2][e] = b * cs.x + a * cs.y;

@@ -15,7 +15,13 @@
 namespace dmtd {
 
 constexpr int SHARE_HEADER = 16;      // ints in front of the items: sign, tall items, items, rows
+// Query vectors of an entry up to which its tiles are single waves' (us a layer with 32 / 64: 16 requests of 4 vectors behind 16384 shared tokens 31 / 51, 12 of 6 behind 8192, 8-bit, 34 / 36)
+constexpr int SHARE_FEW = 32;
 constexpr int SHARE_SLOTS_FEW = 1024;      // items of single waves that the key ranges are chosen for
+// Items of blocks that the key ranges are chosen for: one on each CU, which reads as fast as it works, and two where one would have SHARE_LONG keys and more: both together do 1.3 times the work, at the
+// cost of twice the parts (us a layer with one / two: 458 rows of 14/2 heads of 64 behind 10000 62 / 56, 5 chunks of 300 behind 3000 102 / 84; 64 rows of 32/8 heads behind 16384 57 / 64)
+constexpr int SHARE_SLOTS_TALL = 256, SHARE_LONG = 1536;
+constexpr int SHARE_KEYS_FP32 = 64;      // shortest range of a wave with an fp32 cache, whose products weigh more (of the others: PAGED_KEYS_FEW)
 constexpr int kShareMaxGroups = kPagedMaxRequests;
 constexpr int SHARE_LDS_ENTRIES = 1024;      // requests, and groups, up to which a plan is worked out in LDS
 
@@ -30,7 +36,7 @@ struct SharePlan {
 
 struct ShareArgs {
   const int *start, *cu, *group, *pages;      // [n_req], [n_req + 1], [n_req], [n_groups]
-  int n_groups, few_shift, tall_shift, few_max;      // query vectors of an entry up to which it goes to the few-rows blocks
+  int n_groups, few_shift, tall_shift, few_max, few_keys;      // few_max: query vectors of an entry up to which its tiles are single waves', few_keys: the shortest range of these
   int sign;
   SharePlan plan;
 };
@@ -132,8 +138,9 @@ __global__ void __launch_bounds__(NT) share_plan_kernel(ShareArgs a, PagedView p
     unsigned long long all = 0;
     for (int w = 0; w < NT / 64; ++w) all += total_s[k][w];
     const int shift = k ? a.tall_shift : a.few_shift;
-    const unsigned long long per = (all + (1ull << shift) - 1) >> shift;
-    kps[k] = (int)min(max((unsigned long long)(k ? PAGED_KEYS_TALL : PAGED_KEYS_FEW), (per + 63) / 64 * 64), 1ull << 30);
+    unsigned long long per = (all + (1ull << shift) - 1) >> shift;
+    if (k && per >= SHARE_LONG) per = (per + 1) / 2;
+    kps[k] = (int)min(max((unsigned long long)(k ? PAGED_KEYS_TALL : a.few_keys), (per + 63) / 64 * 64), 1ull << 30);
   }
   auto ranges_of = [&](int keys, bool tall) { return (int)((unsigned)(keys + kps[tall] - 1) / (unsigned)kps[tall]); };
   // tall and few items of the requests and of the groups, units of either, places in the list: of this thread, in front of it, and of all
@@ -294,16 +301,31 @@ __global__ void __launch_bounds__(256, 2) paged_shared_mfma_kernel(SharePlan pla
 template <typename GT, int HD>
 __global__ void __launch_bounds__(256) paged_shared_join_kernel(SharePlan plan, int sign, PagedOut po, PagedView pv, SharedParts sp) {
   if (plan.head[0] != sign) return;
-  constexpr int T4 = HD / 4, SHARE = 64 / T4;
+  constexpr int T4 = HD / 4, SHARE = 64 / T4, U = 4;      // U: parts of a thread in flight
   const int n_rows = plan.head[3], turn = (threadIdx.x & 63) / T4, d = (threadIdx.x % T4) * 4;
   const long total = (long)n_rows * pv.nh;
   for (long e = (long)blockIdx.x * 4 + (threadIdx.x >> 6); e < total; e += (long)gridDim.x * 4) {
     const int t = (int)(e / pv.nh), head = (int)(e - (long)t * pv.nh);
-    const int4 u = plan.recs[2 * t], v = plan.recs[2 * t + 1];
-    if (u.y == 0) continue;
+    const int4 own = plan.recs[2 * t], front = plan.recs[2 * t + 1];
+    if (own.y == 0) continue;
+    // part k of the row: of the prefix, then its own
+    const int n = front.y + own.y;
+    auto unit = [&](int k) { return k < front.y ? front.x + k * front.z : own.x + (k - front.y) * own.z; };
     PagedSum sum;
-    if (v.y) sum.add_ranges<false>(sp.weights(v.x, pv.nh, head, HD), sp.sums(v.x, head, HD) + d, (size_t)v.z * sp.unit_floats, turn, v.y, SHARE);
-    sum.add_ranges<false>(sp.weights(u.x, pv.nh, head, HD), sp.sums(u.x, head, HD) + d, (size_t)u.z * sp.unit_floats, turn, u.y, SHARE);
+    for (int k0 = turn; k0 < n; k0 += U * SHARE) {
+      float2 w[U];
+      f32x4 x[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (k0 + u * SHARE < n) {
+          const int at = unit(k0 + u * SHARE);
+          w[u] = *(const float2*)sp.weights(at, pv.nh, head, HD);
+          x[u] = *(const f32x4*)(sp.sums(at, head, HD) + d);
+        }
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (k0 + u * SHARE < n) sum.add(w[u].x, w[u].y, x[u]);
+    }
 #pragma unroll
     for (int o = T4; o < 64; o *= 2)
       sum.add(__shfl_xor(sum.m, o, 64), __shfl_xor(sum.l, o, 64), f32x4{__shfl_xor(sum.o.x, o, 64), __shfl_xor(sum.o.y, o, 64), __shfl_xor(sum.o.z, o, 64), __shfl_xor(sum.o.w, o, 64)});

@@ -212,18 +212,19 @@ hipError_t launch_paged_attention(const dmtd_paged_cache* c, const PagedView& v,
 // ---- shared prefixes ----
 
 // How a step with shared prefixes is laid out: log2 of the blocks per KV head that the key ranges are chosen for, the most items there can be, a unit of partial results, and the sizes.
-struct SharedPlanSizes { int few_shift, tall_shift, few_max; long items, units, unit_floats; size_t list, recs, scratch, plan_bytes; };
+struct SharedPlanSizes { int few_shift, tall_shift, few_max, few_keys; long items, units, unit_floats; size_t list, recs, scratch, plan_bytes; };
 SharedPlanSizes shared_sizes(const dmtd_paged_cache* c, int n_groups) {
   SharedPlanSizes z{};
   const int GQ = c->n_q_heads / c->n_kv_heads, rpb_few = 16 / GQ, rpb_tall = 128 / GQ;
   const bool bf16 = c->dtype != DMTD_DTYPE_F32;
   z.few_shift = floor_log2(std::max(SHARE_SLOTS_FEW / c->n_kv_heads, 1));
-  z.tall_shift = floor_log2(std::max(PAGED_SLOTS_TALL / c->n_kv_heads, 1));
-  z.few_max = bf16 ? PAGED_FEW : INT_MAX;
-  // entries are the requests and the groups of two and more; one of n rows has ceil(n / rows of a tile) tiles, and the ranges of all come to a tile's first and at most 2^shift more of either kind
+  z.tall_shift = floor_log2(std::max(SHARE_SLOTS_TALL / c->n_kv_heads, 1));
+  z.few_max = bf16 ? SHARE_FEW : INT_MAX;
+  z.few_keys = bf16 ? PAGED_KEYS_FEW : SHARE_KEYS_FP32;
+  // entries are the requests and the groups of two and more; one of n rows has ceil(n / rows of a tile) tiles, and the ranges of all come to a tile's first and at most 2^shift more of either kind (twice that of tall ones)
   const long R = c->max_rows, reqs = std::min<long>(c->n_req, R);
-  z.items = reqs + std::min<long>(n_groups, reqs / 2) + 2 * (R / rpb_few) + (1L << z.few_shift) + (1L << z.tall_shift);
-  z.units = 2 * R + ((long)rpb_few << z.few_shift) + ((long)rpb_tall << z.tall_shift);
+  z.items = reqs + std::min<long>(n_groups, reqs / 2) + 2 * (R / rpb_few) + (1L << z.few_shift) + (2L << z.tall_shift);
+  z.units = 2 * R + ((long)rpb_few << z.few_shift) + ((long)rpb_tall << (z.tall_shift + 1));
   z.unit_floats = (long)c->n_q_heads * c->head_dim + (2 * c->n_q_heads + 3) / 4 * 4;
   size_t off = SHARE_HEADER * 4 + (size_t)z.items * 32;
   auto take = [&](size_t bytes) { const size_t o = off; off += align_up(bytes, 16); return o; };
@@ -273,7 +274,7 @@ hipError_t launch_shared_t(const PagedView& v, long items, const SharedCall& a, 
   constexpr bool BF = sizeof(GT) == 2;
   const size_t few_lds = (size_t)4 * 16 * (BF ? 2 * (HD + ATT_QPAD) * 2 : (HD + 4) * 4);      // the queries of each wave
   const long want = items * v.nkv;
-  if (BF && (long)v.max_rows * v.gq > PAGED_FEW) {
+  if (BF && (long)v.max_rows * v.gq > SHARE_FEW) {
     if constexpr (BF) {
       auto kern = paged_shared_mfma_kernel<CT, HD, true>;
       const size_t lds = std::max((size_t)4 * 64 * HD * 2 + 1024, few_lds);
@@ -417,7 +418,7 @@ int dmtd_shared_plan_build(const dmtd_paged_cache* c, const dmtd_shared_plan* p,
   PagedView v = paged_view(c, nullptr, 0);
   if (p->positions && p->positions < v.limit) v.limit = p->positions;
   const SharedPlanSizes z = shared_sizes(c, p->n_groups);
-  const ShareArgs a{start, cu_rows, group, prefix_pages, p->n_groups, z.few_shift, z.tall_shift, z.few_max, shared_sign(c, p->n_groups, p->positions), share_plan(z, p->plan)};
+  const ShareArgs a{start, cu_rows, group, prefix_pages, p->n_groups, z.few_shift, z.tall_shift, z.few_max, z.few_keys, shared_sign(c, p->n_groups, p->positions), share_plan(z, p->plan)};
   const size_t tables = (size_t)ShareTables::ints(c->n_req, p->n_groups) * 4;
   static bool big_tables[kMaxDevices], big_counts[kMaxDevices];
   const int most = std::max(c->n_req, p->n_groups);
