@@ -1,6 +1,8 @@
 """Plain 64-bit forms of 8-bit cache rows: e4m3 codes with a power of two a row."""
 import torch
 
+import paged_util as pu
+
 LEAST = 16      # the least scale byte: 2^-111
 
 
@@ -42,3 +44,11 @@ def values(b, e):
     """float64 values of code bytes and scale bytes; a scale of 255 is NaN."""
     v = b.view(torch.float8_e4m3fn).double() * power(e)
     return torch.where((e == 255).unsqueeze(-1), torch.full_like(v, float("nan")), v)
+
+
+def attention(qkv, nq, k, v, *rest):
+    """paged_util.attention over the bf16 values that the codes stand for, queries in two bf16 parts (the last argument), and what one bf16 part of a probability adds to how far a
+    kernel's may be off: each enters its product rounded by at most 2^-8 of itself, so the output is off by at most 2^-8 of sum p |v| (its divisor sums the probabilities unrounded)."""
+    out, tol = pu.attention(qkv, nq, k, v, *rest)
+    size, _ = pu.attention(qkv, nq, k, v.abs(), *rest)
+    return out, tol + 2.0 ** -8 * size

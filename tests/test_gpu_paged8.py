@@ -38,6 +38,9 @@ class Setup8(Setup):
         self.ksd, self.vsd = kw.get("scales") or (self.ke.to(DEV), self.ve.to(DEV))
         return pkg.PagedCache(self.kd, self.vd, ints(self.table), self.nq, self.room, k_scale=self.ksd, v_scale=self.vsd)
 
+    def reference(self):
+        return p8.attention(self.qkv, self.nq, self.k, self.v, self.table, self.page, self.start, self.rows, self.gain, self.rope, True)
+
     def maps(self):
         pad = self.room - self.total
         return ints(self.cu), ints(self.pos + [-1] * pad), ints(self.slots + [-1] * pad, torch.int64)
@@ -437,7 +440,7 @@ def test_the_operators_together(heads, page, graph):
             keys[i] = new_k[a:a + r] if keys[i] is None else torch.cat([keys[i], new_k[a:a + r]])
             values[i] = new_v[a:a + r] if values[i] is None else torch.cat([values[i], new_v[a:a + r]])
             n = keys[i].shape[0]
-            ref, tol = pu.attention(x[:, :nq].reshape(r, -1), nq, keys[i].transpose(0, 1)[None], values[i].transpose(0, 1)[None], [[0]], n, [cached[i]], [r], gain_q, rope, True)
+            ref, tol = p8.attention(x[:, :nq].reshape(r, -1), nq, keys[i].transpose(0, 1)[None], values[i].transpose(0, 1)[None], [[0]], n, [cached[i]], [r], gain_q, rope, True)
             assert ((got[a:a + r].double() - ref).abs() <= tol).all()
             cached[i] += r
             a += r

@@ -5,6 +5,7 @@ import numpy as np
 import pytest
 import torch
 
+import paged8_util as p8
 import paged_util as pu
 import paper_2510_11958_amd as pkg
 from test_gpu_paged import BF, DEV, F32, H1, H4, H6, H7, H8, H16, Maps, Setup, ints
@@ -446,7 +447,7 @@ def test_the_operators_together(heads, dtype, page, graph):
         table = tables.block_table.tolist()
         everything = torch.arange(n_pages * page, device=DEV)
         k, v = [t.view(n_pages, page, nkv, hd).transpose(1, 2).cpu() for t in cache.read(everything)]
-        ref, tol = pu.attention(qkv, nq, k, v, table, page, cached, rows, gain_q, rope, dtype is not F32)
+        ref, tol = (p8.attention if dtype is E8 else pu.attention)(qkv, nq, k, v, table, page, cached, rows, gain_q, rope, dtype is not F32)
         got = out_d.cpu()
         assert ((got[:total].double() - ref).abs() <= tol).all(), turn
         assert (got[total:] == 3.0).all()
