@@ -373,7 +373,7 @@ int dmtd_paged_append(const dmtd_paged_cache* cache, const float* qkv, int64_t l
 
 /* Keys and values out of given places: rows t = 0 .. n - 1 of k_out and v_out, DEVICE [n, ldo] of dtype (DMTD_DTYPE_E4M3: of bf16, the values that the codes stand for, without
  * rounding), n_kv_heads heads of head_dim, 16-byte aligned, ldo a multiple of 8, are what lies in place slots[t] (DEVICE int64 [n], as dmtd_page_tables numbers them, in any order, the same one
- * any number of times).  Rows whose place is outside the pool stay as they were.  n: HOST; 0: nothing is done.  block_table and max_rows are not used.
+ * any number of times).  Rows whose place is outside the pool stay as they were.  n: HOST, times n_kv_heads at most 2^27; 0: nothing is done.  block_table and max_rows are not used.
  * Errors: DMTD_EINVAL, DMTD_EHIP. */
 int dmtd_paged_read(const dmtd_paged_cache* cache, const int64_t* slots, int32_t n, void* k_out, void* v_out, int64_t ldo, void* stream);
 

@@ -633,7 +633,7 @@ class PagedCache(_OnDevice):
     def read(self, slots, k_out=None, v_out=None):
         """Keys and values out of the places ``slots`` (int64 ``[n]``, as :meth:`PageTables.build` numbers them; in any order), into ``k_out`` and ``v_out``
         ``[n, n_kv_heads, head_dim]`` of the cache's type, bfloat16 for 8-bit caches (made if not given).  Rows whose place is outside the pool are not written."""
-        n = slots.shape[0] if len(slots.shape) == 1 and slots.shape[0] <= 1 << 30 else -1
+        n = slots.shape[0] if len(slots.shape) == 1 and slots.shape[0] <= 1 << 27 else -1
         where = _want(slots, "slots", self._i64, self._index, (max(n, 0),))
         shape = (n, *self._kv_heads)
         if k_out is None:

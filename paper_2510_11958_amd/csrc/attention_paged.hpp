@@ -46,12 +46,14 @@ constexpr int PAGED_KEYS_FEW = 128, PAGED_KEYS_TALL = 256;
 // Rows of a request as the kernels read them: none where the lengths do not fit the buffers or the tables.  `descends` is set where cu does not ascend from 0 on: as
 // long as it does, requests share no rows, and what they bring together fits max_rows, which the grids and the workspace are made for.
 struct PagedReq { int first, n, start; };
-__device__ __forceinline__ PagedReq paged_req(const PagedView& pv, const int* cu, const int* start, int max_new, int i, bool& descends) {
-  const int first = cu[i], end = cu[i + 1];
+__device__ __forceinline__ PagedReq paged_req(const PagedView& pv, int first, int end, int start, int max_new, bool& descends) {
   descends |= first < 0 || end < first;
-  PagedReq q{first, (int)((unsigned)end - (unsigned)first), start[i]};
+  PagedReq q{first, (int)((unsigned)end - (unsigned)first), start};
   if (q.first < 0 || q.n < 0 || q.n > max_new || q.first > pv.max_rows - q.n || q.start < 0 || q.start > pv.limit - q.n) q.n = 0;
   return q;
+}
+__device__ __forceinline__ PagedReq paged_req(const PagedView& pv, const int* cu, const int* start, int max_new, int i, bool& descends) {
+  return paged_req(pv, cu[i], cu[i + 1], start[i], max_new, descends);
 }
 
 // Where a launch's results go: rows of the cache's type, or (PLANES) the two bf16 planes that the projections read, in their layout

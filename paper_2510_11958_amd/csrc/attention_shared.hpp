@@ -73,10 +73,11 @@ __global__ void __launch_bounds__(NT) share_plan_kernel(ShareArgs a, PagedView p
   if (!LDS) { T.g_n = share_dyn_smem; T.g_head = share_dyn_smem + n_groups; }
   const int ipr = (n_req + NT - 1) / NT, r0 = min(tid * ipr, n_req), r1 = min(r0 + ipr, n_req);
   const int ipg = (n_groups + NT - 1) / NT, g0 = min(tid * ipg, n_groups), g1 = min(g0 + ipg, n_groups);
-  const int end_of_all = a.cu[n_req];
+  // mostly a thread's only request and group: all asked for before any is waited for
+  const int i0 = min(r0, n_req - 1), end_of_all = a.cu[n_req], first0 = a.cu[i0], end0 = a.cu[i0 + 1], start0 = a.start[i0], group0 = a.group[i0], pages0 = a.pages[min(g0, n_groups - 1)];
 #pragma unroll 1
   for (int g = g0; g < g1; ++g) {
-    const int pages = a.pages[g];
+    const int pages = g == g0 ? pages0 : a.pages[g];
     T.g_n[g] = 0;
     T.g_head[g] = INT_MAX;
     T.g_keys[g] = pages > 0 && pages <= pv.max_pages ? pages << pv.page_shift : 0;
@@ -84,11 +85,12 @@ __global__ void __launch_bounds__(NT) share_plan_kernel(ShareArgs a, PagedView p
   bool descends = false;
 #pragma unroll 1
   for (int i = r0; i < r1; ++i) {
-    const PagedReq q = paged_req(pv, a.cu, a.start, INT_MAX, i, descends);
+    const bool own = i == r0;
+    const PagedReq q = paged_req(pv, own ? first0 : a.cu[i], own ? end0 : a.cu[i + 1], own ? start0 : a.start[i], INT_MAX, descends);
     T.first[i] = q.first;
     T.n[i] = q.n;
     T.start[i] = q.start;
-    T.group[i] = a.group[i];
+    T.group[i] = own ? group0 : a.group[i];
   }
   if (__syncthreads_or(descends)) {
     if (tid == 0) { P.head[0] = a.sign; P.head[1] = P.head[2] = P.head[3] = 0; }

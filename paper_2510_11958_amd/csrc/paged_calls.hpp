@@ -355,7 +355,7 @@ int dmtd_paged_append(const dmtd_paged_cache* c, const float* qkv, int64_t ld, c
 int dmtd_paged_read(const dmtd_paged_cache* c, const int64_t* slots, int32_t n, void* k_out, void* v_out, int64_t ldo, void* stream) {
   int rc = check_cache(c);
   if (rc != DMTD_OK) return rc;
-  if (n < 0 || (long)n * c->n_kv_heads > (1L << 30)) return paged_fail(DMTD_EINVAL, "n must not be negative, and at most 2^30 with the KV heads");
+  if (n < 0 || (long)n * c->n_kv_heads > (1L << 27)) return paged_fail(DMTD_EINVAL, "n must not be negative, and at most 2^27 with the KV heads");
   if (!slots || !aligned(slots, 8)) return paged_fail(DMTD_EINVAL, "slots must be an 8-byte aligned pointer");
   if (!k_out || !v_out || !aligned(k_out, 16) || !aligned(v_out, 16)) return paged_fail(DMTD_EINVAL, "k_out and v_out must be 16-byte aligned pointers");
   if (ldo < (int64_t)c->n_kv_heads * c->head_dim || ldo % 8 || ldo > (1 << 24)) return paged_fail(DMTD_EINVAL, "ldo must be a multiple of 8 that holds a row");

@@ -205,6 +205,10 @@ def test_attention_without_norm_or_rotation(norm, rope):
     Setup8(H8, 32, [70, 0, 200], [1, 40, 3], seed=5, norm=norm, rope=rope).check()
 
 
+def test_ranges_longer_than_a_wave_keeps_page_numbers_for():
+    Setup8((128, 128, 64), 16, [8999], [1], seed=21).check()
+
+
 def test_large_scores():
     Setup8(H8, 16, [300, 40], [1, 90], seed=6, norm=False, spread=100.0).check()
 

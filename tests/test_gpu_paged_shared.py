@@ -125,6 +125,78 @@ def test_more_groups_than_requests(dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+def test_ranges_longer_than_a_wave_keeps_page_numbers_for(dtype):
+    """64 KV heads leave each of them 16 ranges: of a prefix of 20000 tokens a wave's have 1280 keys, 80 groups of 16."""
+    s = shared_setup((64, 64, 64), dtype, 16, [1250], [0, 0], [3, 40], [1, 1], seed=25)
+    s.check(attend(s))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_a_long_prefix(dtype):
+    """One KV head and 130 thousand shared tokens, behind them rows of a block's tile and more."""
+    s = shared_setup((4, 1, 64), dtype, 256, [512], [0, 0, -1, 0], [7, 300, 50, 0], [1, 2, 1, 40], seed=26)
+    s.check(attend(s))
+
+
+def test_as_many_requests_and_groups_as_there_can_be():
+    """8192 of either, whose tables lie in memory instead of LDS, most of the groups of three requests, and rows beyond one round of the join."""
+    n = 8192
+    rng = np.random.RandomState(7)
+    s = shared_setup((2, 1, 64), BF, 16, [1] * n, rng.permutation(np.arange(n) % 2731).tolist(), rng.randint(0, 20, n).tolist(), (rng.rand(n) < 0.7).astype(int).tolist(), seed=27)
+    s.check(attend(s))
+
+
+def test_many_rows_in_groups():
+    """Chunks of thousands of rows behind a shared prefix: more tiles than blocks, more rows than the join's grid."""
+    s = shared_setup((4, 2, 64), BF, 32, [3], [0, 0, 0], [0, 50, 7], [2500, 1, 1700], seed=28)
+    s.check(attend(s))
+
+
+def test_two_plans_at_once():
+    """Two steps of the same caches on two streams, eager and replayed from two graphs in turn, each with its plan and output."""
+    steps = [shared_setup(H8, BF, 16, [40, 3], [0, 1, 0, 0, -1, 1], [5, 60, 0, 700, 30, 2], rows, seed=29) for rows in ([1, 2, 1, 1, 3, 1], [30, 1, 1, 60, 1, 2])]
+    want, runs = [], []
+    for s in steps:
+        c = s.cache()
+        plan = pkg.SharedPlan(c, 2)
+        args = [ints(s.start), ints(s.cu), ints(s.group), ints(s.pages)]
+        qkv, out, gain, rope = s.qkv.to(DEV), torch.zeros(s.room, s.nq, s.hd, dtype=BF, device=DEV), s.dev(s.gain), s.dev(s.rope)
+
+        def run(c=c, plan=plan, args=args, qkv=qkv, out=out, gain=gain, rope=rope):
+            plan.build(*args)
+            c.attention_shared(plan, qkv, out, q_norm=gain, rope=rope, eps=pu.EPS)
+            return out
+
+        s.check(run()[:s.total].cpu())
+        want.append(run().clone())
+        runs.append(run)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in runs]
+    for _ in range(5):
+        for st, run in zip(streams, runs):
+            with torch.cuda.stream(st):
+                run().zero_()
+                run()
+    torch.cuda.synchronize()
+    for run, w in zip(runs, want):
+        assert torch.equal(run(), w)
+    graphs = []
+    for st, run in zip(streams, runs):
+        st.wait_stream(torch.cuda.current_stream())
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=st):
+            out = run()
+        graphs.append((g, out))
+    for turn in range(6):
+        for g, out in graphs:
+            out.zero_()
+            g.replay()
+        torch.cuda.synchronize()
+        for (g, out), w in zip(graphs, want):
+            assert torch.equal(out, w), turn
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("rows", [[1, 1, 1], [4, 3, 2], [100, 70, 33]])
 def test_missing_pages(dtype, rows):
     """Pages outside the pool, in the prefix and behind it, are left out; rows that are left without keys come out as 0."""

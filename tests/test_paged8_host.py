@@ -32,7 +32,7 @@ READ = dict(slots=P, n=4, k_out=P, v_out=P, ldo=128)
 
 @pytest.mark.parametrize("dtype", [0, 1, 3])
 @pytest.mark.parametrize("args, word", [
-    (dict(slots=None), "slots"), (dict(slots=P + 4), "slots"), (dict(n=-1), "n must"), (dict(n=1 << 30), "n must"), (dict(k_out=None), "k_out"), (dict(v_out=None), "v_out"),
+    (dict(slots=None), "slots"), (dict(slots=P + 4), "slots"), (dict(n=-1), "n must"), (dict(n=1 << 30), "n must"), (dict(n=(1 << 26) + 1), "n must"), (dict(k_out=None), "k_out"), (dict(v_out=None), "v_out"),
     (dict(k_out=P + 8), "k_out"), (dict(v_out=P + 4), "v_out"), (dict(ldo=120), "ldo"), (dict(ldo=132), "ldo"), (dict(ldo=1 << 25), "ldo"),
 ])
 def test_paged_read_refuses(dtype, args, word):
