@@ -498,220 +498,220 @@ __device__ __forceinline__ void paged_few_item(const ITEM& it, int g, const int 
     return bad;
   };
   if constexpr (G == 1) {
-  for (int base = first, j = 0; base < ke; base += 16 * NW, ++j) {
-    u32x4 ka[KS];
-    vwide_t va[4];
-    const bool here = ok[0];
+    for (int base = first, j = 0; base < ke; base += 16 * NW, ++j) {
+      u32x4 ka[KS];
+      vwide_t va[4];
+      const bool here = ok[0];
 #pragma unroll
-    for (int t = 0; t < KS; ++t) ka[t] = kr[0][t];
+      for (int t = 0; t < KS; ++t) ka[t] = kr[0][t];
 #pragma unroll
-    for (int m = 0; m < 4; ++m) va[m] = __builtin_bit_cast(vwide_t, vr[0][m]);
-    const int next = base + 16 * NW;
-    if (next < ke) {
-      if ((j & 63) == 63) pages = load_pages(next);
-      load_groups(next, j + 1);
-    }
-    if (!here) continue;                                      // a page outside the pool
-    f32x4 s = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int t = 0; t < KS; ++t) {
-      if constexpr (!BF) {
-        const f32x4 k4 = __builtin_bit_cast(f32x4, ka[t]), q4 = *(const f32x4*)&qhi_s[sl][16 * t + 4 * kq];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_16x16x4f32(k4[e], q4[e], s, 0, 0, 0);
-        continue;
-      } else {
-        const bf16x8_t ql = __builtin_bit_cast(bf16x8_t, *(const u32x4*)&qlo_s[sl][32 * t + 8 * kq]), qh = __builtin_bit_cast(bf16x8_t, *(const u32x4*)&qhi_s[sl][32 * t + 8 * kq]);
-        s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, ka[t]), ql, s, 0, 0, 0);
-        s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, ka[t]), qh, s, 0, 0, 0);
+      for (int m = 0; m < 4; ++m) va[m] = __builtin_bit_cast(vwide_t, vr[0][m]);
+      const int next = base + 16 * NW;
+      if (next < ke) {
+        if ((j & 63) == 63) pages = load_pages(next);
+        load_groups(next, j + 1);
       }
-    }
-    float sc[4] = {s.x, s.y, s.z, s.w};
-    if (base + 16 > it.pos0 + 1) {
-      // Keys that some row does not see: their scores are out; values behind the last key are whatever lies there, and values of the item's own
-      // positions may be infinite or NaN, which a probability of 0 would not silence: both go in as 0, and the rows that see such a one become NaN
+      if (!here) continue;                                      // a page outside the pool
+      f32x4 s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int m = 0; m < 4; ++m) {
-        const int key = base + 4 * kq + m;
-        if (key > my_pos || key >= ke) sc[m] = -INFINITY;
-        if (key > it.pos0) {
-          const bool bad = not_finite(va[m]);
-          if (bad && key < ke) {
-            if constexpr (SHARED) poison = min(poison, key);
-            else atomicMin(&poison_s, key);
+      for (int t = 0; t < KS; ++t) {
+        if constexpr (!BF) {
+          const f32x4 k4 = __builtin_bit_cast(f32x4, ka[t]), q4 = *(const f32x4*)&qhi_s[sl][16 * t + 4 * kq];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_16x16x4f32(k4[e], q4[e], s, 0, 0, 0);
+          continue;
+        } else {
+          const bf16x8_t ql = __builtin_bit_cast(bf16x8_t, *(const u32x4*)&qlo_s[sl][32 * t + 8 * kq]), qh = __builtin_bit_cast(bf16x8_t, *(const u32x4*)&qhi_s[sl][32 * t + 8 * kq]);
+          s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, ka[t]), ql, s, 0, 0, 0);
+          s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, ka[t]), qh, s, 0, 0, 0);
+        }
+      }
+      float sc[4] = {s.x, s.y, s.z, s.w};
+      if (base + 16 > it.pos0 + 1) {
+        // Keys that some row does not see: their scores are out; values behind the last key are whatever lies there, and values of the item's own
+        // positions may be infinite or NaN, which a probability of 0 would not silence: both go in as 0, and the rows that see such a one become NaN
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {
+          const int key = base + 4 * kq + m;
+          if (key > my_pos || key >= ke) sc[m] = -INFINITY;
+          if (key > it.pos0) {
+            const bool bad = not_finite(va[m]);
+            if (bad && key < ke) {
+              if constexpr (SHARED) poison = min(poison, key);
+              else atomicMin(&poison_s, key);
+            }
+            if (bad || key >= ke) va[m] = vwide_t(0u);
           }
-          if (bad || key >= ke) va[m] = vwide_t(0u);
+        }
+      }
+      float mx = fmaxf(fmaxf(sc[0], sc[1]), fmaxf(sc[2], sc[3]));
+      mx = column_max(mx);
+      const float m_new = fmaxf(m_run, mx), m_use = m_new == -INFINITY ? 0.f : m_new;
+      const float f = __builtin_amdgcn_exp2f(m_run - m_use);
+      float p[4];
+      float psum = 0.f;
+#pragma unroll
+      for (int m = 0; m < 4; ++m) { p[m] = __builtin_amdgcn_exp2f(sc[m] - m_use); psum += p[m]; }
+      l_run = l_run * f + psum;
+      if (__any(m_new > m_run)) rescale(f);
+      m_run = m_new;
+      if constexpr (!BF) {
+#pragma unroll
+        for (int e = 0; e < DPL; ++e)
+#pragma unroll
+          for (int m = 0; m < 4; ++m) acc[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(p[m], __uint_as_float(va[m][e]), acc[e], 0, 0, 0);
+      } else {
+        uint2 pp[PARTS];
+        if constexpr (PARTS == 3) {
+          paged_split3(p[0], p[1], pp[0].x, pp[1].x, pp[2].x);
+          paged_split3(p[2], p[3], pp[0].y, pp[1].y, pp[2].y);
+        } else {
+          paged_split2(p[0], p[1], pp[0].x, pp[1].x);
+          paged_split2(p[2], p[3], pp[0].y, pp[1].y);
+        }
+#pragma unroll
+        for (int e = 0; e < DPL; ++e) {
+          const unsigned int sel = (e & 1) ? 0x07060302u : 0x05040100u;
+          const uint2 v4 = make_uint2(__builtin_amdgcn_perm(va[1][e >> 1], va[0][e >> 1], sel), __builtin_amdgcn_perm(va[3][e >> 1], va[2][e >> 1], sel));
+#pragma unroll
+          for (int z = PARTS - 1; z >= 0; --z)
+            acc[e] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(bf16x4s_t, pp[z]), __builtin_bit_cast(bf16x4s_t, v4), acc[e], 0, 0, 0);
         }
       }
     }
-    float mx = fmaxf(fmaxf(sc[0], sc[1]), fmaxf(sc[2], sc[3]));
-    mx = column_max(mx);
-    const float m_new = fmaxf(m_run, mx), m_use = m_new == -INFINITY ? 0.f : m_new;
-    const float f = __builtin_amdgcn_exp2f(m_run - m_use);
-    float p[4];
-    float psum = 0.f;
-#pragma unroll
-    for (int m = 0; m < 4; ++m) { p[m] = __builtin_amdgcn_exp2f(sc[m] - m_use); psum += p[m]; }
-    l_run = l_run * f + psum;
-    if (__any(m_new > m_run)) rescale(f);
-    m_run = m_new;
-    if constexpr (!BF) {
-#pragma unroll
-      for (int e = 0; e < DPL; ++e)
-#pragma unroll
-        for (int m = 0; m < 4; ++m) acc[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(p[m], __uint_as_float(va[m][e]), acc[e], 0, 0, 0);
-    } else {
-      uint2 pp[PARTS];
-      if constexpr (PARTS == 3) {
-        paged_split3(p[0], p[1], pp[0].x, pp[1].x, pp[2].x);
-        paged_split3(p[2], p[3], pp[0].y, pp[1].y, pp[2].y);
-      } else {
-        paged_split2(p[0], p[1], pp[0].x, pp[1].x);
-        paged_split2(p[2], p[3], pp[0].y, pp[1].y);
-      }
-#pragma unroll
-      for (int e = 0; e < DPL; ++e) {
-        const unsigned int sel = (e & 1) ? 0x07060302u : 0x05040100u;
-        const uint2 v4 = make_uint2(__builtin_amdgcn_perm(va[1][e >> 1], va[0][e >> 1], sel), __builtin_amdgcn_perm(va[3][e >> 1], va[2][e >> 1], sel));
-#pragma unroll
-        for (int z = PARTS - 1; z >= 0; --z)
-          acc[e] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(bf16x4s_t, pp[z]), __builtin_bit_cast(bf16x4s_t, v4), acc[e], 0, 0, 0);
-      }
-    }
-  }
   } else if constexpr (BF) {
-  // G groups at once: the queries stay in registers, the groups' scores are chains that do not wait for each other, one maximum serves all, and the values enter by pairs of groups
-  // (16x16x32: a lane's eight keys are four of either).  8-bit pieces are 16 consecutive dims of a key a lane, and the products' eight go by that.
-  static_assert(PARTS <= 2 && G % 2 == 0, "up to two parts of a probability, pairs of groups");
-  bf16x8_t qh[KW], ql[KW];
+    // G groups at once: the queries stay in registers, the groups' scores are chains that do not wait for each other, one maximum serves all, and the values enter by pairs of groups
+    // (16x16x32: a lane's eight keys are four of either).  8-bit pieces are 16 consecutive dims of a key a lane, and the products' eight go by that.
+    static_assert(PARTS <= 2 && G % 2 == 0, "up to two parts of a probability, pairs of groups");
+    bf16x8_t qh[KW], ql[KW];
 #pragma unroll
-  for (int t = 0; t < KW; ++t) {
-    const int d0 = Q8 ? 64 * (t >> 1) + 16 * kq + 8 * (t & 1) : 32 * t + 8 * kq;
-    qh[t] = __builtin_bit_cast(bf16x8_t, *(const u32x4*)&qhi_s[sl][d0]);
-    ql[t] = __builtin_bit_cast(bf16x8_t, *(const u32x4*)&qlo_s[sl][d0]);
-  }
-  for (int from = first, j = 0; from < ke; from += 16 * NW * G, j += G) {
-    u32x4 kc[G][KS];
-    vraw_t vc[G][4];
-    bool here[G], all = true, some = false;
-    uint32_t ksc[G], vsc[G];
-#pragma unroll
-    for (int u = 0; u < G; ++u) {
-      here[u] = ok[u];
-      all &= ok[u];
-      some |= ok[u];
-#pragma unroll
-      for (int t = 0; t < KS; ++t) kc[u][t] = kr[u][t];
-#pragma unroll
-      for (int m = 0; m < 4; ++m) vc[u][m] = vr[u][m];
-      if constexpr (Q8) { ksc[u] = ksr[u]; vsc[u] = vsr[u]; }
+    for (int t = 0; t < KW; ++t) {
+      const int d0 = Q8 ? 64 * (t >> 1) + 16 * kq + 8 * (t & 1) : 32 * t + 8 * kq;
+      qh[t] = __builtin_bit_cast(bf16x8_t, *(const u32x4*)&qhi_s[sl][d0]);
+      ql[t] = __builtin_bit_cast(bf16x8_t, *(const u32x4*)&qlo_s[sl][d0]);
     }
-    const int next = from + 16 * NW * G;
-    if (next < ke) {
-      if (((j + G) & 63) == 0) pages = load_pages(next);
-      load_groups(next, j + G);
-    }
-    if (!some) continue;                                      // pages outside the pool
-    f32x4 s[G];
-#pragma unroll
-    for (int u = 0; u < G; ++u) s[u] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int t = 0; t < KS; ++t) {
-      constexpr int STEPS = Q8 ? 2 : 1;
-      bf16x8_t k8[G][STEPS];
+    for (int from = first, j = 0; from < ke; from += 16 * NW * G, j += G) {
+      u32x4 kc[G][KS];
+      vraw_t vc[G][4];
+      bool here[G], all = true, some = false;
+      uint32_t ksc[G], vsc[G];
 #pragma unroll
       for (int u = 0; u < G; ++u) {
-        if constexpr (Q8) {
-          const float sk = e8m0_scale(ksc[u]);
+        here[u] = ok[u];
+        all &= ok[u];
+        some |= ok[u];
 #pragma unroll
-          for (int h = 0; h < 2; ++h)
-            k8[u][h] = __builtin_bit_cast(bf16x8_t, u32x4{e4m3_pair<false>(kc[u][t][2 * h], sk), e4m3_pair<true>(kc[u][t][2 * h], sk), e4m3_pair<false>(kc[u][t][2 * h + 1], sk),
-                                                          e4m3_pair<true>(kc[u][t][2 * h + 1], sk)});
-        } else {
-          k8[u][0] = __builtin_bit_cast(bf16x8_t, kc[u][t]);
-        }
+        for (int t = 0; t < KS; ++t) kc[u][t] = kr[u][t];
+#pragma unroll
+        for (int m = 0; m < 4; ++m) vc[u][m] = vr[u][m];
+        if constexpr (Q8) { ksc[u] = ksr[u]; vsc[u] = vsr[u]; }
       }
-#pragma unroll
-      for (int h = 0; h < STEPS; ++h) {
-#pragma unroll
-        for (int u = 0; u < G; ++u) s[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k8[u][h], ql[STEPS * t + h], s[u], 0, 0, 0);
-#pragma unroll
-        for (int u = 0; u < G; ++u) s[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k8[u][h], qh[STEPS * t + h], s[u], 0, 0, 0);
+      const int next = from + 16 * NW * G;
+      if (next < ke) {
+        if (((j + G) & 63) == 0) pages = load_pages(next);
+        load_groups(next, j + G);
       }
-    }
-    const bool edge = next > it.pos0 + 1;                     // keys that some row does not see
-    if (edge || !all) {
+      if (!some) continue;                                      // pages outside the pool
+      f32x4 s[G];
 #pragma unroll
-      for (int u = 0; u < G; ++u)
+      for (int u = 0; u < G; ++u) s[u] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int m = 0; m < 4; ++m) {
-          const int key = from + 16 * NW * u + 4 * kq + m;
-          if (!here[u] || key > my_pos || key >= ke) s[u][m] = -INFINITY;
-        }
-    }
-    float mx = -INFINITY;
+      for (int t = 0; t < KS; ++t) {
+        constexpr int STEPS = Q8 ? 2 : 1;
+        bf16x8_t k8[G][STEPS];
 #pragma unroll
-    for (int u = 0; u < G; ++u) mx = fmaxf(mx, fmaxf(fmaxf(s[u][0], s[u][1]), fmaxf(s[u][2], s[u][3])));
-    mx = column_max(mx);
-    const float m_new = fmaxf(m_run, mx), m_use = m_new == -INFINITY ? 0.f : m_new;
-    const float f = __builtin_amdgcn_exp2f(m_run - m_use);
-    float psum = 0.f;
-    uint32_t ph[G][2], pl[G][2];
-#pragma unroll
-    for (int u = 0; u < G; ++u) {
-      float p[4];
-#pragma unroll
-      for (int m = 0; m < 4; ++m) { p[m] = __builtin_amdgcn_exp2f(s[u][m] - m_use); psum += p[m]; }
-      if constexpr (PARTS == 1) {
-        ph[u][0] = pack_bf16x2(p[0], p[1]);
-        ph[u][1] = pack_bf16x2(p[2], p[3]);
-      } else {
-        paged_split2(p[0], p[1], ph[u][0], pl[u][0]);
-        paged_split2(p[2], p[3], ph[u][1], pl[u][1]);
-      }
-    }
-    l_run = l_run * f + psum;
-    if (__any(m_new > m_run)) rescale(f);
-    m_run = m_new;
-#pragma unroll
-    for (int u0 = 0; u0 < G; u0 += 2) {
-      vwide_t va[2][4];
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int m = 0; m < 4; ++m) {
+        for (int u = 0; u < G; ++u) {
           if constexpr (Q8) {
-            const float sv = e8m0_scale((vsc[u0 + i] >> (8 * m)) & 0xFFu);
+            const float sk = e8m0_scale(ksc[u]);
 #pragma unroll
-            for (int e = 0; e < VW / 2; ++e) { va[i][m][2 * e] = e4m3_pair<false>(vc[u0 + i][m][e], sv); va[i][m][2 * e + 1] = e4m3_pair<true>(vc[u0 + i][m][e], sv); }
+            for (int h = 0; h < 2; ++h)
+              k8[u][h] = __builtin_bit_cast(bf16x8_t, u32x4{e4m3_pair<false>(kc[u][t][2 * h], sk), e4m3_pair<true>(kc[u][t][2 * h], sk), e4m3_pair<false>(kc[u][t][2 * h + 1], sk),
+                                                            e4m3_pair<true>(kc[u][t][2 * h + 1], sk)});
           } else {
-            va[i][m] = __builtin_bit_cast(vwide_t, vc[u0 + i][m]);
+            k8[u][0] = __builtin_bit_cast(bf16x8_t, kc[u][t]);
           }
         }
-      if (edge || !all) {                                     // (what is silenced here, and why: as above)
+#pragma unroll
+        for (int h = 0; h < STEPS; ++h) {
+#pragma unroll
+          for (int u = 0; u < G; ++u) s[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k8[u][h], ql[STEPS * t + h], s[u], 0, 0, 0);
+#pragma unroll
+          for (int u = 0; u < G; ++u) s[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k8[u][h], qh[STEPS * t + h], s[u], 0, 0, 0);
+        }
+      }
+      const bool edge = next > it.pos0 + 1;                     // keys that some row does not see
+      if (edge || !all) {
+#pragma unroll
+        for (int u = 0; u < G; ++u)
+#pragma unroll
+          for (int m = 0; m < 4; ++m) {
+            const int key = from + 16 * NW * u + 4 * kq + m;
+            if (!here[u] || key > my_pos || key >= ke) s[u][m] = -INFINITY;
+          }
+      }
+      float mx = -INFINITY;
+#pragma unroll
+      for (int u = 0; u < G; ++u) mx = fmaxf(mx, fmaxf(fmaxf(s[u][0], s[u][1]), fmaxf(s[u][2], s[u][3])));
+      mx = column_max(mx);
+      const float m_new = fmaxf(m_run, mx), m_use = m_new == -INFINITY ? 0.f : m_new;
+      const float f = __builtin_amdgcn_exp2f(m_run - m_use);
+      float psum = 0.f;
+      uint32_t ph[G][2], pl[G][2];
+#pragma unroll
+      for (int u = 0; u < G; ++u) {
+        float p[4];
+#pragma unroll
+        for (int m = 0; m < 4; ++m) { p[m] = __builtin_amdgcn_exp2f(s[u][m] - m_use); psum += p[m]; }
+        if constexpr (PARTS == 1) {
+          ph[u][0] = pack_bf16x2(p[0], p[1]);
+          ph[u][1] = pack_bf16x2(p[2], p[3]);
+        } else {
+          paged_split2(p[0], p[1], ph[u][0], pl[u][0]);
+          paged_split2(p[2], p[3], ph[u][1], pl[u][1]);
+        }
+      }
+      l_run = l_run * f + psum;
+      if (__any(m_new > m_run)) rescale(f);
+      m_run = m_new;
+#pragma unroll
+      for (int u0 = 0; u0 < G; u0 += 2) {
+        vwide_t va[2][4];
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
           for (int m = 0; m < 4; ++m) {
-            const int key = from + 16 * NW * (u0 + i) + 4 * kq + m;
-            const bool bad = key > it.pos0 && not_finite(va[i][m]);
-            if (bad && here[u0 + i] && key < ke) {
-              if constexpr (SHARED) poison = min(poison, key);
-              else atomicMin(&poison_s, key);
-            }
-            if (bad || !here[u0 + i] || key >= ke) va[i][m] = vwide_t(0u);
-          }
-      }
+            if constexpr (Q8) {
+              const float sv = e8m0_scale((vsc[u0 + i] >> (8 * m)) & 0xFFu);
 #pragma unroll
-      for (int e = 0; e < DPL; ++e) {
-        const unsigned int sel = (e & 1) ? 0x07060302u : 0x05040100u;
-        const bf16x8_t v8 = __builtin_bit_cast(bf16x8_t, u32x4{__builtin_amdgcn_perm(va[0][1][e >> 1], va[0][0][e >> 1], sel), __builtin_amdgcn_perm(va[0][3][e >> 1], va[0][2][e >> 1], sel),
-                                                               __builtin_amdgcn_perm(va[1][1][e >> 1], va[1][0][e >> 1], sel), __builtin_amdgcn_perm(va[1][3][e >> 1], va[1][2][e >> 1], sel)});
-        if constexpr (PARTS == 2) acc[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, u32x4{pl[u0][0], pl[u0][1], pl[u0 + 1][0], pl[u0 + 1][1]}), v8, acc[e], 0, 0, 0);
-        acc[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, u32x4{ph[u0][0], ph[u0][1], ph[u0 + 1][0], ph[u0 + 1][1]}), v8, acc[e], 0, 0, 0);
+              for (int e = 0; e < VW / 2; ++e) { va[i][m][2 * e] = e4m3_pair<false>(vc[u0 + i][m][e], sv); va[i][m][2 * e + 1] = e4m3_pair<true>(vc[u0 + i][m][e], sv); }
+            } else {
+              va[i][m] = __builtin_bit_cast(vwide_t, vc[u0 + i][m]);
+            }
+          }
+        if (edge || !all) {                                     // (what is silenced here, and why: as above)
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int m = 0; m < 4; ++m) {
+              const int key = from + 16 * NW * (u0 + i) + 4 * kq + m;
+              const bool bad = key > it.pos0 && not_finite(va[i][m]);
+              if (bad && here[u0 + i] && key < ke) {
+                if constexpr (SHARED) poison = min(poison, key);
+                else atomicMin(&poison_s, key);
+              }
+              if (bad || !here[u0 + i] || key >= ke) va[i][m] = vwide_t(0u);
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < DPL; ++e) {
+          const unsigned int sel = (e & 1) ? 0x07060302u : 0x05040100u;
+          const bf16x8_t v8 = __builtin_bit_cast(bf16x8_t, u32x4{__builtin_amdgcn_perm(va[0][1][e >> 1], va[0][0][e >> 1], sel), __builtin_amdgcn_perm(va[0][3][e >> 1], va[0][2][e >> 1], sel),
+                                                                 __builtin_amdgcn_perm(va[1][1][e >> 1], va[1][0][e >> 1], sel), __builtin_amdgcn_perm(va[1][3][e >> 1], va[1][2][e >> 1], sel)});
+          if constexpr (PARTS == 2) acc[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, u32x4{pl[u0][0], pl[u0][1], pl[u0 + 1][0], pl[u0 + 1][1]}), v8, acc[e], 0, 0, 0);
+          acc[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, u32x4{ph[u0][0], ph[u0][1], ph[u0 + 1][0], ph[u0 + 1][1]}), v8, acc[e], 0, 0, 0);
+        }
       }
     }
-  }
   }
   l_run = column_sum(l_run);
   if constexpr (SHARED) {
@@ -739,48 +739,48 @@ __device__ __forceinline__ void paged_few_item(const ITEM& it, int g, const int 
     }
     return;
   } else {
-  // the waves' results of a vector, 4 consecutive dims a thread
-  __syncthreads();
-  if (kq == 0 && sl < QV) { wm[wave][sl] = m_run; wl[wave][sl] = l_run; }
+    // the waves' results of a vector, 4 consecutive dims a thread
+    __syncthreads();
+    if (kq == 0 && sl < QV) { wm[wave][sl] = m_run; wl[wave][sl] = l_run; }
 #pragma unroll
-  for (int q = 0; q < 4; ++q) {
-    if (4 * kq + q < QV) {
-      float* dst = wacc + ((size_t)wave * QV + 4 * kq + q) * HD + DPL * sl;
+    for (int q = 0; q < 4; ++q) {
+      if (4 * kq + q < QV) {
+        float* dst = wacc + ((size_t)wave * QV + 4 * kq + q) * HD + DPL * sl;
 #pragma unroll
-      for (int e = 0; e < DPL; ++e) dst[e] = acc[e][q];
+        for (int e = 0; e < DPL; ++e) dst[e] = acc[e][q];
+      }
     }
-  }
-  __syncthreads();
-  constexpr size_t SLOT = (size_t)QVT * (HD + 2);
-  float* part = wk.part + ((size_t)(it.slot + it.split) * pv.nkv + g) * SLOT;
-  auto store = [&](int v, int d, const f32x4& x) {
-    const int r = pv.row_of(v);
-    paged_store4<GT, PLANES>(po, it.first + it.row0 + r, (g * GQ + v - r * GQ) * HD + d, x);
-  };
-  for (int e = tid; e < QV * (HD / 4); e += NT) {
-    const int v = e / (HD / 4), d = (e % (HD / 4)) * 4;
-    float mm = wm[0][v];
+    __syncthreads();
+    constexpr size_t SLOT = (size_t)QVT * (HD + 2);
+    float* part = wk.part + ((size_t)(it.slot + it.split) * pv.nkv + g) * SLOT;
+    auto store = [&](int v, int d, const f32x4& x) {
+      const int r = pv.row_of(v);
+      paged_store4<GT, PLANES>(po, it.first + it.row0 + r, (g * GQ + v - r * GQ) * HD + d, x);
+    };
+    for (int e = tid; e < QV * (HD / 4); e += NT) {
+      const int v = e / (HD / 4), d = (e % (HD / 4)) * 4;
+      float mm = wm[0][v];
 #pragma unroll
-    for (int w = 1; w < NW; ++w) mm = fmaxf(mm, wm[w][v]);
-    const float mu = mm == -INFINITY ? 0.f : mm;
-    f32x4 o = {0.f, 0.f, 0.f, 0.f};
-    float l = 0.f;
+      for (int w = 1; w < NW; ++w) mm = fmaxf(mm, wm[w][v]);
+      const float mu = mm == -INFINITY ? 0.f : mm;
+      f32x4 o = {0.f, 0.f, 0.f, 0.f};
+      float l = 0.f;
 #pragma unroll
-    for (int w = 0; w < NW; ++w) {
-      const float fw = __builtin_amdgcn_exp2f(wm[w][v] - mu);
-      o += fw * *(const f32x4*)(wacc + ((size_t)w * QV + v) * HD + d);
-      l += fw * wl[w][v];
+      for (int w = 0; w < NW; ++w) {
+        const float fw = __builtin_amdgcn_exp2f(wm[w][v] - mu);
+        o += fw * *(const f32x4*)(wacc + ((size_t)w * QV + v) * HD + d);
+        l += fw * wl[w][v];
+      }
+      if (it.pos0 + pv.row_of(v) >= poison_s) l = __uint_as_float(0x7FC00000u);
+      if (it.n == 1) {
+        const float inv = l == 0.f ? 0.f : 1.0f / l;
+        store(v, d, f32x4{o.x * inv, o.y * inv, o.z * inv, o.w * inv});
+      } else {
+        put_through4(part + (size_t)v * HD + d, o);
+        if (d == 0) put_through(part + (size_t)QVT * HD + 2 * v, mm, l);
+      }
     }
-    if (it.pos0 + pv.row_of(v) >= poison_s) l = __uint_as_float(0x7FC00000u);
-    if (it.n == 1) {
-      const float inv = l == 0.f ? 0.f : 1.0f / l;
-      store(v, d, f32x4{o.x * inv, o.y * inv, o.z * inv, o.w * inv});
-    } else {
-      put_through4(part + (size_t)v * HD + d, o);
-      if (d == 0) put_through(part + (size_t)QVT * HD + 2 * v, mm, l);
-    }
-  }
-  if (it.n > 1) paged_join<HD, QVT, NT>(wk, it, pv.nkv, g, QV, (f32x4*)paged_dyn_smem, store);
+    if (it.n > 1) paged_join<HD, QVT, NT>(wk, it, pv.nkv, g, QV, (f32x4*)paged_dyn_smem, store);
   }
 }
 
@@ -951,7 +951,7 @@ __device__ __forceinline__ void paged_tall_item(const ITEM& it, int g, const int
 #pragma unroll
       for (int e = 0; e < 4; ++e) { x[t][e] = a[e]; x[t][4 + e] = c[e]; }
     }
-    // gains and angles are asked for together with the row, in front of the keys: one latency instead of three (4.6 us to here without, of a block's 18 with 256 keys)
+    // gains and angles are asked for together with the row, in front of the keys: one latency instead of three (64 rows of 32/8 heads behind 16384 shared tokens, four layers, 249 -> 245 us)
     f32x4 turn[T / 2][4];
     u32x4 gains[T];
     if (q_gain) {
@@ -1204,26 +1204,26 @@ __device__ __forceinline__ void paged_tall_item(const ITEM& it, int g, const int
           paged_store4<bf16_t, PLANES>(po, to, co + 32 * t + 8 * q, f32x4{acc[t][4 * q] * inv, acc[t][4 * q + 1] * inv, acc[t][4 * q + 2] * inv, acc[t][4 * q + 3] * inv});
     }
   } else {
-  constexpr size_t SLOT = (size_t)QVT * (HD + 2);
-  if (it.n == 1) {
+    constexpr size_t SLOT = (size_t)QVT * (HD + 2);
+    if (it.n == 1) {
+      if (qo < QV) {
+        const float inv = l_run == 0.f ? 0.f : 1.0f / l_run;
+#pragma unroll
+        for (int t = 0; t < DT; ++t)
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+            paged_store4<bf16_t, PLANES>(po, it.first + ro, co + 32 * t + 8 * q, f32x4{acc[t][4 * q] * inv, acc[t][4 * q + 1] * inv, acc[t][4 * q + 2] * inv, acc[t][4 * q + 3] * inv});
+      }
+      return;
+    }
+    float* part = wk.part + ((size_t)(it.slot + it.split) * pv.nkv + g) * SLOT;
     if (qo < QV) {
-      const float inv = l_run == 0.f ? 0.f : 1.0f / l_run;
 #pragma unroll
       for (int t = 0; t < DT; ++t)
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
-          paged_store4<bf16_t, PLANES>(po, it.first + ro, co + 32 * t + 8 * q, f32x4{acc[t][4 * q] * inv, acc[t][4 * q + 1] * inv, acc[t][4 * q + 2] * inv, acc[t][4 * q + 3] * inv});
+        for (int q = 0; q < 4; ++q) *(f32x4*)(part + (size_t)qo * HD + 32 * t + 8 * q + 4 * (ln >> 5)) = f32x4{acc[t][4 * q], acc[t][4 * q + 1], acc[t][4 * q + 2], acc[t][4 * q + 3]};
+      if (ln < 32) *(float2*)(part + (size_t)QVT * HD + 2 * qo) = make_float2(m_run, l_run);
     }
-    return;
-  }
-  float* part = wk.part + ((size_t)(it.slot + it.split) * pv.nkv + g) * SLOT;
-  if (qo < QV) {
-#pragma unroll
-    for (int t = 0; t < DT; ++t)
-#pragma unroll
-      for (int q = 0; q < 4; ++q) *(f32x4*)(part + (size_t)qo * HD + 32 * t + 8 * q + 4 * (ln >> 5)) = f32x4{acc[t][4 * q], acc[t][4 * q + 1], acc[t][4 * q + 2], acc[t][4 * q + 3]};
-    if (ln < 32) *(float2*)(part + (size_t)QVT * HD + 2 * qo) = make_float2(m_run, l_run);
-  }
   }
 }
 

@@ -397,12 +397,12 @@ __global__ void __launch_bounds__(256) paged_append_kernel(const float* __restri
     if (l == 0) { pv.ks[sc] = (unsigned char)ek; pv.vs[sc] = (unsigned char)ev; }
     return;
   } else {
-  store_elems<HL>((CT*)pv.k + at, x0);
-  store_elems<HL>((CT*)pv.k + at + half, x1);
+    store_elems<HL>((CT*)pv.k + at, x0);
+    store_elems<HL>((CT*)pv.k + at + half, x1);
 #pragma unroll
-  for (int e = 0; e < HL; ++e) { x0[e] = w.a[e]; x1[e] = w.b[e]; }
-  store_elems<HL>((CT*)pv.v + at, x0);
-  store_elems<HL>((CT*)pv.v + at + half, x1);
+    for (int e = 0; e < HL; ++e) { x0[e] = w.a[e]; x1[e] = w.b[e]; }
+    store_elems<HL>((CT*)pv.v + at, x0);
+    store_elems<HL>((CT*)pv.v + at + half, x1);
   }
 }
 
