@@ -19,7 +19,7 @@ constexpr int SHARE_HEADER = 16;      // ints in front of the items: sign, tall 
 constexpr int SHARE_FEW = 32;
 constexpr int SHARE_SLOTS_FEW = 1024;      // items of single waves that the key ranges are chosen for
 // Items of blocks that the key ranges are chosen for: one on each CU, which reads as fast as it works, and two where one would have SHARE_LONG keys and more: both together do 1.3 times the work, at the
-// cost of twice the parts (us a layer with one / two: 458 rows of 14/2 heads of 64 behind 10000 62 / 56, 5 chunks of 300 behind 3000 102 / 84; 64 rows of 32/8 heads behind 16384 57 / 64)
+// cost of twice the parts (us a layer with one / two: 458 rows of 14/2 heads of 64 behind 10000 73 / 56, 5 chunks of 300 behind 3000 107 / 89; 64 rows of 32/8 heads behind 16384 60 / 67)
 constexpr int SHARE_SLOTS_TALL = 256, SHARE_LONG = 1536;
 constexpr int SHARE_KEYS_FP32 = 64;      // shortest range of a wave with an fp32 cache, whose products weigh more (of the others: PAGED_KEYS_FEW)
 constexpr int kShareMaxGroups = kPagedMaxRequests;
@@ -60,12 +60,12 @@ struct ShareTables {
 // The plan of a step, in one block.  Own entries are the requests, with the keys behind their prefix; prefix entries are the groups of two requests and more that have rows.  A request
 // takes part in its group if its tokens reach beyond the prefix, and goes by itself over its whole table otherwise.  Its place among the group's rows is given out by an atomic add: where a
 // row stands in its tile has no influence on its results.  All ranges of a kind have kps keys, chosen as in paged_find.
-// Bound by its chain of round trips and barriers: three of the former, the tables being in LDS (57 requests, 750 items: 4.6 us; with the tables in memory 11.8).
+// Bound by its chain of round trips and barriers: three of the former, the tables being in LDS (57 requests: 7.0 us; with the tables in memory 11.8).
 // LDS false: more requests or groups than that; the tables are in the plan's scratch, the groups' counts still in LDS.
 template <int NT, bool LDS>
 __global__ void __launch_bounds__(NT) share_plan_kernel(ShareArgs a, PagedView pv) {
   extern __shared__ int share_dyn_smem[];
-  __shared__ unsigned long long total_s[2][NT / 64];
+  __shared__ unsigned long long total_s[3][NT / 64];
   __shared__ int scan_s[7][NT / 64];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n_req = pv.n_req, n_groups = a.n_groups;
   const SharePlan& P = a.plan;
@@ -111,13 +111,15 @@ __global__ void __launch_bounds__(NT) share_plan_kernel(ShareArgs a, PagedView p
   auto rpb_of = [&](bool tall) { return tall ? pv.rpb_tall : pv.rpb_few; };
   auto tiles_of = [&](int n, bool tall) { return (int)((unsigned)(n + rpb_of(tall) - 1) / (unsigned)rpb_of(tall)); };
   // a group that is one request goes by itself
-  unsigned long long sum[2] = {0, 0};
+  unsigned long long sum[3] = {0, 0, 0};      // keys of the tiles of either kind, tall tiles
 #pragma unroll 1
   for (int i = r0; i < r1; ++i) {
     const int n = T.n[i], g = T.group[i];
     if (T.prefix[i] && T.g_n[g] == n) T.prefix[i] = 0;
     const bool tall = tall_of(n);
-    sum[tall] += (unsigned long long)tiles_of(n, tall) * (unsigned)(T.start[i] + n - T.prefix[i]);
+    const int tiles = tiles_of(n, tall);
+    sum[tall] += (unsigned long long)tiles * (unsigned)(T.start[i] + n - T.prefix[i]);
+    sum[2] += tall ? tiles : 0;
   }
 #pragma unroll 1
   for (int g = g0; g < g1; ++g) {
@@ -125,23 +127,31 @@ __global__ void __launch_bounds__(NT) share_plan_kernel(ShareArgs a, PagedView p
     if (n == 0) continue;
     if (T.n[h] == n) { T.g_keys[g] = 0; continue; }      // (no rows of it below either)
     const bool tall = tall_of(n);
-    sum[tall] += (unsigned long long)tiles_of(n, tall) * (unsigned)T.g_keys[g];
+    const int tiles = tiles_of(n, tall);
+    sum[tall] += (unsigned long long)tiles * (unsigned)T.g_keys[g];
+    sum[2] += tall ? tiles : 0;
   }
 #pragma unroll
-  for (int k = 0; k < 2; ++k) {
+  for (int k = 0; k < 3; ++k) {
     sum[k] = wave_reduce(sum[k], [](unsigned long long x, unsigned long long y) { return x + y; });
     if (lane == 0) total_s[k][wave] = sum[k];
   }
   __syncthreads();
   // keys of a range of either kind: rows are at most 2^24, keys 2^30
   int kps[2];
+  unsigned long long tall_tiles = 0;
+  for (int w = 0; w < NT / 64; ++w) tall_tiles += total_s[2][w];
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
     unsigned long long all = 0;
     for (int w = 0; w < NT / 64; ++w) all += total_s[k][w];
     const int shift = k ? a.tall_shift : a.few_shift;
     unsigned long long per = (all + (1ull << shift) - 1) >> shift;
-    if (k && per >= SHARE_LONG) per = (per + 1) / 2;
+    if (k && per >= SHARE_LONG) {
+      // every tile's last range may be a short one: of 2^(shift + 1) items, no more than the chip holds, those are set aside, if that leaves most of them (16 items in a second round: 66 us for 56)
+      const unsigned items = (2u << shift) - (tall_tiles < (1ull << shift) ? (unsigned)tall_tiles : 0u);
+      per = (all + items - 1) / items;
+    }
     kps[k] = (int)min(max((unsigned long long)(k ? PAGED_KEYS_TALL : a.few_keys), (per + 63) / 64 * 64), 1ull << 30);
   }
   auto ranges_of = [&](int keys, bool tall) { return (int)((unsigned)(keys + kps[tall] - 1) / (unsigned)kps[tall]); };

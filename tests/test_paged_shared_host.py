@@ -97,7 +97,9 @@ def test_the_memory_holds_every_plan(seed):
         entries += [(r, s + r - f, f > 0) for r, s, f in zip(rows, start, front) if r]
         kind = [not f32 and n * gq > 32 for n, _, _ in entries]
         per = [ceil(sum(ceil(e[0], tall if k else few) * e[1] for e, t in zip(entries, kind) if t == k), slots[k]) for k in (0, 1)]
-        per[1] = ceil(per[1], 2) if per[1] >= 1024 else per[1]
+        if per[1] >= 1536:
+            in_all, tiles = sum(ceil(e[0], tall) * e[1] for e, t in zip(entries, kind) if t), sum(ceil(e[0], tall) for e, t in zip(entries, kind) if t)
+            per[1] = ceil(in_all, 2 * slots[1] - (tiles if tiles < slots[1] else 0))
         keys = [max((64 if f32 else 128, 256)[k], ceil(per[k], 64) * 64) for k in (0, 1)]
         items = sum(ceil(n, tall if t else few) * ceil(length, keys[t]) for (n, length, _), t in zip(entries, kind))
         units = sum(n * ceil(length, keys[t]) for (n, length, apart), t in zip(entries, kind) if apart or ceil(length, keys[t]) > 1)
