@@ -15,7 +15,7 @@
 namespace dmtd {
 
 constexpr int SHARE_HEADER = 16;      // ints in front of the items: sign, tall items, items, rows
-// Query vectors of an entry up to which its tiles are single waves' (us a layer with 32 / 64: 16 requests of 4 vectors behind 16384 shared tokens 31 / 51, 12 of 6 behind 8192, 8-bit, 34 / 36)
+// Query vectors of an entry up to which its tiles are single waves' (us a layer with 32 / 64: 16 requests of 4 vectors behind 16384 shared tokens 36 / 54, 12 of 6 behind 8192, 8-bit, 36 / 38)
 constexpr int SHARE_FEW = 32;
 constexpr int SHARE_SLOTS_FEW = 1024;      // items of single waves that the key ranges are chosen for
 // Items of blocks that the key ranges are chosen for: one on each CU, which reads as fast as it works, and two where one would have SHARE_LONG keys and more: both together do 1.3 times the work, at the
