@@ -366,7 +366,8 @@ typedef struct dmtd_paged_cache {
  * qkv: DEVICE float32 [max_rows, ld], the fused projection's rows: n_q_heads query heads, then n_kv_heads keys, then n_kv_heads values, of head_dim
  * each; 16-byte aligned, ld a multiple of 4.  cu_rows, row_pos, slots: of dmtd_page_tables (of cu_rows only the last entry is read).
  * rope: DEVICE float32 [rope_len][head_dim / 2][2], (cos, sin) of the pair (i, i + head_dim / 2) at each position; NULL: no rotation.
- * Rows with a place outside the pool, or a position outside the block table or the rotary table, are not stored.  Two rows with the same place leave either's values there.
+ * Rows with a place outside the pool, or a position outside the block table or the rotary table, are not stored.  Two rows with the same place leave either's values there
+ * (DMTD_DTYPE_E4M3: codes of one may meet the power of two of the other, a value of neither; dmtd_page_tables gives every row a place of its own).
  * Errors: DMTD_EINVAL, DMTD_EHIP. */
 int dmtd_paged_append(const dmtd_paged_cache* cache, const float* qkv, int64_t ld, const int32_t* cu_rows, const int32_t* row_pos, const int64_t* slots,
                       const void* k_norm, float eps, const float* rope, int32_t rope_len, void* stream);
@@ -382,7 +383,8 @@ size_t dmtd_paged_workspace_bytes(const dmtd_paged_cache* cache);
 
 /* Attention of a step's rows over their requests' pages: out[t, h] = sum_j p_j v_j with p = softmax(q_t,h . k_j / sqrt(head_dim)) over the keys
  * j = 0 .. position of row t of its request, whose own key is in the cache already; queries are normalised (q_norm, eps) and rotated (rope) as the keys
- * were by dmtd_paged_append.  Softmax and sums in float32; products of bf16 and e4m3 caches on the matrix cores, queries and probabilities as two bf16 parts each.
+ * were by dmtd_paged_append.  Softmax and sums in float32; products of bf16 and e4m3 caches on the matrix cores, queries and probabilities as two bf16 parts each
+ * (DMTD_DTYPE_E4M3: probabilities as one, off by up to 2^-8 beside the 2^-4 that a code may be).
  * qkv: as above; only its query heads are read (ld >= n_q_heads * head_dim).  start: DEVICE int32 [n_req].  cu_rows: DEVICE int32 [n_req + 1], ascending from 0 on.
  * max_new: HOST, the most rows that one request brings (0: max_rows): a launch of many rows per request is left out where none has them.
  * out: DEVICE [max_rows, ldo] of dtype, n_q_heads heads of head_dim; 16-byte aligned, ldo a multiple of 8.

@@ -624,7 +624,7 @@ class PagedCache(_OnDevice):
 
     def append(self, qkv, cu_rows, row_pos, slots, k_norm=None, rope=None, eps: float = 1e-6):
         """Keys (normalised with ``k_norm``, rotated by ``rope`` [positions, head_dim / 2, (cos, sin)]) and values of the fused projection's rows
-        ``qkv`` into the places that :meth:`PageTables.build` gave them."""
+        ``qkv`` into the places that :meth:`PageTables.build` gave them: each its own (of rows with the same place, an 8-bit cache may pair one's codes with another's scale)."""
         x, ld, gain, tab, n_tab = self._rows(qkv, self._cols, k_norm, rope)
         i32, dev = self._i32, self._index
         self._call(self._lib.dmtd_paged_append, self._p, x, ld, _want(cu_rows, "cu_rows", i32, dev, self._per_end), _want(row_pos, "row_pos", i32, dev, self._per_row),

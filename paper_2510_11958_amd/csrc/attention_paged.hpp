@@ -17,7 +17,7 @@ namespace dmtd {
 // bf16 parts in which a probability of a bf16 cache enters its products.  Rows of bf16: two, 16 of its 24 bits, twice what the output keeps (2048 rows behind 6144, 32/8 heads of 128:
 // 438 us, with three 516; 0.0017 off 64 bits with either, the output's rounding).  The planes that the projections read keep 16 bits: three, which add up to all 24, as
 // in the attention of the other calls (attention_mfma.hpp, attention_prefill.hpp); values that cancel would show the roundings of two.
-// Values of 8-bit caches have 4 significant bits: one part, which is off by 2^-9 (at most 2^-8), beside the 2^-5 that each value was off by when it was stored (2048 rows behind 6144, 32/8 heads of 128: 362 us,
+// Values of 8-bit caches have 4 significant bits: one part, which is off by up to 2^-8, beside the 2^-4 that each value may have been off by when it was stored (2048 rows behind 6144, 32/8 heads of 128: 362 us,
 // with two parts 428; 0.0020 off 64 bits on the stored values, with two 0.0017, the output's rounding).  The sum of the probabilities is that of all their bits with either.
 template <typename CT, bool PLANES> constexpr int PAGED_PARTS = sizeof(CT) == 1 ? 1 : PLANES ? 3 : 2;
 
