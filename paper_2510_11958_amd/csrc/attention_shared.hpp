@@ -274,17 +274,20 @@ __global__ void __launch_bounds__(NT) share_plan_kernel(ShareArgs a, PagedView p
 
 // The items of a plan, head by head, over a grid of blocks that the chip holds.  Tall ones are a block's: with 8 KV heads (or a multiple) block b's are of one head, whose keys stay in
 // the L2 of the block's die.  Then the others, a wave's each: those of the blocks with fewer tall ones come first.
+// The first item is asked for beside the plan's numbers, which say whether it is one.  most: items that the plan has room for.
 template <typename CT, int HD, bool TALL>
-__global__ void __launch_bounds__(256, 2) paged_shared_mfma_kernel(SharePlan plan, int sign, const float* __restrict__ qkv, long ld, const typename PagedWide<CT>::type* __restrict__ q_gain,
+__global__ void __launch_bounds__(256, 2) paged_shared_mfma_kernel(SharePlan plan, int sign, int most, const float* __restrict__ qkv, long ld, const typename PagedWide<CT>::type* __restrict__ q_gain,
                                                                    const float2* __restrict__ rope_tab, float eps, PagedOut po, PagedView pv, SharedParts sp) {
-  if (plan.head[0] != sign) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), grid = gridDim.x;
-  const int n_tall = TALL ? plan.head[1] : 0, all_tall = n_tall * pv.nkv, all_few = plan.head[2] * pv.nkv - all_tall;
   auto item_at = [&](int item) {
     const int4 u = plan.items[2 * item], v = plan.items[2 * item + 1];
     return SharedItem{__builtin_amdgcn_readfirstlane(u.x), __builtin_amdgcn_readfirstlane(u.y), __builtin_amdgcn_readfirstlane(u.z), __builtin_amdgcn_readfirstlane(u.w),
                       __builtin_amdgcn_readfirstlane(v.x), __builtin_amdgcn_readfirstlane(v.y), __builtin_amdgcn_readfirstlane(v.z), __builtin_amdgcn_readfirstlane(v.w)};
   };
+  const int4 head = *(const int4*)plan.head;
+  SharedItem it = item_at(min((int)((unsigned)(TALL ? blockIdx.x : wave * grid + blockIdx.x) / (unsigned)pv.nkv), most - 1));
+  if (__builtin_amdgcn_readfirstlane(head.x) != sign) return;
+  const int n_tall = TALL ? __builtin_amdgcn_readfirstlane(head.y) : 0, all_tall = n_tall * pv.nkv, all_few = __builtin_amdgcn_readfirstlane(head.z) * pv.nkv - all_tall;
   // the lane's number and what follows from it are worked out anew for each item: kept through the loop they would be spilled
   auto lane_now = [&] {
     unsigned zero = 0;
@@ -294,7 +297,7 @@ __global__ void __launch_bounds__(256, 2) paged_shared_mfma_kernel(SharePlan pla
   if constexpr (TALL) {
     for (int y = blockIdx.x; y < all_tall; y += grid) {
       const int item = (int)((unsigned)y / (unsigned)pv.nkv), g = y - item * pv.nkv;
-      const SharedItem it = item_at(item);
+      if (y != (int)blockIdx.x) it = item_at(item);
       if (it.kb < it.ke) paged_tall_item<CT, HD, false, true>(it, g, 64 * wave + lane_now(), qkv, ld, q_gain, rope_tab, eps, po, pv, PagedWork{}, sp);      // (or keys that the tile's rows do not reach)
       __syncthreads();                          // the item's LDS is free
     }
@@ -302,7 +305,7 @@ __global__ void __launch_bounds__(256, 2) paged_shared_mfma_kernel(SharePlan pla
   const int more = all_tall % grid, fewer = grid - more, rank = (int)blockIdx.x >= more ? blockIdx.x - more : fewer + blockIdx.x;
   for (int y = rank < fewer ? wave * fewer + rank : 4 * fewer + wave * more + rank - fewer; y < all_few; y += 4 * grid) {
     const int item = (int)((unsigned)y / (unsigned)pv.nkv), g = y - item * pv.nkv;
-    const SharedItem it = item_at(n_tall + item);
+    if (TALL || y >= 4 * grid) it = item_at(n_tall + item);
     if (it.kb < it.ke) paged_few_item<CT, HD, false, true>(it, g, lane_now(), wave, qkv, ld, q_gain, rope_tab, eps, po, pv, PagedWork{}, sp);
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");      // the item's LDS is free
     __builtin_amdgcn_wave_barrier();
@@ -312,13 +315,18 @@ __global__ void __launch_bounds__(256, 2) paged_shared_mfma_kernel(SharePlan pla
 // A row's parts joined, first the prefix's, then its own, each in the order of the keys: 4 dims of a head a thread, and as many threads as a wave has for it share the parts.  Rows with one part have been written.
 template <typename GT, int HD>
 __global__ void __launch_bounds__(256) paged_shared_join_kernel(SharePlan plan, int sign, PagedOut po, PagedView pv, SharedParts sp) {
-  if (plan.head[0] != sign) return;
   constexpr int T4 = HD / 4, SHARE = 64 / T4, U = 4;      // U: parts of a thread in flight
-  const int n_rows = plan.head[3], turn = (threadIdx.x & 63) / T4, d = (threadIdx.x % T4) * 4;
-  const long total = (long)n_rows * pv.nh;
-  for (long e = (long)blockIdx.x * 4 + (threadIdx.x >> 6); e < total; e += (long)gridDim.x * 4) {
+  const int turn = (threadIdx.x & 63) / T4, d = (threadIdx.x % T4) * 4;
+  const long first = (long)blockIdx.x * 4 + (threadIdx.x >> 6);
+  // the first row's parts are asked for beside the plan's numbers
+  const int4 numbers = *(const int4*)plan.head;
+  const int t0 = min((int)(first / pv.nh), pv.max_rows - 1);
+  int4 own = plan.recs[2 * t0], front = plan.recs[2 * t0 + 1];
+  if (numbers.x != sign) return;
+  const long total = (long)numbers.w * pv.nh;
+  for (long e = first; e < total; e += (long)gridDim.x * 4) {
     const int t = (int)(e / pv.nh), head = (int)(e - (long)t * pv.nh);
-    const int4 own = plan.recs[2 * t], front = plan.recs[2 * t + 1];
+    if (e != first) { own = plan.recs[2 * t]; front = plan.recs[2 * t + 1]; }
     if (own.y == 0) continue;
     // part k of the row: of the prefix, then its own
     const int n = front.y + own.y;

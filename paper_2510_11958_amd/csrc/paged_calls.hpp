@@ -281,11 +281,11 @@ hipError_t launch_shared_t(const PagedView& v, long items, const SharedCall& a, 
       static bool big_lds[kMaxDevices];
       const hipError_t e = lds_room(kern, lds, (size_t)4 * 64 * 128 * 2 + 1024, big_lds);
       if (e != hipSuccess) return e;
-      hipLaunchKernelGGL(kern, dim3((unsigned)std::min<long>(want, PAGED_RESIDENT_TALL)), dim3(256), lds, a.stream, a.plan, a.sign, a.qkv, a.ld, (const GT*)a.gain, (const float2*)a.rope, a.eps, out, v, sp);
+      hipLaunchKernelGGL(kern, dim3((unsigned)std::min<long>(want, PAGED_RESIDENT_TALL)), dim3(256), lds, a.stream, a.plan, a.sign, (int)items, a.qkv, a.ld, (const GT*)a.gain, (const float2*)a.rope, a.eps, out, v, sp);
     }
   } else {
     constexpr int resident = 512;
-    hipLaunchKernelGGL((paged_shared_mfma_kernel<CT, HD, false>), dim3((unsigned)std::min<long>((want + 3) / 4, resident)), dim3(256), few_lds, a.stream, a.plan, a.sign, a.qkv, a.ld, (const GT*)a.gain,
+    hipLaunchKernelGGL((paged_shared_mfma_kernel<CT, HD, false>), dim3((unsigned)std::min<long>((want + 3) / 4, resident)), dim3(256), few_lds, a.stream, a.plan, a.sign, (int)items, a.qkv, a.ld, (const GT*)a.gain,
                        (const float2*)a.rope, a.eps, out, v, sp);
   }
   const long waves = (long)v.max_rows * v.nh;
