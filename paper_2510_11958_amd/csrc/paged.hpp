@@ -361,26 +361,36 @@ __global__ void __launch_bounds__(256) paged_append_kernel(const float* __restri
   const int l = threadIdx.x & 15;
   const long v = (long)blockIdx.x * 16 + (threadIdx.x >> 4);
   const int t = (int)(v / pv.nkv), g = (int)(v - (long)t * pv.nkv);
-  if (t >= min(pv.max_rows, cu[pv.n_req])) return;          // whole rows of 16 lanes
-  const int pos = row_pos[t];
-  const long long slot = slots[t];
+  // two trips to memory one behind the other: the number of rows, then the row, beside position and place, then the angles
+  const int end = cu[pv.n_req], pos = row_pos[min(t, pv.max_rows - 1)];
+  const long long slot = slots[min(t, pv.max_rows - 1)];
+  if (t >= min(pv.max_rows, end)) return;          // whole rows of 16 lanes
   AttRow<HD> k, w;
   k.load(qkv + (size_t)t * ld + (size_t)(pv.nh + g) * HD, l);
   w.load(qkv + (size_t)t * ld + (size_t)(pv.nh + pv.nkv + g) * HD, l);
+  GT g0[HL], g1[HL];
+  if (k_gain) {
+#pragma unroll
+    for (int e = 0; e < HL; ++e) { g0[e] = k_gain[HL * l + e]; g1[e] = k_gain[half + HL * l + e]; }
+  }
   if (pos < 0 || pos >= pv.limit || slot < 0 || slot >= ((long long)pv.n_pages << pv.page_shift)) return;
+  float2 turn[HL];
+  if (rope_tab) {
+#pragma unroll
+    for (int e = 0; e < HL; ++e) turn[e] = rope_tab[(size_t)pos * half + HL * l + e];
+  }
   float x0[HL], x1[HL], ss = 0.f;
 #pragma unroll
   for (int e = 0; e < HL; ++e) { x0[e] = k.a[e]; x1[e] = k.b[e]; ss += x0[e] * x0[e] + x1[e] * x1[e]; }
   if (k_gain) {
     const float rs = rsqrtf(row16_sum(ss) / (float)HD + eps);
 #pragma unroll
-    for (int e = 0; e < HL; ++e) { x0[e] *= rs * Elem<GT>::to_f32(k_gain[HL * l + e]); x1[e] *= rs * Elem<GT>::to_f32(k_gain[half + HL * l + e]); }
+    for (int e = 0; e < HL; ++e) { x0[e] *= rs * Elem<GT>::to_f32(g0[e]); x1[e] *= rs * Elem<GT>::to_f32(g1[e]); }
   }
   if (rope_tab) {
-    const float2* rp = rope_tab + (size_t)pos * half + HL * l;
 #pragma unroll
     for (int e = 0; e < HL; ++e) {
-      const float2 cs = rp[e];
+      const float2 cs = turn[e];
       const float a = x0[e], b = x1[e];
       x0[e] = a * cs.x - b * cs.y;
       x1[e] = b * cs.x + a * cs.y;
