@@ -318,6 +318,28 @@ template <int N> __device__ __forceinline__ void store_elems(bf16_t* p, const fl
   for (int e = 0; e < N; e += 2) *(uint32_t*)(p + e) = pack_bf16x2(x[e], x[e + 1]);
 }
 
+// Sum over the 16 lanes of a DPP row, as row16_sum
+__device__ __forceinline__ double row16_sum64(double v) {
+  auto turned = [](double x, auto ctrl) {
+    const unsigned long long b = __builtin_bit_cast(unsigned long long, x);
+    const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)b, decltype(ctrl)::value, 0xF, 0xF, false), hi = __builtin_amdgcn_update_dpp(0, (int)(b >> 32), decltype(ctrl)::value, 0xF, 0xF, false);
+    return __builtin_bit_cast(double, ((unsigned long long)hi << 32) | lo);
+  };
+  v += turned(v, std::integral_constant<int, 0x128>());      // row_ror:8, 4, 2, 1
+  v += turned(v, std::integral_constant<int, 0x124>());
+  v += turned(v, std::integral_constant<int, 0x122>());
+  v += turned(v, std::integral_constant<int, 0x121>());
+  return v;
+}
+// x in 32 bits such that rounding the result to fewer gives what rounding x gives: cut off, with the last bit set where that leaves something out
+__device__ __forceinline__ float to_odd(double x) {
+  const float f = (float)x;
+  const double rest = x - (double)f;
+  uint32_t b = __float_as_uint(f);
+  if (rest != 0.0 && fabsf(f) < INFINITY) b = (b - ((rest < 0.0) != (f < 0.f) ? 1u : 0u)) | 1u;
+  return __uint_as_float(b);
+}
+
 // A row of 16 lanes' values as codes: N consecutive ones from p on and as many from p + half on.  Returns the row's scale.
 template <int N> __device__ __forceinline__ uint32_t store_codes(unsigned char* p, int half, const float (&x0)[N], const float (&x1)[N]) {
   float most = 0.f;
@@ -351,7 +373,7 @@ template <int N> __device__ __forceinline__ uint32_t store_codes(unsigned char* 
 // its key and its value, HD/32 pairs a lane, so that a wave's loads are runs of 256 bytes and the norm's sum stays inside a DPP row.  Rows at
 // and behind cu[n_req], and rows whose place or position is out of range, are not stored.
 // 8-bit pools: the 16 lanes' largest finite magnitude a gives the row's power of two, the least with a <= 448 times it; values that are not finite become NaN, with no
-// say in the power.  Codes are rounded to nearest even, once.
+// say in the power.  Norm and rotation are worked out in 64 bits and codes rounded from there to nearest even, once: in 32 bits about one code of a million lands on the other side of a border, 2^-3 of itself away.
 template <typename CT, int HD>
 __global__ void __launch_bounds__(256) paged_append_kernel(const float* __restrict__ qkv, long ld, const int* __restrict__ cu, const int* __restrict__ row_pos,
                                                            const long long* __restrict__ slots, const typename PagedWide<CT>::type* __restrict__ k_gain,
@@ -379,21 +401,36 @@ __global__ void __launch_bounds__(256) paged_append_kernel(const float* __restri
 #pragma unroll
     for (int e = 0; e < HL; ++e) turn[e] = rope_tab[(size_t)pos * half + HL * l + e];
   }
-  float x0[HL], x1[HL], ss = 0.f;
+  float x0[HL], x1[HL];
+  if constexpr (sizeof(CT) == 1) {
+    double a[HL], b[HL], ss = 0.0;
 #pragma unroll
-  for (int e = 0; e < HL; ++e) { x0[e] = k.a[e]; x1[e] = k.b[e]; ss += x0[e] * x0[e] + x1[e] * x1[e]; }
-  if (k_gain) {
-    const float rs = rsqrtf(row16_sum(ss) / (float)HD + eps);
-#pragma unroll
-    for (int e = 0; e < HL; ++e) { x0[e] *= rs * Elem<GT>::to_f32(g0[e]); x1[e] *= rs * Elem<GT>::to_f32(g1[e]); }
-  }
-  if (rope_tab) {
+    for (int e = 0; e < HL; ++e) { a[e] = k.a[e]; b[e] = k.b[e]; ss += a[e] * a[e] + b[e] * b[e]; }
+    const double rs = k_gain ? rsqrt(row16_sum64(ss) / (double)HD + (double)eps) : 1.0;
 #pragma unroll
     for (int e = 0; e < HL; ++e) {
-      const float2 cs = turn[e];
-      const float a = x0[e], b = x1[e];
-      x0[e] = a * cs.x - b * cs.y;
-      x1[e] = b * cs.x + a * cs.y;
+      if (k_gain) { a[e] *= rs * (double)Elem<GT>::to_f32(g0[e]); b[e] *= rs * (double)Elem<GT>::to_f32(g1[e]); }
+      const double c = rope_tab ? turn[e].x : 1.f, n = rope_tab ? turn[e].y : 0.f;
+      x0[e] = to_odd(rope_tab ? a[e] * c - b[e] * n : a[e]);
+      x1[e] = to_odd(rope_tab ? b[e] * c + a[e] * n : b[e]);
+    }
+  } else {
+    float ss = 0.f;
+#pragma unroll
+    for (int e = 0; e < HL; ++e) { x0[e] = k.a[e]; x1[e] = k.b[e]; ss += x0[e] * x0[e] + x1[e] * x1[e]; }
+    if (k_gain) {
+      const float rs = rsqrtf(row16_sum(ss) / (float)HD + eps);
+#pragma unroll
+      for (int e = 0; e < HL; ++e) { x0[e] *= rs * Elem<GT>::to_f32(g0[e]); x1[e] *= rs * Elem<GT>::to_f32(g1[e]); }
+    }
+    if (rope_tab) {
+#pragma unroll
+      for (int e = 0; e < HL; ++e) {
+        const float2 cs = turn[e];
+        const float a = x0[e], b = x1[e];
+        x0[e] = a * cs.x - b * cs.y;
+        x1[e] = b * cs.x + a * cs.y;
+      }
     }
   }
   const size_t row = ((size_t)g << pv.page_shift) + (size_t)(slot & ((1 << pv.page_shift) - 1));

@@ -85,6 +85,24 @@ def test_append(heads, page, start, rows, norm, rope):
         assert torch.equal(g.transpose(1, 2)[~touched], was.transpose(1, 2)[~touched])
 
 
+@pytest.mark.parametrize("heads, norm, rope", [((8, 4, 128), True, True), ((8, 4, 64), True, True), ((8, 4, 128), True, False), ((8, 4, 64), False, True)])
+def test_keys_are_rounded_from_more_than_32_bits(heads, norm, rope):
+    """Half a million elements of keys: every code and scale is that of the 64-bit value.  Roundings of 32 bits, about 2^-23 of a key against codes 2^-4 to 2^-3 of it apart, would have about one of a
+    million on the other side of a border; those of 64 bits are 2^-29 as many."""
+    s = Setup8(heads, 32, [100, 0], [700, 400], seed=23, norm=norm, rope=rope)
+    c = s.cache()
+    cu, pos, slots = s.maps()
+    for seed in range(3):
+        s.qkv[:s.total] = torch.randn(s.total, s.qkv.shape[1], generator=torch.Generator().manual_seed(seed))
+        c.append(s.qkv.to(DEV), cu, pos, slots, k_norm=s.dev(s.gain), rope=s.dev(s.rope), eps=pu.EPS)
+        x = s.qkv[:s.total].double().view(s.total, -1, s.hd)
+        want, _ = pu.normed_rotated(x[:, s.nq:s.nq + s.nkv], s.gain, s.rope, torch.tensor(s.pos))
+        b, e, _ = p8.stored(want)
+        slot = torch.tensor(s.slots)
+        assert torch.equal(at(s.ksd.cpu(), slot, s.page), e)
+        assert torch.equal(at(s.kd.view(torch.uint8).cpu(), slot, s.page), b)
+
+
 def test_append_at_the_borders_of_codes_and_scales():
     """Rows around each power of two's limit, halves between codes, subnormal codes, zeros, the smallest and largest magnitudes, and values that are not finite."""
     hd, page = 64, 16
