@@ -333,11 +333,9 @@ __device__ __forceinline__ double row16_sum64(double v) {
 }
 // x in 32 bits such that rounding the result to fewer gives what rounding x gives: cut off, with the last bit set where that leaves something out
 __device__ __forceinline__ float to_odd(double x) {
-  const float f = (float)x;
-  const double rest = x - (double)f;
-  uint32_t b = __float_as_uint(f);
-  if (rest != 0.0 && fabsf(f) < INFINITY) b = (b - ((rest < 0.0) != (f < 0.f) ? 1u : 0u)) | 1u;
-  return __uint_as_float(b);
+  unsigned long long b = __builtin_bit_cast(unsigned long long, x);
+  b = (b & ~0x1FFFFFFFull) | ((b & 0x1FFFFFFFull) ? 0x20000000ull : 0ull);      // 29 bits more than 32-bit values have (below 2^-126, far below a code's step, some more are rounded)
+  return (float)__builtin_bit_cast(double, b);
 }
 
 // A row of 16 lanes' values as codes: N consecutive ones from p on and as many from p + half on.  Returns the row's scale.
@@ -373,7 +371,8 @@ template <int N> __device__ __forceinline__ uint32_t store_codes(unsigned char* 
 // its key and its value, HD/32 pairs a lane, so that a wave's loads are runs of 256 bytes and the norm's sum stays inside a DPP row.  Rows at
 // and behind cu[n_req], and rows whose place or position is out of range, are not stored.
 // 8-bit pools: the 16 lanes' largest finite magnitude a gives the row's power of two, the least with a <= 448 times it; values that are not finite become NaN, with no
-// say in the power.  Norm and rotation are worked out in 64 bits and codes rounded from there to nearest even, once: in 32 bits about one code of a million lands on the other side of a border, 2^-3 of itself away.
+// say in the power.  Norm and rotation are worked out in 64 bits and codes rounded from there to nearest even, once: in 32 bits about one code of a million lands on the other
+// side of a border, 2^-3 of itself away (2000 rows of 8 heads 8.6 us, in 32 bits 7.4; 32 bits first, and 64 where a code lies near a border, 9.4: the look costs more).
 template <typename CT, int HD>
 __global__ void __launch_bounds__(256) paged_append_kernel(const float* __restrict__ qkv, long ld, const int* __restrict__ cu, const int* __restrict__ row_pos,
                                                            const long long* __restrict__ slots, const typename PagedWide<CT>::type* __restrict__ k_gain,
