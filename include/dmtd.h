@@ -383,8 +383,7 @@ size_t dmtd_paged_workspace_bytes(const dmtd_paged_cache* cache);
 
 /* Attention of a step's rows over their requests' pages: out[t, h] = sum_j p_j v_j with p = softmax(q_t,h . k_j / sqrt(head_dim)) over the keys
  * j = 0 .. position of row t of its request, whose own key is in the cache already; queries are normalised (q_norm, eps) and rotated (rope) as the keys
- * were by dmtd_paged_append.  Softmax and sums in float32; products of bf16 and e4m3 caches on the matrix cores, queries and probabilities as two bf16 parts each
- * (DMTD_DTYPE_E4M3: probabilities as one, off by up to 2^-8 beside the 2^-4 that a code may be).
+ * were by dmtd_paged_append.  Softmax and sums in float32; products of bf16 and e4m3 caches on the matrix cores, queries and probabilities as two bf16 parts each.
  * qkv: as above; only its query heads are read (ld >= n_q_heads * head_dim).  start: DEVICE int32 [n_req].  cu_rows: DEVICE int32 [n_req + 1], ascending from 0 on.
  * max_new: HOST, the most rows that one request brings (0: max_rows): a launch of many rows per request is left out where none has them.
  * out: DEVICE [max_rows, ldo] of dtype, n_q_heads heads of head_dim; 16-byte aligned, ldo a multiple of 8.

@@ -17,9 +17,9 @@ namespace dmtd {
 // bf16 parts in which a probability of a bf16 cache enters its products.  Rows of bf16: two, 16 of its 24 bits, twice what the output keeps (2048 rows behind 6144, 32/8 heads of 128:
 // 438 us, with three 516; 0.0017 off 64 bits with either, the output's rounding).  The planes that the projections read keep 16 bits: three, which add up to all 24, as
 // in the attention of the other calls (attention_mfma.hpp, attention_prefill.hpp); values that cancel would show the roundings of two.
-// Values of 8-bit caches have 4 significant bits: one part, which is off by up to 2^-8, beside the 2^-4 that each value may have been off by when it was stored (2048 rows behind 6144, 32/8 heads of 128: 362 us,
-// with two parts 428; 0.0020 off 64 bits on the stored values, with two 0.0017, the output's rounding).  The sum of the probabilities is that of all their bits with either.
-template <typename CT, bool PLANES> constexpr int PAGED_PARTS = sizeof(CT) == 1 ? 1 : PLANES ? 3 : 2;
+// 8-bit caches: two as well, although a value may have been off by 2^-4 when it was stored: what is stored is what the caller has, and a part of 8 bits would add an error of the size of the
+// output's own rounding (2048 rows behind 6144, 32/8 heads of 128: two parts 428 us and 0.0017 off 64 bits on the stored values, one part 354 and 0.0023).
+template <bool PLANES> constexpr int PAGED_PARTS = PLANES ? 3 : 2;
 
 // A pair of probabilities in three bf16 parts: the leading 8 bits, the next 8, the rest
 __device__ __forceinline__ void paged_split3(float a, float b, uint32_t& h, uint32_t& m, uint32_t& l) {
@@ -354,7 +354,7 @@ __device__ __forceinline__ void paged_few_item(const ITEM& it, int g, const int 
                                                const float2* __restrict__ rope_tab, float eps, const PagedOut& po, const PagedView& pv, const PagedWork& wk, const SharedParts& sp) {
   typedef typename PagedWide<CT>::type GT;
   constexpr bool BF = sizeof(GT) == 2, Q8 = sizeof(CT) == 1;
-  constexpr int PARTS = PAGED_PARTS<CT, PLANES>;
+  constexpr int PARTS = PAGED_PARTS<PLANES>;
   constexpr int QVT = 16, NW = SHARED ? 1 : PAGED_WAVES, NT = 64 * NW, DPL = HD / 16, half = HD / 2, HL = HD / 32;
   constexpr int QI = 16 * QVT / NT;                          // query vectors that 16 lanes make ready
   constexpr int KS = HD * (int)sizeof(CT) / 64;              // 16-byte pieces of a key a lane carries
@@ -582,7 +582,7 @@ __device__ __forceinline__ void paged_few_item(const ITEM& it, int g, const int 
   } else if constexpr (BF) {
     // G groups at once: the queries stay in registers, the groups' scores are chains that do not wait for each other, one maximum serves all, and the values enter by pairs of groups
     // (16x16x32: a lane's eight keys are four of either).  8-bit pieces are 16 consecutive dims of a key a lane, and the products' eight go by that.
-    static_assert(PARTS <= 2 && G % 2 == 0, "up to two parts of a probability, pairs of groups");
+    static_assert(PARTS == 2 && G % 2 == 0, "two parts of a probability, pairs of groups");
     bf16x8_t qh[KW], ql[KW];
 #pragma unroll
     for (int t = 0; t < KW; ++t) {
@@ -662,13 +662,8 @@ __device__ __forceinline__ void paged_few_item(const ITEM& it, int g, const int 
         float p[4];
 #pragma unroll
         for (int m = 0; m < 4; ++m) { p[m] = __builtin_amdgcn_exp2f(s[u][m] - m_use); psum += p[m]; }
-        if constexpr (PARTS == 1) {
-          ph[u][0] = pack_bf16x2(p[0], p[1]);
-          ph[u][1] = pack_bf16x2(p[2], p[3]);
-        } else {
-          paged_split2(p[0], p[1], ph[u][0], pl[u][0]);
-          paged_split2(p[2], p[3], ph[u][1], pl[u][1]);
-        }
+        paged_split2(p[0], p[1], ph[u][0], pl[u][0]);
+        paged_split2(p[2], p[3], ph[u][1], pl[u][1]);
       }
       l_run = l_run * f + psum;
       if (__any(m_new > m_run)) rescale(f);
@@ -707,7 +702,7 @@ __device__ __forceinline__ void paged_few_item(const ITEM& it, int g, const int 
           const unsigned int sel = (e & 1) ? 0x07060302u : 0x05040100u;
           const bf16x8_t v8 = __builtin_bit_cast(bf16x8_t, u32x4{__builtin_amdgcn_perm(va[0][1][e >> 1], va[0][0][e >> 1], sel), __builtin_amdgcn_perm(va[0][3][e >> 1], va[0][2][e >> 1], sel),
                                                                  __builtin_amdgcn_perm(va[1][1][e >> 1], va[1][0][e >> 1], sel), __builtin_amdgcn_perm(va[1][3][e >> 1], va[1][2][e >> 1], sel)});
-          if constexpr (PARTS == 2) acc[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, u32x4{pl[u0][0], pl[u0][1], pl[u0 + 1][0], pl[u0 + 1][1]}), v8, acc[e], 0, 0, 0);
+          acc[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, u32x4{pl[u0][0], pl[u0][1], pl[u0 + 1][0], pl[u0 + 1][1]}), v8, acc[e], 0, 0, 0);
           acc[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, u32x4{ph[u0][0], ph[u0][1], ph[u0 + 1][0], ph[u0 + 1][1]}), v8, acc[e], 0, 0, 0);
         }
       }
@@ -808,7 +803,7 @@ __device__ __forceinline__ void paged_attention_few(int y, const int* __restrict
 template <typename CT, int HD, bool PLANES, bool SHARED, typename ITEM>
 __device__ __forceinline__ void paged_tall_item(const ITEM& it, int g, const int tid, const float* __restrict__ qkv, long ld, const bf16_t* __restrict__ q_gain,
                                                 const float2* __restrict__ rope_tab, float eps, const PagedOut& po, const PagedView& pv, const PagedWork& wk, const SharedParts& sp) {
-  constexpr int PARTS = PAGED_PARTS<CT, PLANES>;
+  constexpr int PARTS = PAGED_PARTS<PLANES>;
   constexpr int QVT = 128, NT = 256, KT = 64;
   constexpr int T = HD / 16;           // steps over d for the scores
   constexpr int DT = HD / 32;          // 32-dim tiles of the output
@@ -1090,10 +1085,8 @@ __device__ __forceinline__ void paged_tall_item(const ITEM& it, int g, const int
     };
     if (more) scores(std::integral_constant<bool, true>());
     else scores(std::integral_constant<bool, false>());
-    constexpr int VD = PARTS == 1 ? 3 : 2;      // V fragments: the one in its products, and those read ahead of theirs: with one part a product hides less (354 us, with 2 362)
-    bf16x8_t vf[VD];
-#pragma unroll
-    for (int n = 0; n + 1 < VD; ++n) vf[n] = read_v(n / DT, n % DT);
+    bf16x8_t vf[2];
+    vf[0] = read_v(0, 0);
     if (base + KT > it.pos0 + 1) {      // keys beyond some row's position in this tile
 #pragma unroll
       for (int k = 0; k < 2; ++k)
@@ -1140,12 +1133,12 @@ __device__ __forceinline__ void paged_tall_item(const ITEM& it, int g, const int
         if (PARTS == 3) return;
         const uint32_t h = pack_bf16x2(a, d);
         pp[q & 1][0][j] = h;
-        if constexpr (PARTS == 2) pp[q & 1][1][j] = pack_bf16x2(a - __uint_as_float(h << 16), d - __uint_as_float(h & 0xFFFF0000u));
+        pp[q & 1][1][j] = pack_bf16x2(a - __uint_as_float(h << 16), d - __uint_as_float(h & 0xFFFF0000u));
       }
     };
     constexpr int PG = 4 / DT;          // pairs of the next step beside a V fragment's products
 #pragma unroll
-    for (int z = 0; z < (PARTS == 1 ? 2 : PARTS); ++z)
+    for (int z = 0; z < PARTS; ++z)
 #pragma unroll
       for (int j = 0; j < 4; ++j) piece(0, j, z);
     __builtin_amdgcn_sched_barrier(0);
@@ -1154,17 +1147,14 @@ __device__ __forceinline__ void paged_tall_item(const ITEM& it, int g, const int
 #pragma unroll
       for (int t = 0; t < DT; ++t) {
         const int n = q * DT + t;
-        if (n + VD - 1 < 4 * DT) vf[(n + VD - 1) % VD] = read_v((n + VD - 1) / DT, (n + VD - 1) % DT);
+        if (n + 1 < 4 * DT) vf[(n + 1) & 1] = read_v((n + 1) / DT, (n + 1) % DT);
 #pragma unroll
         for (int z = 0; z < PARTS; ++z) {
           const uint32_t* f = pp[q & 1][PARTS - 1 - z];
-          acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[n % VD], __builtin_bit_cast(bf16x8_t, u32x4{f[0], f[1], f[2], f[3]}), acc[t], 0, 0, 0);
+          acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[n & 1], __builtin_bit_cast(bf16x8_t, u32x4{f[0], f[1], f[2], f[3]}), acc[t], 0, 0, 0);
           if (q < 3) {
 #pragma unroll
-            for (int j = 0; j < PG; ++j) {
-              piece(q + 1, t * PG + j, z);
-              if (PARTS == 1) piece(q + 1, t * PG + j, 1);
-            }
+            for (int j = 0; j < PG; ++j) piece(q + 1, t * PG + j, z);
           }
           __builtin_amdgcn_sched_barrier(0);
         }
