@@ -364,7 +364,8 @@ typedef struct dmtd_paged_cache {
  * rotated by the angles of its position, and rounded to dtype; values are rounded as they are.  DMTD_DTYPE_E4M3: a row of head_dim values gets the least
  * power of two s >= 2^-111 with max |x| <= 448 s, and the codes of x / s, rounded to nearest even (of keys, from norm and rotation in 64 bits); values that are not finite have no say in s and become NaN.
  * qkv: DEVICE float32 [max_rows, ld], the fused projection's rows: n_q_heads query heads, then n_kv_heads keys, then n_kv_heads values, of head_dim
- * each; 16-byte aligned, ld a multiple of 4.  cu_rows, row_pos, slots: of dmtd_page_tables (of cu_rows only the last entry is read).
+ * each; 16-byte aligned, ld a multiple of 4.  cu_rows, row_pos, slots: of dmtd_page_tables (of cu_rows only the last entry is read; of the others,
+ * which may have room for fewer rows than the cache's max_rows, none behind the last row).
  * rope: DEVICE float32 [rope_len][head_dim / 2][2], (cos, sin) of the pair (i, i + head_dim / 2) at each position; NULL: no rotation.
  * Rows with a place outside the pool, or a position outside the block table or the rotary table, are not stored.  Two rows with the same place leave either's values there
  * (DMTD_DTYPE_E4M3: codes of one may meet the power of two of the other, a value of neither; dmtd_page_tables gives every row a place of its own).

@@ -382,10 +382,11 @@ __global__ void __launch_bounds__(256) paged_append_kernel(const float* __restri
   const int l = threadIdx.x & 15;
   const long v = (long)blockIdx.x * 16 + (threadIdx.x >> 4);
   const int t = (int)(v / pv.nkv), g = (int)(v - (long)t * pv.nkv);
-  // two trips to memory one behind the other: the number of rows, then the row, beside position and place, then the angles
-  const int end = cu[pv.n_req], pos = row_pos[min(t, pv.max_rows - 1)];
-  const long long slot = slots[min(t, pv.max_rows - 1)];
-  if (t >= min(pv.max_rows, end)) return;          // whole rows of 16 lanes
+  // Three trips to memory one behind the other: the number of rows, then the row with its position and place, then the angles.  (Position and place beside the number of rows would save 0.1 us
+  // of 1900 rows of 8 bits and nothing of bf16, but the maps may have fewer entries than the handle has rows: what lies behind the last row is not read.)
+  if (t >= min(pv.max_rows, cu[pv.n_req])) return;          // whole rows of 16 lanes
+  const int pos = row_pos[t];
+  const long long slot = slots[t];
   AttRow<HD> k, w;
   k.load(qkv + (size_t)t * ld + (size_t)(pv.nh + g) * HD, l);
   w.load(qkv + (size_t)t * ld + (size_t)(pv.nh + pv.nkv + g) * HD, l);
