@@ -340,7 +340,8 @@ int dmtd_page_tables(const dmtd_page_pool* pool, const int32_t* start, const int
 
 /* The same where requests share pages: shared[i] (DEVICE int32 [n_req]; NULL: as dmtd_page_tables) is the number of pages at the front of request i's table that another one holds and that
  * request i reads only.  The caller writes them into the table, counted in held[i]; they are never given back by request i, which keeps at least these: start = rows = 0 gives back
- * the others.  A shared[i] that is negative or above held[i]: status as for lengths that do not fit, DMTD_EINVAL and i.  Whoever holds the pages for good (shared 0) keeps them as long as another reads them. */
+ * the others.  Its new rows lie behind them: a request whose prompt ends with the shared pages and that needs its last token's row shares one page less.  A shared[i] that is negative or above held[i], or rows[i] > 0
+ * with start[i] < shared[i] * page_size: status as for lengths that do not fit, DMTD_EINVAL and i.  Whoever holds the pages for good (shared 0) keeps them as long as another reads them. */
 int dmtd_page_tables_shared(const dmtd_page_pool* pool, const int32_t* start, const int32_t* rows, const int32_t* shared, int32_t max_rows, int32_t* cu_rows,
                             int32_t* row_pos, int64_t* slots, int32_t* status, void* stream);
 

@@ -519,7 +519,7 @@ class PageTables(_OnDevice):
     def build(self, start, rows, cu_rows, row_pos, slots, status, shared=None):
         """Pages and places for a step: request i has ``start[i]`` tokens and brings ``rows[i]``.  Writes ``cu_rows`` int32 ``[n_req + 1]``, ``row_pos`` int32
         ``[max_rows]``, ``slots`` int64 ``[max_rows]`` and ``status`` int32 ``[2]`` (0, or why the step has no rows: see the header).  ``shared`` int32 ``[n_req]``: the pages at the
-        front of each request's table that another one holds (``dmtd_page_tables_shared``): they stay where they are, and are not given back."""
+        front of each request's table that another one holds (``dmtd_page_tables_shared``): they stay where they are, are not given back, and a step that would bring rows into them is refused by its status."""
         i32, dev = self._i32, self._index
         room = row_pos.shape
         front = None if shared is None else _want(shared, "shared", i32, dev, self._per_req)

@@ -155,7 +155,8 @@ __device__ __forceinline__ PageSums<NT> page_sums(const PageArgs& a) {
   for (int i = p.i0; i < min(p.i0 + p.ipt, a.n_req); ++i) {
     const int s = a.start[i], r = a.rows[i], h = a.held[i];
     const int front = a.shared ? a.shared[i] : 0;
-    if (s < 0 || r < 0 || h < 0 || h > a.max_pages || s > limit || r > limit - s || front < 0 || front > h) { bad = min(bad, i); continue; }
+    const bool inside = r > 0 && front > 0 && front <= a.max_pages && s < front << a.page_shift;      // rows in pages that are only read
+    if (s < 0 || r < 0 || h < 0 || h > a.max_pages || s > limit || r > limit - s || front < 0 || front > h || inside) { bad = min(bad, i); continue; }
     const int need = max((s + r + (1 << a.page_shift) - 1) >> a.page_shift, front);
     if (i == p.i0) { p.h0 = h; p.need0 = need; p.r0 = r; }
     const int v[3] = {max(h - need, 0), max(need - h, 0), r};
