@@ -441,7 +441,7 @@ __device__ __forceinline__ void paged_few_item(const ITEM& it, int g, const int 
     const int qv = (tid >> 4) + i * (NT / 16);
     float x0[HL], x1[HL], ss = 0.f;
 #pragma unroll
-    for (int e = 0; e < HL; ++e) { x0[e] = xa[i][e]; x1[e] = xb[i][e]; ss += x0[e] * x0[e] + x1[e] * x1[e]; }
+    for (int e = 0; e < HL; ++e) { x0[e] = xa[i][e]; x1[e] = xb[i][e]; ss += __builtin_fmaf(x0[e], x0[e], x1[e] * x1[e]); }      // (written out, as the rotation below)
     if (q_gain) {
       const float rs = rsqrtf(row16_sum(ss) / (float)HD + eps);
 #pragma unroll
