@@ -355,7 +355,8 @@ typedef struct dmtd_paged_cache {
   int32_t  n_kv_heads, head_dim /* 64 or 128 */, dtype /* DMTD_DTYPE_* of k, v, gains and output; DMTD_DTYPE_E4M3: of k and v, gains and output are bf16 */;
   int32_t  max_rows;       /* rows there is room for, at most 2^24; times n_kv_heads at most 2^27 */
   /* DMTD_DTYPE_E4M3 only (not read otherwise): k and v hold e4m3 codes (page_stride a multiple of 16), and each head_dim of them a power of two, here as its biased
-   * exponent e: a value is code * 2^(e - 127), which is a bf16 value (e = 255: NaN). */
+   * exponent e: a value is code * 2^(e - 127), e = 255: NaN.  That is a bf16 value for 3 <= e <= 246, and for e = 247 up to code 240, and is rounded to one otherwise
+   * (code 256 and more under e = 247: infinite).  dmtd_paged_append writes 16 <= e <= 247. */
   uint8_t* k_scale;        /* DEVICE [n_pages][n_kv_heads][page_size], 16-byte aligned */
   uint8_t* v_scale;        /* DEVICE, as k_scale */
   int64_t  scale_stride;   /* bytes from one page's scales to the next's, a multiple of 16; 0: pages follow each other */
@@ -363,7 +364,8 @@ typedef struct dmtd_paged_cache {
 
 /* The new tokens' keys and values into their places: a head's key is normalised (RMS norm with gain k_norm, DEVICE [head_dim] of dtype; NULL: not),
  * rotated by the angles of its position, and rounded to dtype; values are rounded as they are.  DMTD_DTYPE_E4M3: a row of head_dim values gets the least
- * power of two s >= 2^-111 with max |x| <= 448 s, and the codes of x / s, rounded to nearest even (of keys, from norm and rotation in 64 bits); values that are not finite have no say in s and become NaN.
+ * power of two s >= 2^-111 with max |x| <= 448 s, and the codes of x / s, rounded to nearest even (of keys, from norm and rotation in 64 bits); values that are not finite (keys: from 2^128 on) have no say in s and become NaN.
+ * Magnitudes from 248 * 2^120 on (3.3e38), whose code rounds to 2^128, come back infinite, those below finite.
  * qkv: DEVICE float32 [max_rows, ld], the fused projection's rows: n_q_heads query heads, then n_kv_heads keys, then n_kv_heads values, of head_dim
  * each; 16-byte aligned, ld a multiple of 4.  cu_rows, row_pos, slots: of dmtd_page_tables (of cu_rows only the last entry is read; of the others,
  * which may have room for fewer rows than the cache's max_rows, none behind the last row).

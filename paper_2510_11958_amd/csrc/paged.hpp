@@ -17,7 +17,7 @@ namespace dmtd {
 constexpr int kPagedMaxRequests = 8192;      // requests of a call: their prefix sums lie in LDS
 
 // An element of an 8-bit pool: an e4m3 code (sign, 4 bits of exponent, 3 of fraction; 0x7F is NaN, there is no infinity).  A code times its row's power of two is a bf16
-// value without rounding (4 significant bits, and PAGED_LEAST_SCALE keeps the smallest normal), so the matrix cores see exactly what is stored, and the chip's
+// value without rounding (4 significant bits, and PAGED_LEAST_SCALE keeps the smallest normal; only code 256 under the largest power, 2^120, is beyond bf16's largest value: infinite), so the matrix cores see exactly what is stored, and the chip's
 // conversion multiplies by the power on the way.
 struct e4m3_t { unsigned char code; };
 // What the kernels compute with, and gains and outputs have, beside a pool's type
