@@ -18,7 +18,7 @@ namespace dmtd {
 // 438 us, with three 516; 0.0017 off 64 bits with either, the output's rounding).  The planes that the projections read keep 16 bits: three, which add up to all 24, as
 // in the attention of the other calls (attention_mfma.hpp, attention_prefill.hpp); values that cancel would show the roundings of two.
 // 8-bit caches: two as well, although a value may have been off by 2^-4 when it was stored: what is stored is what the caller has, and a part of 8 bits would add an error of the size of the
-// output's own rounding (2048 rows behind 6144, 32/8 heads of 128: two parts 428 us and 0.0017 off 64 bits on the stored values, one part 354 and 0.0023).
+// output's own rounding (2048 rows behind 6144, 32/8 heads of 128: two parts 456 us and 0.0017 off 64 bits on the stored values, one part 377 and 0.0023).
 template <bool PLANES> constexpr int PAGED_PARTS = PLANES ? 3 : 2;
 
 // A pair of probabilities in three bf16 parts: the leading 8 bits, the next 8, the rest
@@ -886,7 +886,7 @@ __device__ __forceinline__ void paged_tall_item(const ITEM& it, int g, const int
         const int key = 16 * w + (i * 64 + ln) / (HD / 16), c = 2 * (ln % (HD / 16));
         const float sk = e8m0_scale(((uint32_t)__shfl((int)kscale, key >> 2, 64) >> (8 * (key & 3))) & 0xFFu);
         const uint32_t at = ring + (uint32_t)(buf * TILE + key * HD) * 2;
-        // (a key's eight lanes write chunks of which those 128 bytes apart share banks; with half of the lanes beginning with their second one nothing does, but the swaps cost more: 361 us for 358)
+        // (a key's eight lanes write chunks of which those 128 bytes apart share banks; with half of the lanes beginning with their second one nothing does, but the swaps cost more: 361 us for 358, measured with half of the output's products)
         uint32_t x[8];
 #pragma unroll
         for (int e = 0; e < 4; ++e) { x[2 * e] = e4m3_pair<false>(kraw[i][e], sk); x[2 * e + 1] = e4m3_pair<true>(kraw[i][e], sk); }
@@ -947,7 +947,7 @@ __device__ __forceinline__ void paged_tall_item(const ITEM& it, int g, const int
 #pragma unroll
       for (int e = 0; e < 4; ++e) { x[t][e] = a[e]; x[t][4 + e] = c[e]; }
     }
-    // gains and angles are asked for together with the row, in front of the keys: one latency instead of three (64 rows of 32/8 heads behind 16384 shared tokens, four layers, 249 -> 245 us)
+    // gains and angles are asked for together with the row, in front of the keys: one latency instead of three (a microsecond of a layer's 57, 64 rows of 32/8 heads behind 16384 shared tokens)
     f32x4 turn[T / 2][4];
     u32x4 gains[T];
     if (q_gain) {

@@ -15,13 +15,17 @@
 namespace dmtd {
 
 constexpr int SHARE_HEADER = 16;      // ints in front of the items: sign, tall items, items, rows
-// Query vectors of an entry up to which its tiles are single waves' (us a layer with 32 / 64: 16 requests of 4 vectors behind 16384 shared tokens 36 / 54, 12 of 6 behind 8192, 8-bit, 36 / 38)
+// Query vectors of an entry up to which its tiles are single waves' (us a layer with 32 / 64: 16 requests of 4 vectors behind 16384 shared tokens 39 / 51, 8 of 6 behind 8192, 8-bit, 27 / 30)
 constexpr int SHARE_FEW = 32;
-constexpr int SHARE_SLOTS_FEW = 1024;      // items of single waves that the key ranges are chosen for
+// Items of single waves that the key ranges are chosen for: four on each CU (us a layer with 512 / 1024 / 2048: 40 requests of 2000 own tokens, 8-bit, 70 / 46 / 49, 20 of 3000, 14/2 heads of 64, 21 / 19 / 19,
+// 8 behind 4096 shared tokens 19 / 21 / 21)
+constexpr int SHARE_SLOTS_FEW = 1024;
 // Items of blocks that the key ranges are chosen for: one on each CU, which reads as fast as it works, and two where one would have SHARE_LONG keys and more: both together do 1.3 times the work, at the
 // cost of twice the parts (us a layer with one / two: 458 rows of 14/2 heads of 64 behind 10000 73 / 56, 5 chunks of 300 behind 3000 107 / 89; 64 rows of 32/8 heads behind 16384 60 / 67)
 constexpr int SHARE_SLOTS_TALL = 256, SHARE_LONG = 1536;
-constexpr int SHARE_KEYS_FP32 = 64;      // shortest range of a wave with an fp32 cache, whose products weigh more (of the others: PAGED_KEYS_FEW)
+// Shortest range of a wave with an fp32 cache, whose products weigh more (of the others: PAGED_KEYS_FEW; us with 64 / 128: 10 rows of 4/2 heads of 64, one layer and the plan, 17.6 / 20.8, 20 single tokens behind
+// 500 shared ones, a layer, 12 / 15, 6 rows of 32/8 heads of 128 behind 1000 17 / 22)
+constexpr int SHARE_KEYS_FP32 = 64;
 constexpr int kShareMaxGroups = kPagedMaxRequests;
 constexpr int SHARE_LDS_ENTRIES = 1024;      // requests, and groups, up to which a plan is worked out in LDS
 
@@ -60,7 +64,7 @@ struct ShareTables {
 // The plan of a step, in one block.  Own entries are the requests, with the keys behind their prefix; prefix entries are the groups of two requests and more that have rows.  A request
 // takes part in its group if its tokens reach beyond the prefix, and goes by itself over its whole table otherwise.  Its place among the group's rows is given out by an atomic add: where a
 // row stands in its tile has no influence on its results.  All ranges of a kind have kps keys, chosen as in paged_find.
-// Bound by its chain of round trips and barriers: three of the former, the tables being in LDS (57 requests: 7.0 us; with the tables in memory 11.8).
+// Bound by its chain of round trips and barriers: three of the former, the tables being in LDS (57 requests: 7.0 to 7.4 us; with the tables in memory 11.8).
 // LDS false: more requests or groups than that; the tables are in the plan's scratch, the groups' counts still in LDS.
 template <int NT, bool LDS>
 __global__ void __launch_bounds__(NT) share_plan_kernel(ShareArgs a, PagedView pv) {

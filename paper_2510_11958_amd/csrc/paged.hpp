@@ -373,7 +373,7 @@ template <int N> __device__ __forceinline__ uint32_t store_codes(unsigned char* 
 // and behind cu[n_req], and rows whose place or position is out of range, are not stored.
 // 8-bit pools: the 16 lanes' largest finite magnitude a gives the row's power of two, the least with a <= 448 times it; values that are not finite become NaN, with no
 // say in the power.  Norm and rotation are worked out in 64 bits and codes rounded from there to nearest even, once: in 32 bits about one code of a million lands on the other
-// side of a border, 2^-3 of itself away (1900 rows of 8 heads 8.3 us, in 32 bits 7.4; 32 bits first, and 64 where a code lies near a border, 9.2: the look costs more).
+// side of a border, 2^-3 of itself away (1900 rows of 8 heads 8.4 us, in 32 bits 0.9 less; 32 bits first, and 64 where a code lies near a border, 0.9 more: the look costs more).
 template <typename CT, int HD>
 __global__ void __launch_bounds__(256) paged_append_kernel(const float* __restrict__ qkv, long ld, const int* __restrict__ cu, const int* __restrict__ row_pos,
                                                            const long long* __restrict__ slots, const typename PagedWide<CT>::type* __restrict__ k_gain,
